@@ -27,6 +27,15 @@
  *   avits_merge_final         Sec. 3.2 Stage 3   dense full-resolution latent
  *   avits_selftest_bounded_wait  test hook for the device-side failure path
  *
+ * and, for the language model that conditions an editing pipeline and answers
+ * token by token, the same three steps (attention that gives a weight, top-K by
+ * the weight, packing) over a paged key-value cache:
+ *
+ *   avits_cache_append        new keys and values into the pages
+ *   avits_cache_attention     one new token per sequence over its cached tokens,
+ *                             with the weight each of them got
+ *   avits_cache_evict         the tokens of the largest accumulated weights kept
+ *
  * Conventions shared by every call
  * --------------------------------
  *  - Every tensor pointer is DEVICE memory owned by the caller.  The library
@@ -43,8 +52,8 @@
  *  - A failed launch returns AVITS_ERR_CUDA (the CUDA error is cleared and
  *    its text kept for avits_last_error_string()).
  *  - Errors found on the device (a bounded wait that ran out, a NaN score, a
- *    mixed sequence that does not tile the output frame) are OR-ed into a
- *    per-device status word, read and cleared by avits_device_status().
+ *    mixed sequence that does not tile the output frame, a page number outside
+ *    the pool) are OR-ed into a per-device status word, read and cleared by avits_device_status().
  *  - Dtypes: AVITS_BF16 (bfloat16 inputs, fp32 arithmetic) and AVITS_F32.
  *    Scores are always fp32.
  *  - Latent tokens hold C*p*p values ordered (channel, patch-row, patch-col),
@@ -69,7 +78,8 @@ typedef enum {
   AVITS_ERR_CUDA = 3,
   AVITS_ERR_TIMEOUT = 4,   /* device: a bounded wait gave up */
   AVITS_ERR_NAN = 5,       /* device: a NaN reached the fused score */
-  AVITS_ERR_COVERAGE = 6   /* device: merge input does not tile the frame */
+  AVITS_ERR_COVERAGE = 6,  /* device: merge input does not tile the frame */
+  AVITS_ERR_PAGE = 7       /* device: a cache length or page number out of range */
 } avits_status;
 
 typedef enum { AVITS_F32 = 0, AVITS_BF16 = 1 } avits_dtype;
@@ -452,6 +462,103 @@ size_t avits_merge_final_workspace(avits_upmode mode, int B, int full_h, int ful
  * and clears the word.  The only call that blocks the host.
  * ---------------------------------------------------------------------- */
 avits_status avits_device_status(void* stream);
+
+/* ------------------------------------------------------------------------
+ * A paged key-value cache: a pool of num_pages pages of page_size tokens each,
+ * and for every sequence b the numbers of its pages in order (block_table) and
+ * its cached tokens (lens).  Token j of sequence b lies in page
+ * block_table[b][j / page_size] at place j % page_size.  Pages may be shared
+ * between sequences (a common prompt) where they are only read.
+ *
+ * k_pages, v_pages : [num_pages, page_size, Hkv, d] seen through element
+ *         strides (page *_sp, token *_st, head *_sh; d contiguous), so the
+ *         order of the axes in memory, and whether keys and values share an
+ *         allocation, is the caller's choice.  16-byte aligned bases and
+ *         strides; d a multiple of 16 bytes, at most 256 values.
+ * block_table : [B, >= ceil(max_len / page_size)] int32, row stride table_sb.
+ *         Entries past a sequence's pages are not read.
+ * lens  : [B] int32, 0 <= lens[b] <= max_len.  0: no cached token.
+ * max_len : an upper bound of the lengths that the host knows; workspaces and
+ *         grids are sized by it.
+ * acc   : NULL or [B, Hkv, >= max_len] fp32 (row strides acc_sb, acc_sh, the
+ *         last axis contiguous): the accumulated attention weight of each
+ *         cached token under each KV head.
+ *
+ * A length outside [0, max_len] is cut to it and a page number outside
+ * [0, num_pages) makes its tokens count as masked (read) or be left out
+ * (written); both raise AVITS_ERR_PAGE in the status word.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  void* k_pages;
+  void* v_pages;
+  const int32_t* block_table;
+  int32_t* lens;
+  float* acc;
+  int64_t k_sp, k_st, k_sh;
+  int64_t v_sp, v_st, v_sh;
+  int64_t table_sb, acc_sb, acc_sh;
+  int32_t dt;          /* avits_dtype */
+  int32_t B, Hkv, d;
+  int32_t num_pages, page_size, max_len;
+} avits_kv_cache;
+
+/* New tokens into the cache.  lens already counts them: sequence b's new
+ * tokens are k_new / v_new rows cu_new[b] .. cu_new[b+1]-1 ([T, Hkv, d] of the
+ * cache's type, element strides *_st, *_sh, 16-byte aligned) and go to places
+ * lens[b] - n_b .. lens[b]-1.  cu_new [B+1] int32 does not decrease from 0; rows
+ * past cu_new[B] are ignored, and where a sequence is given more tokens than
+ * lens[b] the first ones are left out (AVITS_ERR_PAGE).  With acc the entries
+ * of the new tokens are set to zero.  T = 0 launches nothing. */
+avits_status avits_cache_append(const avits_kv_cache* cache, const void* k_new, const void* v_new,
+                                int T, const int32_t* cu_new, int64_t k_st, int64_t k_sh,
+                                int64_t v_st, int64_t v_sh, void* stream);
+
+/* Attention of one new token per sequence over its cached tokens (grouped
+ * heads: query heads hk*G .. hk*G+G-1, G = H / Hkv, share KV head hk):
+ *
+ *     x_bhj = softmax_scale * <q_bh, k_bj(h/G)>          j = 0 .. lens[b]-1
+ *     lse   = log sum_j exp(x_bhj)
+ *     o_bh  = sum_j exp(x_bhj - lse) v_bj(h/G)
+ *     acc[b,hk,j] = (old) + weight * (1/G) * sum_{h of hk} exp(x_bhj - lse_bh)
+ *
+ * the last as in Eq. 3, the mean over heads of the weight a key got.  A
+ * sequence without cached tokens gets o = 0 and lse = -inf.
+ * q, o  : [B,H,d] of the cache's type, element strides *_sb, *_sh, d contiguous.
+ * lse_opt : NULL or [B,H] fp32 contiguous, natural log.
+ * weights : AVITS_WEIGHTS_NONE leaves acc alone; _WRITE sets acc (old = 0) for
+ *         the places below lens[b], _ADD adds to it; places past lens[b] are
+ *         left as they were.  Sums have a fixed order: the same inputs give the
+ *         same bits.
+ * H a multiple of Hkv, at most 256 heads to a KV head.
+ * workspace/ws_bytes : at least avits_cache_attention_workspace(...) bytes,
+ *         16-byte aligned, of any content; not used by two calls at once. */
+typedef enum {
+  AVITS_WEIGHTS_NONE = 0, AVITS_WEIGHTS_WRITE = 1, AVITS_WEIGHTS_ADD = 2
+} avits_weights;
+
+avits_status avits_cache_attention(const avits_kv_cache* cache, const void* q, int H,
+                                   int64_t q_sb, int64_t q_sh, float softmax_scale, void* o,
+                                   int64_t o_sb, int64_t o_sh, float* lse_opt, int weights,
+                                   float weight, void* workspace, size_t ws_bytes, void* stream);
+
+/* Workspace bytes for these sizes on the CURRENT device (0 for invalid ones). */
+size_t avits_cache_attention_workspace(const avits_kv_cache* cache, int H, int weights);
+
+/* Eviction by accumulated weight.  For every sequence b and KV head, n =
+ * lens[b]: all tokens are kept if n <= keep; else the first `sinks`, the last
+ * `recent` and, of those between, the keep - sinks - recent of the largest acc
+ * (ties: the lower place; a NaN counts as lowest), in their order.  Each head
+ * keeps tokens of its own.  The kept keys, values and accumulated weights are
+ * copied to places 0 .. min(n, keep)-1 of dst, whose lens are written.  dst's
+ * pages must be none that src reads: a page may be shared with another
+ * sequence, so nothing is moved in place (the pool, the table's memory and acc
+ * may be the same allocations; lens and acc rows must not overlap src's).
+ * keep_idx : [B,Hkv,keep] int32 contiguous, receives the kept tokens' places in
+ *         src, ascending, -1 past min(n, keep).
+ * keep >= 1, sinks, recent >= 0, sinks + recent <= keep <= dst->max_len; both
+ * caches have acc, and the same type, B, Hkv and d. */
+avits_status avits_cache_evict(const avits_kv_cache* src, const avits_kv_cache* dst, int keep,
+                               int sinks, int recent, int32_t* keep_idx, void* stream);
 
 /* ------------------------------------------------------------------------
  * Test hook for the failure detection of the device-side waits (a library

@@ -20,6 +20,10 @@ Calls:
   avits_selective_upsample  Sec. 3.2 Stage 2  packed mixed-resolution sequence
   avits_select_upsample     selection + upsample in one launch
   avits_merge_final         Sec. 3.2 Stage 3  dense full-resolution latent
+  avits_cache_append        new tokens into a paged key-value cache (KVCache)
+  avits_cache_attention     one new token per sequence over its cached tokens,
+                            with the weight each of them got
+  avits_cache_evict         the cached tokens of the largest accumulated weights
   avits_device_status       device-side error word (read and cleared)
 """
 from __future__ import annotations
@@ -27,6 +31,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from _thread import get_ident
 from typing import Optional, Sequence
 
 from . import _build
@@ -40,13 +45,16 @@ __all__ = [
     "avits_score_temporal_var", "avits_fuse_select",
     "avits_selective_upsample", "avits_select_upsample",
     "avits_merge_final", "avits_merge_final_workspace", "avits_device_status",
+    "KVCache", "avits_cache_append", "avits_cache_attention", "avits_cache_attention_workspace",
+    "avits_cache_evict",
     "avits_selftest_bounded_wait", "avits_status_string", "avits_version", "SpatialWorkspace",
 ]
 
 F32, BF16 = 0, 1
 NEAREST, BILINEAR = 0, 1
 STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported", 3: "CUDA error",
-          4: "device wait timed out", 5: "NaN in fused score", 6: "coverage"}
+          4: "device wait timed out", 5: "NaN in fused score", 6: "coverage",
+          7: "cache length or page number out of range"}
 
 _lib = None
 
@@ -107,6 +115,11 @@ def lib():
                                         i64, i64, i64, f32, f32, i32, vp, vp, vp],
         "avits_score_spatial_noalloc_limit": [],
         "avits_score_spatial_noalloc_error": [],
+        "avits_cache_append": [vp, vp, vp, i32, vp, i64, i64, i64, i64, vp],
+        "avits_cache_attention": [vp, vp, i32, i64, i64, f32, vp, i64, i64, vp, i32, f32, vp, sz,
+                                  vp],
+        "avits_cache_attention_workspace": [vp, i32, i32],
+        "avits_cache_evict": [vp, vp, i32, i32, i32, vp, vp],
         "avits_device_status": [vp],
         "avits_selftest_bounded_wait": [ctypes.c_ulonglong, vp, vp],
         "avits_status_string": [i32],
@@ -119,7 +132,7 @@ def lib():
         fn.restype = ctypes.c_int
     for name in ("avits_score_spatial_workspace", "avits_merge_final_workspace",
                  "avits_score_spatial_noalloc_limit", "avits_attention_forward_workspace",
-                 "avits_selective_upsample_workspace"):
+                 "avits_selective_upsample_workspace", "avits_cache_attention_workspace"):
         getattr(L, name).restype = ctypes.c_size_t
     for name in ("avits_status_string", "avits_last_error_string", "avits_version",
                  "avits_score_spatial_noalloc_error"):
@@ -522,3 +535,194 @@ def avits_score_spatial_noalloc(q_img, k_all, L: int, softmax_scale: float, A, w
 def avits_score_spatial_noalloc_limit() -> int:
     """Bytes of the fixed scratch array behind avits_score_spatial_noalloc."""
     return int(lib().avits_score_spatial_noalloc_limit())
+
+
+# ------------------------------------------------- paged key-value cache --
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("acc", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in ("k_sp", "k_st", "k_sh", "v_sp", "v_st", "v_sh",
+                                              "table_sb", "acc_sb", "acc_sh")] + \
+               [(n, ctypes.c_int32) for n in ("dt", "B", "Hkv", "d", "num_pages", "page_size",
+                                              "max_len")]
+
+
+class KVCache:
+    """The buffers of a paged key-value cache, described to the library once
+    and used by any number of calls (which read the tensors' current contents).
+
+    k_pages, v_pages  [num_pages, page_size, Hkv, d] bf16 or fp32, any strides
+                      with d contiguous (pages may lie in memory head by head,
+                      or keys and values side by side: pass the view)
+    block_table       [B, columns] int32, a sequence's pages in order
+    lens              [B] int32, its cached tokens
+    acc               [B, Hkv, >= max_len] fp32, optional: accumulated weights
+    max_len           an upper bound of lens known here (default: all that the
+                      table can hold); a smaller one costs less workspace
+    """
+    __slots__ = ("k_pages", "v_pages", "block_table", "lens", "acc", "B", "Hkv", "d", "dtype",
+                 "page_size", "max_len", "device", "_index", "_struct", "_ref", "_need")
+
+    def __init__(self, k_pages, v_pages, block_table, lens, acc=None, max_len: Optional[int] = None):
+        torch = _torch()
+        if k_pages.dim() != 4 or tuple(v_pages.shape) != tuple(k_pages.shape):
+            raise ValueError("k_pages and v_pages must be [num_pages, page_size, Hkv, d]")
+        num_pages, page_size, Hkv, d = k_pages.shape
+        dt = _dtype_code(k_pages)
+        if _dtype_code(v_pages) != dt:
+            raise TypeError("k_pages and v_pages dtypes differ")
+        if k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
+            raise ValueError("the head-dim axis must be contiguous")
+        if block_table.dim() != 2 or block_table.dtype != torch.int32 or \
+                (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+            raise ValueError("block_table must be an int32 [B, columns] tensor, rows contiguous")
+        B, cols = block_table.shape
+        if max_len is None:
+            max_len = cols * page_size
+        if not 0 < max_len <= cols * page_size:
+            raise ValueError("max_len must be positive and fit the block table")
+        if tuple(lens.shape) != (B,) or lens.dtype != torch.int32 or not lens.is_contiguous():
+            raise ValueError("lens must be a contiguous int32 [B] tensor")
+        if acc is not None and (acc.dim() != 3 or tuple(acc.shape[:2]) != (B, Hkv) or
+                                acc.shape[2] < max_len or acc.dtype != torch.float32 or
+                                (acc.shape[2] > 1 and acc.stride(2) != 1)):
+            raise ValueError("acc must be a float32 [B, Hkv, >= max_len] tensor, rows contiguous")
+        for t in (v_pages, block_table, lens, acc):
+            if t is not None and t.device != k_pages.device:
+                raise ValueError("the cache's tensors must be on one device")
+        self.k_pages, self.v_pages, self.block_table = k_pages, v_pages, block_table
+        self.lens, self.acc = lens, acc
+        self.B, self.Hkv, self.d, self.dtype = B, Hkv, d, k_pages.dtype
+        self.page_size, self.max_len, self.device = page_size, int(max_len), k_pages.device
+        self._index = k_pages.get_device()
+        ks, vs = k_pages.stride(), v_pages.stride()
+        sa = acc.stride() if acc is not None else (0, 0, 0)
+        self._struct = _CacheStruct(_ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(lens),
+                                    _ptr(acc), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                                    block_table.stride(0), sa[0], sa[1], dt, B, Hkv, d, num_pages,
+                                    page_size, self.max_len)
+        self._ref = ctypes.addressof(self._struct)
+        self._need = {}   # (H, weights) -> workspace bytes
+
+
+def _on_device(cache: KVCache, *tensors):
+    """The calls launch on the current device, and every tensor is there."""
+    index = cache._index
+    if index != _torch()._C._cuda_getDevice():
+        raise ValueError("the cache is on %s, which is not the current device" % cache.device)
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError("tensor on %s, the cache is on %s" % (t.device, cache.device))
+
+
+_cache_ws = {}
+
+
+def _scratch(cache: KVCache, need: int, handle: int):
+    """Workspace of a call on a stream.  Outside a capture one buffer per stream
+    and calling thread, grown on demand: a call is two launches, which calls of
+    other threads may come between.  In a capture a buffer of that graph's own:
+    two graphs may be replayed at once.  It is allocated on the stream that
+    uses it, so the allocator hands it on in that stream's order."""
+    torch = _torch()
+    if handle != torch._C._cuda_getCurrentRawStream(cache._index):
+        s = torch.cuda.ExternalStream(handle, device=cache.device) if handle else \
+            torch.cuda.default_stream(cache.device)
+        with torch.cuda.stream(s):
+            return _scratch(cache, need, handle)
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(need, dtype=torch.uint8, device=cache.device)
+    key = (cache._index, handle, get_ident())
+    buf = _cache_ws.get(key)
+    if buf is None or buf.numel() < need:
+        buf = _cache_ws[key] = torch.empty(need, dtype=torch.uint8, device=cache.device)
+    return buf
+
+
+def avits_cache_append(cache: KVCache, k_new, v_new, cu_new, stream=None):
+    """New tokens into the cache: k_new, v_new [T,Hkv,d] (any 16-byte aligned
+    strides, d contiguous), sequence b's being rows cu_new[b] .. cu_new[b+1]-1
+    (int32 [B+1]).  cache.lens already counts them; they go to the last places.
+    With cache.acc their accumulated weights are set to zero."""
+    T, Hkv, d = k_new.shape
+    if Hkv != cache.Hkv or d != cache.d or tuple(v_new.shape) != (T, Hkv, d):
+        raise ValueError("k_new / v_new must be [T, Hkv, d] of the cache")
+    if k_new.dtype != cache.dtype or v_new.dtype != cache.dtype:
+        raise TypeError("k_new / v_new and cache dtypes differ")
+    ks, vs = k_new.stride(), v_new.stride()
+    if ks[2] != 1 or vs[2] != 1:
+        raise ValueError("the head-dim axis must be contiguous")
+    if tuple(cu_new.shape) != (cache.B + 1,) or cu_new.dtype != _torch().int32 or \
+            not cu_new.is_contiguous():
+        raise ValueError("cu_new must be a contiguous int32 [B+1] tensor")
+    _on_device(cache, k_new, v_new, cu_new)
+    rc = lib().avits_cache_append(cache._ref, k_new.data_ptr(), v_new.data_ptr(), T,
+                                  cu_new.data_ptr(), ks[0], ks[1], vs[0], vs[1], _stream(stream))
+    _check("avits_cache_append", rc)
+
+
+def avits_cache_attention_workspace(cache: KVCache, H: int, weights: bool) -> int:
+    return int(lib().avits_cache_attention_workspace(cache._ref, H, 2 if weights else 0))
+
+
+def avits_cache_attention(cache: KVCache, q, softmax_scale: float, o, lse=None,
+                          weight: Optional[float] = None, accumulate: bool = True,
+                          workspace=None, stream=None):
+    """One new token per sequence over its cached tokens: q [B,H,d] into o
+    [B,H,d] (the cache's type, any strides, d contiguous; query heads hk*G ..
+    hk*G+G-1 share KV head hk, G = H / Hkv) and lse [B,H] fp32.  With ``weight``
+    cache.acc gets weight times the mean over a KV head's query heads of the
+    softmax weight of each cached token, added (or written).  ``workspace``: a
+    device byte tensor of avits_cache_attention_workspace() bytes, of the
+    caller's own where calls may overlap; by default the library's."""
+    B, H, d = q.shape
+    if B != cache.B or d != cache.d or o.shape != q.shape:
+        raise ValueError("q and o must be [B, H, d] of the cache")
+    if q.dtype != cache.dtype or o.dtype != cache.dtype:
+        raise TypeError("q, o and cache dtypes differ")
+    qs, os_ = q.stride(), o.stride()
+    if qs[2] != 1 or os_[2] != 1:
+        raise ValueError("the head-dim axis must be contiguous")
+    if lse is not None and (tuple(lse.shape) != (B, H) or lse.dtype != _torch().float32 or
+                            not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous float32 [B,H] tensor")
+    mode = 0 if weight is None else (2 if accumulate else 1)
+    if mode and cache.acc is None:
+        raise ValueError("weights are wanted of a cache without acc")
+    _on_device(cache, q, o, lse, workspace)
+    handle = _stream(stream)
+    L = lib()
+    need = cache._need.get((H, mode))
+    if need is None:
+        need = cache._need[(H, mode)] = int(L.avits_cache_attention_workspace(cache._ref, H, mode))
+    if workspace is None:
+        workspace = _scratch(cache, max(need, 16), handle)
+    rc = L.avits_cache_attention(
+        cache._ref, q.data_ptr(), H, qs[0], qs[1], float(softmax_scale), o.data_ptr(), os_[0],
+        os_[1], None if lse is None else lse.data_ptr(), mode, 0.0 if weight is None else
+        float(weight), workspace.data_ptr(), workspace.numel() * workspace.element_size(), handle)
+    _check("avits_cache_attention", rc)
+    return o
+
+
+def avits_cache_evict(src: KVCache, dst: KVCache, keep: int, sinks: int, recent: int, keep_idx,
+                      stream=None):
+    """Per sequence and KV head: all cached tokens if there are at most
+    ``keep``, else the first ``sinks``, the last ``recent`` and those of the
+    largest src.acc between them (ties: the lower place), in order, copied with
+    their weights to the places 0 .. of dst (pages that src does not read), whose
+    lens are written.  keep_idx [B,Hkv,keep] int32: their places in src, -1 past
+    the kept ones."""
+    if tuple(keep_idx.shape) != (src.B, src.Hkv, keep) or keep_idx.dtype != _torch().int32 or \
+            not keep_idx.is_contiguous():
+        raise ValueError("keep_idx must be a contiguous int32 [B, Hkv, keep] tensor")
+    if src.dtype != dst.dtype or (src.B, src.Hkv, src.d) != (dst.B, dst.Hkv, dst.d):
+        raise ValueError("the two caches' types or sizes differ")
+    if src.acc is None or dst.acc is None:
+        raise ValueError("eviction goes by accumulated weights: both caches need acc")
+    _on_device(src, dst.k_pages, keep_idx)
+    rc = lib().avits_cache_evict(src._ref, dst._ref, int(keep), int(sinks), int(recent),
+                                 keep_idx.data_ptr(), _stream(stream))
+    _check("avits_cache_evict", rc)
+    return keep_idx

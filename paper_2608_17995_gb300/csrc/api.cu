@@ -45,6 +45,31 @@ bool mixed_bilinear_ok(avits_upmode mode, const int32_t* pos_in, int B, int M, i
   return ws && aligned16(ws) && ws_bytes >= merge_workspace_bytes(B, gh, gw);
 }
 
+// A cache's description: INVALID_ARG for what cannot be one, UNSUPPORTED for a
+// layout that the kernels' 16-byte accesses do not take.
+avits_status check_cache(const avits_kv_cache* c) {
+  if (!c || !c->k_pages || !c->v_pages || !c->block_table || !c->lens) return AVITS_ERR_INVALID_ARG;
+  if (c->dt != AVITS_F32 && c->dt != AVITS_BF16) return AVITS_ERR_INVALID_ARG;
+  if (c->B <= 0 || c->Hkv <= 0 || c->d <= 0 || c->num_pages <= 0 || c->page_size <= 0 ||
+      c->max_len <= 0)
+    return AVITS_ERR_INVALID_ARG;
+  if (c->k_sp < 0 || c->k_st < 0 || c->k_sh < 0 || c->v_sp < 0 || c->v_st < 0 || c->v_sh < 0)
+    return AVITS_ERR_INVALID_ARG;
+  if (c->table_sb < 0) return AVITS_ERR_INVALID_ARG;
+  if (c->acc && (c->acc_sb < 0 || c->acc_sh < 0 || (c->Hkv > 1 && c->acc_sh < c->max_len) ||
+                 (c->B > 1 && c->acc_sb < c->max_len)))
+    return AVITS_ERR_INVALID_ARG;
+  const int per16 = c->dt == AVITS_BF16 ? 8 : 4;
+  if (c->d > 256 || c->d % per16) return AVITS_ERR_UNSUPPORTED;
+  if (c->max_len > (1 << 30) || c->page_size > (1 << 30) || c->B > (1 << 24) ||
+      c->Hkv > (1 << 16) || (int64_t)c->B * c->Hkv > (1 << 26))
+    return AVITS_ERR_UNSUPPORTED;
+  if (!aligned16(c->k_pages) || !aligned16(c->v_pages)) return AVITS_ERR_UNSUPPORTED;
+  for (int64_t st : {c->k_sp, c->k_st, c->k_sh, c->v_sp, c->v_st, c->v_sh})
+    if (st % per16) return AVITS_ERR_UNSUPPORTED;
+  return AVITS_OK;
+}
+
 }  // namespace
 
 // The device address of g_status on the current device, looked up once per
@@ -82,6 +107,7 @@ const char* avits_status_string(avits_status s) {
     case AVITS_ERR_TIMEOUT: return "device wait timed out";
     case AVITS_ERR_NAN: return "NaN in fused score";
     case AVITS_ERR_COVERAGE: return "mixed sequence does not tile the frame";
+    case AVITS_ERR_PAGE: return "cache length or page number out of range";
   }
   return "unknown status";
 }
@@ -383,6 +409,75 @@ avits_status avits_merge_final(const void* mixed, avits_dtype dt, int B, int N, 
     return AVITS_ERR_INVALID_ARG;
   return cuda_status(launch_merge(mixed, dt, B, N, pos, span, full_h, full_w, C, mode, out_full,
                                   workspace, status_word(), static_cast<cudaStream_t>(stream)));
+}
+
+avits_status avits_cache_append(const avits_kv_cache* cache, const void* k_new, const void* v_new,
+                                int T, const int32_t* cu_new, int64_t k_st, int64_t k_sh,
+                                int64_t v_st, int64_t v_sh, void* stream) {
+  AVITS_RANGE();
+  if (T < 0 || !cu_new || (T > 0 && (!k_new || !v_new))) return AVITS_ERR_INVALID_ARG;
+  if (k_st < 0 || k_sh < 0 || v_st < 0 || v_sh < 0) return AVITS_ERR_INVALID_ARG;
+  const avits_status ok = check_cache(cache);
+  if (ok != AVITS_OK) return ok;
+  if (T == 0) return AVITS_OK;
+  const int per16 = cache->dt == AVITS_BF16 ? 8 : 4;
+  if (!aligned16(k_new) || !aligned16(v_new) || k_st % per16 || k_sh % per16 || v_st % per16 ||
+      v_sh % per16)
+    return AVITS_ERR_UNSUPPORTED;
+  return cuda_status(launch_cache_append(*cache, k_new, v_new, T, cu_new, k_st, k_sh, v_st, v_sh,
+                                         status_word(), static_cast<cudaStream_t>(stream)));
+}
+
+size_t avits_cache_attention_workspace(const avits_kv_cache* cache, int H, int weights) {
+  if (check_cache(cache) != AVITS_OK || H <= 0 || H % cache->Hkv ||
+      !cache_attention_sizes_ok(*cache, H) || weights < AVITS_WEIGHTS_NONE ||
+      weights > AVITS_WEIGHTS_ADD)
+    return 0;
+  return cache_attention_workspace(*cache, H, weights != AVITS_WEIGHTS_NONE, num_sms_current());
+}
+
+avits_status avits_cache_attention(const avits_kv_cache* cache, const void* q, int H,
+                                   int64_t q_sb, int64_t q_sh, float softmax_scale, void* o,
+                                   int64_t o_sb, int64_t o_sh, float* lse_opt, int weights,
+                                   float weight, void* workspace, size_t ws_bytes, void* stream) {
+  AVITS_RANGE();
+  if (!q || !o || H <= 0 || q_sb < 0 || q_sh < 0 || o_sb < 0 || o_sh < 0)
+    return AVITS_ERR_INVALID_ARG;
+  if (!(softmax_scale > 0.f) || !(softmax_scale < 3.0e38f)) return AVITS_ERR_INVALID_ARG;
+  if (weights < AVITS_WEIGHTS_NONE || weights > AVITS_WEIGHTS_ADD) return AVITS_ERR_INVALID_ARG;
+  const avits_status ok = check_cache(cache);
+  if (ok != AVITS_OK) return ok;
+  if (H % cache->Hkv || (weights != AVITS_WEIGHTS_NONE && !cache->acc))
+    return AVITS_ERR_INVALID_ARG;
+  if ((H > 1 && o_sh < cache->d) || (cache->B > 1 && o_sb < cache->d)) return AVITS_ERR_INVALID_ARG;
+  if (!cache_attention_sizes_ok(*cache, H)) return AVITS_ERR_UNSUPPORTED;
+  const int sms = num_sms_current();
+  if (!workspace || !aligned16(workspace) ||
+      ws_bytes < cache_attention_workspace(*cache, H, weights != AVITS_WEIGHTS_NONE, sms))
+    return AVITS_ERR_INVALID_ARG;
+  const CacheAttnCall call{*cache, q, H, q_sb, q_sh, softmax_scale, o, o_sb, o_sh, lse_opt,
+                           weights, weight, workspace};
+  return cuda_status(
+      launch_cache_attention(call, sms, status_word(), static_cast<cudaStream_t>(stream)));
+}
+
+avits_status avits_cache_evict(const avits_kv_cache* src, const avits_kv_cache* dst, int keep,
+                               int sinks, int recent, int32_t* keep_idx, void* stream) {
+  AVITS_RANGE();
+  if (!keep_idx || keep < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep)
+    return AVITS_ERR_INVALID_ARG;
+  for (const avits_kv_cache* c : {src, dst}) {
+    const avits_status ok = check_cache(c);
+    if (ok != AVITS_OK) return ok;
+    if (!c->acc) return AVITS_ERR_INVALID_ARG;
+  }
+  if (src->dt != dst->dt || src->B != dst->B || src->Hkv != dst->Hkv || src->d != dst->d ||
+      keep > dst->max_len || src->lens == dst->lens || src->acc == dst->acc)
+    return AVITS_ERR_INVALID_ARG;
+  if ((int64_t)src->B * src->Hkv * ((int64_t)keep / 8 + 1) >= (1ll << 31))
+    return AVITS_ERR_UNSUPPORTED;
+  return cuda_status(launch_cache_evict(*src, *dst, keep, sinks, recent, keep_idx, status_word(),
+                                        static_cast<cudaStream_t>(stream)));
 }
 
 avits_status avits_selftest_bounded_wait(unsigned long long limit_ns, long long* result,

@@ -144,4 +144,31 @@ cudaError_t launch_merge(const void* mixed, avits_dtype dt, int B, int N, const 
                          const int32_t* span, int fh, int fw, int C, avits_upmode mode,
                          void* out, void* ws, unsigned int* status, cudaStream_t s);
 
+// ---- paged key-value cache ----------------------------------------------------
+struct CacheAttnCall {
+  avits_kv_cache cache;
+  const void* q;
+  int H;
+  int64_t q_sb, q_sh;
+  float scale;
+  void* o;
+  int64_t o_sb, o_sh;
+  float* lse;          // [B,H] or NULL
+  int weights;         // avits_weights
+  float weight;
+  void* ws;
+};
+// Whether the line of tiles and the row counts fit the kernels' indexes.
+bool cache_attention_sizes_ok(const avits_kv_cache& c, int H);
+size_t cache_attention_workspace(const avits_kv_cache& c, int H, bool score, int num_sms);
+cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsigned int* status,
+                                   cudaStream_t s);
+// Strides of the new rows in elements.
+cudaError_t launch_cache_append(const avits_kv_cache& c, const void* k_new, const void* v_new,
+                                int T, const int32_t* cu, int64_t k_st, int64_t k_sh, int64_t v_st,
+                                int64_t v_sh, unsigned int* status, cudaStream_t s);
+cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& dst, int keep,
+                               int sinks, int recent, int32_t* idx, unsigned int* status,
+                               cudaStream_t s);
+
 }  // namespace avits
