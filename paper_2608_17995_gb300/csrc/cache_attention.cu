@@ -7,13 +7,15 @@
 // Every key and value is read once, so HBM bounds it: 4 G operations per bf16
 // element of K and V.
 //
-// Split.  A sequence's keys are cut into tiles of 16; all tiles of all (b, hk,
+// Split.  A sequence's keys are cut into tiles; all tiles of all units (b, hk,
 // row group) form one line, cut into equal pieces, one per CTA, so that uneven
 // lengths and few heads load the SMs alike.  A CTA finds its piece by a scan of
-// the lengths.  Inside a piece each warp takes tiles of its own with a running
-// maximum, sum and O in registers; the warps meet once per (b, hk) at the end.
-// A (b, hk) that lies in one piece is finished there; of the others each piece
-// leaves its maximum, sum and O, and the second kernel joins them.
+// the lengths.  Its warps take the piece's tiles in turn, each with a running
+// maximum, sum and O in registers and a ring of tiles of its own in shared
+// memory, filled by asynchronous copies that run ahead over unit borders; the
+// warps meet once per unit.  A unit that lies in one piece is finished there; of
+// the others each piece leaves its maximum, sum and O, and the second kernel
+// joins them.
 //
 // The weights need the whole row's lse: the first kernel leaves the logits
 // (fp32), the second sums exp(x - lse) over the group's heads, in a fixed order.
@@ -23,7 +25,6 @@
 namespace avits {
 namespace {
 
-constexpr int kTile = 16;         // keys per tile
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMinTiles = 4;      // tiles of the smallest piece: one per warp
@@ -38,59 +39,126 @@ struct CacheAttn {
   int64_t q_sb, q_sh, o_sb, o_sh;
   float* lse;
   int H, G;
-  int rt;           // row tiles of 8 heads side by side in a CTA (1, 2 or 4)
-  int groups;       // row groups (units) per KV head: ceil(G / (8 rt))
+  int rows;         // rows (query heads) of a unit
+  int groups;       // units per KV head: ceil(G / rows)
+  int tile;         // keys per tile
   int grid;         // CTAs of the first kernel
+  int score;        // weights wanted: logits are kept
   float scale2;     // scale * log2(e)
   float wmean;      // weight / G
   int add;
   // workspace
   int* starts;      // [B+1] first tile of a sequence on the line
   float* lse2;      // [B,H] log2-domain lse of rows finished in one piece
-  float2* pml;      // [2 grid][8 rt] maximum and sum of a piece's row
-  float* po;        // [2 grid][8 rt][d] its O
+  float2* pml;      // [2 grid][rows] maximum and sum of a piece's row
+  float* po;        // [2 grid][rows][d] its O
   float* logits;    // [B,H,ld] log2-domain logits (weights wanted)
   int64_t ld;
   unsigned int* status;
 };
 
-__device__ __forceinline__ int tiles_of(const CacheAttn& a, int b) {
-  return (cache_len(a.c, b) + kTile - 1) / kTile;
+__device__ __forceinline__ int tiles_of(const CacheAttn& a, int len) {
+  return (len + a.tile - 1) / a.tile;
 }
 
-// The piece's row: what the CTA's warps agree on for one (b, hk, row group).
-struct Unit {
-  int b, hk, row0;    // first row (query head of the group) of this warp's row tile
-  int rows;           // rows of this warp's tile (<= 8; <= 0: nothing to do)
-  int len;
-};
-
-// Rows' pages of one tile: lane l holds the page and the place of key l % 16.
-struct TileKeys {
-  int page, slot;
-};
-
-__device__ __forceinline__ int table_entry(const CacheAttn& a, const int32_t* table, int tile,
-                                           int len, int lane) {
-  const int j = tile * kTile + (lane & 15);
-  return j < len ? table[a.page.div(j)] : -1;
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
+  // nothing is read, and zeros are written, where !ok
+  const int n = ok ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n));
 }
-__device__ __forceinline__ TileKeys tile_keys(const CacheAttn& a, int entry, int tile, int len,
-                                              int lane) {
-  const int j = tile * kTile + (lane & 15);
-  TileKeys t;
-  t.slot = j - a.page.div(j) * a.c.page_size;
-  t.page = j < len ? checked_page(a.c, entry, a.status) : -1;
-  return t;
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// A warp's place on the line of tiles: what it copies next.
+struct Cursor {
+  int b, u, t;      // sequence, unit in it, tile in the unit
+  int nt, len;
+  int left;         // tiles still to come
+  int entry;        // table entry of this lane's key of that tile
+
+  __device__ __forceinline__ void settle(const CacheAttn& a, int units) {
+    while (t >= nt) {
+      t -= nt;
+      if (++u == units) {
+        u = 0;
+        do {
+          len = cache_len(a.c, ++b);
+          nt = tiles_of(a, len);
+        } while (nt == 0);
+      }
+    }
+  }
+  template <int kTile>
+  __device__ __forceinline__ void look_up(const CacheAttn& a, int lane) {
+    const int j = t * kTile + (lane & (kTile - 1));
+    entry = j < len ? a.c.block_table[(int64_t)b * a.c.table_sb + a.page.div(j)] : -1;
+  }
+};
+
+// Copies the cursor's tile, keys then values, to `dst` and steps on.  `mask`
+// receives a bit for each key that is there.  The rows of a tile are kTile rows
+// of kRowBytes (a multiple of 128); pieces past the head width are not written,
+// but for a zero one where it ends inside a step of 16 columns.  kSwizzle: piece c of row r lies at c ^ (r % 8), for ldmatrix.
+template <int kTile, int kRowBytes, bool kSwizzle>
+__device__ __forceinline__ void copy_tile(const CacheAttn& a, Cursor& cur, uint32_t dst,
+                                          uint32_t* mask, int units, int lane) {
+  constexpr int kEs = kSwizzle ? 2 : 4;
+  constexpr int kPieces = kRowBytes / 16;
+  constexpr int kSide = kPieces < 32 ? 32 / kPieces : 1;       // rows side by side
+  constexpr int kSteps = kPieces < 32 ? 1 : kPieces / 32;      // steps along a row
+  const int hk = a.groups == 1 ? cur.u : cur.u / a.groups;
+  const int j = cur.t * kTile + (lane & (kTile - 1));
+  const int page = j < cur.len ? checked_page(a.c, cur.entry, a.status) : -1;
+  const unsigned ok = __ballot_sync(0xffffffffu, page >= 0);
+  const int slot = j - a.page.div(j) * a.c.page_size;
+  // lanes below 16 hold the key's offset, the others the value's
+  const int64_t off = page < 0 ? 0
+                      : lane < 16
+                          ? (int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st + hk * a.c.k_sh
+                          : (int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st + hk * a.c.v_sh;
+  const int side = kPieces < 32 ? lane / kPieces : 0, piece = kPieces < 32 ? lane % kPieces : lane;
+  const int row_pieces = a.c.d * kEs / 16;
+  const int fill_pieces = kSwizzle ? (row_pieces + 1) & ~1 : row_pieces;   // whole 16-column steps
+#pragma unroll
+  for (int i = 0; i < kTile / kSide; ++i) {
+    const int row = i * kSide + side;
+    const int64_t ko = __shfl_sync(0xffffffffu, off, row);
+    const int64_t vo = __shfl_sync(0xffffffffu, off, row + 16);
+    const bool there = (ok >> row) & 1u;
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) {
+      const int c = piece + 32 * st;
+      if (c < fill_pieces) {
+        const bool some = there && c < row_pieces;
+        const uint32_t to = dst + row * kRowBytes + ((kSwizzle ? c ^ (row & 7) : c) << 4);
+        cp16(to, static_cast<const char*>(a.c.k_pages) + ko * kEs + c * 16, some);
+        cp16(to + kTile * kRowBytes, static_cast<const char*>(a.c.v_pages) + vo * kEs + c * 16,
+             some);
+      }
+    }
+  }
+  if (lane == 0) *mask = ok;
+  if (--cur.left > 0) {
+    cur.t += kWarps;
+    cur.settle(a, units);
+    cur.look_up<kTile>(a, lane);
+  }
+}
+
+// The place of O's column d of a row in a warp's buffer (bank conflicts).
+__device__ __forceinline__ int o_at(int row, int d, int D) {
+  return row * D + ((((d >> 3) ^ (row & 7)) << 3) | (d & 7));
 }
 
 // ------------------------------------------------------------------ bf16 --
-// m16n8k16 with the 8 heads of a row tile in rows 0-7.  The product over d may
-// take d in any order, the same for Q and K, and O's columns may come in any
-// order: a lane loads 16 bytes of a key's row and 16 bytes of a value's row
-// straight into operand registers, no shared memory in between.  The weights
-// enter P V as two bf16 parts (value and rest, 16 significant bits together),
-// the rest in rows 8-15 that are free: O is as exact as with fp32 weights.
+// m16n8k16, heads in the rows.  kR = 8 heads or fewer: the weights enter P V as
+// two bf16 parts (value and rest, 16 significant bits together), the value in
+// rows 0-7 and the rest in rows 8-15, which are free.  kR = 16, 32: one or two
+// row tiles, the rest in a second product.  Either way O is as exact as with
+// weights in fp32.
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                          uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -99,236 +167,276 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm2(uint32_t& r0, uint32_t& r1, uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];"
+               : "=r"(r0), "=r"(r1)
+               : "r"(at)
+               : "memory");
+}
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <int D, bool kScore>
+template <int D_, int kR_>
 struct RowsBf16 {
-  static constexpr int kC = D / 32;     // 16-byte pieces of a key's row per lane
-  static constexpr int kV = D / 64;     // of a value's row
-  static constexpr int kQBytes = D / 16 * 32 * 8;   // Q fragments of a row tile
+  using T = __nv_bfloat16;
+  static constexpr int D = D_, kR = kR_;
+  static constexpr bool kSplit8 = kR == 8;
+  static constexpr int kM = kR == 32 ? 2 : 1;      // row tiles
+  static constexpr int kTile = 16;
+  static constexpr int kRowBytes = D * 2;
+  static constexpr bool kSwizzle = true;
+  static constexpr int kStage = 2 * kTile * kRowBytes;
+  static constexpr int kQBytes = kR * kRowBytes;
+  static constexpr int kQPieces = kQBytes / 16;
+  static constexpr int kBufRows = kR < 16 ? kR : 16;     // rows of O in a free stage
   static constexpr int kWarpBytes = 0;
-  static constexpr int kStride = D + 4; // row stride of the CTA's O buffer
 
-  float m, l;
-  float o[kV][8][4];
+  float m[kM][2], l[kM][2];        // of rows g and g + 8 of a row tile
+  float o[kM][D / 8][4];
 
-  // Q's fragments of one row tile: per step of 16 d values and lane, the pairs
-  // a lane multiplies with the two words of its key piece.
-  __device__ static void stage_q(const CacheAttn& a, const Unit& u, char* sq, int lane) {
-    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + (int64_t)u.b * a.q_sb;
-    const int g = lane >> 2, t = lane & 3;
-    const bool ok = g < u.rows;
-    const __nv_bfloat16* row = q + (int64_t)(u.hk * a.G + u.row0 + (ok ? g : 0)) * a.q_sh;
-    uint2* out = reinterpret_cast<uint2*>(sq);
+  // 16 bytes of Q: piece i of the unit's rows
+  __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, int b, int h0, int rows,
+                                                 int i) {
+    const int row = i / (D / 8), d = (i % (D / 8)) * 8;
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if (row < rows && d < a.c.d) {
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)b * a.q_sb +
+                          (int64_t)(h0 + row) * a.q_sh + d;
+      if ((reinterpret_cast<uintptr_t>(q) & 15u) == 0) return *reinterpret_cast<const uint4*>(q);
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      const int d0 = (s >> 1) * 32 + t * 8 + (s & 1) * 4;
-      uint32_t w[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int dd = d0 + 2 * i;
-        uint32_t x = 0u;
-        if (ok && dd < a.c.d)
-          x = (uint32_t)__bfloat16_as_ushort(row[dd]) |
-              ((uint32_t)__bfloat16_as_ushort(row[dd + 1]) << 16);
-        w[i] = x;
-      }
-      out[s * 32 + lane] = make_uint2(w[0], w[1]);
+      for (int k = 0; k < 4; ++k) w[k] = (uint32_t)q[2 * k] | ((uint32_t)q[2 * k + 1] << 16);
     }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ static __forceinline__ void store_q(char* sq, int i, const uint4& v) {
+    const int row = i / (D / 8), c = i % (D / 8);
+    *reinterpret_cast<uint4*>(sq + row * kRowBytes + ((c ^ (row & 7)) << 4)) = v;
   }
 
   __device__ __forceinline__ void reset() {
-    m = -INFINITY;
-    l = 0.f;
 #pragma unroll
-    for (int c = 0; c < kV; ++c)
+    for (int mt = 0; mt < kM; ++mt) {
+      m[mt][0] = m[mt][1] = -INFINITY;
+      l[mt][0] = l[mt][1] = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < D / 8; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[c][j][e] = 0.f;
-  }
-
-  __device__ __forceinline__ void load_k(const CacheAttn& a, const TileKeys& tk,
-                                         const __nv_bfloat16* kb, uint4 (&k)[2][kC], int lane) {
-    const int g = lane >> 2, t = lane & 3;
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const int page = __shfl_sync(0xffffffffu, tk.page, g + 8 * n);
-      const int slot = __shfl_sync(0xffffffffu, tk.slot, g + 8 * n);
-      const __nv_bfloat16* row = kb + (int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st;
-#pragma unroll
-      for (int c = 0; c < kC; ++c) {
-        k[n][c] = make_uint4(0u, 0u, 0u, 0u);
-        if (page >= 0 && c * 32 + t * 8 < a.c.d) {
-          const void* p = row + c * 32 + t * 8;
-          k[n][c] = a.rt == 1 ? ld_once(p) : ld_shared_by_warps(p);
-        }
-      }
+        for (int e = 0; e < 4; ++e) o[mt][j][e] = 0.f;
     }
   }
 
-  __device__ __forceinline__ void run(const CacheAttn& a, const Unit& u, const char* sq, char*,
-                                      int tile, int t1, int step, int lane) {
-    reset();
-    const int g = lane >> 2, t = lane & 3;
-    const int32_t* table = a.c.block_table + (int64_t)u.b * a.c.table_sb;
-    const __nv_bfloat16* kb =
-        static_cast<const __nv_bfloat16*>(a.c.k_pages) + (int64_t)u.hk * a.c.k_sh;
-    const __nv_bfloat16* vb =
-        static_cast<const __nv_bfloat16*>(a.c.v_pages) + (int64_t)u.hk * a.c.v_sh;
-    float* lg = kScore ? a.logits + ((int64_t)u.b * a.H + u.hk * a.G + u.row0 + g) * a.ld : nullptr;
-    const bool keep_logits = kScore && g < u.rows;
-    const uint2* qf = reinterpret_cast<const uint2*>(sq);
-    if (tile >= t1) return;
-    uint4 k[2][kC];
-    TileKeys tk = tile_keys(a, table_entry(a, table, tile, u.len, lane), tile, u.len, lane);
-    load_k(a, tk, kb, k, lane);
-    for (; tile < t1; tile += step) {
-      // this tile's values, and the next one's page numbers, on their way
-      uint4 v[4][kV];
-      bool live[4];
+  // one tile; lg: the logits of row g of row tile 0 at the tile's first key
+  __device__ __forceinline__ void tile(const CacheAttn& a, uint32_t kt, const char* sq, char*,
+                                       uint32_t mask, float* lg, int rows, int lane) {
+    const int g = lane >> 2, t = lane & 3, r8 = lane & 7;
+    const uint32_t vt = kt + kTile * kRowBytes;
+    const uint32_t qt = smem_u32(sq);
+    const int steps = (a.c.d + 15) / 16;
+    float s[kM][2][4] = {};
+    {
+      const int krow = r8 + ((lane >> 4) << 3), kc = (lane >> 3) & 1;
+      const int qrow = kSplit8 ? r8 : r8 + (((lane >> 3) & 1) << 3);
+      const int qc = kSplit8 ? (lane >> 3) & 1 : lane >> 4;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = 2 * t + (i & 1) + 8 * (i >> 1);
-        const int page = __shfl_sync(0xffffffffu, tk.page, key);
-        const int slot = __shfl_sync(0xffffffffu, tk.slot, key);
-        live[i] = page >= 0;
-        const __nv_bfloat16* row = vb + (int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st;
+      for (int st = 0; st < D / 16; ++st) {
+        if (st < steps) {
+          uint32_t k[4];
+          ldsm4(k, kt + krow * kRowBytes + (((2 * st + kc) ^ r8) << 4));
 #pragma unroll
-        for (int c = 0; c < kV; ++c) {
-          v[i][c] = make_uint4(0u, 0u, 0u, 0u);
-          if (live[i] && c * 64 + g * 8 < a.c.d) {
-            const void* p = row + c * 64 + g * 8;
-            v[i][c] = a.rt == 1 ? ld_once(p) : ld_shared_by_warps(p);
+          for (int mt = 0; mt < kM; ++mt) {
+            uint32_t q[4] = {0u, 0u, 0u, 0u};
+            const uint32_t at =
+                qt + (mt * 16 + qrow) * kRowBytes + (((2 * st + qc) ^ r8) << 4);
+            if (kSplit8) ldsm2(q[0], q[2], at); else ldsm4(q, at);
+            mma16816(s[mt][0], q[0], q[1], q[2], q[3], k[0], k[1]);
+            mma16816(s[mt][1], q[0], q[1], q[2], q[3], k[2], k[3]);
           }
         }
       }
-      const int next = tile + step;
-      const int entry = next < t1 ? table_entry(a, table, next, u.len, lane) : -1;
-      float s[2][4] = {};
+    }
+    // keys 2t, 2t+1 (s[.][0]) and 8+2t, 9+2t (s[.][1]); rows g (e 0, 1), g + 8 (e 2, 3)
+    const unsigned here = mask >> (2 * t);
+    uint32_t p[kM][4], r[kM][4];     // A fragments of the weights and their rests
+    bool raise = false;
+    float top[kM][2];
 #pragma unroll
-      for (int c = 0; c < kC; ++c) {
-        const uint2 q0 = qf[(2 * c) * 32 + lane], q1 = qf[(2 * c + 1) * 32 + lane];
+    for (int mt = 0; mt < kM; ++mt) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          mma16816(s[n], q0.x, 0u, q0.y, 0u, k[n][c].x, k[n][c].y);
-          mma16816(s[n], q1.x, 0u, q1.y, 0u, k[n][c].z, k[n][c].w);
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s[mt][n][e] = (here >> (8 * n + (e & 1))) & 1u ? s[mt][n][e] * a.scale2 : -INFINITY;
+      if (a.score) {
+#pragma unroll
+        for (int hf = 0; hf < (kSplit8 ? 1 : 2); ++hf) {
+          const int row = mt * 16 + hf * 8 + g;
+          if (row < rows) {
+            float2* to = reinterpret_cast<float2*>(lg + (int64_t)(mt * 16 + hf * 8) * a.ld + 2 * t);
+            to[0] = make_float2(s[mt][0][2 * hf], s[mt][0][2 * hf + 1]);
+            to[4] = make_float2(s[mt][1][2 * hf], s[mt][1][2 * hf + 1]);
+          }
         }
       }
-      if (next < t1) {
-        tk = tile_keys(a, entry, next, u.len, lane);
-        load_k(a, tk, kb, k, lane);
+#pragma unroll
+      for (int hf = 0; hf < (kSplit8 ? 1 : 2); ++hf) {
+        float x = fmaxf(fmaxf(s[mt][0][2 * hf], s[mt][0][2 * hf + 1]),
+                        fmaxf(s[mt][1][2 * hf], s[mt][1][2 * hf + 1]));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+        top[mt][hf] = x;
+        raise |= x > m[mt][hf];
       }
-      // keys 2t, 2t+1 (s[0]) and 8+2t, 9+2t (s[1]) of row g
-      float x[4];
+    }
+    if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = live[i] ? s[i >> 1][i & 1] * a.scale2 : -INFINITY;
-      if (keep_logits) {
-        float2* to = reinterpret_cast<float2*>(lg + (int64_t)tile * kTile + 2 * t);
-        to[0] = make_float2(x[0], x[1]);
-        to[4] = make_float2(x[2], x[3]);
-      }
-      float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      if (__any_sync(0xffffffffu, top > m)) {
-        const float mn = fmaxf(m, top);
-        const float f = mn == m ? 1.f : ex2(m - mn);   // m = -inf: 0
-        m = mn;
-        l *= f;
+      for (int mt = 0; mt < kM; ++mt) {
+        float f[2] = {1.f, 1.f};
 #pragma unroll
-        for (int c = 0; c < kV; ++c)
+        for (int hf = 0; hf < (kSplit8 ? 1 : 2); ++hf) {
+          const float mn = fmaxf(m[mt][hf], top[mt][hf]);
+          f[hf] = mn == m[mt][hf] ? 1.f : ex2(m[mt][hf] - mn);   // from -inf: 0
+          m[mt][hf] = mn;
+          l[mt][hf] *= f[hf];
+        }
+        if (kSplit8) f[1] = f[0];
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[c][j][e] *= f;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      float p[4], r[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[i] = ex2(x[i] - ref);
-        l += p[i];
-        r[i] = p[i] - __bfloat162float(__float2bfloat16_rn(p[i]));
-      }
-      const uint32_t a0 = pack_bf16(p[0], p[1]), a2 = pack_bf16(p[2], p[3]);
-      const uint32_t a1 = pack_bf16(r[0], r[1]), a3 = pack_bf16(r[2], r[3]);
-#pragma unroll
-      for (int c = 0; c < kV; ++c) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t v0 = (&v[0][c].x)[w], v1 = (&v[1][c].x)[w];
-          const uint32_t v2 = (&v[2][c].x)[w], v3 = (&v[3][c].x)[w];
-          mma16816(o[c][2 * w], a0, a1, a2, a3, __byte_perm(v0, v1, 0x5410),
-                   __byte_perm(v2, v3, 0x5410));
-          mma16816(o[c][2 * w + 1], a0, a1, a2, a3, __byte_perm(v0, v1, 0x7632),
-                   __byte_perm(v2, v3, 0x7632));
+        for (int j = 0; j < D / 8; ++j) {
+          o[mt][j][0] *= f[0];
+          o[mt][j][1] *= f[0];
+          o[mt][j][2] *= f[1];
+          o[mt][j][3] *= f[1];
         }
       }
     }
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
+#pragma unroll
+    for (int mt = 0; mt < kM; ++mt) {
+      float rest[2][4];
+#pragma unroll
+      for (int hf = 0; hf < (kSplit8 ? 1 : 2); ++hf) {
+        const float ref = m[mt][hf] == -INFINITY ? 0.f : m[mt][hf];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float x = ex2(s[mt][n][2 * hf + e] - ref);
+            l[mt][hf] += x;
+            s[mt][n][2 * hf + e] = x;
+            rest[n][2 * hf + e] = x - __bfloat162float(__float2bfloat16_rn(x));
+          }
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        p[mt][2 * n] = pack_bf16(s[mt][n][0], s[mt][n][1]);
+        r[mt][2 * n] = pack_bf16(rest[n][0], rest[n][1]);
+        if (kSplit8) {
+          p[mt][2 * n + 1] = r[mt][2 * n];
+        } else {
+          p[mt][2 * n + 1] = pack_bf16(s[mt][n][2], s[mt][n][3]);
+          r[mt][2 * n + 1] = pack_bf16(rest[n][2], rest[n][3]);
+        }
+      }
+    }
+    {
+      const int vrow = r8 + (((lane >> 3) & 1) << 3), vc = lane >> 4;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        if (j < steps) {
+          uint32_t v[4];
+          ldsm4t(v, vt + vrow * kRowBytes + (((2 * j + vc) ^ r8) << 4));
+#pragma unroll
+          for (int mt = 0; mt < kM; ++mt) {
+            mma16816(o[mt][2 * j], p[mt][0], p[mt][1], p[mt][2], p[mt][3], v[0], v[1]);
+            mma16816(o[mt][2 * j + 1], p[mt][0], p[mt][1], p[mt][2], p[mt][3], v[2], v[3]);
+            if (!kSplit8) {
+              mma16816(o[mt][2 * j], r[mt][0], r[mt][1], r[mt][2], r[mt][3], v[0], v[1]);
+              mma16816(o[mt][2 * j + 1], r[mt][0], r[mt][1], r[mt][2], r[mt][3], v[2], v[3]);
+            }
+          }
+        }
+      }
+    }
   }
 
-  // (maximum, sum) of the warp's rows, one lane per row
-  __device__ __forceinline__ void put_ml(float2* ml, int lane) const {
-    if ((lane & 3) == 0) ml[lane >> 2] = make_float2(m, l);
-  }
-  // O times f(row) into the CTA's buffer
-  __device__ __forceinline__ void put_o(float* buf, const float* f, int lane) const {
+  // rows [16 part, 16 part + kBufRows) of this warp: (maximum, sum), and O
+  __device__ __forceinline__ void put(int part, float2* ml, float* buf, int lane) {
     const int g = lane >> 2, t = lane & 3;
-    const float fr = f[g];
 #pragma unroll
-    for (int c = 0; c < kV; ++c) {
-      float4* to = reinterpret_cast<float4*>(buf + g * kStride + c * 64 + 16 * t);
+    for (int mt = 0; mt < kM; ++mt) {
+      if (mt != part) continue;
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int hf = 0; hf < (kSplit8 ? 1 : 2); ++hf) {
+        float x = l[mt][hf];
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        if (t == 0) ml[g + 8 * hf] = make_float2(m[mt][hf], x);
+      }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float4 x;
-          float* px = &x.x;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) px[j] = (o[c][4 * h + j][e] + o[c][4 * h + j][e + 2]) * fr;
-          to[2 * e + h] = x;
+      for (int j = 0; j < D / 8; ++j) {
+        const float* x = o[mt][j];
+        if (kSplit8) {
+          *reinterpret_cast<float2*>(buf + o_at(g, 8 * j + 2 * t, D)) =
+              make_float2(x[0] + x[2], x[1] + x[3]);
+        } else {
+          *reinterpret_cast<float2*>(buf + o_at(g, 8 * j + 2 * t, D)) = make_float2(x[0], x[1]);
+          *reinterpret_cast<float2*>(buf + o_at(g + 8, 8 * j + 2 * t, D)) =
+              make_float2(x[2], x[3]);
         }
+      }
     }
   }
 };
 
 // ------------------------------------------------------------------ fp32 --
-// CUDA cores in fp32.  Q K^T: 8 lanes to a key (16-byte pieces of its row), 4
-// keys at a time; a lane's partial dot products of the 8 heads are summed over
-// the 8 lanes by halving, which leaves head lane % 8 with the lane.  P V: a
-// lane owns columns of O and reads the weights from shared memory.
-template <int D, bool kScore>
+// CUDA cores in fp32, 8 heads.  Q K^T: 8 lanes to a key (16-byte pieces of its
+// row), 4 keys at a time; a lane's partial dot products of the 8 heads are
+// summed over the 8 lanes by halving, which leaves head lane % 8 with the lane.
+// P V: a lane owns columns of O and reads the weights from shared memory.
+template <int D_, int>
 struct RowsF32 {
-  static constexpr int kC = D / 32;
+  using T = float;
+  static constexpr int D = D_, kR = 8;
+  static constexpr int kTile = 8;
+  static constexpr int kRowBytes = D * 4;
+  static constexpr bool kSwizzle = false;
+  static constexpr int kStage = 2 * kTile * kRowBytes;
+  static constexpr int kQBytes = kR * kRowBytes;
+  static constexpr int kQPieces = kQBytes / 16;
+  static constexpr int kBufRows = kR, kM = 1;
+  static constexpr int kWarpBytes = kTile * 8 * 4;
   static constexpr int kKeysPerV = D >= 128 ? 1 : 128 / D;   // value rows read side by side
   static constexpr int kV = D >= 128 ? D / 128 : 1;
-  static constexpr int kBlock = kC < 4 ? kC : 4;             // pieces of a key in registers
-  static constexpr int kQBytes = 8 * D * 4;
-  static constexpr int kWarpBytes = kTile * 8 * 4;
-  static constexpr int kStride = D + 4;
 
   float m, l;            // of row lane % 8; l: this lane's keys only until the end
   float o[8][kV][4];
 
-  __device__ static void stage_q(const CacheAttn& a, const Unit& u, char* sq, int lane) {
-    const float* q = static_cast<const float*>(a.q) + (int64_t)u.b * a.q_sb;
-    float* out = reinterpret_cast<float*>(sq);
-#pragma unroll 1
-    for (int g = 0; g < 8; ++g) {
-      const float* row = q + (int64_t)(u.hk * a.G + u.row0 + (g < u.rows ? g : 0)) * a.q_sh;
-      for (int d = lane; d < D; d += 32) out[g * D + d] = g < u.rows && d < a.c.d ? row[d] : 0.f;
-    }
+  __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, int b, int h0, int rows,
+                                                 int i) {
+    const int row = i / (D / 4), d = (i % (D / 4)) * 4;
+    if (row >= rows || d >= a.c.d) return make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t* q = static_cast<const uint32_t*>(a.q) + (int64_t)b * a.q_sb +
+                        (int64_t)(h0 + row) * a.q_sh + d;
+    return make_uint4(q[0], q[1], q[2], q[3]);
+  }
+  __device__ static __forceinline__ void store_q(char* sq, int i, const uint4& v) {
+    reinterpret_cast<uint4*>(sq)[i] = v;
   }
 
-  __device__ __forceinline__ void run(const CacheAttn& a, const Unit& u, const char* sq, char* sw,
-                                      int tile, int t1, int step, int lane) {
+  __device__ __forceinline__ void reset() {
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
@@ -337,180 +445,150 @@ struct RowsF32 {
       for (int c = 0; c < kV; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[g][c][e] = 0.f;
-    const int kg = lane >> 3, t8 = lane & 7;
-    const int32_t* table = a.c.block_table + (int64_t)u.b * a.c.table_sb;
-    const float* kb = static_cast<const float*>(a.c.k_pages) + (int64_t)u.hk * a.c.k_sh;
-    const float* vb = static_cast<const float*>(a.c.v_pages) + (int64_t)u.hk * a.c.v_sh;
-    const float* q = reinterpret_cast<const float*>(sq);
-    float* sp = reinterpret_cast<float*>(sw);
-    float* lg = kScore ? a.logits + ((int64_t)u.b * a.H + u.hk * a.G + u.row0 + t8) * a.ld : nullptr;
-    const bool keep_logits = kScore && t8 < u.rows;
-    for (; tile < t1; tile += step) {
-      const TileKeys tk = tile_keys(a, table_entry(a, table, tile, u.len, lane), tile, u.len, lane);
-      // a lane's keys: kg*4 .. kg*4+3
-      const float* row[4];
-      bool live[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int page = __shfl_sync(0xffffffffu, tk.page, kg * 4 + i);
-        const int slot = __shfl_sync(0xffffffffu, tk.slot, kg * 4 + i);
-        live[i] = page >= 0;
-        row[i] = kb + (int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st;
-      }
-      float s[4][8] = {};
-#pragma unroll 1
-      for (int cb = 0; cb < kC; cb += kBlock) {
-        float4 k[4][kBlock];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int c = 0; c < kBlock; ++c) {
-            const int d = (cb + c) * 32 + t8 * 4;
-            k[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (live[i] && d < a.c.d) {
-              const uint4 w = ld_shared_by_warps(row[i] + d);
-              k[i][c] = make_float4(__uint_as_float(w.x), __uint_as_float(w.y),
-                                    __uint_as_float(w.z), __uint_as_float(w.w));
-            }
-          }
-#pragma unroll
-        for (int g = 0; g < 8; ++g)
-#pragma unroll
-          for (int c = 0; c < kBlock; ++c) {
-            const float4 qv =
-                *reinterpret_cast<const float4*>(q + g * D + (cb + c) * 32 + t8 * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              s[i][g] = fmaf(qv.x, k[i][c].x, fmaf(qv.y, k[i][c].y,
-                        fmaf(qv.z, k[i][c].z, fmaf(qv.w, k[i][c].w, s[i][g]))));
-          }
-      }
-      float x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float h4[4], h2[2];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float mine = (t8 & 4) ? s[i][j + 4] : s[i][j], give = (t8 & 4) ? s[i][j] : s[i][j + 4];
-          h4[j] = mine + __shfl_xor_sync(0xffffffffu, give, 4);
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float mine = (t8 & 2) ? h4[j + 2] : h4[j], give = (t8 & 2) ? h4[j] : h4[j + 2];
-          h2[j] = mine + __shfl_xor_sync(0xffffffffu, give, 2);
-        }
-        const float mine = (t8 & 1) ? h2[1] : h2[0], give = (t8 & 1) ? h2[0] : h2[1];
-        const float dot = mine + __shfl_xor_sync(0xffffffffu, give, 1);
-        x[i] = live[i] ? dot * a.scale2 : -INFINITY;
-      }
-      if (keep_logits)
-        *reinterpret_cast<float4*>(lg + (int64_t)tile * kTile + kg * 4) =
-            make_float4(x[0], x[1], x[2], x[3]);
-      float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-      if (__any_sync(0xffffffffu, top > m)) {
-        const float mn = fmaxf(m, top);
-        const float f = mn == m ? 1.f : ex2(m - mn);
-        m = mn;
-        l *= f;
-#pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          const float fg = __shfl_sync(0xffffffffu, f, g);
-#pragma unroll
-          for (int c = 0; c < kV; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[g][c][e] *= fg;
-        }
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = ex2(x[i] - ref);
-        l += p;
-        sp[(kg * 4 + i) * 8 + t8] = p;
-      }
-      __syncwarp();
-      const int sub = kKeysPerV == 1 ? 0 : lane / (32 / kKeysPerV);
-      const int col = kKeysPerV == 1 ? lane * 4 : (lane % (32 / kKeysPerV)) * 4;
-#pragma unroll 1
-      for (int j0 = 0; j0 < kTile; j0 += 8) {
-        float4 v[8 / kKeysPerV][kV];
-#pragma unroll
-        for (int j = 0; j < 8 / kKeysPerV; ++j) {
-          const int key = j0 + j * kKeysPerV + sub;
-          const int page = __shfl_sync(0xffffffffu, tk.page, key);
-          const int slot = __shfl_sync(0xffffffffu, tk.slot, key);
-          const float* vr = vb + (int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st;
-#pragma unroll
-          for (int c = 0; c < kV; ++c) {
-            v[j][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (page >= 0 && col + c * 128 < a.c.d) {
-              const uint4 w = ld_shared_by_warps(vr + col + c * 128);
-              v[j][c] = make_float4(__uint_as_float(w.x), __uint_as_float(w.y),
-                                    __uint_as_float(w.z), __uint_as_float(w.w));
-            }
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 8 / kKeysPerV; ++j) {
-          const float4* pp =
-              reinterpret_cast<const float4*>(sp + (j0 + j * kKeysPerV + sub) * 8);
-          const float4 pa = pp[0], pb = pp[1];
-          const float p[8] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
-#pragma unroll
-          for (int g = 0; g < 8; ++g)
-#pragma unroll
-            for (int c = 0; c < kV; ++c) {
-              o[g][c][0] = fmaf(p[g], v[j][c].x, o[g][c][0]);
-              o[g][c][1] = fmaf(p[g], v[j][c].y, o[g][c][1]);
-              o[g][c][2] = fmaf(p[g], v[j][c].z, o[g][c][2]);
-              o[g][c][3] = fmaf(p[g], v[j][c].w, o[g][c][3]);
-            }
-        }
-      }
-    }
-    l += __shfl_xor_sync(0xffffffffu, l, 8);
-    l += __shfl_xor_sync(0xffffffffu, l, 16);
-    if (kKeysPerV > 1) {
-#pragma unroll
-      for (int g = 0; g < 8; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          o[g][0][e] += __shfl_xor_sync(0xffffffffu, o[g][0][e], 16);
-    }
   }
 
-  __device__ __forceinline__ void put_ml(float2* ml, int lane) const {
-    if (lane < 8) ml[lane] = make_float2(m, l);
+  __device__ __forceinline__ void tile(const CacheAttn& a, uint32_t, const char* sq, char* sw,
+                                       uint32_t mask, float* lg, int rows, int lane,
+                                       const char* st) {
+    const int kg = lane >> 3, t8 = lane & 7;
+    const float* q = reinterpret_cast<const float*>(sq);
+    const float* kt = reinterpret_cast<const float*>(st);
+    const float* vt = kt + kTile * D;
+    float* sp = reinterpret_cast<float*>(sw);
+    // a lane's keys: 2 kg, 2 kg + 1
+    float s[2][8] = {};
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      const int d = c * 32 + t8 * 4;
+      if (d < a.c.d) {
+        const float4 k0 = *reinterpret_cast<const float4*>(kt + (2 * kg) * D + d);
+        const float4 k1 = *reinterpret_cast<const float4*>(kt + (2 * kg + 1) * D + d);
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          const float4 qv = *reinterpret_cast<const float4*>(q + g * D + d);
+          s[0][g] = fmaf(qv.x, k0.x, fmaf(qv.y, k0.y, fmaf(qv.z, k0.z, fmaf(qv.w, k0.w, s[0][g]))));
+          s[1][g] = fmaf(qv.x, k1.x, fmaf(qv.y, k1.y, fmaf(qv.z, k1.z, fmaf(qv.w, k1.w, s[1][g]))));
+        }
+      }
+    }
+    float x[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float h4[4], h2[2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float mine = (t8 & 4) ? s[i][j + 4] : s[i][j], give = (t8 & 4) ? s[i][j] : s[i][j + 4];
+        h4[j] = mine + __shfl_xor_sync(0xffffffffu, give, 4);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float mine = (t8 & 2) ? h4[j + 2] : h4[j], give = (t8 & 2) ? h4[j] : h4[j + 2];
+        h2[j] = mine + __shfl_xor_sync(0xffffffffu, give, 2);
+      }
+      const float mine = (t8 & 1) ? h2[1] : h2[0], give = (t8 & 1) ? h2[0] : h2[1];
+      const float dot = mine + __shfl_xor_sync(0xffffffffu, give, 1);
+      x[i] = (mask >> (2 * kg + i)) & 1u ? dot * a.scale2 : -INFINITY;
+    }
+    if (a.score && t8 < rows)
+      *reinterpret_cast<float2*>(lg + 2 * kg) = make_float2(x[0], x[1]);
+    float top = fmaxf(x[0], x[1]);
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+    if (__any_sync(0xffffffffu, top > m)) {
+      const float mn = fmaxf(m, top);
+      const float f = mn == m ? 1.f : ex2(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        const float fg = __shfl_sync(0xffffffffu, f, g);
+#pragma unroll
+        for (int c = 0; c < kV; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[g][c][e] *= fg;
+      }
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float p = ex2(x[i] - ref);
+      l += p;
+      sp[(2 * kg + i) * 8 + t8] = p;
+    }
+    __syncwarp();
+    const int sub = kKeysPerV == 1 ? 0 : lane / (32 / kKeysPerV);
+    const int col = kKeysPerV == 1 ? lane * 4 : (lane % (32 / kKeysPerV)) * 4;
+#pragma unroll
+    for (int j = 0; j < kTile / kKeysPerV; ++j) {
+      const int key = j * kKeysPerV + sub;
+      const float4* pp = reinterpret_cast<const float4*>(sp + key * 8);
+      const float4 pa = pp[0], pb = pp[1];
+      const float p[8] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+      for (int c = 0; c < kV; ++c) {
+        const float4 v = *reinterpret_cast<const float4*>(vt + key * D + col + c * 128);
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          o[g][c][0] = fmaf(p[g], v.x, o[g][c][0]);
+          o[g][c][1] = fmaf(p[g], v.y, o[g][c][1]);
+          o[g][c][2] = fmaf(p[g], v.z, o[g][c][2]);
+          o[g][c][3] = fmaf(p[g], v.w, o[g][c][3]);
+        }
+      }
+    }
   }
-  __device__ __forceinline__ void put_o(float* buf, const float* f, int lane) const {
-    if (kKeysPerV > 1 && lane >= 16) return;
+  __device__ __forceinline__ void put(int, float2* ml, float* buf, int lane) {
+    float x = l;
+    x += __shfl_xor_sync(0xffffffffu, x, 8);
+    x += __shfl_xor_sync(0xffffffffu, x, 16);
+    if (lane < 8) ml[lane] = make_float2(m, x);
 #pragma unroll
     for (int g = 0; g < 8; ++g)
 #pragma unroll
       for (int c = 0; c < kV; ++c) {
-        const float fr = f[g];
-        *reinterpret_cast<float4*>(buf + g * kStride + lane * 4 + c * 128) = make_float4(
-            o[g][c][0] * fr, o[g][c][1] * fr, o[g][c][2] * fr, o[g][c][3] * fr);
+        float4 v = make_float4(o[g][c][0], o[g][c][1], o[g][c][2], o[g][c][3]);
+        if (kKeysPerV > 1) {
+          v.x += __shfl_xor_sync(0xffffffffu, v.x, 16);
+          v.y += __shfl_xor_sync(0xffffffffu, v.y, 16);
+          v.z += __shfl_xor_sync(0xffffffffu, v.z, 16);
+          v.w += __shfl_xor_sync(0xffffffffu, v.w, 16);
+          if (lane >= 16) continue;
+        }
+        *reinterpret_cast<float4*>(buf + o_at(g, lane * 4 + c * 128, D)) = v;
       }
   }
 };
 
 // ----------------------------------------------------------- first kernel --
+// Stages of a warp's ring: three tiles where two CTAs' rings fit an SM.
 template <typename Rows>
-constexpr size_t smem_bytes(int rt) {
-  return (size_t)kWarps * 8 * Rows::kStride * 4 + (size_t)rt * Rows::kQBytes +
-         (size_t)kWarps * Rows::kWarpBytes;
+constexpr int stages() { return Rows::kStage <= 4096 ? 4 : 3; }
+template <typename Rows>
+constexpr int ctas_per_sm() { return Rows::kStage <= 8192 ? 2 : 1; }
+template <typename Rows>
+constexpr int smem_bytes() {
+  return kWarps * stages<Rows>() * Rows::kStage + Rows::kQBytes + kWarps * Rows::kWarpBytes;
 }
 
-template <typename T, int D, typename Rows, int kMinCtas>
-__global__ void __launch_bounds__(kThreads, kMinCtas)
+template <typename Rows>
+__device__ __forceinline__ void one_tile(Rows& r, const CacheAttn& a, const char* st, const char* sq,
+                                         char* sw, uint32_t mask, float* lg, int rows, int lane) {
+  if constexpr (Rows::kSwizzle)
+    r.tile(a, smem_u32(st), sq, sw, mask, lg, rows, lane);
+  else
+    r.tile(a, 0u, sq, sw, mask, lg, rows, lane, st);
+}
+
+template <typename Rows>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm<Rows>())
 cache_attention_kernel(const __grid_constant__ CacheAttn a) {
-  extern __shared__ __align__(16) char smem[];
-  __shared__ float2 s_ml[kWarps][8];
-  __shared__ float s_f[kWarps][8];
+  using T = typename Rows::T;
+  constexpr int D = Rows::D, kR = Rows::kR, kTile = Rows::kTile, NS = stages<Rows>();
+  extern __shared__ __align__(128) char smem[];
+  __shared__ float2 s_ml[2][kWarps][Rows::kBufRows];
+  __shared__ int s_free[2][kWarps];
+  __shared__ uint32_t s_mask[kWarps][NS];
   __shared__ int s_scan[kWarps], s_b, s_off;
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
   pdl_wait_then_trigger();
@@ -521,7 +599,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
   const int b0 = min(B, tid * each), b1 = min(B, b0 + each);
   int sum = 0;
   for (int b = b0; b < b1; ++b) {
-    sum += tiles_of(a, b) * units;
+    sum += tiles_of(a, cache_len(a.c, b)) * units;
     if (blockIdx.x == 0) check_cache_len(a.c, b, a.status);
   }
   int inc = sum;
@@ -542,7 +620,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
     int at = before;
     for (int b = b0; b < b1; ++b) {
       a.starts[b] = at;
-      at += tiles_of(a, b) * units;
+      at += tiles_of(a, cache_len(a.c, b)) * units;
     }
     if (tid == 0) a.starts[B] = total;
   }
@@ -552,91 +630,142 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
   if (before <= first && first < before + sum) {
     int at = before, b = b0;
     for (;; ++b) {
-      const int n = tiles_of(a, b) * units;
+      const int n = tiles_of(a, cache_len(a.c, b)) * units;
       if (first < at + n) break;
       at += n;
     }
     s_b = b;
     s_off = first - at;
   }
+  char* ring = smem + w * NS * Rows::kStage;
+  char* s_q = smem + kWarps * NS * Rows::kStage;
+  char* s_w = s_q + Rows::kQBytes + w * Rows::kWarpBytes;
   __syncthreads();
 
-  float* s_o = reinterpret_cast<float*>(smem);
-  char* s_q = smem + kWarps * 8 * Rows::kStride * 4;
-  char* s_w = s_q + a.rt * Rows::kQBytes + w * Rows::kWarpBytes;
-  int left = min(per, total - first), b = s_b, off = s_off;
-  const int rt = w & (a.rt - 1), step = kWarps / a.rt, lead = w / a.rt;
-  bool is_first = true;
+  int left = min(per, total - first), b = s_b;
+  int len = cache_len(a.c, b), nt = tiles_of(a, len);
+  int u = s_off / nt, t0 = s_off - u * nt;
+  Cursor cur{b, u, t0 + w, nt, len, (left - w + kWarps - 1) / kWarps, -1};
+  if (cur.left > 0) {
+    cur.settle(a, units);
+    cur.look_up<kTile>(a, lane);
+  }
+  auto h_of = [&](int uu) {      // first query head of a unit, its rows
+    const int hk = a.groups == 1 ? uu : uu / a.groups, row0 = (uu - hk * a.groups) * kR;
+    return make_int2(hk * a.G + row0, min(kR, a.G - row0));
+  };
+  {
+    const int2 h = h_of(u);
+    for (int i = tid; i < Rows::kQPieces; i += kThreads)
+      Rows::store_q(s_q, i, Rows::load_q(a, b, h.x, h.y, i));
+  }
+  const uint32_t ring_at = smem_u32(ring);
+  // stage `fill` is the free one: the tile after the last issued goes there
+  int fill = 0, use = 0;
+  auto issue = [&]() {
+    if (cur.left > 0)
+      copy_tile<kTile, Rows::kRowBytes, Rows::kSwizzle>(a, cur, ring_at + fill * Rows::kStage,
+                                                        &s_mask[w][fill], units, lane);
+    cp_commit();
+    fill = fill + 1 == NS ? 0 : fill + 1;
+  };
+#pragma unroll 1
+  for (int i = 0; i < NS - 1; ++i) issue();
+  __syncthreads();      // Q is there
+
+  constexpr int kQEach = (Rows::kQPieces + kThreads - 1) / kThreads;
+  int f0 = 0, seg = 0;
   Rows rows;
   while (left > 0) {
-    Unit u;
-    u.len = cache_len(a.c, b);
-    const int nt = (u.len + kTile - 1) / kTile;
-    if (nt == 0) {
-      ++b;
-      continue;
+    const int t1 = min(nt, t0 + left);
+    const int2 h = h_of(u);
+    // the next unit, and its Q on the way
+    int nb = b, nu = u + 1, nlen = len, nnt = nt;
+    const int after = left - (t1 - t0);
+    uint4 nq[kQEach];
+    if (after > 0) {
+      if (nu == units) {
+        nu = 0;
+        do {
+          nlen = cache_len(a.c, ++nb);
+          nnt = tiles_of(a, nlen);
+        } while (nnt == 0);
+      }
+      const int2 nh = h_of(nu);
+#pragma unroll
+      for (int k = 0; k < kQEach; ++k)
+        if (tid + k * kThreads < Rows::kQPieces)
+          nq[k] = Rows::load_q(a, nb, nh.x, nh.y, tid + k * kThreads);
     }
-    const int unit = off / nt, t0 = off - unit * nt, t1 = min(nt, t0 + left);
-    const int rg = unit % a.groups;
-    u.b = b;
-    u.hk = unit / a.groups;
-    u.row0 = (rg * a.rt + rt) * 8;
-    u.rows = a.G - u.row0;
-    if (lead == 0) Rows::stage_q(a, u, s_q + rt * Rows::kQBytes, lane);
-    __syncthreads();   // Q is there; everybody is done with the last unit's buffers
-    rows.run(a, u, s_q + rt * Rows::kQBytes, s_w, t0 + lead, u.rows > 0 ? t1 : 0, step, lane);
-    rows.put_ml(s_ml[w], lane);
-    __syncthreads();
-    if (lane < 8) {   // this warp's rows relative to the row's maximum over the warps
-      float top = -INFINITY;
-      for (int i = rt; i < kWarps; i += a.rt) top = fmaxf(top, s_ml[i][lane].x);
-      const float mine = s_ml[w][lane].x;
-      s_f[w][lane] = mine == -INFINITY ? 0.f : ex2(mine - top);
+    rows.reset();
+    const int lrow = Rows::kSwizzle ? lane >> 2 : lane & 7;
+    float* lg = a.score ? a.logits + ((int64_t)b * a.H + h.x + lrow) * a.ld : nullptr;
+#pragma unroll 1
+    for (int t = t0 + ((w - f0) & (kWarps - 1)); t < t1; t += kWarps) {
+      __syncwarp();
+      issue();
+      cp_wait<NS - 1>();
+      __syncwarp();
+      one_tile(rows, a, ring + use * Rows::kStage, s_q, s_w, s_mask[w][use],
+               a.score ? lg + t * kTile : nullptr, h.y, lane);
+      use = use + 1 == NS ? 0 : use + 1;
     }
-    __syncwarp();
-    rows.put_o(s_o + w * 8 * Rows::kStride, s_f[w], lane);
-    __syncthreads();
-    // sum over the warps, and out: finished, or as this piece's part
+    // the warps meet: each leaves its rows in the free stage of its ring
     const bool whole = t0 == 0 && t1 == nt;
-    const int slot = 2 * blockIdx.x + (is_first ? 0 : 1);
-    const int nrow = 8 * a.rt;
-    for (int i = tid; i < nrow * (D / 4); i += kThreads) {
-      const int r = i / (D / 4), d = (i - r * (D / 4)) * 4, r8 = r & 7, wr = r >> 3;
-      const int row = rg * nrow + r;
-      if (row >= a.G || d >= a.c.d) continue;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      float top = -INFINITY, l = 0.f;
-      for (int k = wr; k < kWarps; k += a.rt) {
-        const float4 x = *reinterpret_cast<const float4*>(s_o + (k * 8 + r8) * Rows::kStride + d);
-        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-        top = fmaxf(top, s_ml[k][r8].x);
-        l += s_f[k][r8] * s_ml[k][r8].y;
+    const int slot = 2 * blockIdx.x + (seg == 0 ? 0 : 1);
+#pragma unroll
+    for (int part = 0; part < Rows::kM; ++part) {
+      const int par = (seg * Rows::kM + part) & 1;
+      __syncwarp();
+      rows.put(part, s_ml[par][w], reinterpret_cast<float*>(ring + fill * Rows::kStage), lane);
+      if (lane == 0) s_free[par][w] = (w * NS + fill) * Rows::kStage;
+      __syncthreads();
+      if (part == 0 && after > 0) {
+#pragma unroll
+        for (int k = 0; k < kQEach; ++k)
+          if (tid + k * kThreads < Rows::kQPieces) Rows::store_q(s_q, tid + k * kThreads, nq[k]);
       }
-      const int h = u.hk * a.G + row;
-      if (whole) {
-        const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
-        T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh + d;
-        store_elem(out, 0, v.x * inv);
-        store_elem(out, 1, v.y * inv);
-        store_elem(out, 2, v.z * inv);
-        store_elem(out, 3, v.w * inv);
-        if (d == 0) {
-          const float e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
-          a.lse2[(int64_t)b * a.H + h] = e;
-          if (a.lse) a.lse[(int64_t)b * a.H + h] = e * kLn2;
+      for (int i = tid; i < Rows::kBufRows * (D / 4); i += kThreads) {
+        const int r = i / (D / 4), d = (i - r * (D / 4)) * 4, row = part * 16 + r;
+        if (row >= h.y || d >= a.c.d) continue;
+        float top = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) top = fmaxf(top, s_ml[par][k][r].x);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) {
+          const float2 ml = s_ml[par][k][r];
+          const float4 x = *reinterpret_cast<const float4*>(smem + s_free[par][k] +
+                                                            o_at(r, d, D) * 4);
+          const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+          v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
+          v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+          l = fmaf(f, ml.y, l);
         }
-      } else {
-        *reinterpret_cast<float4*>(a.po + ((int64_t)slot * nrow + r) * a.c.d + d) = v;
-        if (d == 0) a.pml[slot * nrow + r] = make_float2(top, l);
+        const int hh = h.x + row;
+        if (whole) {
+          const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+          T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)hh * a.o_sh + d;
+          store_elem(out, 0, v.x * inv);
+          store_elem(out, 1, v.y * inv);
+          store_elem(out, 2, v.z * inv);
+          store_elem(out, 3, v.w * inv);
+          if (d == 0) {
+            const float e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
+            a.lse2[(int64_t)b * a.H + hh] = e;
+            if (a.lse) a.lse[(int64_t)b * a.H + hh] = e * kLn2;
+          }
+        } else {
+          *reinterpret_cast<float4*>(a.po + ((int64_t)slot * kR + row) * a.c.d + d) = v;
+          if (d == 0) a.pml[slot * kR + row] = make_float2(top, l);
+        }
       }
+      __syncthreads();     // the free stages are free again
     }
-    is_first = false;
-    left -= t1 - t0;
-    off += t1 - t0;
-    if (off == nt * units) {
-      ++b;
-      off = 0;
-    }
+    ++seg;
+    f0 += t1 - t0;
+    left = after;
+    b = nb; u = nu; len = nlen; nt = nnt; t0 = 0;
   }
 }
 
@@ -648,15 +777,15 @@ constexpr int kMaxGroup = 256;
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads)
-cache_join_kernel(const __grid_constant__ CacheAttn a, int parts, int keys, int score) {
+cache_join_kernel(const __grid_constant__ CacheAttn a, int parts, int keys) {
   __shared__ float s_lse2[kMaxGroup];
   __shared__ float4 s_sum[kJoinThreads];
   pdl_wait_then_trigger();
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
   const int bh = blockIdx.x / parts, part = blockIdx.x - bh * parts;
   const int b = bh / a.c.Hkv, hk = bh - b * a.c.Hkv;
-  const int len = cache_len(a.c, b), nt = (len + kTile - 1) / kTile;
-  const int nrow = 8 * a.rt, d4 = a.c.d / 4;
+  const int len = cache_len(a.c, b), nt = tiles_of(a, len);
+  const int nrow = a.rows, d4 = a.c.d / 4;
   if (nt == 0) {
     for (int r = part; r < a.G; r += parts) {
       const int h = hk * a.G + r;
@@ -698,19 +827,34 @@ cache_join_kernel(const __grid_constant__ CacheAttn a, int parts, int keys, int 
     if (lane == 0) s_lse2[r] = e;
   }
   __syncthreads();
-  if (score) {
+  if (a.score) {
     const int j1 = min(len, (part + 1) * keys);
     float* acc = a.c.acc + (int64_t)b * a.c.acc_sb + (int64_t)hk * a.c.acc_sh;
     const float* lg = a.logits + ((int64_t)b * a.H + hk * a.G) * a.ld;
-    for (int j = part * keys + tid; j < j1; j += kJoinThreads) {
-      float s = 0.f;
-      for (int r = 0; r < a.G; ++r) {
-        const float e = s_lse2[r];
-        // nothing to attend to (every page out of range): no weight
-        s += e == -INFINITY ? 0.f : ex2(lg[(int64_t)r * a.ld + j] - e);
+    constexpr int kDeep = 4;     // keys of a thread at once
+    for (int j0 = part * keys + tid; j0 < j1; j0 += kDeep * kJoinThreads) {
+      float s[kDeep] = {}, old[kDeep] = {};
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) {
+        const int j = j0 + k * kJoinThreads;
+        if (a.add && j < j1) old[k] = acc[j];
       }
-      s *= a.wmean;
-      acc[j] = a.add ? acc[j] + s : s;
+#pragma unroll 4
+      for (int r = 0; r < a.G; ++r) {
+        // nothing to attend to (every page out of range): no weight
+        const float e = s_lse2[r] == -INFINITY ? INFINITY : s_lse2[r];
+        float x[kDeep];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k)
+          x[k] = lg[(int64_t)r * a.ld + min(j0 + k * kJoinThreads, j1 - 1)];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) s[k] += ex2(x[k] - e);
+      }
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) {
+        const int j = j0 + k * kJoinThreads;
+        if (j < j1) acc[j] = fmaf(s[k], a.wmean, old[k]);
+      }
     }
   }
   // O of the rows that were cut
@@ -752,23 +896,26 @@ cache_join_kernel(const __grid_constant__ CacheAttn a, int parts, int keys, int 
   }
 }
 
-constexpr int ctas_per_sm(int D) { return D <= 128 ? 3 : 2; }
-
-int padded_d(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-
+// How a call is cut: the widths 64, 128 and 256 have kernels of their own; a
+// unit has 8 rows (fp32), or 8, 16 or 32 by the group's size (bf16), so that a
+// tile in shared memory serves all the heads that share it (256 columns: 16 at
+// most, by registers).
 struct Shape {
-  int G, rt, groups, grid;
+  int G, D, rows, groups, tile, grid;
   long long tiles;
 };
 
 Shape shape_of(const avits_kv_cache& c, int H, int num_sms) {
   Shape s;
+  const bool bf = c.dt == AVITS_BF16;
   s.G = H / c.Hkv;
-  s.rt = s.G <= 8 ? 1 : s.G <= 16 ? 2 : 4;
-  s.groups = (s.G + 8 * s.rt - 1) / (8 * s.rt);
-  s.tiles = (long long)c.B * c.Hkv * s.groups * ((c.max_len + kTile - 1) / kTile);
+  s.D = c.d <= 64 ? 64 : c.d <= 128 ? 128 : 256;
+  s.rows = !bf || s.G <= 8 ? 8 : s.G <= 16 || s.D == 256 ? 16 : 32;
+  s.groups = (s.G + s.rows - 1) / s.rows;
+  s.tile = bf ? 16 : 8;
+  s.tiles = (long long)c.B * c.Hkv * s.groups * ((c.max_len + s.tile - 1) / s.tile);
   const long long most = (s.tiles + kMinTiles - 1) / kMinTiles;
-  const long long full = (long long)num_sms * ctas_per_sm(padded_d(c.d));
+  const long long full = (long long)num_sms * (s.D <= 128 ? 2 : 1);
   s.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
   return s;
 }
@@ -782,8 +929,8 @@ struct Layout {
 
 Layout layout_of(const avits_kv_cache& c, int H, const Shape& s, bool score) {
   Layout l;
-  const size_t nrow = 8 * s.rt;
-  l.ld = (c.max_len + kTile - 1) / kTile * (int64_t)kTile;
+  const size_t nrow = s.rows;
+  l.ld = ((int64_t)c.max_len + 15) / 16 * 16;
   l.starts = 0;
   l.lse2 = up16(((size_t)c.B + 1) * 4);
   l.pml = l.lse2 + up16((size_t)c.B * H * 4);
@@ -793,45 +940,35 @@ Layout layout_of(const avits_kv_cache& c, int H, const Shape& s, bool score) {
   return l;
 }
 
-template <typename T, int D, typename Rows>
+template <typename Rows>
 cudaError_t launch_rows(const CacheAttn& a, cudaStream_t s) {
-  constexpr int kCtas = ctas_per_sm(D);
-  constexpr auto kernel = cache_attention_kernel<T, D, Rows, kCtas>;
-  const cudaError_t e = prefer_max_shared<kernel, (int)smem_bytes<Rows>(4)>();
+  constexpr auto kernel = cache_attention_kernel<Rows>;
+  cudaError_t e = prefer_max_shared<kernel, smem_bytes<Rows>()>();
   if (e != cudaSuccess) return e;
-  return launch_pdl(kernel, dim3(a.grid), dim3(kThreads), smem_bytes<Rows>(a.rt), s, a);
-}
-
-template <typename T, template <int, bool> class Rows>
-cudaError_t launch_typed(const CacheAttn& a, bool score, cudaStream_t s) {
-  cudaError_t e;
-  switch (padded_d(a.c.d)) {
-    case 64:
-      e = score ? launch_rows<T, 64, Rows<64, true>>(a, s) : launch_rows<T, 64, Rows<64, false>>(a, s);
-      break;
-    case 128:
-      e = score ? launch_rows<T, 128, Rows<128, true>>(a, s)
-                : launch_rows<T, 128, Rows<128, false>>(a, s);
-      break;
-    default:
-      e = score ? launch_rows<T, 256, Rows<256, true>>(a, s)
-                : launch_rows<T, 256, Rows<256, false>>(a, s);
-  }
+  e = launch_pdl(kernel, dim3(a.grid), dim3(kThreads), smem_bytes<Rows>(), s, a);
   if (e != cudaSuccess) return e;
-  constexpr auto join = cache_join_kernel<T>;
+  constexpr auto join = cache_join_kernel<typename Rows::T>;
   e = prefer_max_shared<join>();
   if (e != cudaSuccess) return e;
   // parts of a (b, hk): as many as its keys' weights or its rows' joins are
   // worth, about two blocks per SM in all
   const long long bh = (long long)a.c.B * a.c.Hkv;
-  const int most = score ? (a.c.max_len + kJoinThreads - 1) / kJoinThreads : a.G;
+  const int most = a.score ? (a.c.max_len + kJoinThreads - 1) / kJoinThreads : a.G;
   long long parts = (304 + bh - 1) / bh;
   parts = parts < most ? parts : most;
-  if (score && (a.c.max_len + parts - 1) / parts > 4096) parts = (a.c.max_len + 4095) / 4096;
+  if (a.score && (a.c.max_len + parts - 1) / parts > 4096) parts = (a.c.max_len + 4095) / 4096;
   if (parts < 1) parts = 1;
   const int keys = (int)((a.c.max_len + parts - 1) / parts);
   return launch_pdl(join, dim3((unsigned)(bh * parts)), dim3(kJoinThreads), 0, s, a, (int)parts,
-                    keys, score ? 1 : 0);
+                    keys);
+}
+
+template <template <int, int> class Rows, int kR>
+cudaError_t launch_width(const CacheAttn& a, int D, cudaStream_t s) {
+  if (D == 64) return launch_rows<Rows<64, kR>>(a, s);
+  if (D == 128) return launch_rows<Rows<128, kR>>(a, s);
+  if constexpr (kR <= 16) return launch_rows<Rows<256, kR>>(a, s);
+  return cudaErrorInvalidValue;
 }
 
 }  // namespace
@@ -862,9 +999,11 @@ cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsig
   a.lse = call.lse;
   a.H = call.H;
   a.G = sh.G;
-  a.rt = sh.rt;
+  a.rows = sh.rows;
   a.groups = sh.groups;
+  a.tile = sh.tile;
   a.grid = sh.grid;
+  a.score = score;
   a.scale2 = call.scale * kLog2e;
   a.wmean = call.weight / (float)sh.G;
   a.add = call.weights == AVITS_WEIGHTS_ADD;
@@ -875,8 +1014,10 @@ cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsig
   a.logits = reinterpret_cast<float*>(ws + l.logits);
   a.ld = l.ld;
   a.status = status;
-  return c.dt == AVITS_BF16 ? launch_typed<__nv_bfloat16, RowsBf16>(a, score, s)
-                            : launch_typed<float, RowsF32>(a, score, s);
+  if (c.dt != AVITS_BF16) return launch_width<RowsF32, 8>(a, sh.D, s);
+  if (sh.rows == 8) return launch_width<RowsBf16, 8>(a, sh.D, s);
+  if (sh.rows == 16) return launch_width<RowsBf16, 16>(a, sh.D, s);
+  return launch_width<RowsBf16, 32>(a, sh.D, s);
 }
 
 }  // namespace avits
