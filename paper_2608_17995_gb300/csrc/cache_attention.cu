@@ -14,11 +14,12 @@
 // maximum, sum and O in registers and a ring of tiles of its own in shared
 // memory, filled by asynchronous copies that run ahead over unit borders; the
 // warps meet once per unit.  A unit that lies in one piece is finished there; of
-// the others each piece leaves its maximum, sum and O, and the second kernel
-// joins them.
+// the others each piece leaves its maximum, sum and O, and the CTA that is last
+// to do so joins them, in the pieces' order.
 //
 // The weights need the whole row's lse: the first kernel leaves the logits
-// (fp32), the second sums exp(x - lse) over the group's heads, in a fixed order.
+// (fp32), a second one sums exp(x - lse) over the group's heads, in a fixed
+// order.  Where units have many pieces, it joins their O as well.
 #include "cache_common.cuh"
 #include "avits_internal.h"
 
@@ -28,6 +29,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMinTiles = 4;      // tiles of the smallest piece: one per warp
+constexpr int kMaxPieces = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -43,13 +45,17 @@ struct CacheAttn {
   int groups;       // units per KV head: ceil(G / rows)
   int tile;         // keys per tile
   int grid;         // CTAs of the first kernel
+  int in_page;      // a tile never crosses a page: page_size is a multiple of it
   int score;        // weights wanted: logits are kept
+  int defer;        // the second kernel joins O
   float scale2;     // scale * log2(e)
   float wmean;      // weight / G
   int add;
   // workspace
-  int* starts;      // [B+1] first tile of a sequence on the line
-  float* lse2;      // [B,H] log2-domain lse of rows finished in one piece
+  unsigned* count;  // [kMaxPieces] pieces that left their part, by a unit's first piece;
+                    // zero between calls
+  int* starts;      // [B+1] first tile of a sequence on the line (defer)
+  float* lse2;      // [B,H] log2-domain lse (weights wanted, or defer)
   float2* pml;      // [2 grid][rows] maximum and sum of a piece's row
   float* po;        // [2 grid][rows][d] its O
   float* logits;    // [B,H,ld] log2-domain logits (weights wanted)
@@ -93,7 +99,7 @@ struct Cursor {
   }
   template <int kTile>
   __device__ __forceinline__ void look_up(const CacheAttn& a, int lane) {
-    const int j = t * kTile + (lane & (kTile - 1));
+    const int j = t * kTile + (a.in_page ? 0 : lane & (kTile - 1));
     entry = j < len ? a.c.block_table[(int64_t)b * a.c.table_sb + a.page.div(j)] : -1;
   }
 };
@@ -110,33 +116,58 @@ __device__ __forceinline__ void copy_tile(const CacheAttn& a, Cursor& cur, uint3
   constexpr int kSide = kPieces < 32 ? 32 / kPieces : 1;       // rows side by side
   constexpr int kSteps = kPieces < 32 ? 1 : kPieces / 32;      // steps along a row
   const int hk = a.groups == 1 ? cur.u : cur.u / a.groups;
-  const int j = cur.t * kTile + (lane & (kTile - 1));
-  const int page = j < cur.len ? checked_page(a.c, cur.entry, a.status) : -1;
-  const unsigned ok = __ballot_sync(0xffffffffu, page >= 0);
-  const int slot = j - a.page.div(j) * a.c.page_size;
-  // lanes below 16 hold the key's offset, the others the value's
-  const int64_t off = page < 0 ? 0
-                      : lane < 16
-                          ? (int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st + hk * a.c.k_sh
-                          : (int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st + hk * a.c.v_sh;
   const int side = kPieces < 32 ? lane / kPieces : 0, piece = kPieces < 32 ? lane % kPieces : lane;
   const int row_pieces = a.c.d * kEs / 16;
   const int fill_pieces = kSwizzle ? (row_pieces + 1) & ~1 : row_pieces;   // whole 16-column steps
+  const char* kp = static_cast<const char*>(a.c.k_pages) + (int64_t)hk * a.c.k_sh * kEs;
+  const char* vp = static_cast<const char*>(a.c.v_pages) + (int64_t)hk * a.c.v_sh * kEs;
+  auto put = [&](int row, int c, const char* k, const char* v, bool there) {
+    const bool some = there && c < row_pieces;
+    const uint32_t to = dst + row * kRowBytes + ((kSwizzle ? c ^ (row & 7) : c) << 4);
+    cp16(to, k + c * 16, some);
+    cp16(to + kTile * kRowBytes, v + c * 16, some);
+  };
+  unsigned ok;
+  if (a.in_page) {
+    // one page holds the whole tile
+    const int j0 = cur.t * kTile, n = cur.len - j0;
+    const int page = checked_page(a.c, cur.entry, a.status);
+    const int slot = j0 - a.page.div(j0) * a.c.page_size + side;
+    ok = page < 0 ? 0u : n >= kTile ? (1u << kTile) - 1u : (1u << n) - 1u;
+    if (page >= 0) {
+      kp += ((int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st) * kEs;
+      vp += ((int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st) * kEs;
+    }
+    const int64_t ks = a.c.k_st * (kSide * kEs), vs = a.c.v_st * (kSide * kEs);
 #pragma unroll
-  for (int i = 0; i < kTile / kSide; ++i) {
-    const int row = i * kSide + side;
-    const int64_t ko = __shfl_sync(0xffffffffu, off, row);
-    const int64_t vo = __shfl_sync(0xffffffffu, off, row + 16);
-    const bool there = (ok >> row) & 1u;
+    for (int i = 0; i < kTile / kSide; ++i) {
+      const int row = i * kSide + side;
 #pragma unroll
-    for (int st = 0; st < kSteps; ++st) {
-      const int c = piece + 32 * st;
-      if (c < fill_pieces) {
-        const bool some = there && c < row_pieces;
-        const uint32_t to = dst + row * kRowBytes + ((kSwizzle ? c ^ (row & 7) : c) << 4);
-        cp16(to, static_cast<const char*>(a.c.k_pages) + ko * kEs + c * 16, some);
-        cp16(to + kTile * kRowBytes, static_cast<const char*>(a.c.v_pages) + vo * kEs + c * 16,
-             some);
+      for (int st = 0; st < kSteps; ++st) {
+        const int c = piece + 32 * st;
+        if (c < fill_pieces) put(row, c, kp, vp, (ok >> row) & 1u);
+      }
+      kp += ks;
+      vp += vs;
+    }
+  } else {
+    const int j = cur.t * kTile + (lane & (kTile - 1));
+    const int page = j < cur.len ? checked_page(a.c, cur.entry, a.status) : -1;
+    ok = __ballot_sync(0xffffffffu, page >= 0) & ((1u << kTile) - 1u);
+    const int slot = j - a.page.div(j) * a.c.page_size;
+    // lanes below 16 hold the key's offset, the others the value's
+    const int64_t off = page < 0 ? 0
+                        : lane < 16 ? (int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st
+                                    : (int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st;
+#pragma unroll
+    for (int i = 0; i < kTile / kSide; ++i) {
+      const int row = i * kSide + side;
+      const int64_t ko = __shfl_sync(0xffffffffu, off, row) * kEs;
+      const int64_t vo = __shfl_sync(0xffffffffu, off, row + 16) * kEs;
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        const int c = piece + 32 * st;
+        if (c < fill_pieces) put(row, c, kp + ko, vp + vo, (ok >> row) & 1u);
       }
     }
   }
@@ -580,6 +611,68 @@ __device__ __forceinline__ void one_tile(Rows& r, const CacheAttn& a, const char
     r.tile(a, 0u, sq, sw, mask, lg, rows, lane, st);
 }
 
+// The lse of a unit's rows from the pieces c0 .. c1 (the first piece's part is
+// its CTA's second where `second`), and O unless that is left to the second
+// kernel.  Read past L1: other CTAs wrote them.
+__device__ __forceinline__ int part_of(int c, int c0, bool second) {
+  return 2 * c + (c == c0 && second ? 1 : 0);
+}
+
+template <typename Rows>
+__device__ __noinline__ void join_unit(const CacheAttn& a, int b, int2 h, int c0, int c1,
+                                       bool second, float* s_e) {
+  using T = typename Rows::T;
+  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
+  for (int r = w; r < h.y; r += kWarps) {
+    float top = -INFINITY, l = 0.f;
+    for (int c = c0 + lane; c <= c1; c += 32) {
+      const float2 x = __ldcg(a.pml + part_of(c, c0, second) * Rows::kR + r);
+      const float mn = fmaxf(top, x.x), ref = mn == -INFINITY ? 0.f : mn;
+      l = l * ex2(top - ref) + x.y * ex2(x.x - ref);   // a NaN stays one
+      top = mn;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float tx = __shfl_xor_sync(0xffffffffu, top, o);
+      const float lx = __shfl_xor_sync(0xffffffffu, l, o);
+      const float mn = fmaxf(top, tx), ref = mn == -INFINITY ? 0.f : mn;
+      l = l * ex2(top - ref) + lx * ex2(tx - ref);
+      top = mn;
+    }
+    const float e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
+    if (lane == 0) {
+      s_e[r] = e;
+      if (a.score || a.defer) a.lse2[(int64_t)b * a.H + h.x + r] = e;
+      if (a.lse) a.lse[(int64_t)b * a.H + h.x + r] = e * kLn2;
+    }
+  }
+  if (a.defer) return;
+  __syncthreads();
+  const int d4 = a.c.d / 4;
+  for (int i = tid; i < h.y * d4; i += kThreads) {
+    const int r = i / d4, d = (i - r * d4) * 4;
+    const float e = s_e[r];
+    const float none = e != e ? e : 0.f;
+    float4 v = make_float4(none, none, none, none);
+    if (e != -INFINITY) {
+#pragma unroll 4
+      for (int c = c0; c <= c1; ++c) {
+        const int at = part_of(c, c0, second) * Rows::kR + r;
+        const float mx = __ldcg(&a.pml[at].x);
+        const float4 x = __ldcg(reinterpret_cast<const float4*>(a.po + (int64_t)at * a.c.d + d));
+        const float f = ex2(mx - e);     // mx = -inf: 0
+        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
+        v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+      }
+    }
+    T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)(h.x + r) * a.o_sh + d;
+    store_elem(out, 0, v.x);
+    store_elem(out, 1, v.y);
+    store_elem(out, 2, v.z);
+    store_elem(out, 3, v.w);
+  }
+}
+
 template <typename Rows>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm<Rows>())
 cache_attention_kernel(const __grid_constant__ CacheAttn a) {
@@ -589,9 +682,21 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
   __shared__ float2 s_ml[2][kWarps][Rows::kBufRows];
   __shared__ int s_free[2][kWarps];
   __shared__ uint32_t s_mask[kWarps][NS];
-  __shared__ int s_scan[kWarps], s_b, s_off;
+  __shared__ int s_scan[kWarps], s_b, s_off, s_last;
+  __shared__ float s_e[kR];
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
   pdl_wait_then_trigger();
+
+  // sequences without cached tokens
+  for (int b = blockIdx.x; b < a.c.B; b += gridDim.x) {
+    if (cache_len(a.c, b) > 0) continue;
+    for (int i = tid; i < a.H * a.c.d; i += kThreads) {
+      const int h = i / a.c.d;
+      store_elem(static_cast<T*>(a.o), (int64_t)b * a.o_sb + (int64_t)h * a.o_sh + (i - h * a.c.d),
+                 0.f);
+      if (a.lse && i == h * a.c.d) a.lse[(int64_t)b * a.H + h] = -INFINITY;
+    }
+  }
 
   // where this CTA's piece of the line of tiles begins
   const int B = a.c.B, units = a.c.Hkv * a.groups;
@@ -616,7 +721,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
     if (i < w) before += s_scan[i];
     total += s_scan[i];
   }
-  if (blockIdx.x == 0) {
+  if (blockIdx.x == 0 && a.defer) {
     int at = before;
     for (int b = b0; b < b1; ++b) {
       a.starts[b] = at;
@@ -752,7 +857,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
           store_elem(out, 3, v.w * inv);
           if (d == 0) {
             const float e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
-            a.lse2[(int64_t)b * a.H + hh] = e;
+            if (a.score) a.lse2[(int64_t)b * a.H + hh] = e;
             if (a.lse) a.lse[(int64_t)b * a.H + hh] = e * kLn2;
           }
         } else {
@@ -762,6 +867,18 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
       }
       __syncthreads();     // the free stages are free again
     }
+    if (!whole) {
+      const int T0 = first + f0 - t0, c0 = T0 / per, c1 = (T0 + nt - 1) / per;
+      if (tid == 0) {
+        __threadfence();
+        s_last = atomicAdd(&a.count[c0], 1u) == (unsigned)(c1 - c0);
+        if (s_last) a.count[c0] = 0u;
+        __threadfence();
+      }
+      __syncthreads();
+      if (s_last) join_unit<Rows>(a, b, h, c0, c1, T0 != c0 * per, s_e);
+      __syncthreads();
+    }
     ++seg;
     f0 += t1 - t0;
     left = after;
@@ -769,131 +886,109 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
   }
 }
 
-// ---------------------------------------------------------- second kernel --
-// Block (b, hk, part): the lse of the group's rows from their pieces, the
-// weights of the part's keys, and O of the rows part, part + parts, ...
-constexpr int kJoinThreads = 256;
+// --------------------------------------------------------- second kernels --
+// Weights: block (b, hk, 512 keys), 4 keys to a thread, the group's logits in
+// 16-byte loads.  The loads wait for nothing but the length.
+constexpr int kWeightThreads = 128;
+constexpr int kWeightKeys = 4 * kWeightThreads;
 constexpr int kMaxGroup = 256;
 
-template <typename T>
-__global__ void __launch_bounds__(kJoinThreads)
-cache_join_kernel(const __grid_constant__ CacheAttn a, int parts, int keys) {
-  __shared__ float s_lse2[kMaxGroup];
-  __shared__ float4 s_sum[kJoinThreads];
-  pdl_wait_then_trigger();
-  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
-  const int bh = blockIdx.x / parts, part = blockIdx.x - bh * parts;
-  const int b = bh / a.c.Hkv, hk = bh - b * a.c.Hkv;
-  const int len = cache_len(a.c, b), nt = tiles_of(a, len);
-  const int nrow = a.rows, d4 = a.c.d / 4;
-  if (nt == 0) {
-    for (int r = part; r < a.G; r += parts) {
-      const int h = hk * a.G + r;
-      T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh;
-      for (int d = tid; d < a.c.d; d += kJoinThreads) store_elem(out, d, 0.f);
-      if (a.lse && tid == 0) a.lse[(int64_t)b * a.H + h] = -INFINITY;
-    }
-    return;
+__device__ __forceinline__ void weights_block(const CacheAttn& a, int bh, int part) {
+  __shared__ float s_e[kMaxGroup];
+  const int b = bh / a.c.Hkv, hk = bh - b * a.c.Hkv, tid = threadIdx.x;
+  const int len = cache_len(a.c, b), j = part * kWeightKeys + tid * 4;
+  if (part * kWeightKeys >= len) return;
+  for (int r = tid; r < a.G; r += kWeightThreads) {
+    const float e = a.lse2[(int64_t)b * a.H + hk * a.G + r];
+    s_e[r] = e == -INFINITY ? INFINITY : e;   // nothing to attend to: no weight
   }
-  const int per = max(kMinTiles, (a.starts[a.c.B] + a.grid - 1) / a.grid);
-  const int start = a.starts[b];
-  for (int r = w; r < a.G; r += kJoinThreads / 32) {
-    const int rg = r / nrow, T0 = start + (hk * a.groups + rg) * nt, T1 = T0 + nt;
-    const int c0 = T0 / per, c1 = (T1 - 1) / per;
-    const int h = hk * a.G + r;
-    float e;
-    if (c0 == c1) {
-      e = a.lse2[(int64_t)b * a.H + h];
+  float* acc = a.c.acc + (int64_t)b * a.c.acc_sb + (int64_t)hk * a.c.acc_sh + j;
+  const bool vec = (reinterpret_cast<uintptr_t>(acc) & 15u) == 0 && j + 4 <= len;
+  float old[4] = {};
+  if (a.add && j < len) {
+    if (vec) {
+      const float4 x = *reinterpret_cast<const float4*>(acc);
+      old[0] = x.x; old[1] = x.y; old[2] = x.z; old[3] = x.w;
     } else {
-      float top = -INFINITY, l = 0.f;
-      for (int c = c0 + lane; c <= c1; c += 32) {
-        const int slot = 2 * c + (c == c0 && T0 != c0 * per ? 1 : 0);
-        const float2 x = a.pml[slot * nrow + (r - rg * nrow)];
-        const float mn = fmaxf(top, x.x), ref = mn == -INFINITY ? 0.f : mn;
-        l = l * ex2(top - ref) + x.y * ex2(x.x - ref);   // a NaN stays one
-        top = mn;
-      }
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const float tx = __shfl_xor_sync(0xffffffffu, top, o);
-        const float lx = __shfl_xor_sync(0xffffffffu, l, o);
-        const float mn = fmaxf(top, tx), ref = mn == -INFINITY ? 0.f : mn;
-        l = l * ex2(top - ref) + lx * ex2(tx - ref);
-        top = mn;
-      }
-      e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
-      if (a.lse && lane == 0 && r % parts == part) a.lse[(int64_t)b * a.H + h] = e * kLn2;
+      for (int k = 0; k < 4; ++k)
+        if (j + k < len) old[k] = acc[k];
     }
-    if (lane == 0) s_lse2[r] = e;
   }
   __syncthreads();
-  if (a.score) {
-    const int j1 = min(len, (part + 1) * keys);
-    float* acc = a.c.acc + (int64_t)b * a.c.acc_sb + (int64_t)hk * a.c.acc_sh;
-    const float* lg = a.logits + ((int64_t)b * a.H + hk * a.G) * a.ld;
-    constexpr int kDeep = 4;     // keys of a thread at once
-    for (int j0 = part * keys + tid; j0 < j1; j0 += kDeep * kJoinThreads) {
-      float s[kDeep] = {}, old[kDeep] = {};
+  if (j >= len) return;
+  const float* lg = a.logits + ((int64_t)b * a.H + hk * a.G) * a.ld + j;
+  float s[4] = {};
+#pragma unroll 8
+  for (int r = 0; r < a.G; ++r) {
+    const float4 x = *reinterpret_cast<const float4*>(lg + (int64_t)r * a.ld);
+    const float e = s_e[r];
+    s[0] += ex2(x.x - e);
+    s[1] += ex2(x.y - e);
+    s[2] += ex2(x.z - e);
+    s[3] += ex2(x.w - e);
+  }
 #pragma unroll
-      for (int k = 0; k < kDeep; ++k) {
-        const int j = j0 + k * kJoinThreads;
-        if (a.add && j < j1) old[k] = acc[j];
-      }
-#pragma unroll 4
-      for (int r = 0; r < a.G; ++r) {
-        // nothing to attend to (every page out of range): no weight
-        const float e = s_lse2[r] == -INFINITY ? INFINITY : s_lse2[r];
-        float x[kDeep];
+  for (int k = 0; k < 4; ++k) s[k] = fmaf(s[k], a.wmean, old[k]);
+  if (vec) {
+    *reinterpret_cast<float4*>(acc) = make_float4(s[0], s[1], s[2], s[3]);
+  } else {
 #pragma unroll
-        for (int k = 0; k < kDeep; ++k)
-          x[k] = lg[(int64_t)r * a.ld + min(j0 + k * kJoinThreads, j1 - 1)];
-#pragma unroll
-        for (int k = 0; k < kDeep; ++k) s[k] += ex2(x[k] - e);
-      }
-#pragma unroll
-      for (int k = 0; k < kDeep; ++k) {
-        const int j = j0 + k * kJoinThreads;
-        if (j < j1) acc[j] = fmaf(s[k], a.wmean, old[k]);
-      }
+    for (int k = 0; k < 4; ++k)
+      if (j + k < len) acc[k] = s[k];
+  }
+}
+
+// O of one row that was cut into pieces: threads side by side along the row and
+// over the pieces.
+template <typename T>
+__device__ __forceinline__ void join_block(const CacheAttn& a, int b, int h) {
+  __shared__ float4 s_sum[kWeightThreads];
+  const int tid = threadIdx.x, len = cache_len(a.c, b), nt = tiles_of(a, len);
+  if (nt == 0) return;
+  const int hk = h / a.G, r = h - hk * a.G, rg = r / a.rows, rr = r - rg * a.rows;
+  const int per = max(kMinTiles, (a.starts[a.c.B] + a.grid - 1) / a.grid);
+  const int T0 = a.starts[b] + (hk * a.groups + rg) * nt;
+  const int c0 = T0 / per, c1 = (T0 + nt - 1) / per;
+  if (c0 == c1) return;
+  const float e = a.lse2[(int64_t)b * a.H + h];
+  const int d4 = a.c.d / 4, lanes = kWeightThreads / d4, col = tid % d4, sub = tid / d4;
+  const float none = e != e ? e : 0.f;
+  float4 v = make_float4(none, none, none, none);
+  if (sub < lanes && e != -INFINITY) {
+#pragma unroll 8
+    for (int c = c0 + sub; c <= c1; c += lanes) {
+      const int at = part_of(c, c0, T0 != c0 * per) * a.rows + rr;
+      const float mx = a.pml[at].x;
+      const float4 x = *reinterpret_cast<const float4*>(a.po + (int64_t)at * a.c.d + col * 4);
+      const float f = ex2(mx - e);
+      v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
+      v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
     }
   }
-  // O of the rows that were cut
-  for (int r = part; r < a.G; r += parts) {
-    const int rg = r / nrow, T0 = start + (hk * a.groups + rg) * nt, T1 = T0 + nt;
-    const int c0 = T0 / per, c1 = (T1 - 1) / per;
-    if (c0 == c1) continue;
-    const float e = s_lse2[r];
-    const int h = hk * a.G + r, rr = r - rg * nrow;
-    const int lanes = kJoinThreads / d4, col = tid % d4, sub = tid / d4;
-    const float none = e != e ? e : 0.f;
-    float4 v = make_float4(none, none, none, none);
-    if (sub < lanes && e != -INFINITY) {
-      for (int c = c0 + sub; c <= c1; c += lanes) {
-        const int slot = 2 * c + (c == c0 && T0 != c0 * per ? 1 : 0);
-        const float mx = a.pml[slot * nrow + rr].x;
-        if (mx == -INFINITY) continue;
-        const float f = ex2(mx - e);
-        const float4 x =
-            *reinterpret_cast<const float4*>(a.po + ((int64_t)slot * nrow + rr) * a.c.d + col * 4);
-        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
-        v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
-      }
-    }
-    __syncthreads();
-    s_sum[tid] = v;
-    __syncthreads();
-    if (sub == 0) {
-      for (int k = 1; k < lanes; ++k) {
-        const float4 x = s_sum[k * d4 + col];
-        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-      }
-      T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh + col * 4;
-      store_elem(out, 0, v.x);
-      store_elem(out, 1, v.y);
-      store_elem(out, 2, v.z);
-      store_elem(out, 3, v.w);
-    }
+  s_sum[tid] = v;
+  __syncthreads();
+  if (sub != 0) return;
+  for (int k = 1; k < lanes; ++k) {
+    const float4 x = s_sum[k * d4 + col];
+    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
   }
+  T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh + col * 4;
+  store_elem(out, 0, v.x);
+  store_elem(out, 1, v.y);
+  store_elem(out, 2, v.z);
+  store_elem(out, 3, v.w);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kWeightThreads)
+cache_finish_kernel(const __grid_constant__ CacheAttn a, int joins, int parts) {
+  pdl_wait_then_trigger();
+  const int i = (int)blockIdx.x - joins;
+  if (i < 0)
+    join_block<T>(a, (int)blockIdx.x / a.H, (int)blockIdx.x % a.H);
+  else
+    weights_block(a, i / parts, i % parts);
 }
 
 // How a call is cut: the widths 64, 128 and 256 have kernels of their own; a
@@ -902,6 +997,7 @@ cache_join_kernel(const __grid_constant__ CacheAttn a, int parts, int keys) {
 // most, by registers).
 struct Shape {
   int G, D, rows, groups, tile, grid;
+  bool defer;
   long long tiles;
 };
 
@@ -915,8 +1011,11 @@ Shape shape_of(const avits_kv_cache& c, int H, int num_sms) {
   s.tile = bf ? 16 : 8;
   s.tiles = (long long)c.B * c.Hkv * s.groups * ((c.max_len + s.tile - 1) / s.tile);
   const long long most = (s.tiles + kMinTiles - 1) / kMinTiles;
-  const long long full = (long long)num_sms * (s.D <= 128 ? 2 : 1);
+  long long full = (long long)num_sms * (s.D <= 128 ? 2 : 1);
+  if (full > kMaxPieces) full = kMaxPieces;
   s.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
+  // units of 16 pieces and more: their O is joined by blocks of its own
+  s.defer = (long long)c.B * c.Hkv * s.groups * 16 <= s.grid;
   return s;
 }
 
@@ -931,8 +1030,8 @@ Layout layout_of(const avits_kv_cache& c, int H, const Shape& s, bool score) {
   Layout l;
   const size_t nrow = s.rows;
   l.ld = ((int64_t)c.max_len + 15) / 16 * 16;
-  l.starts = 0;
-  l.lse2 = up16(((size_t)c.B + 1) * 4);
+  l.starts = kMaxPieces * 4;
+  l.lse2 = l.starts + up16(((size_t)c.B + 1) * 4);
   l.pml = l.lse2 + up16((size_t)c.B * H * 4);
   l.po = l.pml + up16((size_t)2 * s.grid * nrow * 8);
   l.logits = l.po + up16((size_t)2 * s.grid * nrow * c.d * 4);
@@ -947,20 +1046,14 @@ cudaError_t launch_rows(const CacheAttn& a, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = launch_pdl(kernel, dim3(a.grid), dim3(kThreads), smem_bytes<Rows>(), s, a);
   if (e != cudaSuccess) return e;
-  constexpr auto join = cache_join_kernel<typename Rows::T>;
-  e = prefer_max_shared<join>();
+  const int joins = a.defer ? a.c.B * a.H : 0;
+  const int parts = a.score ? (a.c.max_len + kWeightKeys - 1) / kWeightKeys : 0;
+  if (joins == 0 && parts == 0) return cudaSuccess;
+  constexpr auto finish = cache_finish_kernel<typename Rows::T>;
+  e = prefer_max_shared<finish>();
   if (e != cudaSuccess) return e;
-  // parts of a (b, hk): as many as its keys' weights or its rows' joins are
-  // worth, about two blocks per SM in all
-  const long long bh = (long long)a.c.B * a.c.Hkv;
-  const int most = a.score ? (a.c.max_len + kJoinThreads - 1) / kJoinThreads : a.G;
-  long long parts = (304 + bh - 1) / bh;
-  parts = parts < most ? parts : most;
-  if (a.score && (a.c.max_len + parts - 1) / parts > 4096) parts = (a.c.max_len + 4095) / 4096;
-  if (parts < 1) parts = 1;
-  const int keys = (int)((a.c.max_len + parts - 1) / parts);
-  return launch_pdl(join, dim3((unsigned)(bh * parts)), dim3(kJoinThreads), 0, s, a, (int)parts,
-                    keys);
+  const unsigned blocks = (unsigned)joins + (unsigned)(a.c.B * a.c.Hkv) * (unsigned)parts;
+  return launch_pdl(finish, dim3(blocks), dim3(kWeightThreads), 0, s, a, joins, parts > 0 ? parts : 1);
 }
 
 template <template <int, int> class Rows, int kR>
@@ -1003,10 +1096,13 @@ cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsig
   a.groups = sh.groups;
   a.tile = sh.tile;
   a.grid = sh.grid;
+  a.in_page = c.page_size % sh.tile == 0;
   a.score = score;
+  a.defer = sh.defer;
   a.scale2 = call.scale * kLog2e;
   a.wmean = call.weight / (float)sh.G;
   a.add = call.weights == AVITS_WEIGHTS_ADD;
+  a.count = reinterpret_cast<unsigned*>(ws);
   a.starts = reinterpret_cast<int*>(ws + l.starts);
   a.lse2 = reinterpret_cast<float*>(ws + l.lse2);
   a.pml = reinterpret_cast<float2*>(ws + l.pml);
