@@ -12,16 +12,21 @@
 // lengths and few heads load the SMs alike.  A CTA finds its piece by a scan of
 // the lengths.  Its warps take the piece's tiles in turn, each with a running
 // maximum, sum and O in registers and a ring of tiles of its own in shared
-// memory, filled by asynchronous copies that run ahead over unit borders; the
-// warps meet once per unit.  A unit that lies in one piece is finished there; of
+// memory, filled by TMA copies that run ahead over unit borders; the warps meet
+// once per unit.  A unit that lies in one piece is finished there; of
 // the others each piece leaves its maximum, sum and O, and the CTA that is last
 // to do so joins them, in the pieces' order.
 //
 // The weights need the whole row's lse: the first kernel leaves the logits
 // (fp32), a second one sums exp(x - lse) over the group's heads, in a fixed
 // order.  Where units have many pieces, it joins their O as well.
+#include <cooperative_groups.h>
+
 #include "cache_common.cuh"
 #include "avits_internal.h"
+#include "tc_common.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace avits {
 namespace {
@@ -30,6 +35,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMinTiles = 4;      // tiles of the smallest piece: one per warp
 constexpr int kMaxPieces = 1024;
+constexpr unsigned long long kLateNs = 1000ull * 1000ull;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -45,7 +51,7 @@ struct CacheAttn {
   int groups;       // units per KV head: ceil(G / rows)
   int tile;         // keys per tile
   int grid;         // CTAs of the first kernel
-  int in_page;      // a tile never crosses a page: page_size is a multiple of it
+  int box;          // tokens of a TMA box; 0: rows come by 16-byte copies
   int score;        // weights wanted: logits are kept
   int defer;        // the second kernel joins O
   float scale2;     // scale * log2(e)
@@ -67,15 +73,19 @@ __device__ __forceinline__ int tiles_of(const CacheAttn& a, int len) {
   return (len + a.tile - 1) / a.tile;
 }
 
+// 16 bytes from global to shared memory; zeros where !ok (nothing is read).
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
-  // nothing is read, and zeros are written, where !ok
   const int n = ok ? 16 : 0;
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n));
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+// `bar` gets this thread's arrival when its 16-byte copies so far are done.
+__device__ __forceinline__ void cp_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar))
+               : "memory");
+}
+// Orders this thread's accesses of shared memory before later bulk copies into it.
+__device__ __forceinline__ void before_copies() {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
 // A warp's place on the line of tiles: what it copies next.
@@ -83,7 +93,7 @@ struct Cursor {
   int b, u, t;      // sequence, unit in it, tile in the unit
   int nt, len;
   int left;         // tiles still to come
-  int entry;        // table entry of this lane's key of that tile
+  int entry;        // table entry: of this lane's key, or of its box, of that tile
 
   __device__ __forceinline__ void settle(const CacheAttn& a, int units) {
     while (t >= nt) {
@@ -99,66 +109,63 @@ struct Cursor {
   }
   template <int kTile>
   __device__ __forceinline__ void look_up(const CacheAttn& a, int lane) {
-    const int j = t * kTile + (a.in_page ? 0 : lane & (kTile - 1));
+    const int j = t * kTile + (a.box ? lane * a.box & (kTile - 1) : lane & (kTile - 1));
     entry = j < len ? a.c.block_table[(int64_t)b * a.c.table_sb + a.page.div(j)] : -1;
   }
 };
 
-// Copies the cursor's tile, keys then values, to `dst` and steps on.  `mask`
-// receives a bit for each key that is there.  The rows of a tile are kTile rows
-// of kRowBytes (a multiple of 128); pieces past the head width are not written,
-// but for a zero one where it ends inside a step of 16 columns.  kSwizzle: piece c of row r lies at c ^ (r % 8), for ldmatrix.
-template <int kTile, int kRowBytes, bool kSwizzle>
-__device__ __forceinline__ void copy_tile(const CacheAttn& a, Cursor& cur, uint32_t dst,
+// Copies the cursor's tile to `dst`, keys then values, and steps on.  `mask` gets
+// a bit for each key that is there (below the length, its page in range).  A tile
+// lies as columns of 128 bytes: in bf16 [D / 64][16 rows][128 bytes] with the
+// 16-byte pieces of row r at c ^ (r % 8) (TMA's 128-byte swizzle, for ldmatrix),
+// in fp32 plain rows.  By TMA where boxes of 16 or 8 tokens never cross a page:
+// what lies outside the tensors (columns past the width, a page out of range)
+// comes as zeros.  Else by 16-byte copies, a row's pieces side by side.
+template <typename Rows>
+__device__ __forceinline__ void copy_tile(const CUtensorMap& mk, const CUtensorMap& mv,
+                                          const CacheAttn& a, Cursor& cur, char* dst, uint64_t* bar,
                                           uint32_t* mask, int units, int lane) {
-  constexpr int kEs = kSwizzle ? 2 : 4;
-  constexpr int kPieces = kRowBytes / 16;
-  constexpr int kSide = kPieces < 32 ? 32 / kPieces : 1;       // rows side by side
-  constexpr int kSteps = kPieces < 32 ? 1 : kPieces / 32;      // steps along a row
+  constexpr int kTile = Rows::kTile, kEs = sizeof(typename Rows::T), D = Rows::D;
   const int hk = a.groups == 1 ? cur.u : cur.u / a.groups;
-  const int side = kPieces < 32 ? lane / kPieces : 0, piece = kPieces < 32 ? lane % kPieces : lane;
-  const int row_pieces = a.c.d * kEs / 16;
-  const int fill_pieces = kSwizzle ? (row_pieces + 1) & ~1 : row_pieces;   // whole 16-column steps
-  const char* kp = static_cast<const char*>(a.c.k_pages) + (int64_t)hk * a.c.k_sh * kEs;
-  const char* vp = static_cast<const char*>(a.c.v_pages) + (int64_t)hk * a.c.v_sh * kEs;
-  auto put = [&](int row, int c, const char* k, const char* v, bool there) {
-    const bool some = there && c < row_pieces;
-    const uint32_t to = dst + row * kRowBytes + ((kSwizzle ? c ^ (row & 7) : c) << 4);
-    cp16(to, k + c * 16, some);
-    cp16(to + kTile * kRowBytes, v + c * 16, some);
-  };
+  const int j0 = cur.t * kTile;
   unsigned ok;
-  if (a.in_page) {
-    // one page holds the whole tile
-    const int j0 = cur.t * kTile, n = cur.len - j0;
-    const int page = checked_page(a.c, cur.entry, a.status);
-    const int slot = j0 - a.page.div(j0) * a.c.page_size + side;
-    ok = page < 0 ? 0u : n >= kTile ? (1u << kTile) - 1u : (1u << n) - 1u;
-    if (page >= 0) {
-      kp += ((int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st) * kEs;
-      vp += ((int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st) * kEs;
-    }
-    const int64_t ks = a.c.k_st * (kSide * kEs), vs = a.c.v_st * (kSide * kEs);
+  if (a.box) {
+    const int jb = j0 + (lane * a.box & (kTile - 1));
+    const int page = jb < cur.len ? checked_page(a.c, cur.entry, a.status) : -1;
+    const int p0 = __shfl_sync(0xffffffffu, page, 0), p1 = __shfl_sync(0xffffffffu, page, 1);
+    const int n = cur.len - j0;
+    ok = n >= kTile ? (1u << kTile) - 1u : (1u << n) - 1u;
+    if (p0 < 0) ok &= ~((1u << a.box) - 1u);
+    if (p1 < 0) ok &= a.box < kTile ? (1u << a.box) - 1u : 0u;
+    if (tc::elect_one()) {
+      mbar_arrive_expect_tx(bar, Rows::kStage);
+#pragma unroll 1
+      for (int at = 0; at < kTile; at += a.box) {
+        const int jj = j0 + at, slot = jj - a.page.div(jj) * a.c.page_size, pg = at ? p1 : p0;
 #pragma unroll
-    for (int i = 0; i < kTile / kSide; ++i) {
-      const int row = i * kSide + side;
-#pragma unroll
-      for (int st = 0; st < kSteps; ++st) {
-        const int c = piece + 32 * st;
-        if (c < fill_pieces) put(row, c, kp, vp, (ok >> row) & 1u);
+        for (int c = 0; c < Rows::kCols; ++c) {
+          char* to = dst + c * Rows::kColBytes + at * Rows::kColPitch;
+          tc::tma_load_4d(to, &mk, c * Rows::kColWidth, hk, slot, pg, bar);
+          tc::tma_load_4d(to + Rows::kStage / 2, &mv, c * Rows::kColWidth, hk, slot, pg, bar);
+        }
       }
-      kp += ks;
-      vp += vs;
     }
   } else {
-    const int j = cur.t * kTile + (lane & (kTile - 1));
+    constexpr int kPieces = D * kEs / 16;
+    constexpr int kSide = kPieces < 32 ? 32 / kPieces : 1;       // rows side by side
+    constexpr int kSteps = kPieces < 32 ? 1 : kPieces / 32;      // steps along a row
+    const int side = kPieces < 32 ? lane / kPieces : 0;
+    const int piece = kPieces < 32 ? lane % kPieces : lane;
+    const int some = a.c.d * kEs / 16, upto = kEs == 2 ? (some + 1) & ~1 : some;
+    const int j = j0 + (lane & (kTile - 1));
     const int page = j < cur.len ? checked_page(a.c, cur.entry, a.status) : -1;
     ok = __ballot_sync(0xffffffffu, page >= 0) & ((1u << kTile) - 1u);
     const int slot = j - a.page.div(j) * a.c.page_size;
     // lanes below 16 hold the key's offset, the others the value's
     const int64_t off = page < 0 ? 0
-                        : lane < 16 ? (int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st
-                                    : (int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st;
+                        : lane < 16
+                            ? (int64_t)page * a.c.k_sp + (int64_t)slot * a.c.k_st + hk * a.c.k_sh
+                            : (int64_t)page * a.c.v_sp + (int64_t)slot * a.c.v_st + hk * a.c.v_sh;
 #pragma unroll
     for (int i = 0; i < kTile / kSide; ++i) {
       const int row = i * kSide + side;
@@ -167,9 +174,15 @@ __device__ __forceinline__ void copy_tile(const CacheAttn& a, Cursor& cur, uint3
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
         const int c = piece + 32 * st;
-        if (c < fill_pieces) put(row, c, kp + ko, vp + vo, (ok >> row) & 1u);
+        if (c < upto) {
+          const bool there = ((ok >> row) & 1u) && c < some;
+          const uint32_t to = smem_u32(dst) + Rows::piece_at(row, c);
+          cp16(to, static_cast<const char*>(a.c.k_pages) + ko + c * 16, there);
+          cp16(to + Rows::kStage / 2, static_cast<const char*>(a.c.v_pages) + vo + c * 16, there);
+        }
       }
     }
+    cp_arrive(bar);
   }
   if (lane == 0) *mask = ok;
   if (--cur.left > 0) {
@@ -177,6 +190,21 @@ __device__ __forceinline__ void copy_tile(const CacheAttn& a, Cursor& cur, uint3
     cur.settle(a, units);
     cur.look_up<kTile>(a, lane);
   }
+}
+
+// A tile that has come: value rows that are not there are set to zero, since a
+// weight of zero times a NaN is one.
+template <typename Rows>
+__device__ __forceinline__ void clear_rows(char* st, unsigned mask, int lane) {
+  constexpr int kPieces = Rows::D * (int)sizeof(typename Rows::T) / 16;
+  for (int i = lane; i < Rows::kTile * kPieces; i += 32) {
+    const int row = i / kPieces, c = i - row * kPieces;
+    if (!((mask >> row) & 1u))
+      *reinterpret_cast<uint4*>(st + Rows::kStage / 2 + Rows::piece_at(row, c)) =
+          make_uint4(0u, 0u, 0u, 0u);
+  }
+  before_copies();
+  __syncwarp();
 }
 
 // The place of O's column d of a row in a warp's buffer (bank conflicts).
@@ -229,16 +257,22 @@ struct RowsBf16 {
   static constexpr bool kSplit8 = kR == 8;
   static constexpr int kM = kR == 32 ? 2 : 1;      // row tiles
   static constexpr int kTile = 16;
-  static constexpr int kRowBytes = D * 2;
-  static constexpr bool kSwizzle = true;
-  static constexpr int kStage = 2 * kTile * kRowBytes;
-  static constexpr int kQBytes = kR * kRowBytes;
+  static constexpr bool kBf16 = true;
+  static constexpr int kStage = 2 * kTile * D * 2;
+  static constexpr int kCols = D / 64, kColWidth = 64, kColPitch = 128;
+  static constexpr int kColBytes = kTile * kColPitch;
+  static constexpr int kQBytes = kR * D * 2;
   static constexpr int kQPieces = kQBytes / 16;
   static constexpr int kBufRows = kR < 16 ? kR : 16;     // rows of O in a free stage
   static constexpr int kWarpBytes = 0;
 
   float m[kM][2], l[kM][2];        // of rows g and g + 8 of a row tile
   float o[kM][D / 8][4];
+
+  // 16-byte piece c of a row of a tile
+  __device__ static __forceinline__ int piece_at(int row, int c) {
+    return (c >> 3) * kColBytes + row * kColPitch + (((c & 7) ^ (row & 7)) << 4);
+  }
 
   // 16 bytes of Q: piece i of the unit's rows
   __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, int b, int h0, int rows,
@@ -256,7 +290,8 @@ struct RowsBf16 {
   }
   __device__ static __forceinline__ void store_q(char* sq, int i, const uint4& v) {
     const int row = i / (D / 8), c = i % (D / 8);
-    *reinterpret_cast<uint4*>(sq + row * kRowBytes + ((c ^ (row & 7)) << 4)) = v;
+    *reinterpret_cast<uint4*>(sq + (c >> 3) * kR * 128 + row * 128 +
+                              (((c & 7) ^ (row & 7)) << 4)) = v;
   }
 
   __device__ __forceinline__ void reset() {
@@ -273,26 +308,26 @@ struct RowsBf16 {
 
   // one tile; lg: the logits of row g of row tile 0 at the tile's first key
   __device__ __forceinline__ void tile(const CacheAttn& a, uint32_t kt, const char* sq, char*,
-                                       uint32_t mask, float* lg, int rows, int lane) {
+                                       uint32_t mask, float* lg, int64_t ld, int rows, int lane) {
     const int g = lane >> 2, t = lane & 3, r8 = lane & 7;
-    const uint32_t vt = kt + kTile * kRowBytes;
-    const uint32_t qt = smem_u32(sq);
     const int steps = (a.c.d + 15) / 16;
     float s[kM][2][4] = {};
     {
       const int krow = r8 + ((lane >> 4) << 3), kc = (lane >> 3) & 1;
       const int qrow = kSplit8 ? r8 : r8 + (((lane >> 3) & 1) << 3);
       const int qc = kSplit8 ? (lane >> 3) & 1 : lane >> 4;
+      const uint32_t kx = (kc ^ r8) << 4, qx = (qc ^ r8) << 4;
+      const uint32_t kat = kt + krow * 128, qat = smem_u32(sq) + qrow * 128;
 #pragma unroll
       for (int st = 0; st < D / 16; ++st) {
         if (st < steps) {
           uint32_t k[4];
-          ldsm4(k, kt + krow * kRowBytes + (((2 * st + kc) ^ r8) << 4));
+          ldsm4(k, kat + (st >> 2) * kColBytes + (kx ^ ((st & 3) << 5)));
 #pragma unroll
           for (int mt = 0; mt < kM; ++mt) {
             uint32_t q[4] = {0u, 0u, 0u, 0u};
             const uint32_t at =
-                qt + (mt * 16 + qrow) * kRowBytes + (((2 * st + qc) ^ r8) << 4);
+                qat + (st >> 2) * kR * 128 + mt * 16 * 128 + (qx ^ ((st & 3) << 5));
             if (kSplit8) ldsm2(q[0], q[2], at); else ldsm4(q, at);
             mma16816(s[mt][0], q[0], q[1], q[2], q[3], k[0], k[1]);
             mma16816(s[mt][1], q[0], q[1], q[2], q[3], k[2], k[3]);
@@ -317,7 +352,7 @@ struct RowsBf16 {
         for (int hf = 0; hf < (kSplit8 ? 1 : 2); ++hf) {
           const int row = mt * 16 + hf * 8 + g;
           if (row < rows) {
-            float2* to = reinterpret_cast<float2*>(lg + (int64_t)(mt * 16 + hf * 8) * a.ld + 2 * t);
+            float2* to = reinterpret_cast<float2*>(lg + (mt * 16 + hf * 8) * ld + 2 * t);
             to[0] = make_float2(s[mt][0][2 * hf], s[mt][0][2 * hf + 1]);
             to[4] = make_float2(s[mt][1][2 * hf], s[mt][1][2 * hf + 1]);
           }
@@ -384,11 +419,12 @@ struct RowsBf16 {
     }
     {
       const int vrow = r8 + (((lane >> 3) & 1) << 3), vc = lane >> 4;
+      const uint32_t vx = (vc ^ r8) << 4, vat = kt + kStage / 2 + vrow * 128;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) {
         if (j < steps) {
           uint32_t v[4];
-          ldsm4t(v, vt + vrow * kRowBytes + (((2 * j + vc) ^ r8) << 4));
+          ldsm4t(v, vat + (j >> 2) * kColBytes + (vx ^ ((j & 3) << 5)));
 #pragma unroll
           for (int mt = 0; mt < kM; ++mt) {
             mma16816(o[mt][2 * j], p[mt][0], p[mt][1], p[mt][2], p[mt][3], v[0], v[1]);
@@ -442,10 +478,10 @@ struct RowsF32 {
   using T = float;
   static constexpr int D = D_, kR = 8;
   static constexpr int kTile = 8;
-  static constexpr int kRowBytes = D * 4;
-  static constexpr bool kSwizzle = false;
-  static constexpr int kStage = 2 * kTile * kRowBytes;
-  static constexpr int kQBytes = kR * kRowBytes;
+  static constexpr bool kBf16 = false;
+  static constexpr int kStage = 2 * kTile * D * 4;
+  static constexpr int kCols = 1, kColWidth = 0, kColPitch = D * 4, kColBytes = 0;
+  static constexpr int kQBytes = kR * D * 4;
   static constexpr int kQPieces = kQBytes / 16;
   static constexpr int kBufRows = kR, kM = 1;
   static constexpr int kWarpBytes = kTile * 8 * 4;
@@ -454,6 +490,8 @@ struct RowsF32 {
 
   float m, l;            // of row lane % 8; l: this lane's keys only until the end
   float o[8][kV][4];
+
+  __device__ static __forceinline__ int piece_at(int row, int c) { return row * kColPitch + c * 16; }
 
   __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, int b, int h0, int rows,
                                                  int i) {
@@ -592,11 +630,11 @@ struct RowsF32 {
 };
 
 // ----------------------------------------------------------- first kernel --
-// Stages of a warp's ring: three tiles where two CTAs' rings fit an SM.
+// Stages of a warp's ring, and CTAs that share an SM.
 template <typename Rows>
-constexpr int stages() { return Rows::kStage <= 4096 ? 4 : 3; }
+constexpr int stages() { return Rows::D == 64 ? 4 : Rows::D == 128 && Rows::kR < 32 ? 3 : 2; }
 template <typename Rows>
-constexpr int ctas_per_sm() { return Rows::kStage <= 8192 ? 2 : 1; }
+constexpr int ctas_per_sm() { return Rows::D <= 128 ? 2 : 1; }
 template <typename Rows>
 constexpr int smem_bytes() {
   return kWarps * stages<Rows>() * Rows::kStage + Rows::kQBytes + kWarps * Rows::kWarpBytes;
@@ -604,9 +642,10 @@ constexpr int smem_bytes() {
 
 template <typename Rows>
 __device__ __forceinline__ void one_tile(Rows& r, const CacheAttn& a, const char* st, const char* sq,
-                                         char* sw, uint32_t mask, float* lg, int rows, int lane) {
-  if constexpr (Rows::kSwizzle)
-    r.tile(a, smem_u32(st), sq, sw, mask, lg, rows, lane);
+                                         char* sw, uint32_t mask, float* lg, int64_t ld, int rows,
+                                         int lane) {
+  if constexpr (Rows::kBf16)
+    r.tile(a, smem_u32(st), sq, sw, mask, lg, ld, rows, lane);
   else
     r.tile(a, 0u, sq, sw, mask, lg, rows, lane, st);
 }
@@ -675,16 +714,22 @@ __device__ __noinline__ void join_unit(const CacheAttn& a, int b, int2 h, int c0
 
 template <typename Rows>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm<Rows>())
-cache_attention_kernel(const __grid_constant__ CacheAttn a) {
+cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                       const __grid_constant__ CacheAttn a) {
   using T = typename Rows::T;
   constexpr int D = Rows::D, kR = Rows::kR, kTile = Rows::kTile, NS = stages<Rows>();
-  extern __shared__ __align__(128) char smem[];
+  extern __shared__ __align__(1024) char smem[];
   __shared__ float2 s_ml[2][kWarps][Rows::kBufRows];
   __shared__ int s_free[2][kWarps];
+  __shared__ uint64_t s_full[kWarps][NS];
   __shared__ uint32_t s_mask[kWarps][NS];
   __shared__ int s_scan[kWarps], s_b, s_off, s_last;
   __shared__ float s_e[kR];
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
+  if (lane < NS) mbar_init(&s_full[w][lane], a.box ? 1 : 32);   // a warp's barriers are its own
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  before_copies();
+  __syncwarp();
   pdl_wait_then_trigger();
 
   // sequences without cached tokens
@@ -764,14 +809,14 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
     for (int i = tid; i < Rows::kQPieces; i += kThreads)
       Rows::store_q(s_q, i, Rows::load_q(a, b, h.x, h.y, i));
   }
-  const uint32_t ring_at = smem_u32(ring);
   // stage `fill` is the free one: the tile after the last issued goes there
   int fill = 0, use = 0;
+  uint32_t phase = 0;
+  int late = 0;         // a copy did not come in time: the others get little more
   auto issue = [&]() {
     if (cur.left > 0)
-      copy_tile<kTile, Rows::kRowBytes, Rows::kSwizzle>(a, cur, ring_at + fill * Rows::kStage,
-                                                        &s_mask[w][fill], units, lane);
-    cp_commit();
+      copy_tile<Rows>(mk, mv, a, cur, ring + fill * Rows::kStage, &s_full[w][fill], &s_mask[w][fill],
+                      units, lane);
     fill = fill + 1 == NS ? 0 : fill + 1;
   };
 #pragma unroll 1
@@ -803,17 +848,24 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
           nq[k] = Rows::load_q(a, nb, nh.x, nh.y, tid + k * kThreads);
     }
     rows.reset();
-    const int lrow = Rows::kSwizzle ? lane >> 2 : lane & 7;
+    const int lrow = Rows::kBf16 ? lane >> 2 : lane & 7;
     float* lg = a.score ? a.logits + ((int64_t)b * a.H + h.x + lrow) * a.ld : nullptr;
 #pragma unroll 1
     for (int t = t0 + ((w - f0) & (kWarps - 1)); t < t1; t += kWarps) {
       __syncwarp();
       issue();
-      cp_wait<NS - 1>();
+      late |= !mbar_wait_bounded(&s_full[w][use], phase, nullptr, a.status,
+                                 late ? kLateNs : kWaitLimitNs);
       __syncwarp();
-      one_tile(rows, a, ring + use * Rows::kStage, s_q, s_w, s_mask[w][use],
-               a.score ? lg + t * kTile : nullptr, h.y, lane);
-      use = use + 1 == NS ? 0 : use + 1;
+      const unsigned here = s_mask[w][use];
+      if (here != (1u << kTile) - 1u)
+        clear_rows<Rows>(ring + use * Rows::kStage, here, lane);
+      one_tile(rows, a, ring + use * Rows::kStage, s_q, s_w, here,
+               a.score ? lg + t * kTile : nullptr, a.ld, h.y, lane);
+      if (++use == NS) {
+        use = 0;
+        phase ^= 1u;
+      }
     }
     // the warps meet: each leaves its rows in the free stage of its ring
     const bool whole = t0 == 0 && t1 == nt;
@@ -865,6 +917,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
           if (d == 0) a.pml[slot * kR + row] = make_float2(top, l);
         }
       }
+      before_copies();
       __syncthreads();     // the free stages are free again
     }
     if (!whole) {
@@ -884,6 +937,187 @@ cache_attention_kernel(const __grid_constant__ CacheAttn a) {
     left = after;
     b = nb; u = nu; len = nlen; nt = nnt; t0 = 0;
   }
+}
+
+// ---------------------------------------------------------- one launch --
+// Shorter sequences: a cluster of CTAs per unit, each with an equal run of its
+// tiles and their logits in shared memory.  The CTAs' maxima, sums and O meet
+// through distributed shared memory; then every CTA writes a slice of O and the
+// weights of its own keys.  No workspace, no second kernel.
+template <typename Rows>
+constexpr int cluster_smem(int rows, int keys) {   // keys: logits' row stride, 0: none
+  return smem_bytes<Rows>() + Rows::kR * Rows::D * 4 + rows * keys * 4;
+}
+// The row stride of `keys` logits: 8 more than a multiple of 32, which spreads
+// the rows over the banks.
+inline int logit_stride(int keys) { return (keys + 23) / 32 * 32 + 8; }
+
+template <typename Rows>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm<Rows>())
+cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                     const __grid_constant__ CacheAttn a, int stride) {
+  using T = typename Rows::T;
+  constexpr int D = Rows::D, kR = Rows::kR, kTile = Rows::kTile, NS = stages<Rows>();
+  constexpr int kMaxCluster = 8;
+  extern __shared__ __align__(1024) char smem[];
+  __shared__ float2 s_ml[kWarps][Rows::kBufRows];
+  __shared__ float2 s_mine[kR];                  // this CTA's maximum and sum of a row
+  __shared__ float s_f[kMaxCluster][kR], s_e[kR];
+  __shared__ int s_free[kWarps];
+  __shared__ uint64_t s_full[kWarps][NS];
+  __shared__ uint32_t s_mask[kWarps][NS];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int ncta = (int)cluster.num_blocks(), me = (int)cluster.block_rank();
+  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
+  const int unit = blockIdx.x / ncta, units = a.c.Hkv * a.groups;
+  const int b = unit / units, u = unit - b * units;
+  const int hk = u / a.groups, row0 = (u - hk * a.groups) * kR;
+  const int h0 = hk * a.G + row0, rows_here = min(kR, a.G - row0);
+  if (lane < NS) mbar_init(&s_full[w][lane], a.box ? 1 : 32);   // a warp's barriers are its own
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  before_copies();
+  __syncwarp();
+  pdl_wait_then_trigger();
+  if (u == 0 && me == 0 && tid == 0) check_cache_len(a.c, b, a.status);
+  const int len = cache_len(a.c, b);
+  if (len == 0) {      // the whole cluster
+    if (me == 0)
+      for (int i = tid; i < rows_here * a.c.d; i += kThreads) {
+        const int r = i / a.c.d;
+        store_elem(static_cast<T*>(a.o), (int64_t)b * a.o_sb + (int64_t)(h0 + r) * a.o_sh +
+                   (i - r * a.c.d), 0.f);
+        if (a.lse && i == r * a.c.d) a.lse[(int64_t)b * a.H + h0 + r] = -INFINITY;
+      }
+    return;
+  }
+  const int nt = tiles_of(a, len), run = (nt + ncta - 1) / ncta;
+  const int t0 = min(nt, me * run), mine = min(nt, t0 + run) - t0;
+  char* ring = smem + w * NS * Rows::kStage;
+  char* s_q = smem + kWarps * NS * Rows::kStage;
+  char* s_w = s_q + Rows::kQBytes + w * Rows::kWarpBytes;
+  float* s_o = reinterpret_cast<float*>(smem + smem_bytes<Rows>());
+  float* s_lg = s_o + kR * D;
+  Cursor cur{b, u, t0 + w, nt, len, (mine - w + kWarps - 1) / kWarps, -1};
+  if (cur.left > 0) cur.look_up<kTile>(a, lane);
+  constexpr int kQEach = (Rows::kQPieces + kThreads - 1) / kThreads;
+  uint4 q[kQEach];
+#pragma unroll
+  for (int k = 0; k < kQEach; ++k)
+    if (tid + k * kThreads < Rows::kQPieces)
+      q[k] = Rows::load_q(a, b, h0, rows_here, tid + k * kThreads);
+  int fill = 0, use = 0;
+  uint32_t phase = 0;
+  int late = 0;         // a copy did not come in time: the others get little more
+  auto issue = [&]() {
+    if (cur.left > 0)
+      copy_tile<Rows>(mk, mv, a, cur, ring + fill * Rows::kStage, &s_full[w][fill], &s_mask[w][fill],
+                      units, lane);
+    fill = fill + 1 == NS ? 0 : fill + 1;
+  };
+#pragma unroll 1
+  for (int i = 0; i < NS - 1; ++i) issue();
+#pragma unroll
+  for (int k = 0; k < kQEach; ++k)
+    if (tid + k * kThreads < Rows::kQPieces) Rows::store_q(s_q, tid + k * kThreads, q[k]);
+  __syncthreads();
+  Rows rows;
+  rows.reset();
+  const int lrow = Rows::kBf16 ? lane >> 2 : lane & 7;
+#pragma unroll 1
+  for (int t = w; t < mine; t += kWarps) {
+    __syncwarp();
+    issue();
+    late |= !mbar_wait_bounded(&s_full[w][use], phase, nullptr, a.status,
+                                 late ? kLateNs : kWaitLimitNs);
+    __syncwarp();
+    const unsigned here = s_mask[w][use];
+    if (here != (1u << kTile) - 1u)
+      clear_rows<Rows>(ring + use * Rows::kStage, here, lane);
+    one_tile(rows, a, ring + use * Rows::kStage, s_q, s_w, here,
+             s_lg + lrow * stride + t * kTile, stride, rows_here, lane);
+    if (++use == NS) {
+      use = 0;
+      phase ^= 1u;
+    }
+  }
+  // this CTA's rows over its warps
+#pragma unroll
+  for (int part = 0; part < Rows::kM; ++part) {
+    __syncwarp();
+    rows.put(part, s_ml[w], reinterpret_cast<float*>(ring + fill * Rows::kStage), lane);
+    if (lane == 0) s_free[w] = (w * NS + fill) * Rows::kStage;
+    __syncthreads();
+    for (int i = tid; i < Rows::kBufRows * (D / 4); i += kThreads) {
+      const int r = i / (D / 4), d = (i - r * (D / 4)) * 4, row = part * 16 + r;
+      if (row >= rows_here || d >= a.c.d) continue;
+      float top = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) top = fmaxf(top, s_ml[k][r].x);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) {
+        const float2 ml = s_ml[k][r];
+        const float4 x = *reinterpret_cast<const float4*>(smem + s_free[k] + o_at(r, d, D) * 4);
+        const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
+        v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+        l = fmaf(f, ml.y, l);
+      }
+      *reinterpret_cast<float4*>(s_o + row * D + d) = v;
+      if (d == 0) s_mine[row] = make_float2(top, l);
+    }
+    __syncthreads();
+  }
+  cluster.sync();
+  // over the CTAs: a row's lse, and what each CTA's O counts in it
+  if (tid < rows_here) {
+    float2 x[kMaxCluster];
+    float top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kMaxCluster; ++k) {
+      x[k] = make_float2(-INFINITY, 0.f);
+      if (k < ncta) x[k] = cluster.map_shared_rank(s_mine, k)[tid];
+      top = fmaxf(top, x[k].x);
+    }
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int k = 0; k < kMaxCluster; ++k) l = fmaf(ex2(x[k].x - ref), x[k].y, l);
+    const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+#pragma unroll
+    for (int k = 0; k < kMaxCluster; ++k) s_f[k][tid] = ex2(x[k].x - ref) * inv;
+    const float e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
+    s_e[tid] = e == -INFINITY ? INFINITY : e;     // nothing to attend to: no weight
+    if (me == 0 && a.lse) a.lse[(int64_t)b * a.H + h0 + tid] = e * kLn2;
+  }
+  __syncthreads();
+  const int d4 = a.c.d / 4;
+  for (int i = me * kThreads + tid; i < rows_here * d4; i += ncta * kThreads) {
+    const int r = i / d4, d = (i - r * d4) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < ncta; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(s_o, k) + r * D + d);
+      const float f = s_f[k][r];
+      v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
+      v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+    }
+    T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)(h0 + r) * a.o_sh + d;
+    store_elem(out, 0, v.x);
+    store_elem(out, 1, v.y);
+    store_elem(out, 2, v.z);
+    store_elem(out, 3, v.w);
+  }
+  if (a.score) {
+    const int j0 = t0 * kTile, n = min(len - j0, mine * kTile);
+    float* acc = a.c.acc + (int64_t)b * a.c.acc_sb + (int64_t)hk * a.c.acc_sh + j0;
+    for (int j = tid; j < n; j += kThreads) {
+      const float old = a.add ? acc[j] : 0.f;
+      float s = 0.f;
+#pragma unroll 8
+      for (int r = 0; r < rows_here; ++r) s += ex2(s_lg[r * stride + j] - s_e[r]);
+      acc[j] = fmaf(s, a.wmean, old);
+    }
+  }
+  cluster.sync();      // no CTA leaves while another reads its O
 }
 
 // --------------------------------------------------------- second kernels --
@@ -997,11 +1231,28 @@ cache_finish_kernel(const __grid_constant__ CacheAttn a, int joins, int parts) {
 // most, by registers).
 struct Shape {
   int G, D, rows, groups, tile, grid;
+  int cluster;      // CTAs of a unit's cluster; 0: the line of tiles
   bool defer;
   long long tiles;
 };
 
-Shape shape_of(const avits_kv_cache& c, int H, int num_sms) {
+constexpr int kMaxDynamic = 220 * 1024;
+constexpr int kClusterKeys = 512;       // of a CTA
+constexpr int kClusterLogits = 8192;    // rows times keys of a CTA
+
+int cluster_of(const avits_kv_cache& c, const Shape& s, bool score) {
+  if (score && s.groups > 1) return 0;      // a unit has not all the heads of a weight
+  const int rows = s.G < s.rows ? s.G : s.rows;
+  const long long units = (long long)c.B * c.Hkv * s.groups;
+  int n = 1;
+  while (n < 8 && (int64_t)n * kClusterKeys < c.max_len) n *= 2;
+  if ((int64_t)n * kClusterKeys < c.max_len) return 0;
+  if (score && (int64_t)rows * c.max_len > (int64_t)n * kClusterLogits) return 0;
+  if (units * n >= (1 << 30)) return 0;
+  return n;
+}
+
+Shape shape_of(const avits_kv_cache& c, int H, bool score, int num_sms) {
   Shape s;
   const bool bf = c.dt == AVITS_BF16;
   s.G = H / c.Hkv;
@@ -1016,6 +1267,7 @@ Shape shape_of(const avits_kv_cache& c, int H, int num_sms) {
   s.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
   // units of 16 pieces and more: their O is joined by blocks of its own
   s.defer = (long long)c.B * c.Hkv * s.groups * 16 <= s.grid;
+  s.cluster = cluster_of(c, s, score);
   return s;
 }
 
@@ -1039,12 +1291,80 @@ Layout layout_of(const avits_kv_cache& c, int H, const Shape& s, bool score) {
   return l;
 }
 
+// Tensor map of the pages: boxes of `box` tokens of one head and page, in columns
+// of 128 bytes with the 128-byte swizzle (bf16) or whole rows (fp32).
 template <typename Rows>
-cudaError_t launch_rows(const CacheAttn& a, cudaStream_t s) {
+bool map_pages(CUtensorMap* map, const void* pages, int64_t sp, int64_t st, int64_t sh,
+               const avits_kv_cache& c, int box) {
+  const tc::EncodeTiledFn fn = tc::encode_fn();
+  if (!fn) return false;
+  constexpr int64_t es = sizeof(typename Rows::T);
+  // a dimension of extent 1 has a stride that is never used
+  const int64_t row = c.d * es;
+  const cuuint64_t dims[4] = {(cuuint64_t)c.d, (cuuint64_t)c.Hkv, (cuuint64_t)c.page_size,
+                              (cuuint64_t)c.num_pages};
+  const int64_t str[3] = {c.Hkv > 1 ? sh * es : row, c.page_size > 1 ? st * es : row,
+                          c.num_pages > 1 ? sp * es : row};
+  cuuint64_t strides[3];
+  for (int i = 0; i < 3; ++i) {
+    if (str[i] <= 0 || str[i] >= (1ll << 40)) return false;
+    strides[i] = (cuuint64_t)str[i];
+  }
+  const cuuint32_t width = Rows::kBf16 ? 64 : Rows::D;
+  const cuuint32_t shape[4] = {width, 1, (cuuint32_t)box, 1}, step[4] = {1, 1, 1, 1};
+  return fn(map, Rows::kBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
+            4, const_cast<void*>(pages), dims, strides, shape, step,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            Rows::kBf16 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+            row >= 256 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The maps, and a.box: 0 where the pages' layout has none.
+template <typename Rows>
+void map_cache(CacheAttn& a, CUtensorMap* mk, CUtensorMap* mv) {
+  const avits_kv_cache& c = a.c;
+  const int box = c.page_size % Rows::kTile == 0 ? Rows::kTile : c.page_size % 8 == 0 ? 8 : 0;
+  a.box = box && map_pages<Rows>(mk, c.k_pages, c.k_sp, c.k_st, c.k_sh, c, box) &&
+                  map_pages<Rows>(mv, c.v_pages, c.v_sp, c.v_st, c.v_sh, c, box)
+              ? box
+              : 0;
+}
+
+template <typename Rows>
+cudaError_t launch_cluster(const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttn& a,
+                           int ncta, cudaStream_t s) {
+  constexpr auto kernel = cache_cluster_kernel<Rows>;
+  const cudaError_t e = prefer_max_shared<kernel, kMaxDynamic>();
+  if (e != cudaSuccess) return e;
+  const int tiles = (a.c.max_len + a.tile - 1) / a.tile;
+  const int stride = a.score ? logit_stride((tiles + ncta - 1) / ncta * a.tile) : 0;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(a.c.B * a.c.Hkv * a.groups * ncta));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = (size_t)cluster_smem<Rows>(a.G < a.rows ? a.G : a.rows, stride);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)ncta;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, mk, mv, a, stride);
+}
+
+template <typename Rows>
+cudaError_t launch_rows(CacheAttn& a, int ncta, cudaStream_t s) {
+  CUtensorMap mk{}, mv{};
+  map_cache<Rows>(a, &mk, &mv);
+  if (ncta > 0) return launch_cluster<Rows>(mk, mv, a, ncta, s);
   constexpr auto kernel = cache_attention_kernel<Rows>;
   cudaError_t e = prefer_max_shared<kernel, smem_bytes<Rows>()>();
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kernel, dim3(a.grid), dim3(kThreads), smem_bytes<Rows>(), s, a);
+  e = launch_pdl(kernel, dim3(a.grid), dim3(kThreads), smem_bytes<Rows>(), s, mk, mv, a);
   if (e != cudaSuccess) return e;
   const int joins = a.defer ? a.c.B * a.H : 0;
   const int parts = a.score ? (a.c.max_len + kWeightKeys - 1) / kWeightKeys : 0;
@@ -1057,10 +1377,10 @@ cudaError_t launch_rows(const CacheAttn& a, cudaStream_t s) {
 }
 
 template <template <int, int> class Rows, int kR>
-cudaError_t launch_width(const CacheAttn& a, int D, cudaStream_t s) {
-  if (D == 64) return launch_rows<Rows<64, kR>>(a, s);
-  if (D == 128) return launch_rows<Rows<128, kR>>(a, s);
-  if constexpr (kR <= 16) return launch_rows<Rows<256, kR>>(a, s);
+cudaError_t launch_width(CacheAttn& a, int D, int ncta, cudaStream_t s) {
+  if (D == 64) return launch_rows<Rows<64, kR>>(a, ncta, s);
+  if (D == 128) return launch_rows<Rows<128, kR>>(a, ncta, s);
+  if constexpr (kR <= 16) return launch_rows<Rows<256, kR>>(a, ncta, s);
   return cudaErrorInvalidValue;
 }
 
@@ -1068,19 +1388,19 @@ cudaError_t launch_width(const CacheAttn& a, int D, cudaStream_t s) {
 
 bool cache_attention_sizes_ok(const avits_kv_cache& c, int H) {
   if (H / c.Hkv > kMaxGroup) return false;
-  const Shape s = shape_of(c, H, 1);
+  const Shape s = shape_of(c, H, false, 1);
   return s.tiles < (1ll << 30) && (long long)c.B * H < (1ll << 30);
 }
 
 size_t cache_attention_workspace(const avits_kv_cache& c, int H, bool score, int num_sms) {
-  return layout_of(c, H, shape_of(c, H, num_sms), score).total;
+  return layout_of(c, H, shape_of(c, H, score, num_sms), score).total;
 }
 
 cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsigned int* status,
                                    cudaStream_t s) {
   const avits_kv_cache& c = call.cache;
   const bool score = call.weights != AVITS_WEIGHTS_NONE;
-  const Shape sh = shape_of(c, call.H, num_sms);
+  const Shape sh = shape_of(c, call.H, score, num_sms);
   const Layout l = layout_of(c, call.H, sh, score);
   char* ws = static_cast<char*>(call.ws);
   CacheAttn a{};
@@ -1096,7 +1416,6 @@ cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsig
   a.groups = sh.groups;
   a.tile = sh.tile;
   a.grid = sh.grid;
-  a.in_page = c.page_size % sh.tile == 0;
   a.score = score;
   a.defer = sh.defer;
   a.scale2 = call.scale * kLog2e;
@@ -1110,10 +1429,10 @@ cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsig
   a.logits = reinterpret_cast<float*>(ws + l.logits);
   a.ld = l.ld;
   a.status = status;
-  if (c.dt != AVITS_BF16) return launch_width<RowsF32, 8>(a, sh.D, s);
-  if (sh.rows == 8) return launch_width<RowsBf16, 8>(a, sh.D, s);
-  if (sh.rows == 16) return launch_width<RowsBf16, 16>(a, sh.D, s);
-  return launch_width<RowsBf16, 32>(a, sh.D, s);
+  if (c.dt != AVITS_BF16) return launch_width<RowsF32, 8>(a, sh.D, sh.cluster, s);
+  if (sh.rows == 8) return launch_width<RowsBf16, 8>(a, sh.D, sh.cluster, s);
+  if (sh.rows == 16) return launch_width<RowsBf16, 16>(a, sh.D, sh.cluster, s);
+  return launch_width<RowsBf16, 32>(a, sh.D, sh.cluster, s);
 }
 
 }  // namespace avits
