@@ -531,10 +531,7 @@ avits_status avits_cache_append(const avits_kv_cache* cache, const void* k_new, 
  *         same bits.
  * H a multiple of Hkv, at most 256 heads to a KV head.
  * workspace/ws_bytes : at least avits_cache_attention_workspace(...) bytes,
- *         16-byte aligned.  Its first 4096 bytes (counters) must be ZERO before
- *         its first use, and every completed call leaves them zero, so that it
- *         is reused as is, also by calls with other sizes.  Not used by two
- *         calls at once. */
+ *         16-byte aligned, of any content; not used by two calls at once. */
 typedef enum {
   AVITS_WEIGHTS_NONE = 0, AVITS_WEIGHTS_WRITE = 1, AVITS_WEIGHTS_ADD = 2
 } avits_weights;

@@ -632,17 +632,11 @@ def _scratch(cache: KVCache, need: int, handle: int):
         with torch.cuda.stream(s):
             return _scratch(cache, need, handle)
     if torch.cuda.is_current_stream_capturing():
-        return _counters_zeroed(torch, need, cache.device)
+        return torch.empty(need, dtype=torch.uint8, device=cache.device)
     key = (cache._index, handle, get_ident())
     buf = _cache_ws.get(key)
     if buf is None or buf.numel() < need:
-        buf = _cache_ws[key] = _counters_zeroed(torch, need, cache.device)
-    return buf
-
-
-def _counters_zeroed(torch, need, device):
-    buf = torch.empty(need, dtype=torch.uint8, device=device)
-    buf[:4096].zero_()
+        buf = _cache_ws[key] = torch.empty(need, dtype=torch.uint8, device=cache.device)
     return buf
 
 
@@ -680,9 +674,8 @@ def avits_cache_attention(cache: KVCache, q, softmax_scale: float, o, lse=None,
     hk*G+G-1 share KV head hk, G = H / Hkv) and lse [B,H] fp32.  With ``weight``
     cache.acc gets weight times the mean over a KV head's query heads of the
     softmax weight of each cached token, added (or written).  ``workspace``: a
-    device byte tensor of avits_cache_attention_workspace() bytes, zeros before
-    its first use, of the caller's own where calls may overlap; by default the
-    library's."""
+    device byte tensor of avits_cache_attention_workspace() bytes, of the
+    caller's own where calls may overlap; by default the library's."""
     B, H, d = q.shape
     if B != cache.B or d != cache.d or o.shape != q.shape:
         raise ValueError("q and o must be [B, H, d] of the cache")

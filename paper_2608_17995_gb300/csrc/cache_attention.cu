@@ -13,13 +13,14 @@
 // the lengths.  Its warps take the piece's tiles in turn, each with a running
 // maximum, sum and O in registers and a ring of tiles of its own in shared
 // memory, filled by TMA copies that run ahead over unit borders; the warps meet
-// once per unit.  A unit that lies in one piece is finished there; of
-// the others each piece leaves its maximum, sum and O, and the CTA that is last
-// to do so joins them, in the pieces' order.
+// once per unit.  A unit that lies in one piece is finished there; of the others
+// each piece leaves its maximum, sum and O, and a second kernel joins them, in the
+// pieces' order.  The weights need the whole row's lse: the first kernel leaves the
+// logits (fp32), the second sums exp(x - lse) over the group's heads, in a fixed
+// order.
 //
-// The weights need the whole row's lse: the first kernel leaves the logits
-// (fp32), a second one sums exp(x - lse) over the group's heads, in a fixed
-// order.  Where units have many pieces, it joins their O as well.
+// Shorter sequences take one launch: a cluster of CTAs per unit, whose logits
+// stay in shared memory.
 #include <cooperative_groups.h>
 
 #include "cache_common.cuh"
@@ -34,7 +35,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMinTiles = 4;      // tiles of the smallest piece: one per warp
-constexpr int kMaxPieces = 1024;
+constexpr int kMaxGrid = 1024;
 constexpr unsigned long long kLateNs = 1000ull * 1000ull;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -53,15 +54,15 @@ struct CacheAttn {
   int grid;         // CTAs of the first kernel
   int box;          // tokens of a TMA box; 0: rows come by 16-byte copies
   int score;        // weights wanted: logits are kept
-  int defer;        // the second kernel joins O
+  int few;          // units have few pieces each
   float scale2;     // scale * log2(e)
   float wmean;      // weight / G
   int add;
   // workspace
-  unsigned* count;  // [kMaxPieces] pieces that left their part, by a unit's first piece;
-                    // zero between calls
-  int* starts;      // [B+1] first tile of a sequence on the line (defer)
-  float* lse2;      // [B,H] log2-domain lse (weights wanted, or defer)
+  int2* rec;        // [B units] first part of a unit and its pieces; one: it is in lse2
+  int4* own;        // [grid] unit whose first piece is the CTA's, of several: (unit or -1,
+                    // first part, pieces); read where units have few pieces
+  float* lse2;      // [B,H] log2-domain lse of rows finished in one piece
   float2* pml;      // [2 grid][rows] maximum and sum of a piece's row
   float* po;        // [2 grid][rows][d] its O
   float* logits;    // [B,H,ld] log2-domain logits (weights wanted)
@@ -632,9 +633,9 @@ struct RowsF32 {
 // ----------------------------------------------------------- first kernel --
 // Stages of a warp's ring, and CTAs that share an SM.
 template <typename Rows>
-constexpr int stages() { return Rows::D == 64 ? 4 : Rows::D == 128 && Rows::kR < 32 ? 3 : 2; }
+constexpr int stages() { return Rows::D == 64 ? 3 : 2; }
 template <typename Rows>
-constexpr int ctas_per_sm() { return Rows::D <= 128 ? 2 : 1; }
+constexpr int ctas_per_sm() { return Rows::D > 128 ? 1 : Rows::kR == 8 ? 3 : 2; }
 template <typename Rows>
 constexpr int smem_bytes() {
   return kWarps * stages<Rows>() * Rows::kStage + Rows::kQBytes + kWarps * Rows::kWarpBytes;
@@ -650,68 +651,6 @@ __device__ __forceinline__ void one_tile(Rows& r, const CacheAttn& a, const char
     r.tile(a, 0u, sq, sw, mask, lg, rows, lane, st);
 }
 
-// The lse of a unit's rows from the pieces c0 .. c1 (the first piece's part is
-// its CTA's second where `second`), and O unless that is left to the second
-// kernel.  Read past L1: other CTAs wrote them.
-__device__ __forceinline__ int part_of(int c, int c0, bool second) {
-  return 2 * c + (c == c0 && second ? 1 : 0);
-}
-
-template <typename Rows>
-__device__ __noinline__ void join_unit(const CacheAttn& a, int b, int2 h, int c0, int c1,
-                                       bool second, float* s_e) {
-  using T = typename Rows::T;
-  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
-  for (int r = w; r < h.y; r += kWarps) {
-    float top = -INFINITY, l = 0.f;
-    for (int c = c0 + lane; c <= c1; c += 32) {
-      const float2 x = __ldcg(a.pml + part_of(c, c0, second) * Rows::kR + r);
-      const float mn = fmaxf(top, x.x), ref = mn == -INFINITY ? 0.f : mn;
-      l = l * ex2(top - ref) + x.y * ex2(x.x - ref);   // a NaN stays one
-      top = mn;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float tx = __shfl_xor_sync(0xffffffffu, top, o);
-      const float lx = __shfl_xor_sync(0xffffffffu, l, o);
-      const float mn = fmaxf(top, tx), ref = mn == -INFINITY ? 0.f : mn;
-      l = l * ex2(top - ref) + lx * ex2(tx - ref);
-      top = mn;
-    }
-    const float e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
-    if (lane == 0) {
-      s_e[r] = e;
-      if (a.score || a.defer) a.lse2[(int64_t)b * a.H + h.x + r] = e;
-      if (a.lse) a.lse[(int64_t)b * a.H + h.x + r] = e * kLn2;
-    }
-  }
-  if (a.defer) return;
-  __syncthreads();
-  const int d4 = a.c.d / 4;
-  for (int i = tid; i < h.y * d4; i += kThreads) {
-    const int r = i / d4, d = (i - r * d4) * 4;
-    const float e = s_e[r];
-    const float none = e != e ? e : 0.f;
-    float4 v = make_float4(none, none, none, none);
-    if (e != -INFINITY) {
-#pragma unroll 4
-      for (int c = c0; c <= c1; ++c) {
-        const int at = part_of(c, c0, second) * Rows::kR + r;
-        const float mx = __ldcg(&a.pml[at].x);
-        const float4 x = __ldcg(reinterpret_cast<const float4*>(a.po + (int64_t)at * a.c.d + d));
-        const float f = ex2(mx - e);     // mx = -inf: 0
-        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
-        v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
-      }
-    }
-    T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)(h.x + r) * a.o_sh + d;
-    store_elem(out, 0, v.x);
-    store_elem(out, 1, v.y);
-    store_elem(out, 2, v.z);
-    store_elem(out, 3, v.w);
-  }
-}
-
 template <typename Rows>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm<Rows>())
 cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
@@ -723,13 +662,15 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_cons
   __shared__ int s_free[2][kWarps];
   __shared__ uint64_t s_full[kWarps][NS];
   __shared__ uint32_t s_mask[kWarps][NS];
-  __shared__ int s_scan[kWarps], s_b, s_off, s_last;
-  __shared__ float s_e[kR];
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
   if (lane < NS) mbar_init(&s_full[w][lane], a.box ? 1 : 32);   // a warp's barriers are its own
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   before_copies();
   __syncwarp();
+  if (tid == 0 && a.box) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mk));
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mv));
+  }
   pdl_wait_then_trigger();
 
   // sequences without cached tokens
@@ -743,14 +684,14 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_cons
     }
   }
 
-  // where this CTA's piece of the line of tiles begins
+  // where this CTA's piece of the line of tiles begins: every warp scans the
+  // lengths, a lane a contiguous run of them
   const int B = a.c.B, units = a.c.Hkv * a.groups;
-  const int each = (B + kThreads - 1) / kThreads;
-  const int b0 = min(B, tid * each), b1 = min(B, b0 + each);
+  const int each = (B + 31) / 32, b0 = min(B, lane * each), b1 = min(B, b0 + each);
   int sum = 0;
   for (int b = b0; b < b1; ++b) {
     sum += tiles_of(a, cache_len(a.c, b)) * units;
-    if (blockIdx.x == 0) check_cache_len(a.c, b, a.status);
+    if (blockIdx.x == 0 && w == 0) check_cache_len(a.c, b, a.status);
   }
   int inc = sum;
 #pragma unroll
@@ -758,43 +699,31 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_cons
     const int y = __shfl_up_sync(0xffffffffu, inc, o);
     if (lane >= o) inc += y;
   }
-  if (lane == 31) s_scan[w] = inc;
-  __syncthreads();
-  int total = 0, before = inc - sum;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    if (i < w) before += s_scan[i];
-    total += s_scan[i];
-  }
-  if (blockIdx.x == 0 && a.defer) {
-    int at = before;
-    for (int b = b0; b < b1; ++b) {
-      a.starts[b] = at;
-      at += tiles_of(a, cache_len(a.c, b)) * units;
-    }
-    if (tid == 0) a.starts[B] = total;
-  }
+  const int total = __shfl_sync(0xffffffffu, inc, 31);
   const int per = max(kMinTiles, (total + a.grid - 1) / a.grid);
   const int first = blockIdx.x * per;
-  if (first >= total) return;
-  if (before <= first && first < before + sum) {
-    int at = before, b = b0;
-    for (;; ++b) {
-      const int n = tiles_of(a, cache_len(a.c, b)) * units;
-      if (first < at + n) break;
-      at += n;
-    }
-    s_b = b;
-    s_off = first - at;
+  if (first >= total) {
+    if (tid == 0) a.own[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    return;
   }
+  int sb = b0, soff = first - (inc - sum);
+  const bool here_lane = soff >= 0 && soff < sum;
+  if (here_lane)
+    for (;; ++sb) {
+      const int n = tiles_of(a, cache_len(a.c, sb)) * units;
+      if (soff < n) break;
+      soff -= n;
+    }
+  const int src = __ffs(__ballot_sync(0xffffffffu, here_lane)) - 1;
+  sb = __shfl_sync(0xffffffffu, sb, src);
+  soff = __shfl_sync(0xffffffffu, soff, src);
   char* ring = smem + w * NS * Rows::kStage;
   char* s_q = smem + kWarps * NS * Rows::kStage;
   char* s_w = s_q + Rows::kQBytes + w * Rows::kWarpBytes;
-  __syncthreads();
 
-  int left = min(per, total - first), b = s_b;
+  int left = min(per, total - first), b = sb;
   int len = cache_len(a.c, b), nt = tiles_of(a, len);
-  int u = s_off / nt, t0 = s_off - u * nt;
+  int u = soff / nt, t0 = soff - u * nt;
   Cursor cur{b, u, t0 + w, nt, len, (left - w + kWarps - 1) / kWarps, -1};
   if (cur.left > 0) {
     cur.settle(a, units);
@@ -804,11 +733,6 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_cons
     const int hk = a.groups == 1 ? uu : uu / a.groups, row0 = (uu - hk * a.groups) * kR;
     return make_int2(hk * a.G + row0, min(kR, a.G - row0));
   };
-  {
-    const int2 h = h_of(u);
-    for (int i = tid; i < Rows::kQPieces; i += kThreads)
-      Rows::store_q(s_q, i, Rows::load_q(a, b, h.x, h.y, i));
-  }
   // stage `fill` is the free one: the tile after the last issued goes there
   int fill = 0, use = 0;
   uint32_t phase = 0;
@@ -819,12 +743,24 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_cons
                       units, lane);
     fill = fill + 1 == NS ? 0 : fill + 1;
   };
+  constexpr int kQEach = (Rows::kQPieces + kThreads - 1) / kThreads;
+  uint4 nq[kQEach];
+  {
+    const int2 h = h_of(u);
+#pragma unroll
+    for (int k = 0; k < kQEach; ++k)
+      if (tid + k * kThreads < Rows::kQPieces)
+        nq[k] = Rows::load_q(a, b, h.x, h.y, tid + k * kThreads);
+  }
 #pragma unroll 1
   for (int i = 0; i < NS - 1; ++i) issue();
+#pragma unroll
+  for (int k = 0; k < kQEach; ++k)
+    if (tid + k * kThreads < Rows::kQPieces) Rows::store_q(s_q, tid + k * kThreads, nq[k]);
   __syncthreads();      // Q is there
 
-  constexpr int kQEach = (Rows::kQPieces + kThreads - 1) / kThreads;
   int f0 = 0, seg = 0;
+  int4 own = make_int4(-1, 0, 0, 0);
   Rows rows;
   while (left > 0) {
     const int t1 = min(nt, t0 + left);
@@ -832,7 +768,6 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_cons
     // the next unit, and its Q on the way
     int nb = b, nu = u + 1, nlen = len, nnt = nt;
     const int after = left - (t1 - t0);
-    uint4 nq[kQEach];
     if (after > 0) {
       if (nu == units) {
         nu = 0;
@@ -920,23 +855,18 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_cons
       before_copies();
       __syncthreads();     // the free stages are free again
     }
-    if (!whole) {
-      const int T0 = first + f0 - t0, c0 = T0 / per, c1 = (T0 + nt - 1) / per;
-      if (tid == 0) {
-        __threadfence();
-        s_last = atomicAdd(&a.count[c0], 1u) == (unsigned)(c1 - c0);
-        if (s_last) a.count[c0] = 0u;
-        __threadfence();
-      }
-      __syncthreads();
-      if (s_last) join_unit<Rows>(a, b, h, c0, c1, T0 != c0 * per, s_e);
-      __syncthreads();
+    if (t0 == 0) {
+      const int T0 = first + f0, c1 = (T0 + nt - 1) / per;
+      const int pieces = c1 - (int)blockIdx.x + 1;
+      if (pieces > 1) own = make_int4(b * units + u, slot, pieces, 0);
+      if (tid == 0 && (a.score || !a.few)) a.rec[b * units + u] = make_int2(slot, pieces);
     }
     ++seg;
     f0 += t1 - t0;
     left = after;
     b = nb; u = nu; len = nlen; nt = nnt; t0 = 0;
   }
+  if (tid == 0) a.own[blockIdx.x] = own;
 }
 
 // ---------------------------------------------------------- one launch --
@@ -977,6 +907,10 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   before_copies();
   __syncwarp();
+  if (tid == 0 && a.box) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mk));
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mv));
+  }
   pdl_wait_then_trigger();
   if (u == 0 && me == 0 && tid == 0) check_cache_len(a.c, b, a.status);
   const int len = cache_len(a.c, b);
@@ -1120,47 +1054,201 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
   cluster.sync();      // no CTA leaves while another reads its O
 }
 
-// --------------------------------------------------------- second kernels --
-// Weights: block (b, hk, 512 keys), 4 keys to a thread, the group's logits in
-// 16-byte loads.  The loads wait for nothing but the length.
-constexpr int kWeightThreads = 128;
-constexpr int kWeightKeys = 4 * kWeightThreads;
+// ---------------------------------------------------------- second kernel --
+// Block (unit, row), or, where there are many units, (CTA of the first kernel,
+// rows): O of that unit, or of the one whose first of several pieces was that
+// CTA's.  Block (b, hk, 512 keys): their weights, 4 keys to a thread.  What a block reads waits
+// for as little as can be: parts and logits are on their way while the row's lse
+// is put together.
+constexpr int kFinishThreads = 128;
+constexpr int kWeightKeys = 4 * kFinishThreads;
 constexpr int kMaxGroup = 256;
+constexpr int kFewPieces = 8;
+
+// Part of piece k of a unit: the first one's is given, the following CTAs' are
+// their first.
+__device__ __forceinline__ int part_of(int slot, int k) { return k == 0 ? slot : ((slot >> 1) + k) * 2; }
+
+// log2-domain lse of row r over a unit's pieces, in a whole warp.
+__device__ __forceinline__ float join_lse(const CacheAttn& a, int slot, int pieces, int r,
+                                          int lane) {
+  constexpr int kDeep = 4;
+  float top = -INFINITY, l = 0.f;
+  for (int k0 = lane; k0 < pieces; k0 += 32 * kDeep) {
+    float2 x[kDeep];
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      const int k = k0 + 32 * i;
+      x[i] = k < pieces ? a.pml[part_of(slot, k) * a.rows + r] : make_float2(-INFINITY, 0.f);
+    }
+    float mn = top;
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) mn = fmaxf(mn, x[i].x);
+    const float ref = mn == -INFINITY ? 0.f : mn;
+    l *= ex2(top - ref);                                  // a NaN stays one
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) l = fmaf(ex2(x[i].x - ref), x[i].y, l);
+    top = mn;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float tx = __shfl_xor_sync(0xffffffffu, top, o);
+    const float lx = __shfl_xor_sync(0xffffffffu, l, o);
+    const float mn = fmaxf(top, tx), ref = mn == -INFINITY ? 0.f : mn;
+    l = l * ex2(top - ref) + lx * ex2(tx - ref);
+    top = mn;
+  }
+  return l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
+}
+
+// The same in one thread, for few pieces.
+__device__ __forceinline__ float join_lse_serial(const CacheAttn& a, int slot, int pieces, int r) {
+  float top = -INFINITY, l = 0.f;
+  for (int k0 = 0; k0 < pieces; k0 += kFewPieces) {
+    float2 x[kFewPieces];
+#pragma unroll
+    for (int i = 0; i < kFewPieces; ++i)
+      x[i] = k0 + i < pieces ? a.pml[part_of(slot, k0 + i) * a.rows + r]
+                             : make_float2(-INFINITY, 0.f);
+    float mn = top;
+#pragma unroll
+    for (int i = 0; i < kFewPieces; ++i) mn = fmaxf(mn, x[i].x);
+    const float ref = mn == -INFINITY ? 0.f : mn;
+    l *= ex2(top - ref);
+#pragma unroll
+    for (int i = 0; i < kFewPieces; ++i) l = fmaf(ex2(x[i].x - ref), x[i].y, l);
+    top = mn;
+  }
+  return l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
+}
+
+// `wide`: `at` is a unit, threads lie side by side over the pieces of one row;
+// else it is a CTA of the first kernel and threads lie over the rows, each going
+// through its row's pieces.
+template <typename T>
+__device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, int wide) {
+  __shared__ float4 s_sum[kFinishThreads];
+  const int tid = threadIdx.x, units = a.c.Hkv * a.groups;
+  int4 own;
+  if (wide) {
+    if (cache_len(a.c, at0 / units) == 0) return;
+    const int2 rec = a.rec[at0];
+    own = make_int4(rec.y > 1 ? at0 : -1, rec.x, rec.y, 0);
+  } else {
+    own = a.own[at0];
+  }
+  if (own.x < 0) return;
+  const int b = own.x / units, u = own.x - b * units, hk = u / a.groups;
+  const int d4 = a.c.d / 4, lanes = kFinishThreads / d4, col = tid % d4, sub = tid / d4;
+  const int r = wide ? r0 : r0 + sub, step = wide ? lanes : 1;
+  const int row = (u - hk * a.groups) * a.rows + r, h = hk * a.G + row;
+  const bool mine = sub < lanes && r < a.rows && row < a.G;
+  const int pieces = mine ? own.z : 0, k1 = wide ? sub : 0;
+  constexpr int kDeep = 8;
+  float4 x[kDeep];
+  float mx[kDeep];
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      const int k = k0 + i * step;
+      if (k < pieces) {
+        const int at = part_of(own.y, k) * a.rows + r;
+        x[i] = *reinterpret_cast<const float4*>(a.po + (int64_t)at * a.c.d + col * 4);
+        mx[i] = a.pml[at].x;
+      }
+    }
+  };
+  load(k1);
+  const float e = wide ? (row < a.G ? join_lse(a, own.y, own.z, r, tid & 31) : 0.f)
+                       : join_lse_serial(a, own.y, pieces, r);
+  if (mine && k1 == 0 && col == 0 && a.lse) a.lse[(int64_t)b * a.H + h] = e * kLn2;
+  const float none = e != e ? e : 0.f;
+  float4 v = make_float4(none, none, none, none);
+  if (e != -INFINITY) {
+    for (int k0 = k1; k0 < pieces; k0 += kDeep * step) {
+      if (k0 != k1) load(k0);
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i)
+        if (k0 + i * step < pieces) {
+          const float f = ex2(mx[i] - e);     // from -inf: 0
+          v.x = fmaf(f, x[i].x, v.x); v.y = fmaf(f, x[i].y, v.y);
+          v.z = fmaf(f, x[i].z, v.z); v.w = fmaf(f, x[i].w, v.w);
+        }
+    }
+  }
+  if (wide) {
+    s_sum[tid] = v;
+    __syncthreads();
+    if (sub != 0) return;
+    for (int k = 1; k < lanes; ++k) {
+      const float4 y = s_sum[k * d4 + col];
+      v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
+    }
+  }
+  if (!mine) return;
+  T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh + col * 4;
+  store_elem(out, 0, v.x);
+  store_elem(out, 1, v.y);
+  store_elem(out, 2, v.z);
+  store_elem(out, 3, v.w);
+}
 
 __device__ __forceinline__ void weights_block(const CacheAttn& a, int bh, int part) {
   __shared__ float s_e[kMaxGroup];
   const int b = bh / a.c.Hkv, hk = bh - b * a.c.Hkv, tid = threadIdx.x;
   const int len = cache_len(a.c, b), j = part * kWeightKeys + tid * 4;
   if (part * kWeightKeys >= len) return;
-  for (int r = tid; r < a.G; r += kWeightThreads) {
-    const float e = a.lse2[(int64_t)b * a.H + hk * a.G + r];
-    s_e[r] = e == -INFINITY ? INFINITY : e;   // nothing to attend to: no weight
-  }
+  const float* lg = a.logits + ((int64_t)b * a.H + hk * a.G) * a.ld + min(j, len - 1) / 4 * 4;
+  constexpr int kDeep = 8;
+  float4 x[kDeep];
+#pragma unroll
+  for (int r = 0; r < kDeep; ++r)
+    if (r < a.G) x[r] = *reinterpret_cast<const float4*>(lg + (int64_t)r * a.ld);
   float* acc = a.c.acc + (int64_t)b * a.c.acc_sb + (int64_t)hk * a.c.acc_sh + j;
   const bool vec = (reinterpret_cast<uintptr_t>(acc) & 15u) == 0 && j + 4 <= len;
   float old[4] = {};
   if (a.add && j < len) {
     if (vec) {
-      const float4 x = *reinterpret_cast<const float4*>(acc);
-      old[0] = x.x; old[1] = x.y; old[2] = x.z; old[3] = x.w;
+      const float4 y = *reinterpret_cast<const float4*>(acc);
+      old[0] = y.x; old[1] = y.y; old[2] = y.z; old[3] = y.w;
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (j + k < len) old[k] = acc[k];
     }
   }
+  if (a.few) {
+    for (int r = tid; r < a.G; r += kFinishThreads) {
+      const int rg = r / a.rows;
+      const int2 rec = a.rec[(b * a.c.Hkv + hk) * a.groups + rg];
+      const float e = rec.y == 1 ? a.lse2[(int64_t)b * a.H + hk * a.G + r]
+                                 : join_lse_serial(a, rec.x, rec.y, r - rg * a.rows);
+      s_e[r] = e == -INFINITY ? INFINITY : e;   // nothing there: no weight
+    }
+  } else {
+    for (int r = tid >> 5; r < a.G; r += kFinishThreads / 32) {
+      const int rg = r / a.rows;
+      const int2 rec = a.rec[(b * a.c.Hkv + hk) * a.groups + rg];
+      const float e = rec.y == 1 ? a.lse2[(int64_t)b * a.H + hk * a.G + r]
+                                 : join_lse(a, rec.x, rec.y, r - rg * a.rows, tid & 31);
+      if ((tid & 31) == 0) s_e[r] = e == -INFINITY ? INFINITY : e;
+    }
+  }
   __syncthreads();
   if (j >= len) return;
-  const float* lg = a.logits + ((int64_t)b * a.H + hk * a.G) * a.ld + j;
   float s[4] = {};
-#pragma unroll 8
-  for (int r = 0; r < a.G; ++r) {
-    const float4 x = *reinterpret_cast<const float4*>(lg + (int64_t)r * a.ld);
-    const float e = s_e[r];
-    s[0] += ex2(x.x - e);
-    s[1] += ex2(x.y - e);
-    s[2] += ex2(x.z - e);
-    s[3] += ex2(x.w - e);
+  for (int r0 = 0; r0 < a.G; r0 += kDeep) {
+#pragma unroll
+    for (int r = 0; r < kDeep; ++r) {
+      if (r0 + r < a.G) {
+        if (r0 > 0) x[r] = *reinterpret_cast<const float4*>(lg + (int64_t)(r0 + r) * a.ld);
+        const float e = s_e[r0 + r];
+        s[0] += ex2(x[r].x - e);
+        s[1] += ex2(x[r].y - e);
+        s[2] += ex2(x[r].z - e);
+        s[3] += ex2(x[r].w - e);
+      }
+    }
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) s[k] = fmaf(s[k], a.wmean, old[k]);
@@ -1173,56 +1261,18 @@ __device__ __forceinline__ void weights_block(const CacheAttn& a, int bh, int pa
   }
 }
 
-// O of one row that was cut into pieces: threads side by side along the row and
-// over the pieces.
 template <typename T>
-__device__ __forceinline__ void join_block(const CacheAttn& a, int b, int h) {
-  __shared__ float4 s_sum[kWeightThreads];
-  const int tid = threadIdx.x, len = cache_len(a.c, b), nt = tiles_of(a, len);
-  if (nt == 0) return;
-  const int hk = h / a.G, r = h - hk * a.G, rg = r / a.rows, rr = r - rg * a.rows;
-  const int per = max(kMinTiles, (a.starts[a.c.B] + a.grid - 1) / a.grid);
-  const int T0 = a.starts[b] + (hk * a.groups + rg) * nt;
-  const int c0 = T0 / per, c1 = (T0 + nt - 1) / per;
-  if (c0 == c1) return;
-  const float e = a.lse2[(int64_t)b * a.H + h];
-  const int d4 = a.c.d / 4, lanes = kWeightThreads / d4, col = tid % d4, sub = tid / d4;
-  const float none = e != e ? e : 0.f;
-  float4 v = make_float4(none, none, none, none);
-  if (sub < lanes && e != -INFINITY) {
-#pragma unroll 8
-    for (int c = c0 + sub; c <= c1; c += lanes) {
-      const int at = part_of(c, c0, T0 != c0 * per) * a.rows + rr;
-      const float mx = a.pml[at].x;
-      const float4 x = *reinterpret_cast<const float4*>(a.po + (int64_t)at * a.c.d + col * 4);
-      const float f = ex2(mx - e);
-      v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
-      v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
-    }
-  }
-  s_sum[tid] = v;
-  __syncthreads();
-  if (sub != 0) return;
-  for (int k = 1; k < lanes; ++k) {
-    const float4 x = s_sum[k * d4 + col];
-    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-  }
-  T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh + col * 4;
-  store_elem(out, 0, v.x);
-  store_elem(out, 1, v.y);
-  store_elem(out, 2, v.z);
-  store_elem(out, 3, v.w);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kWeightThreads)
+__global__ void __launch_bounds__(kFinishThreads)
 cache_finish_kernel(const __grid_constant__ CacheAttn a, int joins, int parts) {
   pdl_wait_then_trigger();
   const int i = (int)blockIdx.x - joins;
-  if (i < 0)
-    join_block<T>(a, (int)blockIdx.x / a.H, (int)blockIdx.x % a.H);
-  else
+  if (i < 0) {
+    const int lanes = a.few ? kFinishThreads / (a.c.d / 4) : 1;     // rows of a block
+    const int per = (a.rows + lanes - 1) / lanes;                   // blocks of a CTA's unit
+    join_block<T>(a, (int)blockIdx.x / per, (int)blockIdx.x % per * lanes, !a.few);
+  } else {
     weights_block(a, i / parts, i % parts);
+  }
 }
 
 // How a call is cut: the widths 64, 128 and 256 have kernels of their own; a
@@ -1232,7 +1282,6 @@ cache_finish_kernel(const __grid_constant__ CacheAttn a, int joins, int parts) {
 struct Shape {
   int G, D, rows, groups, tile, grid;
   int cluster;      // CTAs of a unit's cluster; 0: the line of tiles
-  bool defer;
   long long tiles;
 };
 
@@ -1240,15 +1289,21 @@ constexpr int kMaxDynamic = 220 * 1024;
 constexpr int kClusterKeys = 512;       // of a CTA
 constexpr int kClusterLogits = 8192;    // rows times keys of a CTA
 
-int cluster_of(const avits_kv_cache& c, const Shape& s, bool score) {
+int cluster_of(const avits_kv_cache& c, const Shape& s, bool score, int num_sms) {
   if (score && s.groups > 1) return 0;      // a unit has not all the heads of a weight
   const int rows = s.G < s.rows ? s.G : s.rows;
   const long long units = (long long)c.B * c.Hkv * s.groups;
+  auto fits = [&](int n) {
+    const int64_t keys = ((int64_t)c.max_len + n - 1) / n;
+    return keys <= (score || n > 1 ? kClusterKeys : 2 * kClusterKeys) && (!score || keys * rows <= kClusterLogits);
+  };
   int n = 1;
-  while (n < 8 && (int64_t)n * kClusterKeys < c.max_len) n *= 2;
-  if ((int64_t)n * kClusterKeys < c.max_len) return 0;
-  if (score && (int64_t)rows * c.max_len > (int64_t)n * kClusterLogits) return 0;
-  if (units * n >= (1 << 30)) return 0;
+  while (n < 8 && !fits(n)) n *= 2;
+  if (!fits(n) || units * n >= (1 << 30)) return 0;
+  const long long resident = (long long)num_sms * (s.D > 128 ? 1 : 2);
+  if (n > 1 && units * n > resident) return 0;
+  while (n < 8 && units * n * 2 <= resident && c.max_len > n * 64) n *= 2;
+  if (units * n < num_sms && c.max_len > n * 256) return 0;
   return n;
 }
 
@@ -1262,19 +1317,17 @@ Shape shape_of(const avits_kv_cache& c, int H, bool score, int num_sms) {
   s.tile = bf ? 16 : 8;
   s.tiles = (long long)c.B * c.Hkv * s.groups * ((c.max_len + s.tile - 1) / s.tile);
   const long long most = (s.tiles + kMinTiles - 1) / kMinTiles;
-  long long full = (long long)num_sms * (s.D <= 128 ? 2 : 1);
-  if (full > kMaxPieces) full = kMaxPieces;
+  long long full = (long long)num_sms * (s.D > 128 ? 1 : s.rows == 8 ? 3 : 2);
+  if (full > kMaxGrid) full = kMaxGrid;
   s.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
-  // units of 16 pieces and more: their O is joined by blocks of its own
-  s.defer = (long long)c.B * c.Hkv * s.groups * 16 <= s.grid;
-  s.cluster = cluster_of(c, s, score);
+  s.cluster = cluster_of(c, s, score, num_sms);
   return s;
 }
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
 struct Layout {
-  size_t starts, lse2, pml, po, logits, total;
+  size_t rec, own, lse2, pml, po, logits, total;
   int64_t ld;
 };
 
@@ -1282,8 +1335,9 @@ Layout layout_of(const avits_kv_cache& c, int H, const Shape& s, bool score) {
   Layout l;
   const size_t nrow = s.rows;
   l.ld = ((int64_t)c.max_len + 15) / 16 * 16;
-  l.starts = kMaxPieces * 4;
-  l.lse2 = l.starts + up16(((size_t)c.B + 1) * 4);
+  l.rec = 0;
+  l.own = up16((size_t)c.B * c.Hkv * s.groups * 8);
+  l.lse2 = l.own + up16((size_t)s.grid * 16);
   l.pml = l.lse2 + up16((size_t)c.B * H * 4);
   l.po = l.pml + up16((size_t)2 * s.grid * nrow * 8);
   l.logits = l.po + up16((size_t)2 * s.grid * nrow * c.d * 4);
@@ -1366,14 +1420,14 @@ cudaError_t launch_rows(CacheAttn& a, int ncta, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = launch_pdl(kernel, dim3(a.grid), dim3(kThreads), smem_bytes<Rows>(), s, mk, mv, a);
   if (e != cudaSuccess) return e;
-  const int joins = a.defer ? a.c.B * a.H : 0;
+  const int lanes = a.few ? kFinishThreads / (a.c.d / 4) : 1;
+  const int joins = (a.few ? a.grid : a.c.B * a.c.Hkv * a.groups) * ((a.rows + lanes - 1) / lanes);
   const int parts = a.score ? (a.c.max_len + kWeightKeys - 1) / kWeightKeys : 0;
-  if (joins == 0 && parts == 0) return cudaSuccess;
   constexpr auto finish = cache_finish_kernel<typename Rows::T>;
   e = prefer_max_shared<finish>();
   if (e != cudaSuccess) return e;
   const unsigned blocks = (unsigned)joins + (unsigned)(a.c.B * a.c.Hkv) * (unsigned)parts;
-  return launch_pdl(finish, dim3(blocks), dim3(kWeightThreads), 0, s, a, joins, parts > 0 ? parts : 1);
+  return launch_pdl(finish, dim3(blocks), dim3(kFinishThreads), 0, s, a, joins, parts > 0 ? parts : 1);
 }
 
 template <template <int, int> class Rows, int kR>
@@ -1417,12 +1471,12 @@ cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsig
   a.tile = sh.tile;
   a.grid = sh.grid;
   a.score = score;
-  a.defer = sh.defer;
+  a.few = (long long)c.B * c.Hkv * sh.groups * kFewPieces > sh.grid;
   a.scale2 = call.scale * kLog2e;
   a.wmean = call.weight / (float)sh.G;
   a.add = call.weights == AVITS_WEIGHTS_ADD;
-  a.count = reinterpret_cast<unsigned*>(ws);
-  a.starts = reinterpret_cast<int*>(ws + l.starts);
+  a.rec = reinterpret_cast<int2*>(ws + l.rec);
+  a.own = reinterpret_cast<int4*>(ws + l.own);
   a.lse2 = reinterpret_cast<float*>(ws + l.lse2);
   a.pml = reinterpret_cast<float2*>(ws + l.pml);
   a.po = reinterpret_cast<float*>(ws + l.po);
