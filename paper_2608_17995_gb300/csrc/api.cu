@@ -476,8 +476,8 @@ avits_status avits_cache_evict(const avits_kv_cache* src, const avits_kv_cache* 
     return AVITS_ERR_INVALID_ARG;
   if ((int64_t)src->B * src->Hkv * ((int64_t)keep / 8 + 1) >= (1ll << 31))
     return AVITS_ERR_UNSUPPORTED;
-  return cuda_status(launch_cache_evict(*src, *dst, keep, sinks, recent, keep_idx, status_word(),
-                                        static_cast<cudaStream_t>(stream)));
+  return cuda_status(launch_cache_evict(*src, *dst, keep, sinks, recent, keep_idx, num_sms_current(),
+                                        status_word(), static_cast<cudaStream_t>(stream)));
 }
 
 avits_status avits_selftest_bounded_wait(unsigned long long limit_ns, long long* result,

@@ -168,7 +168,7 @@ cudaError_t launch_cache_append(const avits_kv_cache& c, const void* k_new, cons
                                 int T, const int32_t* cu, int64_t k_st, int64_t k_sh, int64_t v_st,
                                 int64_t v_sh, unsigned int* status, cudaStream_t s);
 cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& dst, int keep,
-                               int sinks, int recent, int32_t* idx, unsigned int* status,
-                               cudaStream_t s);
+                               int sinks, int recent, int32_t* idx, int num_sms,
+                               unsigned int* status, cudaStream_t s);
 
 }  // namespace avits

@@ -100,14 +100,15 @@ cache_append_kernel(const __grid_constant__ Append a) {
 
 // ------------------------------------------------------------------ evict --
 // Selection: a cluster of CTAs per (b, KV head), each with a contiguous part
-// of the row as 32-bit keys whose order is the weights' order (in shared memory
-// where they fit).  The keep-th largest key by radix digits of 8 bits: each CTA
-// counts its digits, every CTA of the cluster adds up the counts through
-// distributed shared memory.  Then the keys above it, and of the equal ones
-// the lowest places, are written in order: a thread owns a contiguous run, and
-// one scan over runs, CTAs included, gives its first rank.
-constexpr int kSelThreads = 512;
-constexpr int kSelMaxKeys = 40960;   // keys of a CTA in shared memory (padded by 1/32)
+// of the row, seen as 32-bit keys whose order is the weights' order and kept in
+// shared memory where they fit.  The keep-th largest key by radix digits of 8
+// bits: each CTA counts its digits, one warp of every CTA adds up the cluster's
+// counts through distributed shared memory.  Then the keys above it, and of the
+// equal ones the lowest places, in order: a thread owns a contiguous run, one scan
+// over runs, CTAs included, gives its first rank, and the CTA's places go out
+// through a list in shared memory, side by side.
+constexpr int kSelMaxThreads = 1024;
+constexpr int kSelMaxKeys = 32768;   // of a CTA in shared memory
 
 struct Evict {
   avits_kv_cache src, dst;
@@ -126,18 +127,19 @@ __device__ __forceinline__ uint32_t order_of(float s) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-__device__ __forceinline__ int padded(int i) { return i + (i >> 5); }
+__host__ __device__ __forceinline__ int padded(int i) { return i + (i >> 5); }
 
-__global__ void __launch_bounds__(kSelThreads)
+__global__ void __launch_bounds__(kSelMaxThreads)
 cache_select_kernel(const __grid_constant__ Evict a) {
-  extern __shared__ uint32_t s_key[];
-  __shared__ uint32_t s_hist[2][256];
-  __shared__ uint32_t s_warp[kSelThreads / 32];
-  __shared__ uint32_t s_pick[2];      // digit and how many of it are needed
+  extern __shared__ uint32_t s_key[];                // [padded(part)], then the list
+  __shared__ __align__(16) uint32_t s_hist[2][256];
+  __shared__ uint32_t s_pick[3];      // digit, how many of it are needed, whether all are
   __shared__ uint32_t s_count[2];     // this CTA's keys above, and equal to, the threshold
+  __shared__ uint32_t s_a[32], s_e[32];
   cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, threads = blockDim.x;
+  for (int i = tid; i < 512; i += threads) (&s_hist[0][0])[i] = 0u;
   pdl_wait_then_trigger();
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int ncta = (int)cluster.num_blocks(), me = (int)cluster.block_rank();
   const int bh = blockIdx.x / ncta;
   const int b = bh / a.src.Hkv, h = bh - b * a.src.Hkv;
@@ -149,7 +151,7 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   if (h == 0 && me == 0 && tid == 0) a.dst.lens[b] = m;
   // all of them, and the places past the kept ones: the same for every CTA
   if (n <= a.keep) {
-    for (int i = me * kSelThreads + tid; i < a.keep; i += ncta * kSelThreads) {
+    for (int i = me * threads + tid; i < a.keep; i += ncta * threads) {
       idx[i] = i < n ? i : -1;
       if (i < n) acc2[i] = acc[i];
     }
@@ -157,58 +159,87 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   }
   const int lo = min(n, me * a.part), hi = min(n, lo + a.part);
   const int last = n - a.recent;
-  auto key_at = [&](int j) {     // the first and the last ones stand above all
-    return j < a.sinks || j >= last ? 0xFFFFFFFFu : order_of(acc[j]);
+  auto key_of = [&](int j, float x) {     // the first and the last ones stand above all
+    return j < a.sinks || j >= last ? 0xFFFFFFFFu : order_of(x);
   };
-  auto key = [&](int j) { return a.in_smem ? s_key[padded(j - lo)] : key_at(j); };
-  if (a.in_smem)
-    for (int j = lo + tid; j < hi; j += kSelThreads) s_key[padded(j - lo)] = key_at(j);
+  if (a.in_smem) {
+    constexpr int kDeep = 8;      // loads on their way at once
+    for (int j0 = lo + tid; j0 < hi; j0 += kDeep * threads) {
+      float x[kDeep];
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) x[i] = acc[min(j0 + i * threads, hi - 1)];
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i)
+        if (j0 + i * threads < hi)
+          s_key[padded(j0 + i * threads - lo)] = key_of(j0 + i * threads, x[i]);
+    }
+  }
+  auto key = [&](int j) { return a.in_smem ? s_key[padded(j - lo)] : key_of(j, acc[j]); };
+  __syncthreads();
 
   uint32_t prefix = 0u, mask = 0u, need = (uint32_t)a.keep;
-  bool all = false;     // the threshold's whole digit is taken: no ties to count
 #pragma unroll 1
   for (int pass = 0; pass < 4; ++pass) {
     const int shift = 24 - 8 * pass;
     uint32_t* hist = s_hist[pass & 1];
-    for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0u;
-    __syncthreads();
-    for (int j = lo + tid; j < hi; j += kSelThreads) {
-      const uint32_t k = key(j);
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    if (pass == 0) {
+      // the top digits are few: one count per digit and warp
+      for (int j0 = lo; j0 < hi; j0 += threads) {
+        const int j = j0 + tid;
+        const uint32_t d = j < hi ? key(j) >> 24 : 256u;
+        const unsigned same = __match_any_sync(0xffffffffu, d);
+        if (j < hi && lane == __ffs(same) - 1) atomicAdd(&hist[d], (uint32_t)__popc(same));
+      }
+    } else {
+#pragma unroll 4
+      for (int j = lo + tid; j < hi; j += threads) {
+        const uint32_t k = key(j);
+        if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+      }
     }
     cluster.sync();
-    // suffix sums of the cluster's counts: thread t < 256 has digit 255 - t
-    uint32_t mine = 0u;
-    if (tid < 256)
-      for (int r = 0; r < ncta; ++r) mine += cluster.map_shared_rank(hist, r)[255 - tid];
-    uint32_t inc = mine;
+    // the other table was last read before this barrier
+    for (int i = tid; i < 256; i += threads) s_hist[(pass & 1) ^ 1][i] = 0u;
+    if (w == 0) {
+      // lane l: digits 255 - 8 l down to 248 - 8 l, over the cluster
+      uint32_t c[8] = {};
+      for (int r = 0; r < ncta; ++r) {
+        const uint4* other =
+            reinterpret_cast<const uint4*>(cluster.map_shared_rank(hist, r)) + 2 * (31 - lane);
+        const uint4 x = other[0], y = other[1];
+        c[7] += x.x; c[6] += x.y; c[5] += x.z; c[4] += x.w;
+        c[3] += y.x; c[2] += y.y; c[1] += y.z; c[0] += y.w;
+      }
+      uint32_t sum = 0u;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
-    }
-    if (lane == 31) s_warp[w] = inc;
-    __syncthreads();
-    if (tid < 256) {
-      for (int i = 0; i < w; ++i) inc += s_warp[i];
-      const uint32_t above = inc - mine;
-      if (above < need && need <= inc) {
-        s_pick[0] = 255u - tid;
-        s_pick[1] = need - above;
-        s_count[0] = mine == need - above ? 1u : 0u;
+      for (int i = 0; i < 8; ++i) sum += c[i];
+      uint32_t above = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, above, o);
+        if (lane >= o) above += y;
+      }
+      above -= sum;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (above < need && need <= above + c[i]) {
+          s_pick[0] = 255u - 8u * lane - i;
+          s_pick[1] = need - above;
+          s_pick[2] = c[i] == need - above;
+        }
+        above += c[i];
       }
     }
     __syncthreads();
     prefix |= s_pick[0] << shift;
     mask |= 255u << shift;
     need = s_pick[1];
-    all = s_count[0] != 0u;
-    if (all) break;
+    if (s_pick[2]) break;     // the digit is taken whole: no ties to count
   }
   // taken: (key & mask) above the prefix, and of the equal ones the first `need`
-  // (all of them where the digit is taken whole)
   const int r0 = lo + tid * a.run, r1 = min(hi, r0 + a.run);
   uint32_t above = 0u, equal = 0u;
+#pragma unroll 4
   for (int j = r0; j < r1; ++j) {
     const uint32_t k = key(j) & mask;
     above += k > prefix;
@@ -223,94 +254,131 @@ cache_select_kernel(const __grid_constant__ Evict a) {
       ie += ye;
     }
   }
-  __shared__ uint32_t s_a[kSelThreads / 32], s_e[kSelThreads / 32];
   if (lane == 31) {
     s_a[w] = ia;
     s_e[w] = ie;
   }
   __syncthreads();
-  uint32_t before_a = ia - above, before_e = ie - equal, sum_a = 0u, sum_e = 0u;
-  for (int i = 0; i < kSelThreads / 32; ++i) {
-    if (i < w) {
-      before_a += s_a[i];
-      before_e += s_e[i];
+  // every warp scans the warps' counts itself
+  const int warps = threads >> 5;
+  uint32_t wa = lane < warps ? s_a[lane] : 0u, we = lane < warps ? s_e[lane] : 0u;
+  const uint32_t own_a = wa, own_e = we;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t ya = __shfl_up_sync(0xffffffffu, wa, o), ye = __shfl_up_sync(0xffffffffu, we, o);
+    if (lane >= o) {
+      wa += ya;
+      we += ye;
     }
-    sum_a += s_a[i];
-    sum_e += s_e[i];
   }
-  if (tid == 0) {
-    s_count[0] = sum_a;
-    s_count[1] = sum_e;
+  const uint32_t sum_a = __shfl_sync(0xffffffffu, wa, 31), sum_e = __shfl_sync(0xffffffffu, we, 31);
+  uint32_t before_a = __shfl_sync(0xffffffffu, wa - own_a, w) + ia - above;
+  uint32_t before_e = __shfl_sync(0xffffffffu, we - own_e, w) + ie - equal;
+  uint32_t base_a = 0u, base_e = 0u;      // of the CTAs before this one
+  if (ncta > 1) {
+    if (tid == 0) {
+      s_count[0] = sum_a;
+      s_count[1] = sum_e;
+    }
+    cluster.sync();
+    for (int r = 0; r < me; ++r) {
+      const uint32_t* other = cluster.map_shared_rank(s_count, r);
+      base_a += other[0];
+      base_e += other[1];
+    }
   }
-  cluster.sync();
-  for (int r = 0; r < me; ++r) {
-    const uint32_t* other = cluster.map_shared_rank(s_count, r);
-    before_a += other[0];
-    before_e += other[1];
-  }
+  // ranks: of the row, from the CTA's first on
+  const uint32_t base = base_a + min(base_e, need);
+  const uint32_t count = base_a + sum_a + min(base_e + sum_e, need) - base;
+  uint16_t* list = reinterpret_cast<uint16_t*>(s_key + padded(a.part) + 1);
+  before_a += base_a;
+  before_e += base_e;
   for (int j = r0; j < r1; ++j) {
     const uint32_t k = key(j) & mask;
-    const bool take = k > prefix || (k == prefix && before_e < need);
-    if (take) {
+    if (k > prefix || (k == prefix && before_e < need)) {
       const uint32_t rank = before_a + min(before_e, need);
-      idx[rank] = j;
-      acc2[rank] = acc[j];
+      if (a.in_smem) {
+        list[rank - base] = (uint16_t)(j - lo);
+      } else {
+        idx[rank] = j;
+        acc2[rank] = acc[j];
+      }
     }
     before_a += k > prefix;
     before_e += k == prefix;
   }
-  cluster.sync();   // no CTA leaves while another reads its counts
+  if (a.in_smem) {
+    __syncthreads();
+#pragma unroll 4
+    for (uint32_t i = tid; i < count; i += threads) {
+      const int j = lo + list[i];
+      idx[base + i] = j;
+      acc2[base + i] = acc[j];
+    }
+  }
+  if (ncta > 1) cluster.sync();   // no CTA leaves while another reads its counts
 }
 
-// Copy: the kept rows, each of Hkv * 2 * pieces 16-byte pieces, flat over the
-// threads so that neighbouring lanes read neighbouring pieces of a row.
+// Copy: a block takes rows of one (b, head), 32 KB of keys and values.  First
+// where each row lies on both sides, then the 16-byte pieces flat over the
+// threads, neighbouring lanes on neighbouring pieces, 8 to a thread at once.
 constexpr int kCopyThreads = 256;
-constexpr int kCopyDeep = 4;
+constexpr int kCopyDeep = 8;
+constexpr int kCopyPieces = kCopyThreads * kCopyDeep;
+constexpr int kCopyRows = 256;       // of a block, at most
 
 struct Copy {
   avits_kv_cache src, dst;
   FastDiv spage, dpage, pieces;
-  int keep, es, blocks;      // blocks: per (b, head)
+  int keep, es, blocks, rows;      // blocks: per (b, head); rows: of a block
   const int32_t* idx;
   unsigned int* status;
 };
 
 __global__ void __launch_bounds__(kCopyThreads)
 cache_copy_kernel(const __grid_constant__ Copy a) {
+  __shared__ const char* s_from[2 * kCopyRows];    // [row][keys, values]
+  __shared__ char* s_to[2 * kCopyRows];            // nullptr: a page out of range
   pdl_wait_then_trigger();
   const int bh = blockIdx.x / a.blocks, part = blockIdx.x - bh * a.blocks;
-  const int b = bh / a.src.Hkv, h = bh - b * a.src.Hkv;
-  const int m = min(cache_len(a.src, b), a.keep);
+  const int b = bh / a.src.Hkv, h = bh - b * a.src.Hkv, tid = threadIdx.x;
+  const int m = min(cache_len(a.src, b), a.keep), r0 = part * a.rows;
+  const int rows = min(a.rows, m - r0);
+  if (rows <= 0) return;
   const int32_t* idx = a.idx + (int64_t)bh * a.keep;
   const int32_t* ts = a.src.block_table + (int64_t)b * a.src.table_sb;
   const int32_t* td = a.dst.block_table + (int64_t)b * a.dst.table_sb;
-  const int per = 2 * (int)a.pieces.p;
-  const int rows = kCopyThreads * kCopyDeep / per;        // rows of a block, >= 8
-  const int r0 = part * rows, count = min(rows, m - r0) * per;
+  for (int i = tid; i < rows; i += kCopyThreads) {
+    const int r = r0 + i, cd = a.dpage.div(r), pd = td[cd];
+    const int j = idx[r], cs = a.spage.div(j), ps = ts[cs];
+    const int ss = j - cs * a.src.page_size, sd = r - cd * a.dst.page_size;
+    const bool ok = (unsigned)ps < (unsigned)a.src.num_pages &&
+                    (unsigned)pd < (unsigned)a.dst.num_pages;
+    if (!ok) raise_status(a.status, AVITS_ERR_PAGE);
+    s_from[2 * i] = static_cast<const char*>(a.src.k_pages) +
+                    (ps * a.src.k_sp + ss * a.src.k_st + h * a.src.k_sh) * a.es;
+    s_from[2 * i + 1] = static_cast<const char*>(a.src.v_pages) +
+                        (ps * a.src.v_sp + ss * a.src.v_st + h * a.src.v_sh) * a.es;
+    s_to[2 * i] = !ok ? nullptr
+                      : static_cast<char*>(a.dst.k_pages) +
+                            (pd * a.dst.k_sp + sd * a.dst.k_st + h * a.dst.k_sh) * a.es;
+    s_to[2 * i + 1] = !ok ? nullptr
+                          : static_cast<char*>(a.dst.v_pages) +
+                                (pd * a.dst.v_sp + sd * a.dst.v_st + h * a.dst.v_sh) * a.es;
+  }
+  __syncthreads();
+  const int count = rows * 2 * (int)a.pieces.p;
   uint4 x[kCopyDeep];
   char* to[kCopyDeep];
 #pragma unroll
   for (int q = 0; q < kCopyDeep; ++q) {
-    const int i = threadIdx.x + q * kCopyThreads;
+    const int i = tid + q * kCopyThreads;
     to[q] = nullptr;
     if (i < count) {
-      const int half = a.pieces.div(i), row = half >> 1, c = i - half * (int)a.pieces.p;
-      const int r = r0 + row, j = idx[r];
-      const int cs = a.spage.div(j), cd = a.dpage.div(r);
-      const int ps = ts[cs], pd = td[cd];
-      if ((unsigned)ps < (unsigned)a.src.num_pages && (unsigned)pd < (unsigned)a.dst.num_pages) {
-        const int ss = j - cs * a.src.page_size, sd = r - cd * a.dst.page_size;
-        const bool is_v = half & 1;
-        const int64_t so = is_v ? ps * a.src.v_sp + ss * a.src.v_st + h * a.src.v_sh
-                                : ps * a.src.k_sp + ss * a.src.k_st + h * a.src.k_sh;
-        const int64_t dof = is_v ? pd * a.dst.v_sp + sd * a.dst.v_st + h * a.dst.v_sh
-                                 : pd * a.dst.k_sp + sd * a.dst.k_st + h * a.dst.k_sh;
-        const char* from =
-            static_cast<const char*>(is_v ? a.src.v_pages : a.src.k_pages) + so * a.es + c * 16;
-        to[q] = static_cast<char*>(is_v ? a.dst.v_pages : a.dst.k_pages) + dof * a.es + c * 16;
-        x[q] = ld_once(from);
-      } else {
-        raise_status(a.status, AVITS_ERR_PAGE);
+      const int half = a.pieces.div(i), at = (i - half * (int)a.pieces.p) * 16;
+      if (s_to[half]) {
+        to[q] = s_to[half] + at;
+        x[q] = ld_once(s_from[half] + at);
       }
     }
   }
@@ -343,8 +411,8 @@ cudaError_t launch_cache_append(const avits_kv_cache& c, const void* k_new, cons
 }
 
 cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& dst, int keep,
-                               int sinks, int recent, int32_t* idx, unsigned int* status,
-                               cudaStream_t s) {
+                               int sinks, int recent, int32_t* idx, int num_sms,
+                               unsigned int* status, cudaStream_t s) {
   Evict a{};
   a.src = src;
   a.dst = dst;
@@ -353,19 +421,25 @@ cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& 
   a.recent = recent;
   a.idx = idx;
   a.status = status;
-  // CTAs per row: 4096 keys each, up to the 8 of a portable cluster
+  // CTAs of a row: enough for 4096 keys each, and while there are SMs for all of
+  // them down to 512, up to the 8 of a portable cluster
+  const long long bh = (long long)src.B * src.Hkv;
   int ncta = 1;
-  while (ncta < 8 && (int64_t)ncta * 4096 < src.max_len) ncta *= 2;
+  while (ncta < 8 && ((int64_t)ncta * 4096 < src.max_len ||
+                      (bh * ncta * 2 <= num_sms && (int64_t)ncta * 512 < src.max_len)))
+    ncta *= 2;
   a.part = (src.max_len + ncta - 1) / ncta;
-  a.run = (a.part + kSelThreads - 1) / kSelThreads;
+  int threads = 128;
+  while (threads < kSelMaxThreads && threads * 4 < a.part) threads *= 2;
+  a.run = (a.part + threads - 1) / threads;
   a.in_smem = a.part <= kSelMaxKeys;
-  const size_t smem = a.in_smem ? (size_t)(a.part + a.part / 32 + 1) * 4 : 0;
-  cudaError_t e =
-      prefer_max_shared<cache_select_kernel, (kSelMaxKeys + kSelMaxKeys / 32 + 1) * 4>();
+  const size_t smem = a.in_smem ? (size_t)(padded(a.part) + 1) * 4 + (size_t)a.part * 2 + 4 : 0;
+  cudaError_t e = prefer_max_shared<cache_select_kernel,
+                                    (kSelMaxKeys + kSelMaxKeys / 32 + 2) * 4 + kSelMaxKeys * 2>();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(src.B * src.Hkv * ncta));
-  cfg.blockDim = dim3(kSelThreads);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -389,8 +463,9 @@ cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& 
   c.keep = keep;
   c.idx = idx;
   c.status = status;
-  const int rows = kCopyThreads * kCopyDeep / (2 * (src.d * c.es / 16));
-  c.blocks = (keep + rows - 1) / rows;
+  c.rows = kCopyPieces / (2 * (src.d * c.es / 16));
+  if (c.rows > kCopyRows) c.rows = kCopyRows;
+  c.blocks = (keep + c.rows - 1) / c.rows;
   e = prefer_max_shared<cache_copy_kernel>();
   if (e != cudaSuccess) return e;
   return launch_pdl(cache_copy_kernel, dim3((unsigned)(src.B * src.Hkv * c.blocks)),
