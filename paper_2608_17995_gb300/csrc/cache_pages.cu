@@ -100,22 +100,24 @@ cache_append_kernel(const __grid_constant__ Append a) {
 
 // ------------------------------------------------------------------ evict --
 // Selection: a cluster of CTAs per (b, KV head), each with a contiguous part
-// of the row, seen as 32-bit keys whose order is the weights' order and kept in
-// shared memory where they fit.  The keep-th largest key by radix digits of 8
-// bits: each CTA counts its digits, one warp of every CTA adds up the cluster's
-// counts through distributed shared memory.  Then the keys above it, and of the
-// equal ones the lowest places, in order: a thread owns a contiguous run, one scan
-// over runs, CTAs included, gives its first rank, and the CTA's places go out
-// through a list in shared memory, side by side.
+// of the row, a thread with runs of 8 or 16 weights in registers, seen as 32-bit
+// keys whose order is the weights' order.  The keep-th largest key by radix digits
+// of 8 bits: each CTA counts its digits and adds the counts to the first CTA's
+// table (distributed shared memory), from which every CTA finds the digit.  Then
+// the keys above it, and of the equal ones the lowest places, in order: a scan over
+// the runs, CTAs included, gives each its first rank.
+//
+// The cost is latency: a barrier over a cluster takes 1-2 thousand cycles, one of
+// a CTA a tenth of it, so a row has one CTA up to 4096 keys while rows are many.
 constexpr int kSelMaxThreads = 1024;
-constexpr int kSelMaxKeys = 32768;   // of a CTA in shared memory
+constexpr int kSelCopies = 8;       // tables of the first, crowded digit, in banks of
+constexpr int kSelTable = 256 + 4;  // their own
+constexpr int kSelMaxCluster = 8;
 
 struct Evict {
   avits_kv_cache src, dst;
   int keep, sinks, recent;
-  int part;            // keys per CTA
-  int run;             // keys per thread
-  int in_smem;
+  int part;            // keys per CTA, a multiple of 16
   int32_t* idx;
   unsigned int* status;
 };
@@ -127,20 +129,56 @@ __device__ __forceinline__ uint32_t order_of(float s) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-__host__ __device__ __forceinline__ int padded(int i) { return i + (i >> 5); }
+// Sums of two counts over the threads before this one, and over all.
+__device__ __forceinline__ void block_scan(uint32_t x, uint32_t y, uint2* s_warp, int lane, int w,
+                                           int warps, uint32_t& bx, uint32_t& by, uint32_t& tx,
+                                           uint32_t& ty) {
+  uint32_t ix = x, iy = y;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t ux = __shfl_up_sync(0xffffffffu, ix, o), uy = __shfl_up_sync(0xffffffffu, iy, o);
+    if (lane >= o) {
+      ix += ux;
+      iy += uy;
+    }
+  }
+  if (lane == 31) s_warp[w] = make_uint2(ix, iy);
+  __syncthreads();
+  // every warp scans the warps' counts itself
+  const uint2 own = lane < warps ? s_warp[lane] : make_uint2(0u, 0u);
+  uint32_t wx = own.x, wy = own.y;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t ux = __shfl_up_sync(0xffffffffu, wx, o), uy = __shfl_up_sync(0xffffffffu, wy, o);
+    if (lane >= o) {
+      wx += ux;
+      wy += uy;
+    }
+  }
+  tx = __shfl_sync(0xffffffffu, wx, 31);
+  ty = __shfl_sync(0xffffffffu, wy, 31);
+  bx = __shfl_sync(0xffffffffu, wx - own.x, w) + ix - x;
+  by = __shfl_sync(0xffffffffu, wy - own.y, w) + iy - y;
+}
 
+template <int kRun>
 __global__ void __launch_bounds__(kSelMaxThreads)
 cache_select_kernel(const __grid_constant__ Evict a) {
-  extern __shared__ uint32_t s_key[];                // [padded(part)], then the list
-  __shared__ __align__(16) uint32_t s_hist[2][256];
+  __shared__ __align__(16) uint32_t s_total[4][256];   // of the cluster, in its first CTA
+  __shared__ __align__(16) uint32_t s_hist[2][256];    // of this CTA
+  __shared__ uint32_t s_first[kSelCopies][kSelTable];
   __shared__ uint32_t s_pick[3];      // digit, how many of it are needed, whether all are
-  __shared__ uint32_t s_count[2];     // this CTA's keys above, and equal to, the threshold
-  __shared__ uint32_t s_a[32], s_e[32];
+  __shared__ uint2 s_count[kSelMaxCluster];   // the CTAs' keys above, and equal to, the threshold
+  __shared__ uint2 s_warp[2][32];
   cg::cluster_group cluster = cg::this_cluster();
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, threads = blockDim.x;
-  for (int i = tid; i < 512; i += threads) (&s_hist[0][0])[i] = 0u;
-  pdl_wait_then_trigger();
   const int ncta = (int)cluster.num_blocks(), me = (int)cluster.block_rank();
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, threads = blockDim.x;
+  for (int i = tid; i < 1024; i += threads) (&s_total[0][0])[i] = 0u;
+  for (int i = tid; i < 512; i += threads) (&s_hist[0][0])[i] = 0u;
+  for (int i = tid; i < kSelTable * kSelCopies; i += threads) (&s_first[0][0])[i] = 0u;
+  // the first CTA's table is zero once this barrier is waited for
+  if (ncta > 1) cluster.barrier_arrive();
+  pdl_wait_then_trigger();
   const int bh = blockIdx.x / ncta;
   const int b = bh / a.src.Hkv, h = bh - b * a.src.Hkv;
   if (h == 0 && me == 0 && tid == 0) check_cache_len(a.src, b, a.status);
@@ -155,26 +193,32 @@ cache_select_kernel(const __grid_constant__ Evict a) {
       idx[i] = i < n ? i : -1;
       if (i < n) acc2[i] = acc[i];
     }
+    if (ncta > 1) cluster.barrier_wait();
     return;   // the whole cluster takes this way
   }
   const int lo = min(n, me * a.part), hi = min(n, lo + a.part);
-  const int last = n - a.recent;
-  auto key_of = [&](int j, float x) {     // the first and the last ones stand above all
-    return j < a.sinks || j >= last ? 0xFFFFFFFFu : order_of(x);
-  };
-  if (a.in_smem) {
-    constexpr int kDeep = 8;      // loads on their way at once
-    for (int j0 = lo + tid; j0 < hi; j0 += kDeep * threads) {
-      float x[kDeep];
+  const int last = n - a.recent, stripe = threads * kRun;
+  const bool vec = (reinterpret_cast<uintptr_t>(acc) & 15u) == 0;   // lo is a multiple of 4
+  float x[kRun];
+  // this thread's run of a stripe; a part of one stripe is read once
+  auto load = [&](int j0) {
+    if (vec && j0 + kRun <= hi) {
 #pragma unroll
-      for (int i = 0; i < kDeep; ++i) x[i] = acc[min(j0 + i * threads, hi - 1)];
+      for (int i = 0; i < kRun; i += 4) {
+        const float4 p = *reinterpret_cast<const float4*>(acc + j0 + i);
+        x[i] = p.x; x[i + 1] = p.y; x[i + 2] = p.z; x[i + 3] = p.w;
+      }
+    } else {
 #pragma unroll
-      for (int i = 0; i < kDeep; ++i)
-        if (j0 + i * threads < hi)
-          s_key[padded(j0 + i * threads - lo)] = key_of(j0 + i * threads, x[i]);
+      for (int i = 0; i < kRun; ++i) x[i] = j0 + i < hi ? acc[j0 + i] : 0.f;
     }
-  }
-  auto key = [&](int j) { return a.in_smem ? s_key[padded(j - lo)] : key_of(j, acc[j]); };
+  };
+  auto key = [&](int j, float v) {     // the first and the last ones stand above all
+    return j < a.sinks || j >= last ? 0xFFFFFFFFu : order_of(v);
+  };
+  const int j1 = lo + tid * kRun;
+  const bool again = hi - lo > stripe;
+  load(j1);
   __syncthreads();
 
   uint32_t prefix = 0u, mask = 0u, need = (uint32_t)a.keep;
@@ -182,34 +226,38 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   for (int pass = 0; pass < 4; ++pass) {
     const int shift = 24 - 8 * pass;
     uint32_t* hist = s_hist[pass & 1];
-    if (pass == 0) {
-      // the top digits are few: one count per digit and warp
-      for (int j0 = lo; j0 < hi; j0 += threads) {
-        const int j = j0 + tid;
-        const uint32_t d = j < hi ? key(j) >> 24 : 256u;
-        const unsigned same = __match_any_sync(0xffffffffu, d);
-        if (j < hi && lane == __ffs(same) - 1) atomicAdd(&hist[d], (uint32_t)__popc(same));
-      }
-    } else {
-#pragma unroll 4
-      for (int j = lo + tid; j < hi; j += threads) {
-        const uint32_t k = key(j);
-        if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    // a first digit is one of few: lanes count in tables of their own
+    uint32_t* count = pass == 0 ? s_first[lane % kSelCopies] : hist;
+    for (int j0 = j1; j0 < hi; j0 += stripe) {
+      if (again) load(j0);
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        const uint32_t k = key(j0 + i, x[i]);
+        if (j0 + i < hi && (k & mask) == prefix) atomicAdd(&count[(k >> shift) & 255u], 1u);
       }
     }
-    cluster.sync();
-    // the other table was last read before this barrier
-    for (int i = tid; i < 256; i += threads) s_hist[(pass & 1) ^ 1][i] = 0u;
-    if (w == 0) {
-      // lane l: digits 255 - 8 l down to 248 - 8 l, over the cluster
-      uint32_t c[8] = {};
-      for (int r = 0; r < ncta; ++r) {
-        const uint4* other =
-            reinterpret_cast<const uint4*>(cluster.map_shared_rank(hist, r)) + 2 * (31 - lane);
-        const uint4 x = other[0], y = other[1];
-        c[7] += x.x; c[6] += x.y; c[5] += x.z; c[4] += x.w;
-        c[3] += y.x; c[2] += y.y; c[1] += y.z; c[0] += y.w;
+    __syncthreads();
+    if (pass == 0 || ncta > 1) {
+      if (pass == 0 && ncta > 1) cluster.barrier_wait();
+      uint32_t* to = ncta > 1 ? cluster.map_shared_rank(s_total[pass], 0) : hist;
+      for (int i = tid; i < 256; i += threads) {
+        uint32_t sum = hist[i];
+        if (pass == 0)
+#pragma unroll
+          for (int r = 0; r < kSelCopies; ++r) sum += s_first[r][i];
+        if (ncta == 1)
+          to[i] = sum;
+        else if (sum)
+          atomicAdd(&to[i], sum);
       }
+      if (ncta > 1) cluster.sync(); else __syncthreads();
+    }
+    if (w == 0) {
+      // lane l: digits 255 - 8 l down to 248 - 8 l
+      const uint32_t* table = ncta > 1 ? cluster.map_shared_rank(s_total[pass], 0) : hist;
+      const uint4* at = reinterpret_cast<const uint4*>(table) + 2 * (31 - lane);
+      const uint4 p = at[0], q = at[1];
+      const uint32_t c[8] = {q.w, q.z, q.y, q.x, p.w, p.z, p.y, p.x};
       uint32_t sum = 0u;
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += c[i];
@@ -220,15 +268,20 @@ cache_select_kernel(const __grid_constant__ Evict a) {
         if (lane >= o) above += y;
       }
       above -= sum;
+      if (above < need && need <= above + sum) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (above < need && need <= above + c[i]) {
-          s_pick[0] = 255u - 8u * lane - i;
-          s_pick[1] = need - above;
-          s_pick[2] = c[i] == need - above;
+        for (int i = 0; i < 8; ++i) {
+          if (above < need && need <= above + c[i]) {
+            s_pick[0] = 255u - 8u * lane - i;
+            s_pick[1] = need - above;
+            s_pick[2] = c[i] == need - above;
+          }
+          above += c[i];
         }
-        above += c[i];
       }
+    } else if (pass > 0) {
+      // the other table was last read two barriers ago
+      for (int i = tid - 32; i < 256; i += threads - 32) s_hist[(pass & 1) ^ 1][i] = 0u;
     }
     __syncthreads();
     prefix |= s_pick[0] << shift;
@@ -237,86 +290,60 @@ cache_select_kernel(const __grid_constant__ Evict a) {
     if (s_pick[2]) break;     // the digit is taken whole: no ties to count
   }
   // taken: (key & mask) above the prefix, and of the equal ones the first `need`
-  const int r0 = lo + tid * a.run, r1 = min(hi, r0 + a.run);
-  uint32_t above = 0u, equal = 0u;
-#pragma unroll 4
-  for (int j = r0; j < r1; ++j) {
-    const uint32_t k = key(j) & mask;
-    above += k > prefix;
-    equal += k == prefix;
-  }
-  uint32_t ia = above, ie = equal;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t ya = __shfl_up_sync(0xffffffffu, ia, o), ye = __shfl_up_sync(0xffffffffu, ie, o);
-    if (lane >= o) {
-      ia += ya;
-      ie += ye;
-    }
-  }
-  if (lane == 31) {
-    s_a[w] = ia;
-    s_e[w] = ie;
-  }
-  __syncthreads();
-  // every warp scans the warps' counts itself
   const int warps = threads >> 5;
-  uint32_t wa = lane < warps ? s_a[lane] : 0u, we = lane < warps ? s_e[lane] : 0u;
-  const uint32_t own_a = wa, own_e = we;
+  uint32_t above = 0u, equal = 0u;
+  for (int j0 = j1; j0 < hi; j0 += stripe) {
+    if (again) load(j0);
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t ya = __shfl_up_sync(0xffffffffu, wa, o), ye = __shfl_up_sync(0xffffffffu, we, o);
-    if (lane >= o) {
-      wa += ya;
-      we += ye;
+    for (int i = 0; i < kRun; ++i) {
+      const uint32_t k = key(j0 + i, x[i]) & mask;
+      above += j0 + i < hi && k > prefix;
+      equal += j0 + i < hi && k == prefix;
     }
   }
-  const uint32_t sum_a = __shfl_sync(0xffffffffu, wa, 31), sum_e = __shfl_sync(0xffffffffu, we, 31);
-  uint32_t before_a = __shfl_sync(0xffffffffu, wa - own_a, w) + ia - above;
-  uint32_t before_e = __shfl_sync(0xffffffffu, we - own_e, w) + ie - equal;
+  uint32_t bx, by, tx, ty;      // of the threads before, of all
+  block_scan(above, equal, s_warp[0], lane, w, warps, bx, by, tx, ty);
   uint32_t base_a = 0u, base_e = 0u;      // of the CTAs before this one
   if (ncta > 1) {
-    if (tid == 0) {
-      s_count[0] = sum_a;
-      s_count[1] = sum_e;
-    }
+    // told to every CTA, so that nothing of this one is read after the barrier
+    if (tid < ncta) cluster.map_shared_rank(s_count, tid)[me] = make_uint2(tx, ty);
     cluster.sync();
     for (int r = 0; r < me; ++r) {
-      const uint32_t* other = cluster.map_shared_rank(s_count, r);
-      base_a += other[0];
-      base_e += other[1];
+      base_a += s_count[r].x;
+      base_e += s_count[r].y;
     }
   }
-  // ranks: of the row, from the CTA's first on
-  const uint32_t base = base_a + min(base_e, need);
-  const uint32_t count = base_a + sum_a + min(base_e + sum_e, need) - base;
-  uint16_t* list = reinterpret_cast<uint16_t*>(s_key + padded(a.part) + 1);
-  before_a += base_a;
-  before_e += base_e;
-  for (int j = r0; j < r1; ++j) {
-    const uint32_t k = key(j) & mask;
-    if (k > prefix || (k == prefix && before_e < need)) {
-      const uint32_t rank = before_a + min(before_e, need);
-      if (a.in_smem) {
-        list[rank - base] = (uint16_t)(j - lo);
-      } else {
-        idx[rank] = j;
-        acc2[rank] = acc[j];
+  int par = 1;
+  for (int s0 = lo; s0 < hi; s0 += stripe, par ^= 1) {      // the same for all threads
+    const int j0 = s0 + tid * kRun;
+    if (again) {
+      load(j0);
+      above = equal = 0u;
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        const uint32_t k = key(j0 + i, x[i]) & mask;
+        above += j0 + i < hi && k > prefix;
+        equal += j0 + i < hi && k == prefix;
+      }
+      block_scan(above, equal, s_warp[par], lane, w, warps, bx, by, tx, ty);
+    }
+    uint32_t ra = base_a + bx, re = base_e + by;
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      const uint32_t k = key(j0 + i, x[i]) & mask;
+      if (j0 + i < hi) {
+        if (k > prefix || (k == prefix && re < need)) {
+          const uint32_t rank = ra + min(re, need);
+          idx[rank] = j0 + i;
+          acc2[rank] = x[i];
+        }
+        ra += k > prefix;
+        re += k == prefix;
       }
     }
-    before_a += k > prefix;
-    before_e += k == prefix;
+    base_a += tx;
+    base_e += ty;
   }
-  if (a.in_smem) {
-    __syncthreads();
-#pragma unroll 4
-    for (uint32_t i = tid; i < count; i += threads) {
-      const int j = lo + list[i];
-      idx[base + i] = j;
-      acc2[base + i] = acc[j];
-    }
-  }
-  if (ncta > 1) cluster.sync();   // no CTA leaves while another reads its counts
 }
 
 // Copy: a block takes rows of one (b, head), 32 KB of keys and values.  First
@@ -421,26 +448,24 @@ cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& 
   a.recent = recent;
   a.idx = idx;
   a.status = status;
-  // CTAs of a row: enough for 4096 keys each, and while there are SMs for all of
-  // them down to 512, up to the 8 of a portable cluster
+  // CTAs of a row: while there are SMs for them, as many as leave 4096 keys to each;
+  // more than 16 keys to a thread are read again at each digit
   const long long bh = (long long)src.B * src.Hkv;
   int ncta = 1;
-  while (ncta < 8 && ((int64_t)ncta * 4096 < src.max_len ||
-                      (bh * ncta * 2 <= num_sms && (int64_t)ncta * 512 < src.max_len)))
+  while (ncta < kSelMaxCluster && (int64_t)ncta * 4096 < src.max_len &&
+         (bh * ncta * 2 <= num_sms || (int64_t)ncta * kSelMaxThreads * 16 < src.max_len))
     ncta *= 2;
-  a.part = (src.max_len + ncta - 1) / ncta;
-  int threads = 128;
-  while (threads < kSelMaxThreads && threads * 4 < a.part) threads *= 2;
-  a.run = (a.part + threads - 1) / threads;
-  a.in_smem = a.part <= kSelMaxKeys;
-  const size_t smem = a.in_smem ? (size_t)(padded(a.part) + 1) * 4 + (size_t)a.part * 2 + 4 : 0;
-  cudaError_t e = prefer_max_shared<cache_select_kernel,
-                                    (kSelMaxKeys + kSelMaxKeys / 32 + 2) * 4 + kSelMaxKeys * 2>();
+  a.part = ((src.max_len + ncta - 1) / ncta + 15) / 16 * 16;
+  const int run = a.part <= 8 * kSelMaxThreads ? 8 : 16;
+  int threads = (a.part / run + 31) / 32 * 32;
+  threads = threads < 64 ? 64 : threads > kSelMaxThreads ? kSelMaxThreads : threads;
+  const auto kernel = run == 8 ? cache_select_kernel<8> : cache_select_kernel<16>;
+  cudaError_t e = run == 8 ? prefer_max_shared<cache_select_kernel<8>>()
+                           : prefer_max_shared<cache_select_kernel<16>>();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(src.B * src.Hkv * ncta));
   cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -451,7 +476,7 @@ cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& 
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, cache_select_kernel, a);
+  e = cudaLaunchKernelEx(&cfg, kernel, a);
   if (e != cudaSuccess) return e;
   Copy c{};
   c.src = src;
