@@ -531,7 +531,8 @@ avits_status avits_cache_append(const avits_kv_cache* cache, const void* k_new, 
  *         same bits.
  * H a multiple of Hkv, at most 256 heads to a KV head.
  * workspace/ws_bytes : at least avits_cache_attention_workspace(...) bytes,
- *         16-byte aligned, of any content; not used by two calls at once. */
+ *         16-byte aligned, of any content; not used by two calls at once.
+ *         NULL where none is needed (shorter sequences). */
 typedef enum {
   AVITS_WEIGHTS_NONE = 0, AVITS_WEIGHTS_WRITE = 1, AVITS_WEIGHTS_ADD = 2
 } avits_weights;
@@ -541,7 +542,8 @@ avits_status avits_cache_attention(const avits_kv_cache* cache, const void* q, i
                                    int64_t o_sb, int64_t o_sh, float* lse_opt, int weights,
                                    float weight, void* workspace, size_t ws_bytes, void* stream);
 
-/* Workspace bytes for these sizes on the CURRENT device (0 for invalid ones). */
+/* Workspace bytes for these sizes on the CURRENT device (0 where none is
+ * needed, and for invalid sizes). */
 size_t avits_cache_attention_workspace(const avits_kv_cache* cache, int H, int weights);
 
 /* Eviction by accumulated weight.  For every sequence b and KV head, n =

@@ -562,7 +562,8 @@ class KVCache:
                       table can hold); a smaller one costs less workspace
     """
     __slots__ = ("k_pages", "v_pages", "block_table", "lens", "acc", "B", "Hkv", "d", "dtype",
-                 "page_size", "max_len", "device", "_index", "_struct", "_ref", "_need")
+                 "page_size", "max_len", "device", "int32", "float32", "_index", "_struct", "_ref",
+                 "_need", "_append", "_attend", "_evict")
 
     def __init__(self, k_pages, v_pages, block_table, lens, acc=None, max_len: Optional[int] = None):
         torch = _torch()
@@ -604,19 +605,29 @@ class KVCache:
                                     page_size, self.max_len)
         self._ref = ctypes.addressof(self._struct)
         self._need = {}   # (H, weights) -> workspace bytes
-
-
-def _on_device(cache: KVCache, *tensors):
-    """The calls launch on the current device, and every tensor is there."""
-    index = cache._index
-    if index != _torch()._C._cuda_getDevice():
-        raise ValueError("the cache is on %s, which is not the current device" % cache.device)
-    for t in tensors:
-        if t is not None and t.get_device() != index:
-            raise ValueError("tensor on %s, the cache is on %s" % (t.device, cache.device))
+        # looked up once: the calls' host time is most of a small call's
+        self.int32, self.float32 = torch.int32, torch.float32
+        L = lib()
+        self._append, self._attend = L.avits_cache_append, L.avits_cache_attention
+        self._evict = L.avits_cache_evict
 
 
 _cache_ws = {}
+
+
+def _call_stream(cache: KVCache, stream):
+    """The stream's handle.  The calls launch on the current device: the cache
+    has to be there."""
+    C = _torch()._C
+    if C._cuda_getDevice() != cache._index:
+        raise ValueError("the cache is on %s, which is not the current device" % cache.device)
+    return C._cuda_getCurrentRawStream(cache._index) if stream is None else _stream(stream)
+
+
+def _elsewhere(cache: KVCache, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != cache._index:
+            raise ValueError("tensor on %s, the cache is on %s" % (t.device, cache.device))
 
 
 def _scratch(cache: KVCache, need: int, handle: int):
@@ -640,26 +651,32 @@ def _scratch(cache: KVCache, need: int, handle: int):
     return buf
 
 
+# These calls are made once per token and layer, so their checks are plain
+# comparisons: of a small call's time most is spent here and in the launch.
 def avits_cache_append(cache: KVCache, k_new, v_new, cu_new, stream=None):
     """New tokens into the cache: k_new, v_new [T,Hkv,d] (any 16-byte aligned
     strides, d contiguous), sequence b's being rows cu_new[b] .. cu_new[b+1]-1
     (int32 [B+1]).  cache.lens already counts them; they go to the last places.
     With cache.acc their accumulated weights are set to zero."""
-    T, Hkv, d = k_new.shape
-    if Hkv != cache.Hkv or d != cache.d or tuple(v_new.shape) != (T, Hkv, d):
+    T, Hkv, d = shape = k_new.shape
+    if Hkv != cache.Hkv or d != cache.d or v_new.shape != shape:
         raise ValueError("k_new / v_new must be [T, Hkv, d] of the cache")
     if k_new.dtype != cache.dtype or v_new.dtype != cache.dtype:
         raise TypeError("k_new / v_new and cache dtypes differ")
-    ks, vs = k_new.stride(), v_new.stride()
-    if ks[2] != 1 or vs[2] != 1:
+    k_st, k_sh, k_sd = k_new.stride()
+    v_st, v_sh, v_sd = v_new.stride()
+    if k_sd != 1 or v_sd != 1:
         raise ValueError("the head-dim axis must be contiguous")
-    if tuple(cu_new.shape) != (cache.B + 1,) or cu_new.dtype != _torch().int32 or \
+    if cu_new.shape != (cache.B + 1,) or cu_new.dtype != cache.int32 or \
             not cu_new.is_contiguous():
         raise ValueError("cu_new must be a contiguous int32 [B+1] tensor")
-    _on_device(cache, k_new, v_new, cu_new)
-    rc = lib().avits_cache_append(cache._ref, k_new.data_ptr(), v_new.data_ptr(), T,
-                                  cu_new.data_ptr(), ks[0], ks[1], vs[0], vs[1], _stream(stream))
-    _check("avits_cache_append", rc)
+    index = cache._index
+    if k_new.get_device() != index or v_new.get_device() != index or cu_new.get_device() != index:
+        _elsewhere(cache, k_new, v_new, cu_new)
+    rc = cache._append(cache._ref, k_new.data_ptr(), v_new.data_ptr(), T, cu_new.data_ptr(), k_st,
+                       k_sh, v_st, v_sh, _call_stream(cache, stream))
+    if rc != 0:
+        _check("avits_cache_append", rc)
 
 
 def avits_cache_attention_workspace(cache: KVCache, H: int, weights: bool) -> int:
@@ -676,33 +693,48 @@ def avits_cache_attention(cache: KVCache, q, softmax_scale: float, o, lse=None,
     softmax weight of each cached token, added (or written).  ``workspace``: a
     device byte tensor of avits_cache_attention_workspace() bytes, of the
     caller's own where calls may overlap; by default the library's."""
-    B, H, d = q.shape
-    if B != cache.B or d != cache.d or o.shape != q.shape:
+    B, H, d = shape = q.shape
+    if B != cache.B or d != cache.d or o.shape != shape:
         raise ValueError("q and o must be [B, H, d] of the cache")
     if q.dtype != cache.dtype or o.dtype != cache.dtype:
         raise TypeError("q, o and cache dtypes differ")
-    qs, os_ = q.stride(), o.stride()
-    if qs[2] != 1 or os_[2] != 1:
+    q_sb, q_sh, q_sd = q.stride()
+    o_sb, o_sh, o_sd = o.stride()
+    if q_sd != 1 or o_sd != 1:
         raise ValueError("the head-dim axis must be contiguous")
-    if lse is not None and (tuple(lse.shape) != (B, H) or lse.dtype != _torch().float32 or
-                            not lse.is_contiguous()):
-        raise ValueError("lse must be a contiguous float32 [B,H] tensor")
-    mode = 0 if weight is None else (2 if accumulate else 1)
-    if mode and cache.acc is None:
-        raise ValueError("weights are wanted of a cache without acc")
-    _on_device(cache, q, o, lse, workspace)
-    handle = _stream(stream)
-    L = lib()
-    need = cache._need.get((H, mode))
-    if need is None:
-        need = cache._need[(H, mode)] = int(L.avits_cache_attention_workspace(cache._ref, H, mode))
-    if workspace is None:
-        workspace = _scratch(cache, max(need, 16), handle)
-    rc = L.avits_cache_attention(
-        cache._ref, q.data_ptr(), H, qs[0], qs[1], float(softmax_scale), o.data_ptr(), os_[0],
-        os_[1], None if lse is None else lse.data_ptr(), mode, 0.0 if weight is None else
-        float(weight), workspace.data_ptr(), workspace.numel() * workspace.element_size(), handle)
-    _check("avits_cache_attention", rc)
+    index = cache._index
+    if q.get_device() != index or o.get_device() != index:
+        _elsewhere(cache, q, o)
+    lse_at = None
+    if lse is not None:
+        if lse.shape != (B, H) or lse.dtype != cache.float32 or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous float32 [B,H] tensor")
+        if lse.get_device() != index:
+            _elsewhere(cache, lse)
+        lse_at = lse.data_ptr()
+    if weight is None:
+        mode, weight = 0, 0.0
+    else:
+        mode = 2 if accumulate else 1
+        if cache.acc is None:
+            raise ValueError("weights are wanted of a cache without acc")
+    handle = _call_stream(cache, stream)
+    ws_at, ws_bytes = None, 0
+    if workspace is not None:
+        _elsewhere(cache, workspace)
+        ws_at, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    else:
+        need = cache._need.get((H, mode))
+        if need is None:
+            need = cache._need[(H, mode)] = \
+                int(lib().avits_cache_attention_workspace(cache._ref, H, mode))
+        if need:
+            buf = _scratch(cache, need, handle)
+            ws_at, ws_bytes = buf.data_ptr(), need
+    rc = cache._attend(cache._ref, q.data_ptr(), H, q_sb, q_sh, softmax_scale, o.data_ptr(), o_sb,
+                       o_sh, lse_at, mode, weight, ws_at, ws_bytes, handle)
+    if rc != 0:
+        _check("avits_cache_attention", rc)
     return o
 
 
@@ -714,15 +746,17 @@ def avits_cache_evict(src: KVCache, dst: KVCache, keep: int, sinks: int, recent:
     their weights to the places 0 .. of dst (pages that src does not read), whose
     lens are written.  keep_idx [B,Hkv,keep] int32: their places in src, -1 past
     the kept ones."""
-    if tuple(keep_idx.shape) != (src.B, src.Hkv, keep) or keep_idx.dtype != _torch().int32 or \
+    if keep_idx.shape != (src.B, src.Hkv, keep) or keep_idx.dtype != src.int32 or \
             not keep_idx.is_contiguous():
         raise ValueError("keep_idx must be a contiguous int32 [B, Hkv, keep] tensor")
-    if src.dtype != dst.dtype or (src.B, src.Hkv, src.d) != (dst.B, dst.Hkv, dst.d):
+    if src.dtype != dst.dtype or src.B != dst.B or src.Hkv != dst.Hkv or src.d != dst.d:
         raise ValueError("the two caches' types or sizes differ")
     if src.acc is None or dst.acc is None:
         raise ValueError("eviction goes by accumulated weights: both caches need acc")
-    _on_device(src, dst.k_pages, keep_idx)
-    rc = lib().avits_cache_evict(src._ref, dst._ref, int(keep), int(sinks), int(recent),
-                                 keep_idx.data_ptr(), _stream(stream))
-    _check("avits_cache_evict", rc)
+    if dst._index != src._index or keep_idx.get_device() != src._index:
+        _elsewhere(src, dst.k_pages, keep_idx)
+    rc = src._evict(src._ref, dst._ref, keep, sinks, recent, keep_idx.data_ptr(),
+                    _call_stream(src, stream))
+    if rc != 0:
+        _check("avits_cache_evict", rc)
     return keep_idx

@@ -452,8 +452,8 @@ avits_status avits_cache_attention(const avits_kv_cache* cache, const void* q, i
   if ((H > 1 && o_sh < cache->d) || (cache->B > 1 && o_sb < cache->d)) return AVITS_ERR_INVALID_ARG;
   if (!cache_attention_sizes_ok(*cache, H)) return AVITS_ERR_UNSUPPORTED;
   const int sms = num_sms_current();
-  if (!workspace || !aligned16(workspace) ||
-      ws_bytes < cache_attention_workspace(*cache, H, weights != AVITS_WEIGHTS_NONE, sms))
+  const size_t need = cache_attention_workspace(*cache, H, weights != AVITS_WEIGHTS_NONE, sms);
+  if (need > 0 && (!workspace || !aligned16(workspace) || ws_bytes < need))
     return AVITS_ERR_INVALID_ARG;
   const CacheAttnCall call{*cache, q, H, q_sb, q_sh, softmax_scale, o, o_sb, o_sh, lse_opt,
                            weights, weight, workspace};

@@ -1447,7 +1447,8 @@ bool cache_attention_sizes_ok(const avits_kv_cache& c, int H) {
 }
 
 size_t cache_attention_workspace(const avits_kv_cache& c, int H, bool score, int num_sms) {
-  return layout_of(c, H, shape_of(c, H, score, num_sms), score).total;
+  const Shape s = shape_of(c, H, score, num_sms);
+  return s.cluster > 0 ? 0 : layout_of(c, H, s, score).total;
 }
 
 cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsigned int* status,

@@ -200,9 +200,11 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   const int last = n - a.recent, stripe = threads * kRun;
   const bool vec = (reinterpret_cast<uintptr_t>(acc) & 15u) == 0;   // lo is a multiple of 4
   float x[kRun];
-  // this thread's run of a stripe; a part of one stripe is read once
+  uint32_t k[kRun];
+  int here;                // keys of the run that are in the part: the first ones
   auto load = [&](int j0) {
-    if (vec && j0 + kRun <= hi) {
+    here = min(max(hi - j0, 0), kRun);
+    if (vec && here == kRun) {
 #pragma unroll
       for (int i = 0; i < kRun; i += 4) {
         const float4 p = *reinterpret_cast<const float4*>(acc + j0 + i);
@@ -210,15 +212,20 @@ cache_select_kernel(const __grid_constant__ Evict a) {
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) x[i] = j0 + i < hi ? acc[j0 + i] : 0.f;
+      for (int i = 0; i < kRun; ++i) x[i] = i < here ? acc[j0 + i] : 0.f;
     }
   };
-  auto key = [&](int j, float v) {     // the first and the last ones stand above all
-    return j < a.sinks || j >= last ? 0xFFFFFFFFu : order_of(v);
+  // this thread's run of a stripe; a part of one stripe is read once here, and
+  // for its kept weights at the end
+  auto load_keys = [&](int j0) {
+    load(j0);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i)       // the first and the last ones stand above all
+      k[i] = j0 + i < a.sinks || j0 + i >= last ? 0xFFFFFFFFu : order_of(x[i]);
   };
   const int j1 = lo + tid * kRun;
   const bool again = hi - lo > stripe;
-  load(j1);
+  load_keys(j1);
   __syncthreads();
 
   uint32_t prefix = 0u, mask = 0u, need = (uint32_t)a.keep;
@@ -229,12 +236,10 @@ cache_select_kernel(const __grid_constant__ Evict a) {
     // a first digit is one of few: lanes count in tables of their own
     uint32_t* count = pass == 0 ? s_first[lane % kSelCopies] : hist;
     for (int j0 = j1; j0 < hi; j0 += stripe) {
-      if (again) load(j0);
+      if (again) load_keys(j0);
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        const uint32_t k = key(j0 + i, x[i]);
-        if (j0 + i < hi && (k & mask) == prefix) atomicAdd(&count[(k >> shift) & 255u], 1u);
-      }
+      for (int i = 0; i < kRun; ++i)
+        if (i < here && (k[i] & mask) == prefix) atomicAdd(&count[(k[i] >> shift) & 255u], 1u);
     }
     __syncthreads();
     if (pass == 0 || ncta > 1) {
@@ -253,31 +258,32 @@ cache_select_kernel(const __grid_constant__ Evict a) {
       if (ncta > 1) cluster.sync(); else __syncthreads();
     }
     if (w == 0) {
-      // lane l: digits 255 - 8 l down to 248 - 8 l
+      // lane l adds up digits 255 - 8 l down to 248 - 8 l; then lanes 0-7 take one
+      // digit each of those that hold the needed one
       const uint32_t* table = ncta > 1 ? cluster.map_shared_rank(s_total[pass], 0) : hist;
       const uint4* at = reinterpret_cast<const uint4*>(table) + 2 * (31 - lane);
       const uint4 p = at[0], q = at[1];
-      const uint32_t c[8] = {q.w, q.z, q.y, q.x, p.w, p.z, p.y, p.x};
-      uint32_t sum = 0u;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += c[i];
-      uint32_t above = sum;
+      const uint32_t sum = ((p.x + p.y) + (p.z + p.w)) + ((q.x + q.y) + (q.z + q.w));
+      uint32_t upto = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, above, o);
-        if (lane >= o) above += y;
+        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
       }
-      above -= sum;
-      if (above < need && need <= above + sum) {
+      const int from = __ffs(__ballot_sync(0xffffffffu, upto >= need)) - 1;
+      const uint32_t rest = need - __shfl_sync(0xffffffffu, upto - sum, from);
+      const int digit = 255 - 8 * from - (lane & 7);
+      const uint32_t c = table[digit];
+      uint32_t to = c;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (above < need && need <= above + c[i]) {
-            s_pick[0] = 255u - 8u * lane - i;
-            s_pick[1] = need - above;
-            s_pick[2] = c[i] == need - above;
-          }
-          above += c[i];
-        }
+      for (int o = 1; o < 8; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, to, o);
+        if (lane >= o) to += y;
+      }
+      if (lane < 8 && to - c < rest && rest <= to) {
+        s_pick[0] = (uint32_t)digit;
+        s_pick[1] = rest - (to - c);
+        s_pick[2] = to == rest;
       }
     } else if (pass > 0) {
       // the other table was last read two barriers ago
@@ -293,12 +299,11 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   const int warps = threads >> 5;
   uint32_t above = 0u, equal = 0u;
   for (int j0 = j1; j0 < hi; j0 += stripe) {
-    if (again) load(j0);
+    if (again) load_keys(j0);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-      const uint32_t k = key(j0 + i, x[i]) & mask;
-      above += j0 + i < hi && k > prefix;
-      equal += j0 + i < hi && k == prefix;
+      above += i < here && (k[i] & mask) > prefix;
+      equal += i < here && (k[i] & mask) == prefix;
     }
   }
   uint32_t bx, by, tx, ty;      // of the threads before, of all
@@ -317,28 +322,28 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   for (int s0 = lo; s0 < hi; s0 += stripe, par ^= 1) {      // the same for all threads
     const int j0 = s0 + tid * kRun;
     if (again) {
-      load(j0);
+      load_keys(j0);
       above = equal = 0u;
 #pragma unroll
       for (int i = 0; i < kRun; ++i) {
-        const uint32_t k = key(j0 + i, x[i]) & mask;
-        above += j0 + i < hi && k > prefix;
-        equal += j0 + i < hi && k == prefix;
+        above += i < here && (k[i] & mask) > prefix;
+        equal += i < here && (k[i] & mask) == prefix;
       }
       block_scan(above, equal, s_warp[par], lane, w, warps, bx, by, tx, ty);
     }
     uint32_t ra = base_a + bx, re = base_e + by;
+    if (!again) load(j0);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-      const uint32_t k = key(j0 + i, x[i]) & mask;
-      if (j0 + i < hi) {
-        if (k > prefix || (k == prefix && re < need)) {
+      const uint32_t kk = k[i] & mask;
+      if (i < here) {
+        if (kk > prefix || (kk == prefix && re < need)) {
           const uint32_t rank = ra + min(re, need);
           idx[rank] = j0 + i;
           acc2[rank] = x[i];
         }
-        ra += k > prefix;
-        re += k == prefix;
+        ra += kk > prefix;
+        re += kk == prefix;
       }
     }
     base_a += tx;

@@ -126,10 +126,13 @@ def test_append_refusals(lib):
 
 
 def test_attention_refusals(lib):
-    s = struct()
+    # long enough to need a workspace
+    s = struct(max_len=100000, table_sb=6250, acc_sb=2 * 100000, acc_sh=100000)
     ref = ctypes.addressof(s)
     need = lib.avits_cache_attention_workspace(ref, 8, 2)
     assert need > lib.avits_cache_attention_workspace(ref, 8, 0) > 0
+    short = struct()                                                # one launch, no workspace
+    assert lib.avits_cache_attention_workspace(ctypes.addressof(short), 8, 2) == 0
     assert lib.avits_cache_attention_workspace(ref, 7, 0) == 0      # not a multiple of Hkv
     assert lib.avits_cache_attention_workspace(ref, 8, 3) == 0
 

@@ -668,8 +668,10 @@ def test_binding_refusals_on_the_device(av):
         att(w.cache, w.q[:, :3], w.scale, o[:, :3])               # 3 heads over 2
     with pytest.raises(av.AvitsError):
         att(w.cache, w.q, 0.0, o)
+    long = World(av, "bf16", [20, 9], 4, 2, 64, 16, max_len=20000)      # one that needs some
+    assert av.avits_cache_attention_workspace(long.cache, 4, True) > 16
     with pytest.raises(av.AvitsError):
-        att(w.cache, w.q, w.scale, o, workspace=t.empty(16, dtype=t.uint8, device=DEV))
+        att(long.cache, long.q, w.scale, o, workspace=t.empty(16, dtype=t.uint8, device=DEV))
     plain = av.KVCache(w.k_pages, w.v_pages, w.table, w.lens)
     with pytest.raises(ValueError):
         att(plain, w.q, w.scale, o, weight=1.0)
