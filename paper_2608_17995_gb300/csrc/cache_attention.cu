@@ -1057,7 +1057,7 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
 // ---------------------------------------------------------- second kernel --
 // Block (unit, row), or, where there are many units, (CTA of the first kernel,
 // rows): O of that unit, or of the one whose first of several pieces was that
-// CTA's.  Block (b, hk, 512 keys): their weights, 4 keys to a thread.  What a block reads waits
+// CTA's.  Block (b, hk, 512 keys or more): their weights.  What a block reads waits
 // for as little as can be: parts and logits are on their way while the row's lse
 // is put together.
 constexpr int kFinishThreads = 128;
@@ -1122,28 +1122,32 @@ __device__ __forceinline__ float join_lse_serial(const CacheAttn& a, int slot, i
   return l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
 }
 
-// `wide`: `at` is a unit, threads lie side by side over the pieces of one row;
-// else it is a CTA of the first kernel and threads lie over the rows, each going
-// through its row's pieces.
-template <typename T>
-__device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, int wide) {
+// kWide: `at0` is a unit and r0 one of its rows, threads lie over 32 of its columns
+// (from c0) and over its pieces; else at0 is a CTA of the first kernel and threads
+// lie over whole rows from r0 on, each going through its row's pieces.
+constexpr int kWideCols = 8;     // of 4
+
+template <typename T, bool kWide>
+__device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, int c0) {
   __shared__ float4 s_sum[kFinishThreads];
   const int tid = threadIdx.x, units = a.c.Hkv * a.groups;
   int4 own;
-  if (wide) {
-    if (cache_len(a.c, at0 / units) == 0) return;
+  if (kWide) {
+    const int len = cache_len(a.c, at0 / units);
     const int2 rec = a.rec[at0];
+    if (len == 0) return;
     own = make_int4(rec.y > 1 ? at0 : -1, rec.x, rec.y, 0);
   } else {
     own = a.own[at0];
   }
   if (own.x < 0) return;
   const int b = own.x / units, u = own.x - b * units, hk = u / a.groups;
-  const int d4 = a.c.d / 4, lanes = kFinishThreads / d4, col = tid % d4, sub = tid / d4;
-  const int r = wide ? r0 : r0 + sub, step = wide ? lanes : 1;
+  const int d4 = kWide ? kWideCols : a.c.d / 4, lanes = kFinishThreads / d4;
+  const int sub = tid / d4, col = c0 + tid - sub * d4;
+  const int r = kWide ? r0 : r0 + sub, step = kWide ? lanes : 1;
   const int row = (u - hk * a.groups) * a.rows + r, h = hk * a.G + row;
-  const bool mine = sub < lanes && r < a.rows && row < a.G;
-  const int pieces = mine ? own.z : 0, k1 = wide ? sub : 0;
+  const bool mine = sub < lanes && r < a.rows && row < a.G && col < a.c.d / 4;
+  const int pieces = mine ? own.z : 0, k1 = kWide ? sub : 0;
   constexpr int kDeep = 8;
   float4 x[kDeep];
   float mx[kDeep];
@@ -1159,8 +1163,8 @@ __device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, 
     }
   };
   load(k1);
-  const float e = wide ? (row < a.G ? join_lse(a, own.y, own.z, r, tid & 31) : 0.f)
-                       : join_lse_serial(a, own.y, pieces, r);
+  const float e = kWide ? (row < a.G ? join_lse(a, own.y, own.z, r, tid & 31) : 0.f)
+                        : join_lse_serial(a, own.y, pieces, r);
   if (mine && k1 == 0 && col == 0 && a.lse) a.lse[(int64_t)b * a.H + h] = e * kLn2;
   const float none = e != e ? e : 0.f;
   float4 v = make_float4(none, none, none, none);
@@ -1176,12 +1180,12 @@ __device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, 
         }
     }
   }
-  if (wide) {
+  if (kWide) {
     s_sum[tid] = v;
     __syncthreads();
     if (sub != 0) return;
     for (int k = 1; k < lanes; ++k) {
-      const float4 y = s_sum[k * d4 + col];
+      const float4 y = s_sum[k * d4 + tid];
       v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
     }
   }
@@ -1193,85 +1197,131 @@ __device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, 
   store_elem(out, 3, v.w);
 }
 
-__device__ __forceinline__ void weights_block(const CacheAttn& a, int bh, int part) {
+// `parts` parts of kSpan runs of 512 keys, kRows rows at a time.  First the length
+// and where the rows' pieces are; then everything else of the first part at once:
+// logits, old weights, pieces.
+template <int kSpan, int kRows>
+__device__ __forceinline__ void weights_block(const CacheAttn& a, int bh, int part, int parts) {
   __shared__ float s_e[kMaxGroup];
-  const int b = bh / a.c.Hkv, hk = bh - b * a.c.Hkv, tid = threadIdx.x;
-  const int len = cache_len(a.c, b), j = part * kWeightKeys + tid * 4;
-  if (part * kWeightKeys >= len) return;
-  const float* lg = a.logits + ((int64_t)b * a.H + hk * a.G) * a.ld + min(j, len - 1) / 4 * 4;
-  constexpr int kDeep = 8;
-  float4 x[kDeep];
+  const int b = bh / a.c.Hkv, hk = bh - b * a.c.Hkv, tid = threadIdx.x, w = tid >> 5;
+  int jb = part * (kSpan * kWeightKeys);
+  const int2* recs = a.rec + bh * a.groups;
+  const int len = cache_len(a.c, b);
+  int2 rec = recs[0];
+  if (jb >= len) return;
+  const float* lg = a.logits + ((int64_t)b * a.H + hk * a.G) * a.ld;
+  float* acc = a.c.acc + (int64_t)b * a.c.acc_sb + (int64_t)hk * a.c.acc_sh;
+  const bool vec = (reinterpret_cast<uintptr_t>(acc) & 15u) == 0;
+  float4 x[kSpan][kRows];
+  float old[kSpan][4];
+  auto load = [&](int r0) {
 #pragma unroll
-  for (int r = 0; r < kDeep; ++r)
-    if (r < a.G) x[r] = *reinterpret_cast<const float4*>(lg + (int64_t)r * a.ld);
-  float* acc = a.c.acc + (int64_t)b * a.c.acc_sb + (int64_t)hk * a.c.acc_sh + j;
-  const bool vec = (reinterpret_cast<uintptr_t>(acc) & 15u) == 0 && j + 4 <= len;
-  float old[4] = {};
-  if (a.add && j < len) {
-    if (vec) {
-      const float4 y = *reinterpret_cast<const float4*>(acc);
-      old[0] = y.x; old[1] = y.y; old[2] = y.z; old[3] = y.w;
-    } else {
+    for (int g = 0; g < kSpan; ++g) {
+      const int j = jb + g * kWeightKeys + tid * 4;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (j + k < len) old[k] = acc[k];
+      for (int r = 0; r < kRows; ++r)
+        if (j < len && r0 + r < a.G)
+          x[g][r] = *reinterpret_cast<const float4*>(lg + (int64_t)(r0 + r) * a.ld + j);
     }
-  }
-  if (a.few) {
-    for (int r = tid; r < a.G; r += kFinishThreads) {
-      const int rg = r / a.rows;
-      const int2 rec = a.rec[(b * a.c.Hkv + hk) * a.groups + rg];
-      const float e = rec.y == 1 ? a.lse2[(int64_t)b * a.H + hk * a.G + r]
-                                 : join_lse_serial(a, rec.x, rec.y, r - rg * a.rows);
-      s_e[r] = e == -INFINITY ? INFINITY : e;   // nothing there: no weight
-    }
-  } else {
-    for (int r = tid >> 5; r < a.G; r += kFinishThreads / 32) {
-      const int rg = r / a.rows;
-      const int2 rec = a.rec[(b * a.c.Hkv + hk) * a.groups + rg];
-      const float e = rec.y == 1 ? a.lse2[(int64_t)b * a.H + hk * a.G + r]
-                                 : join_lse(a, rec.x, rec.y, r - rg * a.rows, tid & 31);
-      if ((tid & 31) == 0) s_e[r] = e == -INFINITY ? INFINITY : e;
-    }
-  }
-  __syncthreads();
-  if (j >= len) return;
-  float s[4] = {};
-  for (int r0 = 0; r0 < a.G; r0 += kDeep) {
+  };
+  auto load_old = [&]() {
 #pragma unroll
-    for (int r = 0; r < kDeep; ++r) {
-      if (r0 + r < a.G) {
-        if (r0 > 0) x[r] = *reinterpret_cast<const float4*>(lg + (int64_t)(r0 + r) * a.ld);
-        const float e = s_e[r0 + r];
-        s[0] += ex2(x[r].x - e);
-        s[1] += ex2(x[r].y - e);
-        s[2] += ex2(x[r].z - e);
-        s[3] += ex2(x[r].w - e);
+    for (int g = 0; g < kSpan; ++g) {
+      const int j = jb + g * kWeightKeys + tid * 4;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) old[g][k] = 0.f;
+      if (a.add) {
+        if (vec && j + 4 <= len) {
+          const float4 y = *reinterpret_cast<const float4*>(acc + j);
+          old[g][0] = y.x; old[g][1] = y.y; old[g][2] = y.z; old[g][3] = y.w;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (j + k < len) old[g][k] = acc[j + k];
+        }
       }
     }
+  };
+  load(0);
+  load_old();
+  const int step = a.few ? kFinishThreads : kFinishThreads / 32;
+  for (int r = a.few ? tid : w; r < a.G; r += step) {
+    const int rg = a.groups == 1 ? 0 : r / a.rows;
+    if (rg > 0) rec = recs[rg];
+    const int row = r - rg * a.rows;
+    const float e = rec.y == 1 ? a.lse2[(int64_t)b * a.H + hk * a.G + r]
+                    : a.few    ? join_lse_serial(a, rec.x, rec.y, row)
+                               : join_lse(a, rec.x, rec.y, row, tid & 31);
+    if (a.few || (tid & 31) == 0) s_e[r] = e == -INFINITY ? INFINITY : e;   // no weight there
   }
+  __syncthreads();
+  const int end = min(len, jb + parts * (kSpan * kWeightKeys));
+#pragma unroll 1
+  for (;;) {
+    float s[kSpan][4] = {};
+    for (int r0 = 0; r0 < a.G; r0 += kRows) {
+      if (r0 > 0) load(r0);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) s[k] = fmaf(s[k], a.wmean, old[k]);
-  if (vec) {
-    *reinterpret_cast<float4*>(acc) = make_float4(s[0], s[1], s[2], s[3]);
-  } else {
+      for (int r = 0; r < kRows; ++r) {
+        if (r0 + r < a.G) {
+          const float e = s_e[r0 + r];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (j + k < len) acc[k] = s[k];
+          for (int g = 0; g < kSpan; ++g) {
+            s[g][0] += ex2(x[g][r].x - e);
+            s[g][1] += ex2(x[g][r].y - e);
+            s[g][2] += ex2(x[g][r].z - e);
+            s[g][3] += ex2(x[g][r].w - e);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < kSpan; ++g) {
+      const int j = jb + g * kWeightKeys + tid * 4;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[g][k] = fmaf(s[g][k], a.wmean, old[g][k]);
+      if (vec && j + 4 <= len) {
+        *reinterpret_cast<float4*>(acc + j) = make_float4(s[g][0], s[g][1], s[g][2], s[g][3]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (j + k < len) acc[j + k] = s[g][k];
+      }
+    }
+    jb += kSpan * kWeightKeys;
+    if (jb >= end) return;
+    load(0);
+    load_old();
   }
 }
 
+// Runs of 512 keys that a block of weights takes: small groups have few logits.
+inline int weight_span(int G) { return G > 2 ? 1 : 2; }
+
+// The blocks of the second kernel: weights, `weights` blocks per (b, hk) of `parts`
+// parts each, then joins.
+struct Finish {
+  int blocks, weights, parts;      // blocks: of weights, in all
+  int rows, cols;                  // join blocks of a unit: row groups, column groups
+};
+
 template <typename T>
-__global__ void __launch_bounds__(kFinishThreads)
-cache_finish_kernel(const __grid_constant__ CacheAttn a, int joins, int parts) {
+__global__ void __launch_bounds__(kFinishThreads, 6)
+cache_finish_kernel(const __grid_constant__ CacheAttn a, Finish f) {
   pdl_wait_then_trigger();
-  const int i = (int)blockIdx.x - joins;
-  if (i < 0) {
-    const int lanes = a.few ? kFinishThreads / (a.c.d / 4) : 1;     // rows of a block
-    const int per = (a.rows + lanes - 1) / lanes;                   // blocks of a CTA's unit
-    join_block<T>(a, (int)blockIdx.x / per, (int)blockIdx.x % per * lanes, !a.few);
+  int i = blockIdx.x;
+  if (i < f.blocks) {
+    const int bh = i / f.weights, part = (i - bh * f.weights) * f.parts;
+    if (a.G > 2) weights_block<1, 8>(a, bh, part, f.parts);
+    else weights_block<2, 2>(a, bh, part, f.parts);
+    return;
+  }
+  i -= f.blocks;
+  if (a.few) {
+    join_block<T, false>(a, i / f.rows, i % f.rows * (kFinishThreads / (a.c.d / 4)), 0);
   } else {
-    weights_block(a, i / parts, i % parts);
+    const int col = i % f.cols, row = i / f.cols;
+    join_block<T, true>(a, row / f.rows, row % f.rows, col * kWideCols);
   }
 }
 
@@ -1411,7 +1461,7 @@ cudaError_t launch_cluster(const CUtensorMap& mk, const CUtensorMap& mv, const C
 }
 
 template <typename Rows>
-cudaError_t launch_rows(CacheAttn& a, int ncta, cudaStream_t s) {
+cudaError_t launch_rows(CacheAttn& a, int ncta, int num_sms, cudaStream_t s) {
   CUtensorMap mk{}, mv{};
   map_cache<Rows>(a, &mk, &mv);
   if (ncta > 0) return launch_cluster<Rows>(mk, mv, a, ncta, s);
@@ -1420,21 +1470,32 @@ cudaError_t launch_rows(CacheAttn& a, int ncta, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = launch_pdl(kernel, dim3(a.grid), dim3(kThreads), smem_bytes<Rows>(), s, mk, mv, a);
   if (e != cudaSuccess) return e;
-  const int lanes = a.few ? kFinishThreads / (a.c.d / 4) : 1;
-  const int joins = (a.few ? a.grid : a.c.B * a.c.Hkv * a.groups) * ((a.rows + lanes - 1) / lanes);
-  const int parts = a.score ? (a.c.max_len + kWeightKeys - 1) / kWeightKeys : 0;
+  const int bh = a.c.B * a.c.Hkv, d4 = a.c.d / 4;
+  Finish f{};
+  if (a.score) {
+    // about as many blocks as are resident at once
+    const int run = weight_span(a.G) * kWeightKeys, parts = (a.c.max_len + run - 1) / run;
+    const long long all = (long long)bh * parts, most = 6ll * num_sms;
+    f.parts = (int)((all + most - 1) / most);
+    if (f.parts > parts) f.parts = parts;
+    f.weights = (parts + f.parts - 1) / f.parts;
+    f.blocks = bh * f.weights;
+  }
+  const int lanes = kFinishThreads / d4;
+  f.rows = a.few ? (a.rows + lanes - 1) / lanes : a.rows;
+  f.cols = a.few ? 1 : (d4 + kWideCols - 1) / kWideCols;
+  const int joins = (a.few ? a.grid : bh * a.groups) * f.rows * f.cols;
   constexpr auto finish = cache_finish_kernel<typename Rows::T>;
   e = prefer_max_shared<finish>();
   if (e != cudaSuccess) return e;
-  const unsigned blocks = (unsigned)joins + (unsigned)(a.c.B * a.c.Hkv) * (unsigned)parts;
-  return launch_pdl(finish, dim3(blocks), dim3(kFinishThreads), 0, s, a, joins, parts > 0 ? parts : 1);
+  return launch_pdl(finish, dim3((unsigned)(f.blocks + joins)), dim3(kFinishThreads), 0, s, a, f);
 }
 
 template <template <int, int> class Rows, int kR>
-cudaError_t launch_width(CacheAttn& a, int D, int ncta, cudaStream_t s) {
-  if (D == 64) return launch_rows<Rows<64, kR>>(a, ncta, s);
-  if (D == 128) return launch_rows<Rows<128, kR>>(a, ncta, s);
-  if constexpr (kR <= 16) return launch_rows<Rows<256, kR>>(a, ncta, s);
+cudaError_t launch_width(CacheAttn& a, int D, int ncta, int num_sms, cudaStream_t s) {
+  if (D == 64) return launch_rows<Rows<64, kR>>(a, ncta, num_sms, s);
+  if (D == 128) return launch_rows<Rows<128, kR>>(a, ncta, num_sms, s);
+  if constexpr (kR <= 16) return launch_rows<Rows<256, kR>>(a, ncta, num_sms, s);
   return cudaErrorInvalidValue;
 }
 
@@ -1484,10 +1545,10 @@ cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsig
   a.logits = reinterpret_cast<float*>(ws + l.logits);
   a.ld = l.ld;
   a.status = status;
-  if (c.dt != AVITS_BF16) return launch_width<RowsF32, 8>(a, sh.D, sh.cluster, s);
-  if (sh.rows == 8) return launch_width<RowsBf16, 8>(a, sh.D, sh.cluster, s);
-  if (sh.rows == 16) return launch_width<RowsBf16, 16>(a, sh.D, sh.cluster, s);
-  return launch_width<RowsBf16, 32>(a, sh.D, sh.cluster, s);
+  if (c.dt != AVITS_BF16) return launch_width<RowsF32, 8>(a, sh.D, sh.cluster, num_sms, s);
+  if (sh.rows == 8) return launch_width<RowsBf16, 8>(a, sh.D, sh.cluster, num_sms, s);
+  if (sh.rows == 16) return launch_width<RowsBf16, 16>(a, sh.D, sh.cluster, num_sms, s);
+  return launch_width<RowsBf16, 32>(a, sh.D, sh.cluster, num_sms, s);
 }
 
 }  // namespace avits
