@@ -1473,11 +1473,11 @@ cudaError_t launch_rows(CacheAttn& a, int ncta, int num_sms, cudaStream_t s) {
   const int bh = a.c.B * a.c.Hkv, d4 = a.c.d / 4;
   Finish f{};
   if (a.score) {
-    // about as many blocks as are resident at once
+    // one part to a block, or two where there would be more blocks than are resident
+    // at once (131072 keys: 61.0 us with two, 62.6 with one); four in a row took
+    // longer again (48 x <= 4096: 98 us, with two 90)
     const int run = weight_span(a.G) * kWeightKeys, parts = (a.c.max_len + run - 1) / run;
-    const long long all = (long long)bh * parts, most = 6ll * num_sms;
-    f.parts = (int)((all + most - 1) / most);
-    if (f.parts > parts) f.parts = parts;
+    f.parts = parts > 1 && (long long)bh * parts > 6ll * num_sms ? 2 : 1;
     f.weights = (parts + f.parts - 1) / f.parts;
     f.blocks = bh * f.weights;
   }

@@ -12,8 +12,9 @@ namespace avits {
 namespace {
 
 // ----------------------------------------------------------------- append --
-// One warp per new token: the sequence by a search of cu_new 32 ways at a time,
-// the place from the length, then the token's Hkv rows of keys and of values.
+// One warp per new token: its first pieces are on their way while the sequence is
+// found by a search of cu_new 32 ways at a time, and the place from the length;
+// then the token's Hkv rows of keys and of values go there.
 constexpr int kAppendThreads = 256;
 
 struct Append {
@@ -51,6 +52,23 @@ cache_append_kernel(const __grid_constant__ Append a) {
   const int lane = threadIdx.x & 31;
   const int t = blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
   if (t >= a.T) return;
+  const char* kn = a.k_new + t * a.k_st;
+  const char* vn = a.v_new + t * a.v_st;
+  const int n = a.c.Hkv * (int)a.pieces.p;
+  constexpr int kDeep = 4;
+  uint4 k[kDeep], v[kDeep];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int r = 0; r < kDeep; ++r) {
+      const int i = i0 + 32 * r;
+      if (i < n) {
+        const int h = a.pieces.div(i), c = i - h * (int)a.pieces.p;
+        k[r] = ld_once(kn + h * a.k_sh + c * 16);
+        v[r] = ld_once(vn + h * a.v_sh + c * 16);
+      }
+    }
+  };
+  load(lane);
   const int b = sequence_of(a.cu, a.c.B, t, lane);
   if (b >= a.c.B) return;
   if (a.c.lens[b] > a.c.max_len && lane == 0) raise_status(a.status, AVITS_ERR_PAGE);
@@ -71,21 +89,8 @@ cache_append_kernel(const __grid_constant__ Append a) {
   }
   char* kp = static_cast<char*>(a.c.k_pages) + ((int64_t)page * a.c.k_sp + slot * a.c.k_st) * a.es;
   char* vp = static_cast<char*>(a.c.v_pages) + ((int64_t)page * a.c.v_sp + slot * a.c.v_st) * a.es;
-  const char* kn = a.k_new + t * a.k_st;
-  const char* vn = a.v_new + t * a.v_st;
-  const int n = a.c.Hkv * (int)a.pieces.p;
-  constexpr int kDeep = 4;
   for (int i0 = lane; i0 < n; i0 += 32 * kDeep) {
-    uint4 k[kDeep], v[kDeep];
-#pragma unroll
-    for (int r = 0; r < kDeep; ++r) {
-      const int i = i0 + 32 * r;
-      if (i < n) {
-        const int h = a.pieces.div(i), c = i - h * (int)a.pieces.p;
-        k[r] = ld_once(kn + h * a.k_sh + c * 16);
-        v[r] = ld_once(vn + h * a.v_sh + c * 16);
-      }
-    }
+    if (i0 != lane) load(i0);
 #pragma unroll
     for (int r = 0; r < kDeep; ++r) {
       const int i = i0 + 32 * r;
