@@ -121,7 +121,8 @@ struct Cursor {
 // 16-byte pieces of row r at c ^ (r % 8) (TMA's 128-byte swizzle, for ldmatrix),
 // in fp32 plain rows.  By TMA where boxes of 16 or 8 tokens never cross a page:
 // what lies outside the tensors (columns past the width, a page out of range)
-// comes as zeros.  Else by 16-byte copies, a row's pieces side by side.
+// comes as zeros.  Else by 16-byte copies, a row's pieces side by side, zeros past
+// the width.  So the products run over whole widths of 64, 128 or 256 unchecked.
 template <typename Rows>
 __device__ __forceinline__ void copy_tile(const CUtensorMap& mk, const CUtensorMap& mv,
                                           const CacheAttn& a, Cursor& cur, char* dst, uint64_t* bar,
@@ -133,11 +134,17 @@ __device__ __forceinline__ void copy_tile(const CUtensorMap& mk, const CUtensorM
   if (a.box) {
     const int jb = j0 + (lane * a.box & (kTile - 1));
     const int page = jb < cur.len ? checked_page(a.c, cur.entry, a.status) : -1;
-    const int p0 = __shfl_sync(0xffffffffu, page, 0), p1 = __shfl_sync(0xffffffffu, page, 1);
+    int p0 = page, p1 = page;        // one box: the same page in all lanes
     const int n = cur.len - j0;
     ok = n >= kTile ? (1u << kTile) - 1u : (1u << n) - 1u;
-    if (p0 < 0) ok &= ~((1u << a.box) - 1u);
-    if (p1 < 0) ok &= a.box < kTile ? (1u << a.box) - 1u : 0u;
+    if (a.box == kTile) {
+      if (page < 0) ok = 0u;
+    } else {
+      p0 = __shfl_sync(0xffffffffu, page, 0);
+      p1 = __shfl_sync(0xffffffffu, page, 1);
+      if (p0 < 0) ok &= ~((1u << a.box) - 1u);
+      if (p1 < 0) ok &= (1u << a.box) - 1u;
+    }
     if (tc::elect_one()) {
       mbar_arrive_expect_tx(bar, Rows::kStage);
 #pragma unroll 1
@@ -157,7 +164,7 @@ __device__ __forceinline__ void copy_tile(const CUtensorMap& mk, const CUtensorM
     constexpr int kSteps = kPieces < 32 ? 1 : kPieces / 32;      // steps along a row
     const int side = kPieces < 32 ? lane / kPieces : 0;
     const int piece = kPieces < 32 ? lane % kPieces : lane;
-    const int some = a.c.d * kEs / 16, upto = kEs == 2 ? (some + 1) & ~1 : some;
+    const int some = a.c.d * kEs / 16;
     const int j = j0 + (lane & (kTile - 1));
     const int page = j < cur.len ? checked_page(a.c, cur.entry, a.status) : -1;
     ok = __ballot_sync(0xffffffffu, page >= 0) & ((1u << kTile) - 1u);
@@ -175,12 +182,10 @@ __device__ __forceinline__ void copy_tile(const CUtensorMap& mk, const CUtensorM
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
         const int c = piece + 32 * st;
-        if (c < upto) {
-          const bool there = ((ok >> row) & 1u) && c < some;
-          const uint32_t to = smem_u32(dst) + Rows::piece_at(row, c);
-          cp16(to, static_cast<const char*>(a.c.k_pages) + ko + c * 16, there);
-          cp16(to + Rows::kStage / 2, static_cast<const char*>(a.c.v_pages) + vo + c * 16, there);
-        }
+        const bool there = ((ok >> row) & 1u) && c < some;
+        const uint32_t to = smem_u32(dst) + Rows::piece_at(row, c);
+        cp16(to, static_cast<const char*>(a.c.k_pages) + ko + c * 16, there);
+        cp16(to + Rows::kStage / 2, static_cast<const char*>(a.c.v_pages) + vo + c * 16, there);
       }
     }
     cp_arrive(bar);
@@ -311,7 +316,6 @@ struct RowsBf16 {
   __device__ __forceinline__ void tile(const CacheAttn& a, uint32_t kt, const char* sq, char*,
                                        uint32_t mask, float* lg, int64_t ld, int rows, int lane) {
     const int g = lane >> 2, t = lane & 3, r8 = lane & 7;
-    const int steps = (a.c.d + 15) / 16;
     float s[kM][2][4] = {};
     {
       const int krow = r8 + ((lane >> 4) << 3), kc = (lane >> 3) & 1;
@@ -321,23 +325,19 @@ struct RowsBf16 {
       const uint32_t kat = kt + krow * 128, qat = smem_u32(sq) + qrow * 128;
 #pragma unroll
       for (int st = 0; st < D / 16; ++st) {
-        if (st < steps) {
-          uint32_t k[4];
-          ldsm4(k, kat + (st >> 2) * kColBytes + (kx ^ ((st & 3) << 5)));
+        uint32_t k[4];
+        ldsm4(k, kat + (st >> 2) * kColBytes + (kx ^ ((st & 3) << 5)));
 #pragma unroll
-          for (int mt = 0; mt < kM; ++mt) {
-            uint32_t q[4] = {0u, 0u, 0u, 0u};
-            const uint32_t at =
-                qat + (st >> 2) * kR * 128 + mt * 16 * 128 + (qx ^ ((st & 3) << 5));
-            if (kSplit8) ldsm2(q[0], q[2], at); else ldsm4(q, at);
-            mma16816(s[mt][0], q[0], q[1], q[2], q[3], k[0], k[1]);
-            mma16816(s[mt][1], q[0], q[1], q[2], q[3], k[2], k[3]);
-          }
+        for (int mt = 0; mt < kM; ++mt) {
+          uint32_t q[4] = {0u, 0u, 0u, 0u};
+          const uint32_t at = qat + (st >> 2) * kR * 128 + mt * 16 * 128 + (qx ^ ((st & 3) << 5));
+          if (kSplit8) ldsm2(q[0], q[2], at); else ldsm4(q, at);
+          mma16816(s[mt][0], q[0], q[1], q[2], q[3], k[0], k[1]);
+          mma16816(s[mt][1], q[0], q[1], q[2], q[3], k[2], k[3]);
         }
       }
     }
     // keys 2t, 2t+1 (s[.][0]) and 8+2t, 9+2t (s[.][1]); rows g (e 0, 1), g + 8 (e 2, 3)
-    const unsigned here = mask >> (2 * t);
     uint32_t p[kM][4], r[kM][4];     // A fragments of the weights and their rests
     bool raise = false;
     float top[kM][2];
@@ -346,8 +346,15 @@ struct RowsBf16 {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          s[mt][n][e] = (here >> (8 * n + (e & 1))) & 1u ? s[mt][n][e] * a.scale2 : -INFINITY;
+        for (int e = 0; e < 4; ++e) s[mt][n][e] *= a.scale2;
+      if (mask != (1u << kTile) - 1u) {
+        const unsigned here = mask >> (2 * t);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!((here >> (8 * n + (e & 1))) & 1u)) s[mt][n][e] = -INFINITY;
+      }
       if (a.score) {
 #pragma unroll
         for (int hf = 0; hf < (kSplit8 ? 1 : 2); ++hf) {
@@ -392,29 +399,17 @@ struct RowsBf16 {
     }
 #pragma unroll
     for (int mt = 0; mt < kM; ++mt) {
-      float rest[2][4];
 #pragma unroll
       for (int hf = 0; hf < (kSplit8 ? 1 : 2); ++hf) {
         const float ref = m[mt][hf] == -INFINITY ? 0.f : m[mt][hf];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float x = ex2(s[mt][n][2 * hf + e] - ref);
-            l[mt][hf] += x;
-            s[mt][n][2 * hf + e] = x;
-            rest[n][2 * hf + e] = x - __bfloat162float(__float2bfloat16_rn(x));
-          }
-      }
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        p[mt][2 * n] = pack_bf16(s[mt][n][0], s[mt][n][1]);
-        r[mt][2 * n] = pack_bf16(rest[n][0], rest[n][1]);
-        if (kSplit8) {
-          p[mt][2 * n + 1] = r[mt][2 * n];
-        } else {
-          p[mt][2 * n + 1] = pack_bf16(s[mt][n][2], s[mt][n][3]);
-          r[mt][2 * n + 1] = pack_bf16(rest[n][2], rest[n][3]);
+        for (int n = 0; n < 2; ++n) {
+          const float x0 = ex2(s[mt][n][2 * hf] - ref), x1 = ex2(s[mt][n][2 * hf + 1] - ref);
+          l[mt][hf] += x0 + x1;
+          const uint32_t both = pack_bf16(x0, x1);
+          const uint32_t rest = pack_bf16(x0 - bf16_lo(both), x1 - bf16_hi(both));
+          p[mt][2 * n + hf] = both;
+          if (kSplit8) p[mt][2 * n + 1] = rest; else r[mt][2 * n + hf] = rest;
         }
       }
     }
@@ -423,17 +418,15 @@ struct RowsBf16 {
       const uint32_t vx = (vc ^ r8) << 4, vat = kt + kStage / 2 + vrow * 128;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) {
-        if (j < steps) {
-          uint32_t v[4];
-          ldsm4t(v, vat + (j >> 2) * kColBytes + (vx ^ ((j & 3) << 5)));
+        uint32_t v[4];
+        ldsm4t(v, vat + (j >> 2) * kColBytes + (vx ^ ((j & 3) << 5)));
 #pragma unroll
-          for (int mt = 0; mt < kM; ++mt) {
-            mma16816(o[mt][2 * j], p[mt][0], p[mt][1], p[mt][2], p[mt][3], v[0], v[1]);
-            mma16816(o[mt][2 * j + 1], p[mt][0], p[mt][1], p[mt][2], p[mt][3], v[2], v[3]);
-            if (!kSplit8) {
-              mma16816(o[mt][2 * j], r[mt][0], r[mt][1], r[mt][2], r[mt][3], v[0], v[1]);
-              mma16816(o[mt][2 * j + 1], r[mt][0], r[mt][1], r[mt][2], r[mt][3], v[2], v[3]);
-            }
+        for (int mt = 0; mt < kM; ++mt) {
+          mma16816(o[mt][2 * j], p[mt][0], p[mt][1], p[mt][2], p[mt][3], v[0], v[1]);
+          mma16816(o[mt][2 * j + 1], p[mt][0], p[mt][1], p[mt][2], p[mt][3], v[2], v[3]);
+          if (!kSplit8) {
+            mma16816(o[mt][2 * j], r[mt][0], r[mt][1], r[mt][2], r[mt][3], v[0], v[1]);
+            mma16816(o[mt][2 * j + 1], r[mt][0], r[mt][1], r[mt][2], r[mt][3], v[2], v[3]);
           }
         }
       }
@@ -530,15 +523,13 @@ struct RowsF32 {
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       const int d = c * 32 + t8 * 4;
-      if (d < a.c.d) {
-        const float4 k0 = *reinterpret_cast<const float4*>(kt + (2 * kg) * D + d);
-        const float4 k1 = *reinterpret_cast<const float4*>(kt + (2 * kg + 1) * D + d);
+      const float4 k0 = *reinterpret_cast<const float4*>(kt + (2 * kg) * D + d);
+      const float4 k1 = *reinterpret_cast<const float4*>(kt + (2 * kg + 1) * D + d);
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          const float4 qv = *reinterpret_cast<const float4*>(q + g * D + d);
-          s[0][g] = fmaf(qv.x, k0.x, fmaf(qv.y, k0.y, fmaf(qv.z, k0.z, fmaf(qv.w, k0.w, s[0][g]))));
-          s[1][g] = fmaf(qv.x, k1.x, fmaf(qv.y, k1.y, fmaf(qv.z, k1.z, fmaf(qv.w, k1.w, s[1][g]))));
-        }
+      for (int g = 0; g < 8; ++g) {
+        const float4 qv = *reinterpret_cast<const float4*>(q + g * D + d);
+        s[0][g] = fmaf(qv.x, k0.x, fmaf(qv.y, k0.y, fmaf(qv.z, k0.z, fmaf(qv.w, k0.w, s[0][g]))));
+        s[1][g] = fmaf(qv.x, k1.x, fmaf(qv.y, k1.y, fmaf(qv.z, k1.z, fmaf(qv.w, k1.w, s[1][g]))));
       }
     }
     float x[2];
