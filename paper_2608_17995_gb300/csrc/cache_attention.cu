@@ -622,11 +622,12 @@ struct RowsF32 {
 };
 
 // ----------------------------------------------------------- first kernel --
-// Stages of a warp's ring, and CTAs that share an SM.
+// Stages of a warp's ring, and CTAs that share an SM: on the line of tiles, and
+// with a cluster per unit.
 template <typename Rows>
-constexpr int stages() { return Rows::D == 64 ? 3 : 2; }
-template <typename Rows>
-constexpr int ctas_per_sm() { return Rows::D > 128 ? 1 : Rows::kR == 8 ? 3 : 2; }
+constexpr int stages() { return 2; }
+constexpr int line_ctas(int D, int rows) { return D > 128 ? 1 : rows > 8 || D == 128 ? 2 : 4; }
+constexpr int cluster_ctas(int D, int rows) { return D > 128 ? 1 : rows > 8 ? 2 : 3; }
 template <typename Rows>
 constexpr int smem_bytes() {
   return kWarps * stages<Rows>() * Rows::kStage + Rows::kQBytes + kWarps * Rows::kWarpBytes;
@@ -643,7 +644,7 @@ __device__ __forceinline__ void one_tile(Rows& r, const CacheAttn& a, const char
 }
 
 template <typename Rows>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm<Rows>())
+__global__ void __launch_bounds__(kThreads, line_ctas(Rows::D, Rows::kR))
 cache_attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                        const __grid_constant__ CacheAttn a) {
   using T = typename Rows::T;
@@ -874,7 +875,7 @@ constexpr int cluster_smem(int rows, int keys) {   // keys: logits' row stride, 
 inline int logit_stride(int keys) { return (keys + 23) / 32 * 32 + 8; }
 
 template <typename Rows>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm<Rows>())
+__global__ void __launch_bounds__(kThreads, cluster_ctas(Rows::D, Rows::kR))
 cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                      const __grid_constant__ CacheAttn a, int stride) {
   using T = typename Rows::T;
@@ -1358,7 +1359,7 @@ Shape shape_of(const avits_kv_cache& c, int H, bool score, int num_sms) {
   s.tile = bf ? 16 : 8;
   s.tiles = (long long)c.B * c.Hkv * s.groups * ((c.max_len + s.tile - 1) / s.tile);
   const long long most = (s.tiles + kMinTiles - 1) / kMinTiles;
-  long long full = (long long)num_sms * (s.D > 128 ? 1 : s.rows == 8 ? 3 : 2);
+  long long full = (long long)num_sms * line_ctas(s.D, s.rows);
   if (full > kMaxGrid) full = kMaxGrid;
   s.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
   s.cluster = cluster_of(c, s, score, num_sms);
