@@ -170,10 +170,12 @@ SHAPES = [  # dtype, lens, H, Hkv, d, page, layout
 ]
 
 
+@pytest.mark.parametrize("bound", [None, 6000])      # of the lengths: one launch, or two
 @pytest.mark.parametrize("score", [False, True])
 @pytest.mark.parametrize("dtype,lens,H,Hkv,d,page,layout", SHAPES)
-def test_attention(av, dtype, lens, H, Hkv, d, page, layout, score):
-    w = World(av, dtype, lens, H, Hkv, d, page, layout, seed=len(lens) + H + d)
+def test_attention(av, dtype, lens, H, Hkv, d, page, layout, score, bound):
+    w = World(av, dtype, lens, H, Hkv, d, page, layout, seed=len(lens) + H + d, max_len=bound)
+    assert bound is None or av.avits_cache_attention_workspace(w.cache, H, score) > 0
     acc0 = w.acc.cpu().numpy()
     o, lse = run_attention(w, weight=0.75 if score else None)
     w.check(o, lse, acc0, 0.75 if score else None)
@@ -190,13 +192,85 @@ def test_attention_one_long_sequence(av, dtype):
     w.check(o, lse, acc0, 1.0)
 
 
-def test_attention_more_sequences_than_threads(av):
+@pytest.mark.parametrize("bound", [None, 6000])
+def test_attention_more_sequences_than_threads(av, bound):
     rng = np.random.default_rng(5)
     lens = rng.integers(0, 90, 333).tolist()
-    w = World(av, "bf16", lens, 4, 2, 64, 16, "heads", seed=5)
+    w = World(av, "bf16", lens, 4, 2, 64, 16, "heads", seed=5, max_len=bound)
     acc0 = w.acc.cpu().numpy()
     o, lse = run_attention(w, weight=1.0)
     w.check(o, lse, acc0, 1.0)
+
+
+@pytest.mark.parametrize("dtype,H", [("bf16", 8), ("bf16", 64), ("f32", 8)])
+def test_attention_one_long_among_many_short(av, dtype, H):
+    """Many units, one of them in more pieces than the others have keys."""
+    w = World(av, dtype, [50] * 60 + [20011] + [7] * 60, H, 2, 64, 16, seed=12)
+    acc0 = w.acc.cpu().numpy()
+    o, lse = run_attention(w, weight=1.0)
+    w.check(o, lse, acc0, 1.0)
+
+
+def test_attention_pages_that_share_memory(av):
+    """A stride of zero between pages (every page the same one): no TMA map has
+    it, the rows come by 16-byte copies."""
+    t = _torch()
+    w = World(av, "bf16", [100, 40], 4, 2, 64, 16, seed=13)
+    for i in range(2):
+        n = w.lens_l[i]
+        w.table[i, :-(-n // 16)] = w.table[0, 0]
+    k, v = (p[int(w.table[0, 0])][None].expand(w.k_pages.shape) for p in (w.k_pages, w.v_pages))
+    flat = av.KVCache(k, v, w.table, w.lens, acc=w.acc, max_len=w.max_len)
+    (oa, la), (ob, lb) = w.outputs(), w.outputs()
+    av.avits_cache_attention(flat, w.q, w.scale, oa, lse=la)
+    av.avits_cache_attention(w.cache, w.q, w.scale, ob, lse=lb)
+    assert av.avits_device_status() == 0
+    w.check(oa, la)
+    assert t.equal(oa, ob) and t.equal(la, lb)      # the same products in the same order
+
+
+@pytest.mark.parametrize("bound", [None, 6000])
+def test_calls_in_a_row_without_waiting(av, bound):
+    """append -> attention -> eviction -> attention, each reading what the one
+    before wrote, many times over: the bits of a run that waits each time."""
+    t = _torch()
+    B, H, Hkv, d, page, keep = 3, 8, 2, 64, 16, 40
+    lens = [90, 33, 64]
+
+    def run(wait):
+        w = World(av, "bf16", lens, H, Hkv, d, page, seed=14, max_len=bound)
+        g = t.Generator(device=DEV)
+        g.manual_seed(15)
+        k2, v2 = make_pool("tokens", B * 3, page, Hkv, d, t.bfloat16, fill=0.0)
+        dst = av.KVCache(k2, v2, t.arange(B * 3, dtype=t.int32, device=DEV).view(B, 3),
+                         t.zeros(B, dtype=t.int32, device=DEV),
+                         acc=t.zeros(B, Hkv, 48, device=DEV), max_len=48)
+        cu = t.arange(B + 1, dtype=t.int32, device=DEV)
+        kn = t.randn(20, B, Hkv, d, device=DEV, generator=g).bfloat16()
+        idx = t.empty(B, Hkv, keep, dtype=t.int32, device=DEV)
+        q = w.q
+        out = []
+        for r in range(20):
+            o, o2 = t.empty_like(q), t.empty_like(q)
+            av.avits_cache_append(w.cache, kn[r], kn[19 - r], cu)
+            if wait:
+                t.cuda.synchronize()
+            av.avits_cache_attention(w.cache, q, w.scale, o, weight=1.0)
+            if wait:
+                t.cuda.synchronize()
+            av.avits_cache_evict(w.cache, dst, keep, 4, 8, idx)
+            if wait:
+                t.cuda.synchronize()
+            av.avits_cache_attention(dst, q, w.scale, o2, weight=1.0)
+            if wait:
+                t.cuda.synchronize()
+            out += [o, o2, idx.clone(), dst.acc.clone(), w.acc.clone()]
+        t.cuda.synchronize()
+        return out
+
+    for a, b in zip(run(True), run(False)):
+        assert t.equal(a, b)
+    assert av.avits_device_status() == 0
 
 
 def test_attention_no_token_at_all(av):
