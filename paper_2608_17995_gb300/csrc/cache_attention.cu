@@ -29,8 +29,8 @@ namespace {
 using namespace cache;
 
 // How a call is cut: the widths 64, 128 and 256 have kernels of their own; a
-// unit has 8 rows (fp32), or 8, 16 or 32 by the group's size (bf16), so that a
-// tile in shared memory serves all the heads that share it (256 columns: 16 at
+// unit has 4 or 8 rows (fp32), or 8, 16 or 32 (bf16), by the group's size, so that
+// a tile in shared memory serves all the heads that share it (256 columns: 16 at
 // most, by registers).
 struct Shape {
   int G, D, rows, groups, tile, grid;
@@ -78,7 +78,7 @@ Shape shape_of(const avits_kv_cache& c, int H, bool score, int num_sms) {
   const bool bf = c.dt == AVITS_BF16;
   s.G = H / c.Hkv;
   s.D = c.d <= 64 ? 64 : c.d <= 128 ? 128 : 256;
-  s.rows = !bf || s.G <= 8 ? 8 : s.G <= 16 || s.D == 256 ? 16 : 32;
+  s.rows = !bf ? (s.G <= 4 ? 4 : 8) : s.G <= 8 ? 8 : s.G <= 16 || s.D == 256 ? 16 : 32;
   s.groups = (s.G + s.rows - 1) / s.rows;
   s.tile = bf ? 16 : 8;
   s.tiles = (long long)c.B * c.Hkv * s.groups * ((c.max_len + s.tile - 1) / s.tile);

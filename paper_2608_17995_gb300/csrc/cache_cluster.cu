@@ -96,7 +96,7 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
   __syncthreads();
   Rows rows;
   rows.reset();
-  const int lrow = Rows::kBf16 ? lane >> 2 : lane & 7;
+  const int lrow = Rows::logit_row(lane);
 #pragma unroll 1
   for (int t = w; t < mine; t += W) {
     __syncwarp();

@@ -139,7 +139,7 @@ cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant_
           nq[k] = Rows::load_q(a, nb, nh.x, nh.y, tid + k * kThreads);
     }
     rows.reset();
-    const int lrow = Rows::kBf16 ? lane >> 2 : lane & 7;
+    const int lrow = Rows::logit_row(lane);
     float* lg = a.score ? a.logits + ((int64_t)b * a.H + h.x + lrow) * a.ld : nullptr;
 #pragma unroll 1
     for (int t = t0 + ((w - f0) & (kWarps - 1)); t < t1; t += kWarps) {

@@ -256,6 +256,8 @@ struct RowsBf16 {
   float m[kM][2], l[kM][2];        // of rows g and g + 8 of a row tile
   float o[kM][D / 8][4];
 
+  // row of the logits that a lane keeps
+  __device__ static __forceinline__ int logit_row(int lane) { return lane >> 2; }
   // 16-byte piece c of a row of a tile
   __device__ static __forceinline__ int piece_at(int row, int c) {
     return (c >> 3) * kColBytes + row * kColPitch + (((c & 7) ^ (row & 7)) << 4);
@@ -444,14 +446,17 @@ struct RowsBf16 {
 };
 
 // ------------------------------------------------------------------ fp32 --
-// CUDA cores in fp32, 8 heads.  Q K^T: 8 lanes to a key (16-byte pieces of its
-// row), 4 keys at a time; a lane's partial dot products of the 8 heads are
-// summed over the 8 lanes by halving, which leaves head lane % 8 with the lane.
-// P V: a lane owns columns of O and reads the weights from shared memory.
-template <int D_, int>
+// CUDA cores in fp32, kR = 8 heads, or 4: every head of a row tile is multiplied,
+// also those past the group's.  Q K^T: 8 lanes to a key (16-byte pieces of its
+// row), 4 keys at a time; a lane's partial dot products of the heads are summed
+// over the 8 lanes by halving, which leaves a head with each lane (8) or with two
+// lanes (4).  P V: a lane owns columns of O and reads the weights from shared
+// memory.
+template <int D_, int kR_>
 struct RowsF32 {
   using T = float;
-  static constexpr int D = D_, kR = 8;
+  static constexpr int D = D_, kR = kR_;
+  static constexpr int kTwin = 8 / kR;       // lanes that hold the same head
   static constexpr int kTile = 8;
   static constexpr bool kBf16 = false;
   static constexpr int kStage = 2 * kTile * D * 4;
@@ -459,13 +464,14 @@ struct RowsF32 {
   static constexpr int kQBytes = kR * D * 4;
   static constexpr int kQPieces = kQBytes / 16;
   static constexpr int kBufRows = kR, kM = 1;
-  static constexpr int kWarpBytes = kTile * 8 * 4;
+  static constexpr int kWarpBytes = kTile * kR * 4;
   static constexpr int kKeysPerV = D >= 128 ? 1 : 128 / D;   // value rows read side by side
   static constexpr int kV = D >= 128 ? D / 128 : 1;
 
-  float m, l;            // of row lane % 8; l: this lane's keys only until the end
-  float o[8][kV][4];
+  float m, l;            // of row lane % 8 / kTwin; l: this lane's keys only until the end
+  float o[kR][kV][4];
 
+  __device__ static __forceinline__ int logit_row(int lane) { return (lane & 7) / kTwin; }
   __device__ static __forceinline__ int piece_at(int row, int c) { return row * kColPitch + c * 16; }
 
   __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, int b, int h0, int rows,
@@ -484,7 +490,7 @@ struct RowsF32 {
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
-    for (int g = 0; g < 8; ++g)
+    for (int g = 0; g < kR; ++g)
 #pragma unroll
       for (int c = 0; c < kV; ++c)
 #pragma unroll
@@ -494,20 +500,21 @@ struct RowsF32 {
   __device__ __forceinline__ void tile(const CacheAttn& a, uint32_t, const char* sq, char* sw,
                                        uint32_t mask, float* lg, int rows, int lane,
                                        const char* st) {
-    const int kg = lane >> 3, t8 = lane & 7;
+    const int kg = lane >> 3, t8 = lane & 7, row = t8 / kTwin;
     const float* q = reinterpret_cast<const float*>(sq);
     const float* kt = reinterpret_cast<const float*>(st);
     const float* vt = kt + kTile * D;
     float* sp = reinterpret_cast<float*>(sw);
     // a lane's keys: 2 kg, 2 kg + 1
-    float s[2][8] = {};
+    float s[2][kR] = {};
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
+      if (c * 32 >= a.c.d) break;
       const int d = c * 32 + t8 * 4;
       const float4 k0 = *reinterpret_cast<const float4*>(kt + (2 * kg) * D + d);
       const float4 k1 = *reinterpret_cast<const float4*>(kt + (2 * kg + 1) * D + d);
 #pragma unroll
-      for (int g = 0; g < 8; ++g) {
+      for (int g = 0; g < kR; ++g) {
         const float4 qv = *reinterpret_cast<const float4*>(q + g * D + d);
         s[0][g] = fmaf(qv.x, k0.x, fmaf(qv.y, k0.y, fmaf(qv.z, k0.z, fmaf(qv.w, k0.w, s[0][g]))));
         s[1][g] = fmaf(qv.x, k1.x, fmaf(qv.y, k1.y, fmaf(qv.z, k1.z, fmaf(qv.w, k1.w, s[1][g]))));
@@ -516,22 +523,25 @@ struct RowsF32 {
     float x[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      float h4[4], h2[2];
+      // half of the heads go to the lane whose bit is the other
+      auto halve = [&](float (&v)[kR], int n, int bit) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float mine = (t8 & 4) ? s[i][j + 4] : s[i][j], give = (t8 & 4) ? s[i][j] : s[i][j + 4];
-        h4[j] = mine + __shfl_xor_sync(0xffffffffu, give, 4);
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float mine = (t8 & 2) ? h4[j + 2] : h4[j], give = (t8 & 2) ? h4[j] : h4[j + 2];
-        h2[j] = mine + __shfl_xor_sync(0xffffffffu, give, 2);
-      }
-      const float mine = (t8 & 1) ? h2[1] : h2[0], give = (t8 & 1) ? h2[0] : h2[1];
-      const float dot = mine + __shfl_xor_sync(0xffffffffu, give, 1);
+        for (int j = 0; j < kR / 2; ++j)
+          if (j < n) {
+            const float mine = (t8 & bit) ? v[j + n] : v[j], give = (t8 & bit) ? v[j] : v[j + n];
+            v[j] = mine + __shfl_xor_sync(0xffffffffu, give, bit);
+          }
+      };
+      halve(s[i], kR / 2, 4);
+      halve(s[i], kR / 4, 2);
+      if (kR == 8)
+        halve(s[i], 1, 1);
+      else
+        s[i][0] += __shfl_xor_sync(0xffffffffu, s[i][0], 1);
+      const float dot = s[i][0];
       x[i] = (mask >> (2 * kg + i)) & 1u ? dot * a.scale2 : -INFINITY;
     }
-    if (a.score && t8 < rows)
+    if (a.score && row < rows && t8 % kTwin == 0)
       *reinterpret_cast<float2*>(lg + 2 * kg) = make_float2(x[0], x[1]);
     float top = fmaxf(x[0], x[1]);
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
@@ -542,8 +552,8 @@ struct RowsF32 {
       m = mn;
       l *= f;
 #pragma unroll
-      for (int g = 0; g < 8; ++g) {
-        const float fg = __shfl_sync(0xffffffffu, f, g);
+      for (int g = 0; g < kR; ++g) {
+        const float fg = __shfl_sync(0xffffffffu, f, g * kTwin);
 #pragma unroll
         for (int c = 0; c < kV; ++c)
 #pragma unroll
@@ -556,7 +566,7 @@ struct RowsF32 {
     for (int i = 0; i < 2; ++i) {
       const float p = ex2(x[i] - ref);
       l += p;
-      sp[(2 * kg + i) * 8 + t8] = p;
+      if (t8 % kTwin == 0) sp[(2 * kg + i) * kR + row] = p;
     }
     __syncwarp();
     const int sub = kKeysPerV == 1 ? 0 : lane / (32 / kKeysPerV);
@@ -564,14 +574,17 @@ struct RowsF32 {
 #pragma unroll
     for (int j = 0; j < kTile / kKeysPerV; ++j) {
       const int key = j * kKeysPerV + sub;
-      const float4* pp = reinterpret_cast<const float4*>(sp + key * 8);
-      const float4 pa = pp[0], pb = pp[1];
-      const float p[8] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
+      float p[kR];
+#pragma unroll
+      for (int g = 0; g < kR; g += 4) {
+        const float4 pa = *reinterpret_cast<const float4*>(sp + key * kR + g);
+        p[g] = pa.x; p[g + 1] = pa.y; p[g + 2] = pa.z; p[g + 3] = pa.w;
+      }
 #pragma unroll
       for (int c = 0; c < kV; ++c) {
         const float4 v = *reinterpret_cast<const float4*>(vt + key * D + col + c * 128);
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
+        for (int g = 0; g < kR; ++g) {
           o[g][c][0] = fmaf(p[g], v.x, o[g][c][0]);
           o[g][c][1] = fmaf(p[g], v.y, o[g][c][1]);
           o[g][c][2] = fmaf(p[g], v.z, o[g][c][2]);
@@ -584,9 +597,9 @@ struct RowsF32 {
     float x = l;
     x += __shfl_xor_sync(0xffffffffu, x, 8);
     x += __shfl_xor_sync(0xffffffffu, x, 16);
-    if (lane < 8) ml[lane] = make_float2(m, x);
+    if (lane < 8 && lane % kTwin == 0) ml[lane / kTwin] = make_float2(m, x);
 #pragma unroll
-    for (int g = 0; g < 8; ++g)
+    for (int g = 0; g < kR; ++g)
 #pragma unroll
       for (int c = 0; c < kV; ++c) {
         float4 v = make_float4(o[g][c][0], o[g][c][1], o[g][c][2], o[g][c][3]);
@@ -671,9 +684,14 @@ void map_cache(CacheAttn& a, CUtensorMap* mk, CUtensorMap* mv) {
 template <typename F>
 cudaError_t by_rows(const CacheAttn& a, int D, F f) {
   if (a.c.dt != AVITS_BF16) {
-    if (D == 64) return f(RowsF32<64, 8>());
-    if (D == 128) return f(RowsF32<128, 8>());
-    return f(RowsF32<256, 8>());
+    switch (a.rows + D) {
+      case 64 + 4: return f(RowsF32<64, 4>());
+      case 128 + 4: return f(RowsF32<128, 4>());
+      case 256 + 4: return f(RowsF32<256, 4>());
+      case 64 + 8: return f(RowsF32<64, 8>());
+      case 128 + 8: return f(RowsF32<128, 8>());
+      default: return f(RowsF32<256, 8>());
+    }
   }
   switch (a.rows + D) {
     case 64 + 8: return f(RowsBf16<64, 8>());
