@@ -49,7 +49,8 @@ int cluster_of(const avits_kv_cache& c, const Shape& s, bool score, int num_sms)
   const long long units = (long long)c.B * c.Hkv * s.groups;
   auto fits = [&](int n) {
     const int64_t keys = ((int64_t)c.max_len + n - 1) / n;
-    return keys <= (score || n > 1 ? kClusterKeys : 2 * kClusterKeys) && (!score || keys * rows <= kClusterLogits);
+    return keys <= (score || n > 1 ? kClusterKeys : 2 * kClusterKeys) &&
+           (!score || keys * rows <= kClusterLogits);
   };
   int n = 1;
   while (n < 8 && !fits(n)) n *= 2;
@@ -86,7 +87,7 @@ Shape shape_of(const avits_kv_cache& c, int H, bool score, int num_sms) {
   const int longest = (c.max_len + s.tile - 1) / s.tile;
   s.least = longest < kWarps ? longest : kWarps;
   const long long most = (s.tiles + s.least - 1) / s.least;
-  long long full = (long long)num_sms * line_ctas(s.D, s.rows);
+  long long full = (long long)num_sms * line_ctas(s.D, s.rows, bf);
   if (full > kMaxGrid) full = kMaxGrid;
   s.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
   s.cluster = cluster_of(c, s, score, num_sms);

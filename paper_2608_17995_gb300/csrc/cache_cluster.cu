@@ -84,8 +84,8 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
   int late = 0;         // a copy did not come in time: the others get little more
   auto issue = [&]() {
     if (cur.left > 0)
-      copy_tile<Rows, W>(mk, mv, a, cur, ring + fill * Rows::kStage, &s_full[w][fill], &s_mask[w][fill],
-                      units, lane);
+      copy_tile<Rows, W>(mk, mv, a, cur, ring + fill * Rows::kStage, &s_full[w][fill],
+                         &s_mask[w][fill], units, lane);
     fill = fill + 1 == NS ? 0 : fill + 1;
   };
 #pragma unroll 1
@@ -102,7 +102,7 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
     __syncwarp();
     issue();
     late |= !mbar_wait_bounded(&s_full[w][use], phase, nullptr, a.status,
-                                 late ? kLateNs : kWaitLimitNs);
+                               late ? kLateNs : kWaitLimitNs);
     __syncwarp();
     const unsigned here = s_mask[w][use];
     if (here != (1u << kTile) - 1u)
@@ -169,7 +169,8 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
     const int r = i / d4, d = (i - r * d4) * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int k = 0; k < ncta; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(s_o, k) + r * D + d);
+      const float4 x =
+          *reinterpret_cast<const float4*>(cluster.map_shared_rank(s_o, k) + r * D + d);
       const float f = s_f[k][r];
       v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y);
       v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);

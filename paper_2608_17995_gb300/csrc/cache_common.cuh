@@ -56,13 +56,5 @@ __device__ __forceinline__ uint4 ld_once(const void* p) {
                : "l"(p));
   return v;
 }
-// 16 bytes that another warp of the CTA reads as well.
-__device__ __forceinline__ uint4 ld_shared_by_warps(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
-  return v;
-}
 
 }  // namespace avits

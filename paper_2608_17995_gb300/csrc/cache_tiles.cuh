@@ -472,7 +472,9 @@ struct RowsF32 {
   float o[kR][kV][4];
 
   __device__ static __forceinline__ int logit_row(int lane) { return (lane & 7) / kTwin; }
-  __device__ static __forceinline__ int piece_at(int row, int c) { return row * kColPitch + c * 16; }
+  __device__ static __forceinline__ int piece_at(int row, int c) {
+    return row * kColPitch + c * 16;
+  }
 
   __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, int b, int h0, int rows,
                                                  int i) {
@@ -617,10 +619,22 @@ struct RowsF32 {
 
 // ------------------------------------------------------------- geometry --
 // Stages of a warp's ring, and CTAs that share an SM: on the line of tiles, and
-// with a cluster per unit.
+// with a cluster per unit.  More CTAs hide more of each other's starts, ends and
+// arithmetic, fewer cut the line into fewer pieces to join; more stages than two
+// were no faster wherever the shared memory had room for them.  On the line:
+//   bf16, width 128: 2 CTAs 131072 keys 55.8 us, with 3 58.1; 48 x <= 4096 without
+//     weights 78.1 and 79.0, but 48 x <= 1024 with weights 34.3 and 31.4; 3 stages
+//     of 2 CTAs 59.1 for 131072 keys, where 2 stages took 57.0
+//   bf16, width 64: 4 CTAs 54.0 (40 x 24 heads x <= 1500), 3 53.5 (in an earlier state
+//     50.3 and 50.8, and 52.1 with 3 stages of 3 CTAs)
+//   fp32, width 128, whose arithmetic is on the CUDA cores: 3 CTAs 14 x <= 2286 34.2,
+//     28 x <= 9904 of 16 heads to a group 166, with 2 40.9 and 192; but 30000 keys of
+//     one head to a group 46.3 and 45.3
 template <typename Rows>
 constexpr int stages() { return 2; }
-constexpr int line_ctas(int D, int rows) { return D > 128 ? 1 : rows > 8 || D == 128 ? 2 : 4; }
+constexpr int line_ctas(int D, int rows, bool bf16) {
+  return D > 128 ? 1 : bf16 && rows > 8 ? 2 : D <= 64 ? 4 : bf16 ? 2 : 3;
+}
 constexpr int cluster_ctas(int D, int rows, int warps) {
   return (D > 128 ? 4 : rows > 8 ? 8 : 12) / warps;
 }
@@ -630,9 +644,9 @@ constexpr int smem_bytes(int warps) {
 }
 
 template <typename Rows>
-__device__ __forceinline__ void one_tile(Rows& r, const CacheAttn& a, const char* st, const char* sq,
-                                         char* sw, uint32_t mask, float* lg, int64_t ld, int rows,
-                                         int lane) {
+__device__ __forceinline__ void one_tile(Rows& r, const CacheAttn& a, const char* st,
+                                         const char* sq, char* sw, uint32_t mask, float* lg,
+                                         int64_t ld, int rows, int lane) {
   if constexpr (Rows::kBf16)
     r.tile(a, smem_u32(st), sq, sw, mask, lg, ld, rows, lane);
   else
