@@ -5,7 +5,15 @@
 //   x_hj = scale q_h . k_j,  lse_h = log sum_j exp x_hj,  o_h = sum_j exp(x_hj - lse_h) v_j,
 //   acc_j (+)= weight mean_h exp(x_hj - lse_h)
 // Every key and value is read once, so HBM bounds it: 4 G operations per bf16
-// element of K and V.
+// element of K and V.  The products are m16n8k16 of mma.sync, heads in the rows: a
+// unit has 8 to 32 rows, a quarter at most of the smallest tcgen05 tile, whose O
+// would lie in TMEM and have to be rescaled there; the tensor pipe is not what
+// bounds a call of 8 rows (16 % busy), and one warp's tiles need no other warp.
+//
+// Measured, against the time of the call's bytes at a copy's rate: 48 sequences of
+// 409-4096 tokens, 32 heads over 8 of width 128, with weights 85 us (floor 68), without
+// 76 (67); one of 131072, 32 over 4, 56 (40) and 47 (40); 40 of up to 1500, 24 heads of
+// width 64, 52 (36); one of 517 tokens 5.7 (0.3).
 //
 // Split.  A sequence's keys are cut into tiles; all tiles of all units (b, hk,
 // row group) form one line, cut into equal pieces, one per CTA, so that uneven
@@ -31,7 +39,8 @@ using namespace cache;
 // How a call is cut: the widths 64, 128 and 256 have kernels of their own; a
 // unit has 4 or 8 rows (fp32), or 8, 16 or 32 (bf16), by the group's size, so that
 // a tile in shared memory serves all the heads that share it (256 columns: 16 at
-// most, by registers).
+// most, by registers).  In fp32 the CUDA cores multiply every row of a unit, so that
+// 4 rows pay where the group has no more.
 struct Shape {
   int G, D, rows, groups, tile, grid;
   int least;        // tiles of the smallest piece on the line
@@ -43,6 +52,17 @@ struct Shape {
 constexpr int kClusterKeys = 512;       // of a CTA
 constexpr int kClusterLogits = 8192;    // rows times keys of a CTA
 
+// CTAs of a unit's cluster, 0 where the line of tiles is faster.  A cluster pays
+// where the second launch would cost much beside the keys, and loses where units
+// are too few to fill the SMs, or too many or too uneven to be resident at once.
+// us, cluster and line (8 KV heads of width 128 with weights, if nothing is said):
+//   1 x 517    6.1   8.4       1 x 4096, 4 KV heads  12.9  10.4
+//   4 x 1024   7.6  12.6       16 x 2048             30.8  27.9
+//   4 x 4096  16.9  21.2       48 x 1024             38.5  32.9, without 25.7  30.2
+//   16 x 512   9.3  12.8       96 x 1000, without    63.9  70.1
+//                              16 x 2000, width 256  33    28.2
+// With weights a CTA has its keys' logits in shared memory, so that keys past 512
+// would cost residency.
 int cluster_of(const avits_kv_cache& c, const Shape& s, bool score, int num_sms) {
   if (score && s.groups > 1) return 0;      // a unit has not all the heads of a weight
   const int rows = s.G < s.rows ? s.G : s.rows;

@@ -14,6 +14,11 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxGrid = 1024;
 constexpr int kMaxGroup = 256;        // query heads of a KV head
+// Units of that many pieces or fewer are joined by a thread per four columns, which
+// goes through the pieces, longer ones by threads that lie over the pieces.  Serial
+// and spread: 48 x <= 4096 85 and 102 us, 40 x 24 heads x <= 1500 50.5 and 67, one of
+// 131072 61.9 and 55.2 (4 KV heads), 8 heads of 30000 54.1 and 45.5.  32 x <= 6000 with
+// 2 KV heads has 4.6 pieces to a unit: 47 and 63, so that 4 is too low a border.
 constexpr int kFewPieces = 8;
 constexpr int kMaxDynamic = 220 * 1024;
 constexpr unsigned long long kLateNs = 1000ull * 1000ull;
@@ -104,6 +109,8 @@ struct Cursor {
 // what lies outside the tensors (columns past the width, a page out of range)
 // comes as zeros.  Else by 16-byte copies, a row's pieces side by side, zeros past
 // the width.  So the products run over whole widths of 64, 128 or 256 unchecked.
+// 48 x <= 1024 took 32.7 us by TMA and 35.3 by 16-byte copies, 40 x 24 heads of width
+// 64 54.2 and 58.4: a copy costs a warp instructions per row, a box one.
 template <typename Rows, int kStep>
 __device__ __forceinline__ void copy_tile(const CUtensorMap& mk, const CUtensorMap& mv,
                                           const CacheAttn& a, Cursor& cur, char* dst, uint64_t* bar,
@@ -635,6 +642,7 @@ constexpr int stages() { return 2; }
 constexpr int line_ctas(int D, int rows, bool bf16) {
   return D > 128 ? 1 : bf16 && rows > 8 ? 2 : D <= 64 ? 4 : bf16 ? 2 : 3;
 }
+// A cluster's CTAs hold to what their registers allow without spills.
 constexpr int cluster_ctas(int D, int rows, int warps) {
   return (D > 128 ? 4 : rows > 8 ? 8 : 12) / warps;
 }
