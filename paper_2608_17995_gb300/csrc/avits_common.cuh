@@ -90,9 +90,13 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity
 // complete (and its writes to be visible) before touching memory, then lets
 // the next kernel be scheduled; launched with launch_pdl, a kernel's launch
 // and prologue overlap the tail of the one before it.
-__device__ __forceinline__ void pdl_wait_then_trigger() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_trigger() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void pdl_wait_then_trigger() {
+  pdl_wait();
+  pdl_trigger();
 }
 
 // All kernels of the path prefer the same (all shared) L1/shared carveout:

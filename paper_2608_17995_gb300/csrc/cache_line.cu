@@ -27,7 +27,7 @@ cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant_
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mk));
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mv));
   }
-  pdl_wait_then_trigger();
+  pdl_wait();
 
   // sequences without cached tokens
   for (int b = blockIdx.x; b < a.c.B; b += gridDim.x) {
@@ -223,6 +223,10 @@ cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant_
     b = nb; u = nu; len = nlen; nt = nnt; t0 = 0;
   }
   if (tid == 0) a.own[blockIdx.x] = own;
+  // The joining kernel's blocks come onto the SMs only now: let go at the start, they
+  // cost this kernel more than they gained (14 x <= 2286 in fp32, 3 CTAs to an SM, 52
+  // us for 34; 131072 keys 58.5 for 56.4; launched without overlap 58.8).
+  pdl_trigger();
 }
 
 // ---------------------------------------------------------- second kernel --
@@ -525,11 +529,7 @@ cudaError_t launch_rows(CacheAttn& a, int num_sms, cudaStream_t s) {
   constexpr auto finish = cache_finish_kernel<typename Rows::T>;
   e = prefer_max_shared<finish>();
   if (e != cudaSuccess) return e;
-  // Not as a programmatic dependent: its blocks, let onto the SMs while the first
-  // kernel runs, cost that more than their launch takes: 131072 keys 57.5 us as a
-  // dependent, 55.7 so; 4096 keys 9.7 and 8.5; 14 x <= 2286 in fp32 42.9 and 40.9.
-  finish<<<dim3((unsigned)(f.blocks + joins)), dim3(kFinishThreads), 0, s>>>(a, f);
-  return cudaGetLastError();
+  return launch_pdl(finish, dim3((unsigned)(f.blocks + joins)), dim3(kFinishThreads), 0, s, a, f);
 }
 
 }  // namespace

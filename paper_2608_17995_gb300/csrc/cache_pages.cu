@@ -186,7 +186,7 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   for (int i = tid; i < kSelTable * kSelCopies; i += threads) (&s_first[0][0])[i] = 0u;
   // the first CTA's table is zero once this barrier is waited for
   if (ncta > 1) cluster.barrier_arrive();
-  pdl_wait_then_trigger();
+  pdl_wait();
   const int bh = blockIdx.x / ncta;
   const int b = bh / a.src.Hkv, h = bh - b * a.src.Hkv;
   if (h == 0 && me == 0 && tid == 0) check_cache_len(a.src, b, a.status);
@@ -357,6 +357,7 @@ cache_select_kernel(const __grid_constant__ Evict a) {
     base_a += tx;
     base_e += ty;
   }
+  pdl_trigger();
 }
 
 // Copy: a block takes rows of one (b, head), 32 KB of keys and values.  First
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(kCopyThreads)
 cache_copy_kernel(const __grid_constant__ Copy a) {
   __shared__ const char* s_from[2 * kCopyRows];    // [row][keys, values]
   __shared__ char* s_to[2 * kCopyRows];            // nullptr: a page out of range
-  pdl_wait_then_trigger();
+  pdl_wait();
   const int bh = blockIdx.x / a.blocks, part = blockIdx.x - bh * a.blocks;
   const int b = bh / a.src.Hkv, h = bh - b * a.src.Hkv, tid = threadIdx.x;
   const int m = min(cache_len(a.src, b), a.keep), r0 = part * a.rows;
@@ -427,6 +428,9 @@ cache_copy_kernel(const __grid_constant__ Copy a) {
 #pragma unroll
   for (int q = 0; q < kCopyDeep; ++q)
     if (to[q]) *reinterpret_cast<uint4*>(to[q]) = x[q];
+  // here and not at the start: blocks that only wait cost the ones that work (384 rows
+  // of 1000 keys 22.0 us with both kernels' triggers at the start, 20.5 so)
+  pdl_trigger();
 }
 
 }  // namespace
