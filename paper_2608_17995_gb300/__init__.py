@@ -560,6 +560,8 @@ class KVCache:
     acc               [B, Hkv, >= max_len] fp32, optional: accumulated weights
     max_len           an upper bound of lens known here (default: all that the
                       table can hold); a smaller one costs less workspace
+
+    The description is fixed: other tensors are another KVCache.
     """
     __slots__ = ("k_pages", "v_pages", "block_table", "lens", "acc", "B", "Hkv", "d", "dtype",
                  "page_size", "max_len", "device", "int32", "float32", "_index", "_struct", "_ref",
@@ -610,6 +612,11 @@ class KVCache:
         L = lib()
         self._append, self._attend = L.avits_cache_append, L.avits_cache_attention
         self._evict = L.avits_cache_evict
+
+    def __setattr__(self, name, value):
+        if hasattr(self, "_evict"):       # set last
+            raise AttributeError("a KVCache's description is fixed: make another one")
+        object.__setattr__(self, name, value)
 
 
 _cache_ws = {}
@@ -721,6 +728,8 @@ def avits_cache_attention(cache: KVCache, q, softmax_scale: float, o, lse=None,
     handle = _call_stream(cache, stream)
     ws_at, ws_bytes = None, 0
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
         _elsewhere(cache, workspace)
         ws_at, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     else:

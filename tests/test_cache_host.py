@@ -214,3 +214,29 @@ def test_binding_refuses_types_and_host_tensors():
         av.KVCache(**tensors(dt=torch.float16))
     with pytest.raises(ValueError, match="device tensor"):
         av.KVCache(**a)
+
+
+class _DeviceTensor:
+    """A stand-in for a device tensor where there is no device."""
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    is_cuda = True
+
+    def get_device(self):
+        return 0
+
+
+def test_binding_description_is_fixed():
+    c = av.KVCache(**{k: _DeviceTensor(t) for k, t in tensors().items()})
+    with pytest.raises(AttributeError):
+        c.lens = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(AttributeError):
+        c.max_len = 4
+    with pytest.raises(AttributeError):
+        c.another = 1
+    assert c.max_len == 12

@@ -583,8 +583,9 @@ def test_evict_ties_over_the_whole_row(av, n):
     check_evict(w, dst, idx, n // 3, 0, 0)
 
 
-def test_evict_row_beyond_shared_memory(av):
-    """So long a row that a CTA's part does not fit shared memory."""
+def test_evict_row_read_again(av):
+    """So long a row that a thread's keys do not fit its registers: every digit reads
+    the row again."""
     w = World(av, "bf16", [400001], 1, 1, 8, 256, seed=1)
     dst, idx = run_evict(av, w, 1000, 5, 5)
     assert av.avits_device_status() == 0
@@ -746,6 +747,9 @@ def test_binding_refusals_on_the_device(av):
     assert av.avits_cache_attention_workspace(long.cache, 4, True) > 16
     with pytest.raises(av.AvitsError):
         att(long.cache, long.q, w.scale, o, workspace=t.empty(16, dtype=t.uint8, device=DEV))
+    with pytest.raises(ValueError):                                 # one byte, many times
+        att(long.cache, long.q, w.scale, o,
+            workspace=t.empty(1, dtype=t.uint8, device=DEV).expand(1 << 24))
     plain = av.KVCache(w.k_pages, w.v_pages, w.table, w.lens)
     with pytest.raises(ValueError):
         att(plain, w.q, w.scale, o, weight=1.0)
