@@ -160,7 +160,10 @@ SHAPES = [  # dtype, lens, H, Hkv, d, page, layout
     ("bf16", [40, 70], 200, 2, 136, 7, "joint"),                # G 100
     ("bf16", [33] * 70, 4, 4, 64, 32, "tokens"),                # one head each, G 1
     ("bf16", [5000, 12, 1900], 16, 4, 128, 64, "heads"),
+    ("bf16", [50, 0, 300], 256, 1, 64, 16, "tokens"),           # the largest group
+    ("bf16", [5, 999, 1001], 8, 2, 128, 1000, "heads"),         # long pages
     ("f32", [1], 2, 2, 4, 16, "tokens"),
+    ("f32", [50, 131], 256, 1, 128, 8, "joint"),
     ("f32", [0, 1, 15, 16, 17, 33], 6, 2, 64, 16, "heads"),
     ("f32", [300, 129], 14, 2, 128, 24, "joint"),
     ("f32", [100, 250], 16, 1, 100, 5, "tokens"),
