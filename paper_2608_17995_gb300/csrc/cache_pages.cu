@@ -192,25 +192,22 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   if (h == 0 && me == 0 && tid == 0) check_cache_len(a.src, b, a.status);
   const int n = cache_len(a.src, b), m = min(n, a.keep);
   const float* acc = a.src.acc + (int64_t)b * a.src.acc_sb + (int64_t)h * a.src.acc_sh;
-  float* acc2 = a.dst.acc + (int64_t)b * a.dst.acc_sb + (int64_t)h * a.dst.acc_sh;
   int32_t* idx = a.idx + (int64_t)bh * a.keep;
   if (h == 0 && me == 0 && tid == 0) a.dst.lens[b] = m;
   // all of them, and the places past the kept ones: the same for every CTA
   if (n <= a.keep) {
-    for (int i = me * threads + tid; i < a.keep; i += ncta * threads) {
-      idx[i] = i < n ? i : -1;
-      if (i < n) acc2[i] = acc[i];
-    }
+    for (int i = me * threads + tid; i < a.keep; i += ncta * threads) idx[i] = i < n ? i : -1;
     if (ncta > 1) cluster.barrier_wait();
     return;   // the whole cluster takes this way
   }
   const int lo = min(n, me * a.part), hi = min(n, lo + a.part);
   const int last = n - a.recent, stripe = threads * kRun;
   const bool vec = (reinterpret_cast<uintptr_t>(acc) & 15u) == 0;   // lo is a multiple of 4
-  float x[kRun];
   uint32_t k[kRun];
   int here;                // keys of the run that are in the part: the first ones
-  auto load = [&](int j0) {
+  // this thread's run of a stripe; a part of one stripe is read once, here
+  auto load_keys = [&](int j0) {
+    float x[kRun];
     here = min(max(hi - j0, 0), kRun);
     if (vec && here == kRun) {
 #pragma unroll
@@ -222,11 +219,6 @@ cache_select_kernel(const __grid_constant__ Evict a) {
 #pragma unroll
       for (int i = 0; i < kRun; ++i) x[i] = i < here ? acc[j0 + i] : 0.f;
     }
-  };
-  // this thread's run of a stripe; a part of one stripe is read once here, and
-  // for its kept weights at the end
-  auto load_keys = [&](int j0) {
-    load(j0);
 #pragma unroll
     for (int i = 0; i < kRun; ++i)       // the first and the last ones stand above all
       k[i] = j0 + i < a.sinks || j0 + i >= last ? 0xFFFFFFFFu : order_of(x[i]);
@@ -340,16 +332,11 @@ cache_select_kernel(const __grid_constant__ Evict a) {
       block_scan(above, equal, s_warp[par], lane, w, warps, bx, by, tx, ty);
     }
     uint32_t ra = base_a + bx, re = base_e + by;
-    if (!again) load(j0);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
       const uint32_t kk = k[i] & mask;
       if (i < here) {
-        if (kk > prefix || (kk == prefix && re < need)) {
-          const uint32_t rank = ra + min(re, need);
-          idx[rank] = j0 + i;
-          acc2[rank] = x[i];
-        }
+        if (kk > prefix || (kk == prefix && re < need)) idx[ra + min(re, need)] = j0 + i;
         ra += kk > prefix;
         re += kk == prefix;
       }
@@ -361,7 +348,7 @@ cache_select_kernel(const __grid_constant__ Evict a) {
 }
 
 // Copy: a block takes rows of one (b, head), 32 KB of keys and values.  First
-// where each row lies on both sides, then the 16-byte pieces flat over the
+// where each row lies on both sides, and its weight, then the 16-byte pieces flat over the
 // threads, neighbouring lanes on neighbouring pieces, 8 to a thread at once, so that
 // a block's bytes are all on their way before the first is stored.  HBM bounds it: 24 x
 // 8 heads x 1024 rows of 512 bytes 30 us (27.4 at a copy's rate), 8 x 16384 22.6 (19.8).
@@ -389,11 +376,14 @@ cache_copy_kernel(const __grid_constant__ Copy a) {
   const int rows = min(a.rows, m - r0);
   if (rows <= 0) return;
   const int32_t* idx = a.idx + (int64_t)bh * a.keep;
+  const float* acc = a.src.acc + (int64_t)b * a.src.acc_sb + (int64_t)h * a.src.acc_sh;
+  float* acc2 = a.dst.acc + (int64_t)b * a.dst.acc_sb + (int64_t)h * a.dst.acc_sh;
   const int32_t* ts = a.src.block_table + (int64_t)b * a.src.table_sb;
   const int32_t* td = a.dst.block_table + (int64_t)b * a.dst.table_sb;
   for (int i = tid; i < rows; i += kCopyThreads) {
     const int r = r0 + i, cd = a.dpage.div(r), pd = td[cd];
     const int j = idx[r], cs = a.spage.div(j), ps = ts[cs];
+    acc2[r] = acc[j];
     const int ss = j - cs * a.src.page_size, sd = r - cd * a.dst.page_size;
     const bool ok = (unsigned)ps < (unsigned)a.src.num_pages &&
                     (unsigned)pd < (unsigned)a.dst.num_pages;
