@@ -474,7 +474,7 @@ avits_status avits_cache_evict(const avits_kv_cache* src, const avits_kv_cache* 
   if (src->dt != dst->dt || src->B != dst->B || src->Hkv != dst->Hkv || src->d != dst->d ||
       keep > dst->max_len || src->lens == dst->lens || src->acc == dst->acc)
     return AVITS_ERR_INVALID_ARG;
-  if ((int64_t)src->B * src->Hkv * ((int64_t)keep / 8 + 1) >= (1ll << 31))
+  if ((int64_t)src->B * src->Hkv * ((int64_t)keep / 4 + 1) >= (1ll << 31))
     return AVITS_ERR_UNSUPPORTED;
   return cuda_status(launch_cache_evict(*src, *dst, keep, sinks, recent, keep_idx, num_sms_current(),
                                         status_word(), static_cast<cudaStream_t>(stream)));

@@ -15,9 +15,9 @@ namespace {
 // One warp per new token: its first pieces are on their way while the sequence is
 // found by a search of cu_new 32 ways at a time, and the place from the length;
 // then the token's Hkv rows of keys and of values go there.  A step's 64 tokens take
-// 2.7 us, a launch and three dependent reads; prompts are bound by HBM, 43 us where
-// their bytes take 36 at a copy's rate.
-constexpr int kAppendThreads = 256;
+// 2.3 us, a launch and three dependent reads (2.7 with 8 warps to a CTA); prompts are
+// bound by HBM, 43 us where their bytes take 36 at a copy's rate.
+constexpr int kAppendThreads = 128;
 
 struct Append {
   avits_kv_cache c;
@@ -116,10 +116,8 @@ cache_append_kernel(const __grid_constant__ Append a) {
 //
 // The cost is latency: a barrier over a cluster takes 1-2 thousand cycles, one of
 // a CTA a tenth of it, and counting goes with a CTA's keys.  8 rows of 1024 keys
-// take 4 us, of 4096 5, of 131072 24; 192 of up to 4096 keys 12.
+// take 4 us, of 4096 5, of 131072 20; 192 of up to 4096 keys 12.
 constexpr int kSelMaxThreads = 1024;
-constexpr int kSelCopies = 8;       // tables of the first, crowded digit, in banks of
-constexpr int kSelTable = 256 + 4;  // their own
 constexpr int kSelMaxCluster = 8;
 
 struct Evict {
@@ -174,7 +172,6 @@ __global__ void __launch_bounds__(kSelMaxThreads)
 cache_select_kernel(const __grid_constant__ Evict a) {
   __shared__ __align__(16) uint32_t s_total[4][256];   // of the cluster, in its first CTA
   __shared__ __align__(16) uint32_t s_hist[2][256];    // of this CTA
-  __shared__ uint32_t s_first[kSelCopies][kSelTable];
   __shared__ uint32_t s_pick[3];      // digit, how many of it are needed, whether all are
   __shared__ uint2 s_count[kSelMaxCluster];   // the CTAs' keys above, and equal to, the threshold
   __shared__ uint2 s_warp[2][32];
@@ -183,7 +180,6 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, threads = blockDim.x;
   for (int i = tid; i < 1024; i += threads) (&s_total[0][0])[i] = 0u;
   for (int i = tid; i < 512; i += threads) (&s_hist[0][0])[i] = 0u;
-  for (int i = tid; i < kSelTable * kSelCopies; i += threads) (&s_first[0][0])[i] = 0u;
   // the first CTA's table is zero once this barrier is waited for
   if (ncta > 1) cluster.barrier_arrive();
   pdl_wait();
@@ -233,29 +229,21 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   for (int pass = 0; pass < 4; ++pass) {
     const int shift = 24 - 8 * pass;
     uint32_t* hist = s_hist[pass & 1];
-    // a first digit is one of few: lanes count in tables of their own
-    uint32_t* count = pass == 0 ? s_first[lane % kSelCopies] : hist;
+    // (the first digit is one of few; a table per group of lanes was no faster, nor
+    // where all weights are equal)
     for (int j0 = j1; j0 < hi; j0 += stripe) {
       if (again) load_keys(j0);
 #pragma unroll
       for (int i = 0; i < kRun; ++i)
-        if (i < here && (k[i] & mask) == prefix) atomicAdd(&count[(k[i] >> shift) & 255u], 1u);
+        if (i < here && (k[i] & mask) == prefix) atomicAdd(&hist[(k[i] >> shift) & 255u], 1u);
     }
     __syncthreads();
-    if (pass == 0 || ncta > 1) {
-      if (pass == 0 && ncta > 1) cluster.barrier_wait();
-      uint32_t* to = ncta > 1 ? cluster.map_shared_rank(s_total[pass], 0) : hist;
-      for (int i = tid; i < 256; i += threads) {
-        uint32_t sum = hist[i];
-        if (pass == 0)
-#pragma unroll
-          for (int r = 0; r < kSelCopies; ++r) sum += s_first[r][i];
-        if (ncta == 1)
-          to[i] = sum;
-        else if (sum)
-          atomicAdd(&to[i], sum);
-      }
-      if (ncta > 1) cluster.sync(); else __syncthreads();
+    if (ncta > 1) {
+      if (pass == 0) cluster.barrier_wait();
+      uint32_t* to = cluster.map_shared_rank(s_total[pass], 0);
+      for (int i = tid; i < 256; i += threads)
+        if (hist[i]) atomicAdd(&to[i], hist[i]);
+      cluster.sync();
     }
     if (w == 0) {
       // lane l adds up digits 255 - 8 l down to 248 - 8 l; then lanes 0-7 take one
@@ -347,15 +335,18 @@ cache_select_kernel(const __grid_constant__ Evict a) {
   pdl_trigger();
 }
 
-// Copy: a block takes rows of one (b, head), 32 KB of keys and values.  First
-// where each row lies on both sides, and its weight, then the 16-byte pieces flat over the
-// threads, neighbouring lanes on neighbouring pieces, 8 to a thread at once, so that
-// a block's bytes are all on their way before the first is stored.  HBM bounds it: 24 x
-// 8 heads x 1024 rows of 512 bytes 30 us (27.4 at a copy's rate), 8 x 16384 22.6 (19.8).
-constexpr int kCopyThreads = 256;
-constexpr int kCopyDeep = 8;
+// Copy: a block takes rows of one (b, head), 8 KB of keys and values.  First
+// where each row lies on both sides, and its weight, then the 16-byte pieces flat
+// over the threads, neighbouring lanes on neighbouring pieces, 4 to a thread at
+// once, so that a block's bytes are all on their way before the first is stored.
+// HBM bounds it: 24 x 8 heads x 1024 rows of 512 bytes 30 us (27.4 at a copy's rate),
+// 8 x 16384 22 (19.8).  Larger blocks leave calls of few rows on few SMs: 16 KB (256
+// threads) 24 x <= 4096 41.7 us a call, 8 x 512 rows 7.2; 32 KB 42.1 and 7.8; 8 KB
+// 41.2 and 7.2; 8 KB as 2 pieces to each of 256 threads 43.4 and 7.2.
+constexpr int kCopyThreads = 128;
+constexpr int kCopyDeep = 4;
 constexpr int kCopyPieces = kCopyThreads * kCopyDeep;
-constexpr int kCopyRows = 256;       // of a block, at most
+constexpr int kCopyRows = kCopyPieces / 2;       // of a block, at most: rows of one piece
 
 struct Copy {
   avits_kv_cache src, dst;
@@ -501,7 +492,6 @@ cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& 
   c.idx = idx;
   c.status = status;
   c.rows = kCopyPieces / (2 * (src.d * c.es / 16));
-  if (c.rows > kCopyRows) c.rows = kCopyRows;
   c.blocks = (keep + c.rows - 1) / c.rows;
   e = prefer_max_shared<cache_copy_kernel>();
   if (e != cudaSuccess) return e;
