@@ -409,8 +409,8 @@ cache_copy_kernel(const __grid_constant__ Copy a) {
 #pragma unroll
   for (int q = 0; q < kCopyDeep; ++q)
     if (to[q]) *reinterpret_cast<uint4*>(to[q]) = x[q];
-  // here and not at the start: blocks that only wait cost the ones that work (384 rows
-  // of 1000 keys 22.0 us with both kernels' triggers at the start, 20.5 so)
+  // here and not at the start: blocks that only wait cost the ones that work (24 x <=
+  // 4096 tokens 41.2 us with both kernels' triggers at the start, 40.8 so)
   pdl_trigger();
 }
 
@@ -449,10 +449,10 @@ cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& 
   a.idx = idx;
   a.status = status;
   // CTAs of a row: while there are SMs for them, as many as leave 4096 keys to each
-  // (whole calls, 8 rows of 4096 keys: 10.6 us, with 2048 each 11.6; of 16384: 16.3, with
-  // 8192 each 18.8, on one CTA 23.5).  Past 16 keys to a thread, which are read again
+  // (whole calls, 8 rows of 4096 keys: 9.5 us, with 2048 each 10.9; of 16384: 15.2, with
+  // 8192 each 17.0, on one CTA 18.1).  Past 16 keys to a thread, which are read again
   // at each digit, a row is cut whatever the SMs.  Threads have runs of 8 keys (8 x 1024:
-  // 7.6 us, of 16 10.7) while 1024 of them reach (8 x 131072: 47.0 with 16, 51.9 with 8).
+  // 7.0 us, of 16 8.3) while 1024 of them reach (8 x 131072: 42.8 with 16, 52.3 with 8).
   const long long bh = (long long)src.B * src.Hkv;
   int ncta = 1;
   while (ncta < kSelMaxCluster && (int64_t)ncta * 4096 < src.max_len &&
