@@ -8,7 +8,7 @@
 // element of K and V.  The products are m16n8k16 of mma.sync, heads in the rows: a
 // unit has 8 to 32 rows, a quarter at most of the smallest tcgen05 tile, whose O
 // would lie in TMEM and have to be rescaled there; the tensor pipe is not what
-// bounds a call of 8 rows (16 % busy), and one warp's tiles need no other warp.
+// bounds a call of 8 rows (15 % busy), and one warp's tiles need no other warp.
 //
 // Measured, against the time of the call's bytes at a copy's rate: 48 sequences of
 // 409-4096 tokens, 32 heads over 8 of width 128, with weights 85 us (floor 68), without
