@@ -484,8 +484,8 @@ avits_status avits_device_status(void* stream);
  *         last axis contiguous): the accumulated attention weight of each
  *         cached token under each KV head.
  *
- * A length outside [0, max_len] is cut to it and a page number outside
- * [0, num_pages) makes its tokens count as masked (read) or be left out
+ * A length outside [0, max_len] is cut to it where tokens are read; a page number
+ * outside [0, num_pages) makes its tokens count as masked (read) or be left out
  * (written); both raise AVITS_ERR_PAGE in the status word.
  * ---------------------------------------------------------------------- */
 typedef struct {
@@ -506,9 +506,10 @@ typedef struct {
  * tokens are k_new / v_new rows cu_new[b] .. cu_new[b+1]-1 ([T, Hkv, d] of the
  * cache's type, element strides *_st, *_sh, 16-byte aligned) and go to places
  * lens[b] - n_b .. lens[b]-1.  cu_new [B+1] int32 does not decrease from 0; rows
- * past cu_new[B] are ignored, and where a sequence is given more tokens than
- * lens[b] the first ones are left out (AVITS_ERR_PAGE).  With acc the entries
- * of the new tokens are set to zero.  T = 0 launches nothing. */
+ * past cu_new[B] are ignored.  Tokens whose place would lie below 0 (a sequence
+ * is given more than lens[b]) or past max_len - 1 are left out (AVITS_ERR_PAGE):
+ * nothing that was cached is overwritten.  With acc the entries of the new
+ * tokens are set to zero.  T = 0 launches nothing. */
 avits_status avits_cache_append(const avits_kv_cache* cache, const void* k_new, const void* v_new,
                                 int T, const int32_t* cu_new, int64_t k_st, int64_t k_sh,
                                 int64_t v_st, int64_t v_sh, void* stream);

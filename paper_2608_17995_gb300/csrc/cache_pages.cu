@@ -73,10 +73,12 @@ cache_append_kernel(const __grid_constant__ Append a) {
   load(lane);
   const int b = sequence_of(a.cu, a.c.B, t, lane);
   if (b >= a.c.B) return;
-  if (a.c.lens[b] > a.c.max_len && lane == 0) raise_status(a.status, AVITS_ERR_PAGE);
-  const int len = cache_len(a.c, b);
+  // by the length as it is: cut to max_len, it would put tokens past the capacity over
+  // cached ones
+  const int len = a.c.lens[b];
+  if (len > a.c.max_len && lane == 0) raise_status(a.status, AVITS_ERR_PAGE);
   const int64_t place = (int64_t)len - ((int64_t)a.cu[b + 1] - t);
-  if (place < 0 || place >= len) {
+  if (place < 0 || place >= min(len, a.c.max_len)) {
     if (lane == 0) raise_status(a.status, AVITS_ERR_PAGE);
     return;
   }
