@@ -23,9 +23,9 @@
 // memory, filled by TMA copies that run ahead over unit borders; the warps meet
 // once per unit.  A unit that lies in one piece is finished there; of the others
 // each piece leaves its maximum, sum and O, and a second kernel joins them, in the
-// pieces' order.  The weights need the whole row's lse: the first kernel leaves the
-// logits (fp32), the second sums exp(x - lse) over the group's heads, in a fixed
-// order.
+// pieces' order.  The weights need the whole row's maximum and sum: the first kernel
+// leaves the logits (fp32), the second sums exp(x - maximum) / sum over the group's
+// heads, in a fixed order.
 //
 // Shorter sequences take one launch: a cluster of CTAs per unit, whose logits
 // stay in shared memory.
@@ -118,7 +118,7 @@ Shape shape_of(const avits_kv_cache& c, int H, bool score, int num_sms) {
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
 struct Layout {
-  size_t rec, own, lse2, pml, po, logits, total;
+  size_t rec, own, norm, pml, po, logits, total;
   int64_t ld;
 };
 
@@ -128,8 +128,8 @@ Layout layout_of(const avits_kv_cache& c, int H, const Shape& s, bool score) {
   l.ld = ((int64_t)c.max_len + 15) / 16 * 16;
   l.rec = 0;
   l.own = up16((size_t)c.B * c.Hkv * s.groups * 8);
-  l.lse2 = l.own + up16((size_t)s.grid * 16);
-  l.pml = l.lse2 + up16((size_t)c.B * H * 4);
+  l.norm = l.own + up16((size_t)s.grid * 16);
+  l.pml = l.norm + up16((size_t)c.B * H * 8);
   l.po = l.pml + up16((size_t)2 * s.grid * nrow * 8);
   l.logits = l.po + up16((size_t)2 * s.grid * nrow * c.d * 4);
   l.total = l.logits + (score ? (size_t)c.B * H * l.ld * 4 : 0);
@@ -177,7 +177,7 @@ cudaError_t launch_cache_attention(const CacheAttnCall& call, int num_sms, unsig
   a.add = call.weights == AVITS_WEIGHTS_ADD;
   a.rec = reinterpret_cast<int2*>(ws + l.rec);
   a.own = reinterpret_cast<int4*>(ws + l.own);
-  a.lse2 = reinterpret_cast<float*>(ws + l.lse2);
+  a.norm = reinterpret_cast<float2*>(ws + l.norm);
   a.pml = reinterpret_cast<float2*>(ws + l.pml);
   a.po = reinterpret_cast<float*>(ws + l.po);
   a.logits = reinterpret_cast<float*>(ws + l.logits);

@@ -32,7 +32,8 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
   extern __shared__ __align__(1024) char smem[];
   __shared__ float2 s_ml[W][Rows::kBufRows];
   __shared__ float2 s_mine[kR];                  // this CTA's maximum and sum of a row
-  __shared__ float s_f[kMaxCluster][kR], s_e[kR];
+  __shared__ float s_f[kMaxCluster][kR];
+  __shared__ float2 s_norm[kR];
   __shared__ int s_free[W];
   __shared__ uint64_t s_full[W][NS];
   __shared__ uint32_t s_mask[W][NS];
@@ -146,7 +147,7 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
     __syncthreads();
   }
   cluster.sync();
-  // over the CTAs: a row's lse, and what each CTA's O counts in it
+  // over the CTAs: a row's maximum and sum, and what each CTA's O counts in it
   if (tid < rows_here) {
     float2 x[kMaxCluster];
     float top = -INFINITY, l = 0.f;
@@ -159,12 +160,11 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
     const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int k = 0; k < kMaxCluster; ++k) l = fmaf(ex2(x[k].x - ref), x[k].y, l);
-    const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+    const float2 norm = norm_of(top, l);
 #pragma unroll
-    for (int k = 0; k < kMaxCluster; ++k) s_f[k][tid] = ex2(x[k].x - ref) * inv;
-    const float e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
-    s_e[tid] = e == -INFINITY ? INFINITY : e;     // nothing to attend to: no weight
-    if (me == 0 && a.lse) a.lse[(int64_t)b * a.H + h0 + tid] = e * kLn2;
+    for (int k = 0; k < kMaxCluster; ++k) s_f[k][tid] = ex2(x[k].x - ref) * norm.y;
+    s_norm[tid] = norm;
+    if (me == 0 && a.lse) a.lse[(int64_t)b * a.H + h0 + tid] = lse2_of(top, l) * kLn2;
   }
   __syncthreads();
   const int d4 = a.c.d / 4;
@@ -191,7 +191,10 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
       const float old = a.add ? acc[j] : 0.f;
       float s = 0.f;
 #pragma unroll 8
-      for (int r = 0; r < rows_here; ++r) s += ex2(s_lg[r * stride + j] - s_e[r]);
+      for (int r = 0; r < rows_here; ++r) {
+        const float2 norm = s_norm[r];
+        s = fmaf(ex2(s_lg[r * stride + j] - norm.x), norm.y, s);
+      }
       acc[j] = fmaf(s, a.wmean, old);
     }
   }

@@ -195,16 +195,16 @@ cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant_
         }
         const int hh = h.x + row;
         if (whole) {
-          const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+          const float2 norm = norm_of(top, l);
+          const float inv = norm.y;
           T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)hh * a.o_sh + d;
           store_elem(out, 0, v.x * inv);
           store_elem(out, 1, v.y * inv);
           store_elem(out, 2, v.z * inv);
           store_elem(out, 3, v.w * inv);
           if (d == 0) {
-            const float e = l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
-            if (a.score) a.lse2[(int64_t)b * a.H + hh] = e;
-            if (a.lse) a.lse[(int64_t)b * a.H + hh] = e * kLn2;
+            if (a.score) a.norm[(int64_t)b * a.H + hh] = norm;
+            if (a.lse) a.lse[(int64_t)b * a.H + hh] = lse2_of(top, l) * kLn2;
           }
         } else {
           *reinterpret_cast<float4*>(a.po + ((int64_t)slot * kR + row) * a.c.d + d) = v;
@@ -236,8 +236,8 @@ cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant_
 // Block (unit, row), or, where there are many units, (CTA of the first kernel,
 // rows): O of that unit, or of the one whose first of several pieces was that
 // CTA's.  Block (b, hk, 512 keys or more): their weights.  What a block reads waits
-// for as little as can be: parts and logits are on their way while the row's lse
-// is put together.
+// for as little as can be: parts and logits are on their way while the row's maximum and
+// sum are put together.
 constexpr int kFinishThreads = 128;
 constexpr int kWeightKeys = 4 * kFinishThreads;
 
@@ -247,9 +247,9 @@ __device__ __forceinline__ int part_of(int slot, int k) {
   return k == 0 ? slot : ((slot >> 1) + k) * 2;
 }
 
-// log2-domain lse of row r over a unit's pieces, in a whole warp.
-__device__ __forceinline__ float join_lse(const CacheAttn& a, int slot, int pieces, int r,
-                                          int lane) {
+// Maximum and sum of row r over a unit's pieces, in a whole warp.
+__device__ __forceinline__ float2 join_rows(const CacheAttn& a, int slot, int pieces, int r,
+                                            int lane) {
   constexpr int kDeep = 4;
   float top = -INFINITY, l = 0.f;
   for (int k0 = lane; k0 < pieces; k0 += 32 * kDeep) {
@@ -276,11 +276,12 @@ __device__ __forceinline__ float join_lse(const CacheAttn& a, int slot, int piec
     l = l * ex2(top - ref) + lx * ex2(tx - ref);
     top = mn;
   }
-  return l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
+  return make_float2(top, l);
 }
 
 // The same in one thread, for few pieces.
-__device__ __forceinline__ float join_lse_serial(const CacheAttn& a, int slot, int pieces, int r) {
+__device__ __forceinline__ float2 join_rows_serial(const CacheAttn& a, int slot, int pieces,
+                                                   int r) {
   float top = -INFINITY, l = 0.f;
   for (int k0 = 0; k0 < pieces; k0 += kFewPieces) {
     float2 x[kFewPieces];
@@ -297,7 +298,7 @@ __device__ __forceinline__ float join_lse_serial(const CacheAttn& a, int slot, i
     for (int i = 0; i < kFewPieces; ++i) l = fmaf(ex2(x[i].x - ref), x[i].y, l);
     top = mn;
   }
-  return l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
+  return make_float2(top, l);
 }
 
 // kWide: `at0` is a unit and r0 one of its rows, threads lie over 32 of its columns
@@ -341,22 +342,22 @@ __device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, 
     }
   };
   load(k1);
-  const float e = kWide ? (row < a.G ? join_lse(a, own.y, own.z, r, tid & 31) : 0.f)
-                        : join_lse_serial(a, own.y, pieces, r);
-  if (mine && k1 == 0 && col == 0 && a.lse) a.lse[(int64_t)b * a.H + h] = e * kLn2;
-  const float none = e != e ? e : 0.f;
-  float4 v = make_float4(none, none, none, none);
-  if (e != -INFINITY) {
-    for (int k0 = k1; k0 < pieces; k0 += kDeep * step) {
-      if (k0 != k1) load(k0);
+  const float2 ml = kWide ? (row < a.G ? join_rows(a, own.y, own.z, r, tid & 31)
+                                       : make_float2(-INFINITY, 0.f))
+                          : join_rows_serial(a, own.y, pieces, r);
+  if (mine && k1 == 0 && col == 0 && a.lse)
+    a.lse[(int64_t)b * a.H + h] = lse2_of(ml.x, ml.y) * kLn2;
+  const float2 norm = norm_of(ml.x, ml.y);
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = k1; k0 < pieces; k0 += kDeep * step) {
+    if (k0 != k1) load(k0);
 #pragma unroll
-      for (int i = 0; i < kDeep; ++i)
-        if (k0 + i * step < pieces) {
-          const float f = ex2(mx[i] - e);     // from -inf: 0
-          v.x = fmaf(f, x[i].x, v.x); v.y = fmaf(f, x[i].y, v.y);
-          v.z = fmaf(f, x[i].z, v.z); v.w = fmaf(f, x[i].w, v.w);
-        }
-    }
+    for (int i = 0; i < kDeep; ++i)
+      if (k0 + i * step < pieces) {
+        const float f = ex2(mx[i] - norm.x);     // from -inf: 0
+        v.x = fmaf(f, x[i].x, v.x); v.y = fmaf(f, x[i].y, v.y);
+        v.z = fmaf(f, x[i].z, v.z); v.w = fmaf(f, x[i].w, v.w);
+      }
   }
   if (kWide) {
     s_sum[tid] = v;
@@ -369,10 +370,10 @@ __device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, 
   }
   if (!mine) return;
   T* out = static_cast<T*>(a.o) + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh + col * 4;
-  store_elem(out, 0, v.x);
-  store_elem(out, 1, v.y);
-  store_elem(out, 2, v.z);
-  store_elem(out, 3, v.w);
+  store_elem(out, 0, v.x * norm.y);
+  store_elem(out, 1, v.y * norm.y);
+  store_elem(out, 2, v.z * norm.y);
+  store_elem(out, 3, v.w * norm.y);
 }
 
 // `parts` parts of kSpan runs of 512 keys, kRows rows at a time.  First the length
@@ -380,7 +381,7 @@ __device__ __forceinline__ void join_block(const CacheAttn& a, int at0, int r0, 
 // logits, old weights, pieces.
 template <int kSpan, int kRows>
 __device__ __forceinline__ void weights_block(const CacheAttn& a, int bh, int part, int parts) {
-  __shared__ float s_e[kMaxGroup];
+  __shared__ float2 s_norm[kMaxGroup];
   const int b = bh / a.c.Hkv, hk = bh - b * a.c.Hkv, tid = threadIdx.x, w = tid >> 5;
   int jb = part * (kSpan * kWeightKeys);
   const int2* recs = a.rec + bh * a.groups;
@@ -427,10 +428,15 @@ __device__ __forceinline__ void weights_block(const CacheAttn& a, int bh, int pa
     const int rg = a.groups == 1 ? 0 : r / a.rows;
     if (rg > 0) rec = recs[rg];
     const int row = r - rg * a.rows;
-    const float e = rec.y == 1 ? a.lse2[(int64_t)b * a.H + hk * a.G + r]
-                    : a.few    ? join_lse_serial(a, rec.x, rec.y, row)
-                               : join_lse(a, rec.x, rec.y, row, tid & 31);
-    if (a.few || (tid & 31) == 0) s_e[r] = e == -INFINITY ? INFINITY : e;   // no weight there
+    float2 norm;
+    if (rec.y == 1) {
+      norm = a.norm[(int64_t)b * a.H + hk * a.G + r];
+    } else {
+      const float2 ml = a.few ? join_rows_serial(a, rec.x, rec.y, row)
+                              : join_rows(a, rec.x, rec.y, row, tid & 31);
+      norm = norm_of(ml.x, ml.y);
+    }
+    if (a.few || (tid & 31) == 0) s_norm[r] = norm;
   }
   __syncthreads();
   const int end = min(len, jb + parts * (kSpan * kWeightKeys));
@@ -442,13 +448,13 @@ __device__ __forceinline__ void weights_block(const CacheAttn& a, int bh, int pa
 #pragma unroll
       for (int r = 0; r < kRows; ++r) {
         if (r0 + r < a.G) {
-          const float e = s_e[r0 + r];
+          const float2 norm = s_norm[r0 + r];
 #pragma unroll
           for (int g = 0; g < kSpan; ++g) {
-            s[g][0] += ex2(x[g][r].x - e);
-            s[g][1] += ex2(x[g][r].y - e);
-            s[g][2] += ex2(x[g][r].z - e);
-            s[g][3] += ex2(x[g][r].w - e);
+            s[g][0] = fmaf(ex2(x[g][r].x - norm.x), norm.y, s[g][0]);
+            s[g][1] = fmaf(ex2(x[g][r].y - norm.x), norm.y, s[g][1]);
+            s[g][2] = fmaf(ex2(x[g][r].z - norm.x), norm.y, s[g][2]);
+            s[g][3] = fmaf(ex2(x[g][r].w - norm.x), norm.y, s[g][3]);
           }
         }
       }

@@ -45,16 +45,28 @@ struct CacheAttn {
   float wmean;      // weight / G
   int add;
   // workspace
-  int2* rec;        // [B units] first part of a unit and its pieces; one: it is in lse2
+  int2* rec;        // [B units] first part of a unit and its pieces; one: it is in norm
   int4* own;        // [grid] unit whose first piece is the CTA's, of several: (unit or -1,
                     // first part, pieces); read where units have few pieces
-  float* lse2;      // [B,H] log2-domain lse of rows finished in one piece
+  float2* norm;     // [B,H] of rows finished in one piece (see norm_of)
   float2* pml;      // [2 grid][rows] maximum and sum of a piece's row
   float* po;        // [2 grid][rows][d] its O
   float* logits;    // [B,H,ld] log2-domain logits (weights wanted)
   int64_t ld;
   unsigned int* status;
 };
+
+// A row's maximum and sum -> what a weight is: exp2(x - .x) times .y.  Not exp2(x - lse):
+// a step of lse is up to 2^-24 |lse|, an error that all weights of a row would share,
+// while a maximum is one of the logits and the differences from it are as exact as they
+// are.  A row without keys has weights of zero, a row with a NaN NaN.
+__device__ __forceinline__ float2 norm_of(float top, float l) {
+  return make_float2(top == -INFINITY ? 0.f : top, l > 0.f ? 1.f / l : (l != l ? l : 0.f));
+}
+// Its lse in the log2 domain.
+__device__ __forceinline__ float lse2_of(float top, float l) {
+  return l > 0.f ? top + log2f(l) : (l != l ? l : -INFINITY);
+}
 
 __device__ __forceinline__ int tiles_of(const CacheAttn& a, int len) {
   return (len + a.tile - 1) / a.tile;

@@ -1,8 +1,8 @@
 """Cache attention where the logsumexp is large: the softmax is still normalised.
 
-All logits lie at 2^19, where one step of fp32 is 2^-5 (2^-4 after the factor
-log2 e), so that a weight taken as exp2(x - lse) with a rounded lse would be off by
-some per cent.  With the values all one, o = 1; the weights of a row sum to one.
+All logits lie at 2^19, where one step of fp32 is 2^-4 (also after the factor
+log2 e), so that a weight taken as exp2(x - lse) with a rounded lse would be off by up
+to 2 per cent.  With the values all one, o = 1; the weights of a row sum to one.
 
 Tolerance.  o is sum p / sum p over the same fp32 p >= 0, and the weights are such
 p times one reciprocal.  Any order of n positive fp32 terms is off by n 2^-24
@@ -11,7 +11,7 @@ denominator: below n 2^-22 together.  Each exponential has 2^-22; a term carries
 and one for each rise of the maximum since it came and for each joining of parts:
 at most 63 tiles to a warp (2000 keys in tiles of 8 over 4 warps) and 5 + 2.  So
 (n + 72) 2^-22, for bf16 also 2^-17 of o for weights in two parts and half a step
-of o, 2^-8.  Differences of logits are multiples of 2^-6 below 2^18: exact.
+of o, 2^-8.  Differences of logits are multiples of 2^-4 below 2^20: exact.
 """
 import numpy as np
 import pytest
