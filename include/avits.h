@@ -484,6 +484,11 @@ avits_status avits_device_status(void* stream);
  *         last axis contiguous): the accumulated attention weight of each
  *         cached token under each KV head.
  *
+ * What a call writes (o; acc; the pages of an append's cache and of the one that
+ * an eviction fills) may not lie over itself: strides by which two of its rows
+ * meet, or one pool for keys and values, are AVITS_ERR_INVALID_ARG.  Two entries of
+ * a block table that name one page are not looked for.
+ *
  * A length outside [0, max_len] is cut to it where tokens are read; a page number
  * outside [0, num_pages) makes its tokens count as masked (read) or be left out
  * (written); both raise AVITS_ERR_PAGE in the status word.

@@ -1,6 +1,7 @@
 // api.cu — the C ABI of libavits (see include/avits.h): host-side argument
 // checks, workspace sizing and dispatch to the kernels.  Nothing here
 // allocates device memory or synchronises, except avits_device_status().
+#include <algorithm>
 #include <cstdio>
 #include <cstring>
 #include <string>
@@ -43,6 +44,55 @@ bool mixed_bilinear_ok(avits_upmode mode, const int32_t* pos_in, int B, int M, i
   if (mode != AVITS_UP_BILINEAR || !pos_in) return true;
   if ((gh & 1) || (gw & 1) || M > (1 << 28) - 1) return false;
   return ws && aligned16(ws) && ws_bytes >= merge_workspace_bytes(B, gh, gw);
+}
+
+// Whether the rows of `width` elements that a view of up to 3 axes has (extents n,
+// strides st >= 0) lie apart.  Views of a dense tensor nest: each stride passes all
+// that the smaller ones reach.  Others are searched for two rows that meet: over the
+// differences of the two shorter axes' indexes, the third's is then given; where
+// those are more than 2^22 the view counts as one whose rows meet.
+struct Axis {
+  int64_t n, st;
+};
+bool rows_apart(int64_t width, Axis a, Axis b, Axis c = {1, 0}) {
+  Axis ax[3] = {a, b, c};
+  for (Axis& x : ax)
+    if (x.n == 1) x.st = 0;
+  std::sort(ax, ax + 3, [](const Axis& x, const Axis& y) { return x.st < y.st; });
+  __int128 reach = width;
+  bool nested = true;
+  for (const Axis& x : ax) {
+    if (x.n == 1) continue;
+    nested = nested && x.st >= reach;
+    reach += (__int128)(x.n - 1) * x.st;
+  }
+  if (nested) return true;
+  std::sort(ax, ax + 3, [](const Axis& x, const Axis& y) { return x.n < y.n; });
+  if (ax[0].n * ax[1].n > (1 << 22)) return false;
+  const __int128 st = ax[2].st;
+  for (int64_t i = 0; i < ax[0].n; ++i)
+    for (int64_t j = 1 - ax[1].n; j < ax[1].n; ++j) {
+      const __int128 off = (__int128)i * ax[0].st + (__int128)j * ax[1].st;
+      const bool same = i == 0 && j == 0;          // the two rows differ in the third axis alone
+      if (st == 0) {
+        if (off < width && off > -width && (!same || ax[2].n > 1)) return false;
+        continue;
+      }
+      const __int128 k0 = off / st;                // the nearest differences
+      for (__int128 k = k0 - 1; k <= k0 + 1; ++k) {
+        const __int128 d = off - k * st;
+        if (k > -ax[2].n && k < ax[2].n && !(same && k == 0) && d < width && d > -width) return false;
+      }
+    }
+  return true;
+}
+// What is written may not lie over itself: the rows of weights, of the pages.
+bool weights_apart(const avits_kv_cache& c) {
+  return rows_apart(c.max_len, {c.B, c.acc_sb}, {c.Hkv, c.acc_sh});
+}
+bool pages_apart(const avits_kv_cache& c) {
+  return rows_apart(c.d, {c.num_pages, c.k_sp}, {c.page_size, c.k_st}, {c.Hkv, c.k_sh}) &&
+         rows_apart(c.d, {c.num_pages, c.v_sp}, {c.page_size, c.v_st}, {c.Hkv, c.v_sh});
 }
 
 // A cache's description: INVALID_ARG for what cannot be one, UNSUPPORTED for a
@@ -420,10 +470,12 @@ avits_status avits_cache_append(const avits_kv_cache* cache, const void* k_new, 
   const avits_status ok = check_cache(cache);
   if (ok != AVITS_OK) return ok;
   if (T == 0) return AVITS_OK;
+  if (!pages_apart(*cache) || (cache->acc && !weights_apart(*cache))) return AVITS_ERR_INVALID_ARG;
   const int per16 = cache->dt == AVITS_BF16 ? 8 : 4;
   if (!aligned16(k_new) || !aligned16(v_new) || k_st % per16 || k_sh % per16 || v_st % per16 ||
       v_sh % per16)
     return AVITS_ERR_UNSUPPORTED;
+  if (cache->k_pages == cache->v_pages) return AVITS_ERR_INVALID_ARG;
   return cuda_status(launch_cache_append(*cache, k_new, v_new, T, cu_new, k_st, k_sh, v_st, v_sh,
                                          status_word(), static_cast<cudaStream_t>(stream)));
 }
@@ -451,6 +503,9 @@ avits_status avits_cache_attention(const avits_kv_cache* cache, const void* q, i
     return AVITS_ERR_INVALID_ARG;
   if ((H > 1 && o_sh < cache->d) || (cache->B > 1 && o_sb < cache->d)) return AVITS_ERR_INVALID_ARG;
   if (!cache_attention_sizes_ok(*cache, H)) return AVITS_ERR_UNSUPPORTED;
+  if (!rows_apart(cache->d, {cache->B, o_sb}, {H, o_sh}) ||
+      (weights != AVITS_WEIGHTS_NONE && !weights_apart(*cache)))
+    return AVITS_ERR_INVALID_ARG;
   const int sms = num_sms_current();
   const size_t need = cache_attention_workspace(*cache, H, weights != AVITS_WEIGHTS_NONE, sms);
   if (need > 0 && (!workspace || !aligned16(workspace) || ws_bytes < need))
@@ -474,8 +529,10 @@ avits_status avits_cache_evict(const avits_kv_cache* src, const avits_kv_cache* 
   if (src->dt != dst->dt || src->B != dst->B || src->Hkv != dst->Hkv || src->d != dst->d ||
       keep > dst->max_len || src->lens == dst->lens || src->acc == dst->acc)
     return AVITS_ERR_INVALID_ARG;
+  if (!pages_apart(*dst) || !weights_apart(*dst)) return AVITS_ERR_INVALID_ARG;
   if ((int64_t)src->B * src->Hkv * ((int64_t)keep / 4 + 1) >= (1ll << 31))
     return AVITS_ERR_UNSUPPORTED;
+  if (dst->k_pages == dst->v_pages) return AVITS_ERR_INVALID_ARG;
   return cuda_status(launch_cache_evict(*src, *dst, keep, sinks, recent, keep_idx, num_sms_current(),
                                         status_word(), static_cast<cudaStream_t>(stream)));
 }
