@@ -537,6 +537,9 @@ def avits_score_spatial_noalloc_limit() -> int:
 
 
 # ------------------------------------------------- paged key-value cache --
+_INT_MAX = 2 ** 31 - 1       # ctypes passes the low 32 bits of what is larger
+
+
 class _CacheStruct(ctypes.Structure):
     _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
                 ("block_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
@@ -584,6 +587,11 @@ class KVCache:
             max_len = cols * page_size
         if not 0 < max_len <= cols * page_size:
             raise ValueError("max_len must be positive and fit the block table")
+        if max_len > _INT_MAX:
+            raise ValueError("the block table holds %d tokens: give a max_len that fits 32 bits"
+                             % max_len)
+        if max(num_pages, page_size, B, Hkv, d) > _INT_MAX:
+            raise ValueError("sizes of more than 32 bits")
         if tuple(lens.shape) != (B,) or lens.dtype != torch.int32 or not lens.is_contiguous():
             raise ValueError("lens must be a contiguous int32 [B] tensor")
         if acc is not None and (acc.dim() != 3 or tuple(acc.shape[:2]) != (B, Hkv) or
@@ -646,6 +654,8 @@ def avits_cache_append(cache: KVCache, k_new, v_new, cu_new, stream=None):
     T, Hkv, d = shape = k_new.shape
     if Hkv != cache.Hkv or d != cache.d or v_new.shape != shape:
         raise ValueError("k_new / v_new must be [T, Hkv, d] of the cache")
+    if T > _INT_MAX:
+        raise ValueError("more new tokens than 32 bits count")
     if k_new.dtype != cache.dtype or v_new.dtype != cache.dtype:
         raise TypeError("k_new / v_new and cache dtypes differ")
     k_st, k_sh, k_sd = k_new.stride()
@@ -665,6 +675,8 @@ def avits_cache_append(cache: KVCache, k_new, v_new, cu_new, stream=None):
 
 
 def avits_cache_attention_workspace(cache: KVCache, H: int, weights: bool) -> int:
+    if not 0 < H <= _INT_MAX:
+        return 0
     return int(lib().avits_cache_attention_workspace(cache._ref, H, 2 if weights else 0))
 
 
@@ -683,6 +695,8 @@ def avits_cache_attention(cache: KVCache, q, softmax_scale: float, o, lse=None,
     B, H, d = shape = q.shape
     if B != cache.B or d != cache.d or o.shape != shape:
         raise ValueError("q and o must be [B, H, d] of the cache")
+    if H > _INT_MAX:
+        raise ValueError("more heads than 32 bits count")
     if q.dtype != cache.dtype or o.dtype != cache.dtype:
         raise TypeError("q, o and cache dtypes differ")
     q_sb, q_sh, q_sd = q.stride()
@@ -745,6 +759,8 @@ def avits_cache_evict(src: KVCache, dst: KVCache, keep: int, sinks: int, recent:
     if keep_idx.shape != (src.B, src.Hkv, keep) or keep_idx.dtype != src.int32 or \
             not keep_idx.is_contiguous():
         raise ValueError("keep_idx must be a contiguous int32 [B, Hkv, keep] tensor")
+    if not (-_INT_MAX <= sinks <= _INT_MAX and -_INT_MAX <= recent <= _INT_MAX):
+        raise ValueError("sinks and recent must fit 32 bits")
     if src.dtype != dst.dtype or src.B != dst.B or src.Hkv != dst.Hkv or src.d != dst.d:
         raise ValueError("the two caches' types or sizes differ")
     if src.acc is None or dst.acc is None:
