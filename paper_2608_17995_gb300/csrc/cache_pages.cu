@@ -435,7 +435,7 @@ cudaError_t launch_cache_append(const avits_kv_cache& c, const void* k_new, cons
   const cudaError_t e = prefer_max_shared<cache_append_kernel>();
   if (e != cudaSuccess) return e;
   constexpr int kWarps = kAppendThreads / 32;
-  return launch_pdl(cache_append_kernel, dim3((unsigned)((T + kWarps - 1) / kWarps)),
+  return launch_pdl(cache_append_kernel, dim3((unsigned)((T - 1) / kWarps + 1)),
                     dim3(kAppendThreads), 0, s, a);
 }
 

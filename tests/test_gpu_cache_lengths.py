@@ -60,3 +60,18 @@ def test_evict_of_lengths_out_of_range(av):
             assert np.array_equal(rows.float().cpu().numpy(), k[h, want])
             assert (dst.acc[b, h, len(want):] == -1).all()
     assert t.isnan(k2[2:4]).all()                       # the empty sequence's pages
+
+
+def test_append_of_the_most_tokens(av):
+    """T = 2^31 - 1 rows, one row seen so many times; three belong to sequences."""
+    t = _torch()
+    w = World(av, "bf16", [5, 2], 2, 2, 64, 16)
+    want_k, want_v = w.k_pages.clone(), w.v_pages.clone()
+    kn, vn = (t.randn(1, 2, 64, device=DEV).bfloat16() for _ in range(2))
+    for b, j in ((0, 3), (0, 4), (1, 1)):
+        p = int(w.table[b, 0])
+        want_k[p, j], want_v[p, j] = kn[0], vn[0]
+    av.avits_cache_append(w.cache, kn.expand(2 ** 31 - 1, 2, 64), vn.expand(2 ** 31 - 1, 2, 64),
+                          t.tensor([0, 2, 3], dtype=t.int32, device=DEV))
+    assert av.avits_device_status() == 0
+    assert same(w.k_pages, want_k) and same(w.v_pages, want_v)
