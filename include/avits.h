@@ -27,8 +27,8 @@
  *   avits_merge_final         Sec. 3.2 Stage 3   dense full-resolution latent
  *   avits_selftest_bounded_wait  test hook for the device-side failure path
  *
- * and, for the language model that conditions an editing pipeline and answers
- * token by token, the same three steps (attention that gives a weight, top-K by
+ * and beside them, for a language model that answers token by token (the
+ * transition does not call them), the same three steps (attention that gives a weight, top-K by
  * the weight, packing) over a paged key-value cache:
  *
  *   avits_cache_append        new keys and values into the pages
@@ -478,11 +478,15 @@ avits_status avits_device_status(void* stream);
  * block_table : [B, >= ceil(max_len / page_size)] int32, row stride table_sb.
  *         Entries past a sequence's pages are not read.
  * lens  : [B] int32, 0 <= lens[b] <= max_len.  0: no cached token.
- * max_len : an upper bound of the lengths that the host knows; workspaces and
- *         grids are sized by it.
+ * max_len : an upper bound of the lengths that the host knows.  Workspaces (with
+ *         weights 4 B H max_len bytes and more) and grids are sized by it, and the
+ *         kernels chosen: one far above the lengths costs memory and time.
  * acc   : NULL or [B, Hkv, >= max_len] fp32 (row strides acc_sb, acc_sh, the
  *         last axis contiguous): the accumulated attention weight of each
- *         cached token under each KV head.
+ *         cached token under each KV head.  avits_cache_append starts it at zero
+ *         and avits_cache_attention adds to it; the weights that a prompt's tokens
+ *         got from the prompt's own attention, which is no call of this library, are
+ *         the caller's to put there.
  *
  * What a call writes (o; acc; the pages of an append's cache and of the one that
  * an eviction fills) may not lie over itself: strides by which two of its rows

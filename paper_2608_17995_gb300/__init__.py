@@ -561,7 +561,8 @@ class KVCache:
     lens              [B] int32, its cached tokens
     acc               [B, Hkv, >= max_len] fp32, optional: accumulated weights
     max_len           an upper bound of lens known here (default: all that the
-                      table can hold); a smaller one costs less workspace
+                      table can hold); a smaller one costs less workspace and,
+                      where weights are wanted or tokens evicted, less time
 
     The description is fixed: other tensors are another KVCache.
     """

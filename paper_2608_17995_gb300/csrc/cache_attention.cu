@@ -4,16 +4,26 @@
 // For sequence b, KV head hk and the G query heads h that share it:
 //   x_hj = scale q_h . k_j,  lse_h = log sum_j exp x_hj,  o_h = sum_j exp(x_hj - lse_h) v_j,
 //   acc_j (+)= weight mean_h exp(x_hj - lse_h)
-// Every key and value is read once, so HBM bounds it: 4 G operations per bf16
-// element of K and V.  The products are m16n8k16 of mma.sync, heads in the rows: a
-// unit has 8 to 32 rows, a quarter at most of the smallest tcgen05 tile, whose O
-// would lie in TMEM and have to be rescaled there; the tensor pipe is not what
-// bounds a call of 8 rows (15 % busy), and one warp's tiles need no other warp.
+// A key or a value is 2 G operations to an element, so HBM bounds it where the heads of a
+// KV head fit one unit (below), whose keys and values are read once.  Larger groups
+// are several units, each of which copies the tiles again; L2 has part of them (28 x
+// 1180-9904 in fp32, 16 heads in two units of 8: 220 MB from HBM for 155 MB of keys and
+// values).
+//
+// The products are m16n8k16 of mma.sync, heads in the rows, 8 to 32 of them.  tcgen05
+// has at least 64 rows: heads there would leave half of them and more empty, keys there
+// and heads in the columns (8 and more) would fit, but P would pass through shared
+// memory and O be rescaled in TMEM.  It was not tried: the tensor pipe does not bound
+// these calls (15 % busy with 8 rows, 27 % with 32), and one warp's tiles need no other
+// warp.
 //
 // Measured, against the time of the call's bytes at a copy's rate: 48 sequences of
 // 409-4096 tokens, 32 heads over 8 of width 128, with weights 85 us (floor 68), without
-// 76 (67); one of 131072, 32 over 4, 56 (40) and 47 (40); 40 of up to 1500, 24 heads of
-// width 64, 52 (36); one of 517 tokens 5.7 (0.3).
+// 77 (67); one of 131072, 32 over 4, 56 (40); 40 of up to 1500, 24 heads of width 64, 53
+// (36); one of 517 tokens 5.5 (0.3).  These have max_len as the longest length.  The
+// grids, the form and the logits' workspace go by max_len: with 32 times as much the
+// first takes 130 us, the one of 517 tokens 7.8, and without weights there is no
+// difference.
 //
 // Split.  A sequence's keys are cut into tiles; all tiles of all units (b, hk,
 // row group) form one line, cut into equal pieces, one per CTA, so that uneven

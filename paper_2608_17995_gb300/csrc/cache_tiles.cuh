@@ -229,7 +229,7 @@ __device__ __forceinline__ int o_at(int row, int d, int D) {
 // is no part of the result: the value's product alone has it, and its NaN.  kR = 8: the
 // rest's sum is added where the value's is finite.  kR = 16, 32, whose products share
 // their sums: the second one takes V cut to the finite range (two instructions to a
-// register of V: 32 sequences of 600-6000 with 24 heads to each of 2 KV heads 34.1 us,
+// register of V: 32 sequences of 714-6000 with 24 heads to each of 2 KV heads 34.1 us,
 // 33.0 without them; 16 heads of width 256 39.0 and 37.8).
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                          uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -669,8 +669,10 @@ struct RowsF32 {
 //   bf16, width 128: 2 CTAs 131072 keys 55.8 us, with 3 58.1; 48 x <= 4096 without
 //     weights 78.1 and 79.0, but 48 x <= 1024 with weights 34.3 and 31.4; 3 stages
 //     of 2 CTAs 59.1 for 131072 keys, where 2 stages took 57.0
-//   bf16, width 64: 4 CTAs 54.0 (40 x 24 heads x <= 1500), 3 53.5 (in an earlier state
-//     50.3 and 50.8, and 52.1 with 3 stages of 3 CTAs)
+//   width 64: 4 CTAs, chosen when the kernels held fewer registers (50.3 us and 50.8 with
+//     3 for 40 x 24 heads x <= 1500).  As the kernels are, 3 would serve bf16 better
+//     (53.8 and 54.7; 48 x <= 4096 53.8 and 55.1; 131072 keys 35.3 and 36.5; 8 x <= 6000
+//     18.6 and 20.1) and fp32 as well (24 x <= 3000 35.3 and 35.0)
 //   fp32, width 128, whose arithmetic is on the CUDA cores: 3 CTAs 14 x <= 2286 34.2,
 //     28 x <= 9904 of 16 heads to a group 166, with 2 40.9 and 192; but 30000 keys of
 //     one head to a group 46.3 and 45.3
