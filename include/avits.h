@@ -535,6 +535,8 @@ avits_status avits_cache_append(const avits_kv_cache* cache, const void* k_new, 
  * sequence without cached tokens gets o = 0 and lse = -inf.
  * A value that is infinite (or NaN) at a cached token makes its column of o so;
  * where the token's weight, held in 32 bits, is below 2^-126 and so zero, NaN.
+ * The sums of exp(x - max x) v are kept in fp32 before they are divided: finite
+ * values beyond 3.4e38 / lens[b] can pass its range.
  * q, o  : [B,H,d] of the cache's type, element strides *_sb, *_sh, d contiguous.
  * lse_opt : NULL or [B,H] fp32 contiguous, natural log.
  * weights : AVITS_WEIGHTS_NONE leaves acc alone; _WRITE sets acc (old = 0) for
