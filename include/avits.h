@@ -36,6 +36,14 @@
  *                             with the weight each of them got
  *   avits_cache_evict         the tokens of the largest accumulated weights kept
  *
+ * and what a served batch's step needs around them:
+ *
+ *   avits_cache_plan          changes of length become pages, block tables and
+ *                             a place for every new row
+ *   avits_norm_rotate         norm of each head and rotation by position, queries
+ *                             and keys in one pass (also of an image's tokens)
+ *   avits_cache_append_rotated  the same, keys and values into the pages
+ *
  * Conventions shared by every call
  * --------------------------------
  *  - Every tensor pointer is DEVICE memory owned by the caller.  The library
@@ -575,6 +583,128 @@ size_t avits_cache_attention_workspace(const avits_kv_cache* cache, int H, int w
  * caches have acc, and the same type, B, Hkv and d. */
 avits_status avits_cache_evict(const avits_kv_cache* src, const avits_kv_cache* dst, int keep,
                                int sinks, int recent, int32_t* keep_idx, void* stream);
+
+/* ------------------------------------------------------------------------
+ * A step's changes of length become pages.  With n0 = lens[b], c = change[b],
+ * n1 = max(n0 + c, 0) and p(n) = ceil(n / page_size):
+ *   c > 0 : the sequence gets c tokens: columns p(n0) .. p(n1)-1 of its row of the
+ *           block table are filled with pages taken from the end of the free list;
+ *   c < 0 : it loses -c (all of them: c = -n0, or less than that): the pages of
+ *           columns p(n1) .. p(n0)-1 go behind the free ones.
+ * All pages that are given back are on the list, in the order of sequences and columns,
+ * before the first one is taken; the i-th one taken, in the same order, is the list's
+ * i-th from its end.  Entries of the table past a sequence's pages, and of the list past
+ * its count, are left as they were.
+ *
+ * A sequence is left as it was, with its rows marked as padding, and AVITS_ERR_PAGE
+ * raised, if its length is outside [0, max_len] before or after, if its rows do not end
+ * within T, or if it needs pages and the list, less what the sequences before it asked
+ * for, has not as many.
+ *
+ * cache : its block_table (rows apart: table_sb >= ceil(max_len / page_size)) and
+ *         lens are WRITTEN; the pages themselves are not touched.  No two sequences
+ *         may name one page (a shared prompt is a cache of its own, see
+ *         avits_cache_attention_shared).
+ * lens, change : [B] int32.  lens may be the cache's own.
+ * free_pages : [num_pages] int32, of which the first *free_count are free pages; read and
+ *         written.  A count outside [0, num_pages] is cut to it (AVITS_ERR_PAGE).
+ * free_out : receives the new count; may be free_count.
+ * cu_new : [B+1] int32, receives the first row of each sequence: the sums of the c > 0
+ *         before it, cut to T.
+ * slots [T] int64, seq, place [T] int32 (NULL if T = 0): for each row of the step where it
+ *         goes, page * page_size + place in the page, its sequence, and its place in the
+ *         sequence; -1 for padding (rows past the last, of sequences left as they were).
+ *         Rows of a page number outside the pool have slot -1 (AVITS_ERR_PAGE).
+ * pos_opt : NULL or [T] int32, receives place + pos_base[b] (pos_base NULL: place), -1
+ *         for padding.
+ * ---------------------------------------------------------------------- */
+avits_status avits_cache_plan(const avits_kv_cache* cache, const int32_t* lens,
+                              const int32_t* change, int32_t* free_pages,
+                              const int32_t* free_count, int32_t* free_out, int T,
+                              int32_t* cu_new, int64_t* slots, int32_t* seq, int32_t* place,
+                              int32_t* pos_opt, const int32_t* pos_base_opt, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Norm of each head and rotation by position.  For a head's vector x of d values
+ * of a token at position p (an integer on each axis):
+ *
+ *   y = x / sqrt(mean(x^2) + eps) * weight              (norm = 0: y = x)
+ *   pair i < rot/2, of values a, b of y, becomes
+ *     magnitude * (a cos t - b sin t, b cos t + a sin t),  t = 2 pi freq[i] p[axis(i)]
+ *
+ * computed in fp32 and rounded once.  Pair i is values 2i and 2i+1 (interleaved) or i
+ * and i + rot/2; values from rot on are y.  The first sections[0] pairs turn by the
+ * position's axis 0, the next sections[1] by axis 1, ...
+ *
+ * freq  : device [rot/2], turns per position as fractions of 2^64
+ *         (avits_rotary_frequencies).  The product with a position is taken modulo a
+ *         turn in integers, so that positions of any size, and negative ones, are exact
+ *         to 2^-32 of a turn.
+ * rot   : even, 0 <= rot <= d; 0: the norm alone (freq, positions not read).
+ * axes  : 1 .. 4; sections of the axes sum to rot/2.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  const uint64_t* freq;
+  int32_t rot, interleaved, axes;
+  int32_t sections[4];
+  float magnitude;
+} avits_rotary;
+
+/* Frequencies of `width` values (width/2 pairs) into the HOST array freq:
+ * f_i = base^(-2i/width) / (2 pi) turns per position, i < width/2, and for long contexts
+ *   AVITS_SCALE_LINEAR  f_i / factor
+ *   AVITS_SCALE_BASE    base * factor^(width / (width - 2)) in base's place (width > 2)
+ *   AVITS_SCALE_PARTS   g f_i + (1 - g) f_i / factor, where g goes from 0 to 1 as the
+ *                       turns within original_len, original_len f_i, go from low to high
+ * Several axes with ladders of their own: one call for each, one behind the other.
+ * width even, 0 < width <= 256; base > 0; factor >= 1; low < high, original_len > 0
+ * (PARTS).  f_i must be below half a turn. */
+typedef enum {
+  AVITS_SCALE_NONE = 0, AVITS_SCALE_LINEAR = 1, AVITS_SCALE_BASE = 2, AVITS_SCALE_PARTS = 3
+} avits_scaling;
+
+avits_status avits_rotary_frequencies(int width, double base, int scaling, double factor,
+                                      double original_len, double low, double high,
+                                      uint64_t* freq);
+
+/* q [B,N,H,d] into q_out, and k [B,N,Hkv,d] into k_out if k is given (else Hkv = 0, k,
+ * k_out and their strides NULL), in one launch.
+ * dt    : of q, k, their outputs and the weights.  d a multiple of 16 bytes, at most 256
+ *         values.
+ * *_str : element strides (sequence, token, head) as an array of 3 int64, d contiguous;
+ *         multiples of 16 bytes, as the bases.  Views of a joint projection qualify, and
+ *         outputs in the order of the attention ([B,H,N,d], or a part of its rows).
+ * positions : int32, element strides pos_sb (0: the same for all sequences), pos_sn, the
+ *         axes contiguous; as avits_selective_upsample writes them.
+ * weights : [d], 16-byte aligned, or NULL (ones); NULL if norm = 0.
+ * An output may be its own input (the same address and strides) and else lies apart from
+ * the inputs and the other output.  B * N <= 2^30. */
+avits_status avits_norm_rotate(const avits_rotary* rot, avits_dtype dt, int B, int N, int d,
+                               const int32_t* positions, int64_t pos_sb, int64_t pos_sn,
+                               const void* q, int H, const int64_t* q_str, void* q_out,
+                               const int64_t* qo_str, const void* k, int Hkv,
+                               const int64_t* k_str, void* k_out, const int64_t* ko_str, int norm,
+                               const void* q_weight, const void* k_weight, float eps,
+                               void* stream);
+
+/* The same for the T rows of a step: q [T,H,d] into q_out, and k_new, v_new [T,Hkv,d] into
+ * the cache, k_new normed and rotated as well, at the places that slots [T] says
+ * (avits_cache_plan).  A row whose slot is negative is padding: nothing of it is read or
+ * written.  A slot past the pool writes nothing (AVITS_ERR_PAGE).  No two rows may have one slot.
+ * positions : [T, axes] int32, row stride pos_st.
+ * seq, place : [T] int32, needed where the cache has acc (else may be NULL): acc of each
+ *         row's token is set to zero (out of range: AVITS_ERR_PAGE).
+ * Element strides *_st (row), *_sh (head), as for avits_cache_append.  q_out may be q.
+ * T = 0 launches nothing; T <= 2^30. */
+avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits_rotary* rot, int T,
+                                        const int32_t* positions, int64_t pos_st,
+                                        const int64_t* slots, const int32_t* seq,
+                                        const int32_t* place, const void* q, int H, int64_t q_st,
+                                        int64_t q_sh, void* q_out, int64_t qo_st, int64_t qo_sh,
+                                        const void* k_new, int64_t k_st, int64_t k_sh,
+                                        const void* v_new, int64_t v_st, int64_t v_sh, int norm,
+                                        const void* q_weight, const void* k_weight, float eps,
+                                        void* stream);
 
 /* ------------------------------------------------------------------------
  * Test hook for the failure detection of the device-side waits (a library

@@ -24,6 +24,10 @@ Calls:
   avits_cache_attention     one new token per sequence over its cached tokens,
                             with the weight each of them got
   avits_cache_evict         the cached tokens of the largest accumulated weights
+  avits_cache_plan          a step's changes of length become pages and slots
+  avits_norm_rotate         norm of each head and rotation by position (Rotary),
+                            queries and keys in one pass
+  avits_cache_append_rotated  the same, keys and values into a cache's pages
   avits_device_status       device-side error word (read and cleared)
 """
 from __future__ import annotations
@@ -45,7 +49,8 @@ __all__ = [
     "avits_selective_upsample", "avits_select_upsample",
     "avits_merge_final", "avits_merge_final_workspace", "avits_device_status",
     "KVCache", "avits_cache_append", "avits_cache_attention", "avits_cache_attention_workspace",
-    "avits_cache_evict",
+    "avits_cache_evict", "avits_cache_plan", "Rotary", "avits_norm_rotate",
+    "avits_cache_append_rotated",
     "avits_selftest_bounded_wait", "avits_status_string", "avits_version", "SpatialWorkspace",
 ]
 
@@ -119,6 +124,13 @@ def lib():
                                   vp],
         "avits_cache_attention_workspace": [vp, i32, i32],
         "avits_cache_evict": [vp, vp, i32, i32, i32, vp, vp],
+        "avits_cache_plan": [vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp],
+        "avits_rotary_frequencies": [i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double,
+                                     ctypes.c_double, ctypes.c_double, vp],
+        "avits_norm_rotate": [vp, i32, i32, i32, i32, vp, i64, i64, vp, i32, vp, vp, vp, vp, i32, vp,
+                              vp, vp, i32, vp, vp, f32, vp],
+        "avits_cache_append_rotated": [vp, vp, i32, vp, i64, vp, vp, vp, vp, i32, i64, i64, vp, i64,
+                                       i64, vp, i64, i64, vp, i64, i64, i32, vp, vp, f32, vp],
         "avits_device_status": [vp],
         "avits_selftest_bounded_wait": [ctypes.c_ulonglong, vp, vp],
         "avits_status_string": [i32],
@@ -568,7 +580,7 @@ class KVCache:
     """
     __slots__ = ("k_pages", "v_pages", "block_table", "lens", "acc", "B", "Hkv", "d", "dtype",
                  "page_size", "max_len", "device", "int32", "float32", "_index", "_struct", "_ref",
-                 "_need", "_alloc", "_free", "_append", "_attend", "_evict")
+                 "_need", "_alloc", "_free", "_append", "_attend", "_plan", "_append_rotated", "_evict")
 
     def __init__(self, k_pages, v_pages, block_table, lens, acc=None, max_len: Optional[int] = None):
         torch = _torch()
@@ -622,6 +634,7 @@ class KVCache:
         self._free = torch._C._cuda_cudaCachingAllocator_raw_delete
         L = lib()
         self._append, self._attend = L.avits_cache_append, L.avits_cache_attention
+        self._plan, self._append_rotated = L.avits_cache_plan, L.avits_cache_append_rotated
         self._evict = L.avits_cache_evict
 
     def __setattr__(self, name, value):
@@ -773,3 +786,252 @@ def avits_cache_evict(src: KVCache, dst: KVCache, keep: int, sinks: int, recent:
     if rc != 0:
         _check("avits_cache_evict", rc)
     return keep_idx
+
+
+# ------------------------------------------- a served batch's step around it --
+def avits_cache_plan(cache: KVCache, change, free_pages, free_count, cu_new, slots, seq, place,
+                     lens=None, pos=None, pos_base=None, free_out=None, stream=None):
+    """A step's changes of length become pages.  change [B] int32: new tokens of
+    each sequence, or negative: tokens that it loses (all of them when it is done),
+    whose pages go behind the free ones in free_pages ([num_pages] int32, the first
+    free_count[0] of them free).  Pages for new tokens are taken from the list's end.
+    lens [B] int32 are the lengths before (default: the cache's, in place);
+    cache.lens and cache.block_table are written, and free_out [1] (default:
+    free_count).  cu_new [B+1] int32: first row of each sequence's new tokens.
+    slots [T] int64, seq, place, pos [T] int32 (pos optional: place + pos_base[b]):
+    where each of the step's T rows goes, -1 for padding.  A sequence that finds no
+    room is left as it was, its rows padding (avits_device_status: 7)."""
+    B, i32 = cache.B, cache.int32
+    T = slots.shape[0]
+    if lens is None:
+        lens = cache.lens
+    if free_out is None:
+        free_out = free_count
+    if T > _INT_MAX:
+        raise ValueError("more rows than 32 bits count")
+    for t, n in ((change, B), (lens, B), (cu_new, B + 1), (free_count, 1), (free_out, 1), (seq, T),
+                 (place, T), (free_pages, cache._struct.num_pages)):
+        if t.shape != (n,) or t.dtype != i32 or not t.is_contiguous():
+            raise ValueError("change, lens [B], cu_new [B+1], free_count, free_out [1], seq, place [T] "
+                             "and free_pages [num_pages] must be contiguous int32 tensors")
+    if slots.dim() != 1 or slots.dtype != _torch().int64 or not slots.is_contiguous():
+        raise ValueError("slots must be a contiguous int64 [T] tensor")
+    if pos is not None and (pos.shape != (T,) or pos.dtype != i32 or not pos.is_contiguous()):
+        raise ValueError("pos must be a contiguous int32 [T] tensor")
+    if pos_base is not None and (pos is None or pos_base.shape != (B,) or pos_base.dtype != i32 or
+                                 not pos_base.is_contiguous()):
+        raise ValueError("pos_base must be a contiguous int32 [B] tensor, given with pos")
+    _elsewhere(cache, change, lens, cu_new, free_count, free_out, seq, place, free_pages, slots, pos,
+               pos_base)
+    rc = cache._plan(cache._ref, lens.data_ptr(), change.data_ptr(), free_pages.data_ptr(),
+                     free_count.data_ptr(), free_out.data_ptr(), T, cu_new.data_ptr(),
+                     slots.data_ptr(), seq.data_ptr(), place.data_ptr(),
+                     None if pos is None else pos.data_ptr(),
+                     None if pos_base is None else pos_base.data_ptr(), _call_stream(cache, stream))
+    if rc != 0:
+        _check("avits_cache_plan", rc)
+
+
+class _RotaryStruct(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4),
+                ("magnitude", ctypes.c_float)]
+
+
+_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+class Rotary:
+    """How heads turn by position, described once and used by any number of calls.
+
+    rot          values of a head that turn, the first ones (0: none)
+    base         pair i turns base^(-2i/width) radians per position
+    sections     pairs that turn by each axis of the position (default: all by one)
+    joint        False: each axis has frequencies of its own, width being twice its
+                 pairs; True: one ladder over all pairs, width being rot
+    interleaved  pairs of neighbours (2i, 2i+1); else of halves (i, i + rot/2)
+    scaling      for long contexts: "linear" (frequencies over factor), "base" (a base
+                 raised by factor^(width / (width - 2))), "parts" (over factor where
+                 a pair makes low turns or fewer within original_len, unchanged from high
+                 on, in between linearly)
+    magnitude    of the rotated values
+    """
+    __slots__ = ("rot", "axes", "freq", "device", "_struct", "_ref", "_index", "_call")
+
+    def __init__(self, rot: int, base: float = 10000.0, sections: Optional[Sequence[int]] = None,
+                 interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
+                 original_len: float = 0.0, low: float = 1.0, high: float = 32.0,
+                 magnitude: float = 1.0, joint: bool = False, device="cuda"):
+        torch = _torch()
+        if scaling not in _SCALINGS:
+            raise ValueError("scaling must be one of %s" % ", ".join(sorted(_SCALINGS)))
+        if not 0 <= rot <= 256 or rot % 2:
+            raise ValueError("rot must be even, 0 .. 256")
+        parts = [rot // 2] if sections is None else [int(x) for x in sections]
+        if not 1 <= len(parts) <= 4 or min(parts) < 0 or sum(parts) != rot // 2:
+            raise ValueError("sections must be 1 to 4 counts of pairs that sum to rot / 2")
+        turns = (ctypes.c_uint64 * max(rot // 2, 1))()
+        at = 0
+        for n in ([rot // 2] if joint else parts):
+            if n:
+                _check("avits_rotary_frequencies", lib().avits_rotary_frequencies(
+                    2 * n, base, _SCALINGS[scaling], factor, original_len, low, high,
+                    ctypes.addressof(turns) + 8 * at))
+            at += n
+        # the bits: torch's integers are signed
+        bits = [x - (1 << 64) if x >> 63 else x for x in turns]
+        self.freq = torch.tensor(bits, dtype=torch.int64, device=device)
+        self.rot, self.axes, self.device = rot, len(parts), self.freq.device
+        self._struct = _RotaryStruct(_ptr(self.freq), rot, 1 if interleaved else 0, len(parts),
+                                     (ctypes.c_int32 * 4)(*parts), magnitude)
+        self._ref = ctypes.addressof(self._struct)
+        self._index = self.freq.get_device()
+        self._call = lib().avits_norm_rotate
+
+
+def _weight_at(w, d, dtype, index):
+    if w is None:
+        return None
+    if w.shape != (d,) or w.dtype != dtype or not w.is_contiguous():
+        raise ValueError("weights must be contiguous [d] tensors of the type of q")
+    if w.get_device() != index:
+        raise ValueError("weights on %s" % w.device)
+    return w.data_ptr()
+
+
+def _axes4(t):
+    """Strides of [N,heads,d] or [B,N,heads,d], and the shape, as of the latter."""
+    st, sh = t.stride(), t.shape
+    if len(sh) == 3:
+        return (0, *st), (1, *sh)
+    if len(sh) != 4:
+        raise ValueError("[B, N, heads, d] or [N, heads, d] expected")
+    return st, sh
+
+
+def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q_weight=None,
+                      k_weight=None, norm: bool = True, eps: float = 1e-6, stream=None):
+    """Norm of each head (norm=False: none) and rotation by position of q [B,N,H,d]
+    into q_out and, in the same launch, of k [B,N,Hkv,d] into k_out (bf16 or fp32, any
+    16-byte aligned strides, d contiguous; without B for one sequence; an output may
+    be its input).  positions int32 [B,N,axes] or [N,axes] (one axis: [B,N] or [N] as
+    well; None if nothing turns), the axes contiguous."""
+    qs, (B, N, H, d) = _axes4(q)
+    os_, shape = _axes4(q_out)
+    dtype, index = q.dtype, rotary._index
+    if tuple(shape) != (B, N, H, d) or (k is None) != (k_out is None):
+        raise ValueError("q / q_out shapes disagree, or one of k and k_out is missing")
+    dt = _dtype_code(q)
+    tensors = [q, q_out]
+    Hkv = 0
+    k_at = ks = ko_at = kos = None
+    if k is not None:
+        ks, (kB, kN, Hkv, kd) = _axes4(k)
+        kos, kshape = _axes4(k_out)
+        if (kB, kN, kd) != (B, N, d) or tuple(kshape) != (B, N, Hkv, d) or Hkv == 0:
+            raise ValueError("k / k_out must be [B, N, Hkv, d] beside q")
+        if k.dtype != dtype or k_out.dtype != dtype:
+            raise TypeError("q, k and their outputs' dtypes differ")
+        tensors += [k, k_out]
+        if ks[3] != 1 or kos[3] != 1:
+            raise ValueError("the head-dim axis must be contiguous")
+        k_at, ko_at = k.data_ptr(), k_out.data_ptr()
+        ks, kos = _Int64x3(*ks[:3]), _Int64x3(*kos[:3])
+    if q_out.dtype != dtype:
+        raise TypeError("q, k and their outputs' dtypes differ")
+    if qs[3] != 1 or os_[3] != 1:
+        raise ValueError("the head-dim axis must be contiguous")
+    if max(B, N, H, Hkv, d) > _INT_MAX:
+        raise ValueError("sizes of more than 32 bits")
+    p_at, p_sb, p_sn = None, 0, 0
+    if rotary.rot:
+        p_at, p_sb, p_sn = _positions(rotary, positions, B, N)
+        tensors.append(positions)
+    for t in tensors:
+        if t.get_device() != index:
+            raise ValueError("tensor on %s, the rotary is on %s" % (t.device, rotary.device))
+    rc = rotary._call(rotary._ref, dt, B, N, d, p_at, p_sb, p_sn, q.data_ptr(), H, _Int64x3(*qs[:3]),
+                      q_out.data_ptr(), _Int64x3(*os_[:3]), k_at, Hkv, ks, ko_at, kos,
+                      1 if norm else 0, _weight_at(q_weight, d, dtype, index),
+                      _weight_at(k_weight, d, dtype, index), eps, _rotary_stream(rotary, stream))
+    if rc != 0:
+        _check("avits_norm_rotate", rc)
+    return q_out
+
+
+def _positions(rotary: Rotary, p, B, N):
+    """Address and strides (sequence, token) of the positions of [B,N] tokens."""
+    if p is None or p.dtype != _torch().int32:
+        raise ValueError("positions must be an int32 tensor")
+    shape, st = tuple(p.shape), p.stride()
+    if rotary.axes == 1 and shape == (N,):
+        return p.data_ptr(), 0, st[0]
+    if rotary.axes == 1 and shape == (B, N):
+        return p.data_ptr(), st[0], st[1]
+    if shape == (N, rotary.axes):
+        at = (0, st[0])
+    elif shape == (B, N, rotary.axes):
+        at = (st[0], st[1])
+    else:
+        raise ValueError("positions must be [B, N, axes] or [N, axes]")
+    if rotary.axes > 1 and st[-1] != 1:
+        raise ValueError("the positions' axes must be contiguous")
+    return (p.data_ptr(), *at)
+
+
+def _rotary_stream(rotary: Rotary, stream):
+    """The stream's handle, on the current device: the rotary has to be there."""
+    C = _torch()._C
+    if C._cuda_getDevice() != rotary._index:
+        raise ValueError("the rotary is on %s, which is not the current device" % rotary.device)
+    return C._cuda_getCurrentRawStream(rotary._index) if stream is None else _stream(stream)
+
+
+def avits_cache_append_rotated(cache: KVCache, rotary: Rotary, positions, slots, q, q_out, k_new,
+                               v_new, q_weight=None, k_weight=None, norm: bool = True,
+                               eps: float = 1e-6, seq=None, place=None, stream=None):
+    """The T rows of a step: q [T,H,d] normed and rotated into q_out, k_new [T,Hkv,d]
+    likewise into the cache and v_new [T,Hkv,d] as it is, at the places that slots ([T]
+    int64, avits_cache_plan) says; a row of a negative slot is padding and left alone.
+    positions [T] or [T, axes] int32.  A cache with acc needs seq and place ([T] int32):
+    the tokens' accumulated weights start at zero."""
+    T, H, d = shape = q.shape
+    Hkv, dtype, index = cache.Hkv, cache.dtype, cache._index
+    if d != cache.d or q_out.shape != shape or k_new.shape != (T, Hkv, d) or \
+            v_new.shape != (T, Hkv, d):
+        raise ValueError("q / q_out must be [T, H, d], k_new / v_new [T, Hkv, d] of the cache")
+    if T > _INT_MAX or H > _INT_MAX:
+        raise ValueError("sizes of more than 32 bits")
+    if q.dtype != dtype or q_out.dtype != dtype or k_new.dtype != dtype or v_new.dtype != dtype:
+        raise TypeError("q, q_out, k_new, v_new and cache dtypes differ")
+    q_st, q_sh, q_sd = q.stride()
+    o_st, o_sh, o_sd = q_out.stride()
+    k_st, k_sh, k_sd = k_new.stride()
+    v_st, v_sh, v_sd = v_new.stride()
+    if q_sd != 1 or o_sd != 1 or k_sd != 1 or v_sd != 1:
+        raise ValueError("the head-dim axis must be contiguous")
+    if slots.shape != (T,) or slots.dtype != _torch().int64 or not slots.is_contiguous():
+        raise ValueError("slots must be a contiguous int64 [T] tensor")
+    s_at = p_at = None
+    if seq is not None or place is not None or cache.acc is not None:
+        for t in (seq, place):
+            if t is None or t.shape != (T,) or t.dtype != cache.int32 or not t.is_contiguous():
+                raise ValueError("seq and place must be contiguous int32 [T] tensors")
+        _elsewhere(cache, seq, place)
+        s_at, p_at = seq.data_ptr(), place.data_ptr()
+    x_at, x_st = None, 0
+    if rotary.rot:
+        x_at, _, x_st = _positions(rotary, positions, 1, T)
+        _elsewhere(cache, positions)
+    if rotary._index != index or q.get_device() != index or q_out.get_device() != index or \
+            k_new.get_device() != index or v_new.get_device() != index or slots.get_device() != index:
+        _elsewhere(cache, rotary.freq, q, q_out, k_new, v_new, slots)
+    rc = cache._append_rotated(cache._ref, rotary._ref, T, x_at, x_st, slots.data_ptr(), s_at, p_at,
+                               q.data_ptr(), H, q_st, q_sh, q_out.data_ptr(), o_st, o_sh,
+                               k_new.data_ptr(), k_st, k_sh, v_new.data_ptr(), v_st, v_sh,
+                               1 if norm else 0, _weight_at(q_weight, d, dtype, index),
+                               _weight_at(k_weight, d, dtype, index), eps,
+                               _call_stream(cache, stream))
+    if rc != 0:
+        _check("avits_cache_append_rotated", rc)
+    return q_out

@@ -2,6 +2,7 @@
 // checks, workspace sizing and dispatch to the kernels.  Nothing here
 // allocates device memory or synchronises, except avits_device_status().
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <string>
@@ -118,6 +119,25 @@ avits_status check_cache(const avits_kv_cache* c) {
   for (int64_t st : {c->k_sp, c->k_st, c->k_sh, c->v_sp, c->v_st, c->v_sh})
     if (st % per16) return AVITS_ERR_UNSUPPORTED;
   return AVITS_OK;
+}
+
+bool rotary_ok(const avits_rotary* r, int d, const void* positions) {
+  if (!r || r->rot < 0 || r->rot % 2 || r->rot > d) return false;
+  if (r->rot == 0) return true;
+  if (!r->freq || !positions || r->axes < 1 || r->axes > 4 || !(std::fabs(r->magnitude) < 3.0e38f))
+    return false;
+  int64_t pairs = 0;
+  for (int i = 0; i < r->axes; ++i) {
+    if (r->sections[i] < 0) return false;
+    pairs += r->sections[i];
+  }
+  return pairs == r->rot / 2;
+}
+bool norm_ok(int norm, const void* q_weight, const void* k_weight, float eps) {
+  return norm ? eps >= 0.f && eps < 3.0e38f : !q_weight && !k_weight;
+}
+bool same_strides(const int64_t* a, const int64_t* b, int64_t n0, int64_t n1, int64_t n2) {
+  return (n0 == 1 || a[0] == b[0]) && (n1 == 1 || a[1] == b[1]) && (n2 == 1 || a[2] == b[2]);
 }
 
 }  // namespace
@@ -535,6 +555,167 @@ avits_status avits_cache_evict(const avits_kv_cache* src, const avits_kv_cache* 
   if (dst->k_pages == dst->v_pages) return AVITS_ERR_INVALID_ARG;
   return cuda_status(launch_cache_evict(*src, *dst, keep, sinks, recent, keep_idx, num_sms_current(),
                                         status_word(), static_cast<cudaStream_t>(stream)));
+}
+
+avits_status avits_cache_plan(const avits_kv_cache* cache, const int32_t* lens,
+                              const int32_t* change, int32_t* free_pages,
+                              const int32_t* free_count, int32_t* free_out, int T,
+                              int32_t* cu_new, int64_t* slots, int32_t* seq, int32_t* place,
+                              int32_t* pos_opt, const int32_t* pos_base_opt, void* stream) {
+  AVITS_RANGE();
+  if (T < 0 || !lens || !change || !free_pages || !free_count || !free_out || !cu_new ||
+      (T > 0 && (!slots || !seq || !place)))
+    return AVITS_ERR_INVALID_ARG;
+  const avits_status ok = check_cache(cache);
+  if (ok != AVITS_OK) return ok;
+  if (cache->B > 1 && cache->table_sb < ((int64_t)cache->max_len - 1) / cache->page_size + 1)
+    return AVITS_ERR_INVALID_ARG;
+  if (T > (1 << 30)) return AVITS_ERR_UNSUPPORTED;
+  const CachePlanCall call{*cache, lens, change, free_pages, free_count, free_out, T, cu_new,
+                           slots, seq, place, pos_opt, pos_base_opt};
+  return cuda_status(launch_cache_plan(call, status_word(), static_cast<cudaStream_t>(stream)));
+}
+
+avits_status avits_rotary_frequencies(int width, double base, int scaling, double factor,
+                                      double original_len, double low, double high,
+                                      uint64_t* freq) {
+  if (!freq || width <= 0 || width % 2 || width > 256 || !(base > 0.0) || !std::isfinite(base))
+    return AVITS_ERR_INVALID_ARG;
+  if (scaling < AVITS_SCALE_NONE || scaling > AVITS_SCALE_PARTS) return AVITS_ERR_INVALID_ARG;
+  if (scaling != AVITS_SCALE_NONE && (!(factor >= 1.0) || !std::isfinite(factor)))
+    return AVITS_ERR_INVALID_ARG;
+  if (scaling == AVITS_SCALE_PARTS &&
+      (!(original_len > 0.0) || !std::isfinite(original_len) || !(low < high) ||
+       !std::isfinite(low) || !std::isfinite(high)))
+    return AVITS_ERR_INVALID_ARG;
+  if (scaling == AVITS_SCALE_BASE && width > 2)
+    base *= std::pow(factor, (double)width / (width - 2));
+  constexpr double kTurn = 6.283185307179586476925286766559;
+  uint64_t out[128];
+  for (int i = 0; i < width / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / width) / kTurn;
+    if (scaling == AVITS_SCALE_LINEAR) f /= factor;
+    if (scaling == AVITS_SCALE_PARTS) {
+      const double g = std::min(1.0, std::max(0.0, (original_len * f - low) / (high - low)));
+      f = g * f + (1.0 - g) * f / factor;
+    }
+    if (!(f < 0.5)) return AVITS_ERR_INVALID_ARG;
+    out[i] = (uint64_t)std::nearbyint(std::ldexp(f, 64));
+  }
+  std::copy(out, out + width / 2, freq);
+  return AVITS_OK;
+}
+
+avits_status avits_norm_rotate(const avits_rotary* rot, avits_dtype dt, int B, int N, int d,
+                               const int32_t* positions, int64_t pos_sb, int64_t pos_sn,
+                               const void* q, int H, const int64_t* q_str, void* q_out,
+                               const int64_t* qo_str, const void* k, int Hkv,
+                               const int64_t* k_str, void* k_out, const int64_t* ko_str, int norm,
+                               const void* q_weight, const void* k_weight, float eps,
+                               void* stream) {
+  AVITS_RANGE();
+  if (!q || !q_out || !q_str || !qo_str || !valid_dtype(dt) || B <= 0 || N <= 0 || H <= 0 ||
+      Hkv < 0 || d <= 0)
+    return AVITS_ERR_INVALID_ARG;
+  if ((Hkv > 0) != (k != nullptr) || (Hkv > 0 && (!k_out || !k_str || !ko_str)))
+    return AVITS_ERR_INVALID_ARG;
+  if (!rotary_ok(rot, d, positions) || pos_sb < 0 || pos_sn < 0) return AVITS_ERR_INVALID_ARG;
+  if (!norm_ok(norm, q_weight, k_weight, eps)) return AVITS_ERR_INVALID_ARG;
+  const int per16 = dt == AVITS_BF16 ? 8 : 4;
+  if (d > 256 || d % per16 || (int64_t)B * N > (1 << 30) || H > (1 << 16) || Hkv > (1 << 16))
+    return AVITS_ERR_UNSUPPORTED;
+  const int64_t* in[2] = {q_str, k_str};
+  const int64_t* out[2] = {qo_str, ko_str};
+  const void* from[2] = {q, k};
+  const void* to[2] = {q_out, k_out};
+  for (int i = 0; i < (Hkv > 0 ? 2 : 1); ++i) {
+    const int heads = i ? Hkv : H;
+    for (int x = 0; x < 3; ++x) {
+      if (in[i][x] < 0 || out[i][x] < 0) return AVITS_ERR_INVALID_ARG;
+      if (in[i][x] % per16 || out[i][x] % per16) return AVITS_ERR_UNSUPPORTED;
+    }
+    if (!aligned16(from[i]) || !aligned16(to[i])) return AVITS_ERR_UNSUPPORTED;
+    if (!rows_apart(d, {B, out[i][0]}, {N, out[i][1]}, {heads, out[i][2]}))
+      return AVITS_ERR_INVALID_ARG;
+    if (from[i] == to[i] && !same_strides(in[i], out[i], B, N, heads)) return AVITS_ERR_INVALID_ARG;
+    if (to[i] == from[1 - i]) return AVITS_ERR_INVALID_ARG;
+  }
+  if (q_out == k_out) return AVITS_ERR_INVALID_ARG;
+  if (!aligned16(q_weight) || !aligned16(k_weight)) return AVITS_ERR_UNSUPPORTED;
+  RotateCall c{};
+  c.rot = *rot;
+  c.dt = dt;
+  c.tokens = B * N;
+  c.N = N; c.H = H; c.Hkv = Hkv; c.d = d;
+  c.positions = positions;
+  c.pos_sb = pos_sb; c.pos_sn = pos_sn;
+  c.q = q; c.q_out = q_out; c.k = k; c.k_out = k_out;
+  for (int x = 0; x < 3; ++x) {
+    c.q_str[x] = q_str[x];
+    c.qo_str[x] = qo_str[x];
+    c.k_str[x] = Hkv > 0 ? k_str[x] : 0;
+    c.ko_str[x] = Hkv > 0 ? ko_str[x] : 0;
+  }
+  c.norm = norm ? 1 : 0;
+  c.q_weight = q_weight; c.k_weight = k_weight;
+  c.eps = eps;
+  return cuda_status(launch_norm_rotate(c, false, num_sms_current(), status_word(),
+                                        static_cast<cudaStream_t>(stream)));
+}
+
+avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits_rotary* rot, int T,
+                                        const int32_t* positions, int64_t pos_st,
+                                        const int64_t* slots, const int32_t* seq,
+                                        const int32_t* place, const void* q, int H, int64_t q_st,
+                                        int64_t q_sh, void* q_out, int64_t qo_st, int64_t qo_sh,
+                                        const void* k_new, int64_t k_st, int64_t k_sh,
+                                        const void* v_new, int64_t v_st, int64_t v_sh, int norm,
+                                        const void* q_weight, const void* k_weight, float eps,
+                                        void* stream) {
+  AVITS_RANGE();
+  if (T < 0 || H <= 0 || (T > 0 && (!slots || !q || !q_out || !k_new || !v_new)))
+    return AVITS_ERR_INVALID_ARG;
+  for (int64_t st : {q_st, q_sh, qo_st, qo_sh, k_st, k_sh, v_st, v_sh, pos_st})
+    if (st < 0) return AVITS_ERR_INVALID_ARG;
+  const avits_status ok = check_cache(cache);
+  if (ok != AVITS_OK) return ok;
+  if (!rotary_ok(rot, cache->d, T > 0 ? positions : cache->lens) ||
+      !norm_ok(norm, q_weight, k_weight, eps))
+    return AVITS_ERR_INVALID_ARG;
+  if (cache->acc && T > 0 && (!seq || !place)) return AVITS_ERR_INVALID_ARG;
+  if (T > (1 << 30) || H > (1 << 16)) return AVITS_ERR_UNSUPPORTED;
+  if (T == 0) return AVITS_OK;
+  if (!pages_apart(*cache) || (cache->acc && !weights_apart(*cache)) ||
+      cache->k_pages == cache->v_pages)
+    return AVITS_ERR_INVALID_ARG;
+  const int per16 = cache->dt == AVITS_BF16 ? 8 : 4;
+  for (const void* p : {q, static_cast<const void*>(q_out), k_new, v_new, q_weight, k_weight})
+    if (!aligned16(p)) return AVITS_ERR_UNSUPPORTED;
+  for (int64_t st : {q_st, q_sh, qo_st, qo_sh, k_st, k_sh, v_st, v_sh})
+    if (st % per16) return AVITS_ERR_UNSUPPORTED;
+  if (!rows_apart(cache->d, {T, qo_st}, {H, qo_sh})) return AVITS_ERR_INVALID_ARG;
+  if (q == q_out && ((T > 1 && q_st != qo_st) || (H > 1 && q_sh != qo_sh)))
+    return AVITS_ERR_INVALID_ARG;
+  if (q_out == k_new || q_out == v_new || q_out == cache->k_pages || q_out == cache->v_pages)
+    return AVITS_ERR_INVALID_ARG;
+  RotateCall c{};
+  c.rot = *rot;
+  c.dt = static_cast<avits_dtype>(cache->dt);
+  c.tokens = T;
+  c.N = T; c.H = H; c.Hkv = cache->Hkv; c.d = cache->d;
+  c.positions = positions;
+  c.pos_sn = pos_st;
+  c.q = q; c.q_out = q_out; c.k = k_new;
+  c.q_str[1] = q_st; c.q_str[2] = q_sh; c.qo_str[1] = qo_st; c.qo_str[2] = qo_sh;
+  c.k_str[1] = k_st; c.k_str[2] = k_sh;
+  c.norm = norm ? 1 : 0;
+  c.q_weight = q_weight; c.k_weight = k_weight;
+  c.eps = eps;
+  c.cache = *cache;
+  c.slots = slots; c.seq = seq; c.place = place;
+  c.v = v_new; c.v_st = v_st; c.v_sh = v_sh;
+  return cuda_status(launch_norm_rotate(c, true, num_sms_current(), status_word(),
+                                        static_cast<cudaStream_t>(stream)));
 }
 
 avits_status avits_selftest_bounded_wait(unsigned long long limit_ns, long long* result,

@@ -171,4 +171,49 @@ cudaError_t launch_cache_evict(const avits_kv_cache& src, const avits_kv_cache& 
                                int sinks, int recent, int32_t* idx, int num_sms,
                                unsigned int* status, cudaStream_t s);
 
+// ---- a served batch's step around the cache -----------------------------------
+struct CachePlanCall {
+  avits_kv_cache cache;      // its lens and table are written
+  const int32_t* lens;
+  const int32_t* change;
+  int32_t* free_pages;
+  const int32_t* free_count;
+  int32_t* free_out;
+  int T;
+  int32_t* cu_new;
+  int64_t* slots;
+  int32_t* seq;
+  int32_t* place;
+  int32_t* pos;              // or NULL
+  const int32_t* pos_base;   // or NULL
+};
+cudaError_t launch_cache_plan(const CachePlanCall& call, unsigned int* status, cudaStream_t s);
+
+// Norm and rotation: tokens [B,N], or the T rows of an append (B = 1, N = T).
+struct RotateCall {
+  avits_rotary rot;
+  avits_dtype dt;
+  int tokens, N, H, Hkv, d;
+  const int32_t* positions;
+  int64_t pos_sb, pos_sn;
+  const void* q;
+  void* q_out;
+  const void* k;
+  void* k_out;
+  int64_t q_str[3], qo_str[3], k_str[3], ko_str[3];   // elements: sequence, token, head
+  int norm;
+  const void* q_weight;
+  const void* k_weight;
+  float eps;
+  // an append's: k goes to the pages, v beside it
+  avits_kv_cache cache;
+  const int64_t* slots;
+  const int32_t* seq;
+  const int32_t* place;
+  const void* v;
+  int64_t v_st, v_sh;
+};
+cudaError_t launch_norm_rotate(const RotateCall& call, bool append, int num_sms,
+                               unsigned int* status, cudaStream_t s);
+
 }  // namespace avits
