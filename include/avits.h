@@ -43,6 +43,8 @@
  *   avits_norm_rotate         norm of each head and rotation by position, queries
  *                             and keys in one pass (also of an image's tokens)
  *   avits_cache_append_rotated  the same, keys and values into the pages
+ *   avits_cache_attention_shared  one new token per sequence over a prefix that its
+ *                             group shares, read once, and its own cached tokens
  *
  * Conventions shared by every call
  * --------------------------------
@@ -705,6 +707,38 @@ avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits
                                         const void* v_new, int64_t v_st, int64_t v_sh, int norm,
                                         const void* q_weight, const void* k_weight, float eps,
                                         void* stream);
+
+/* ------------------------------------------------------------------------
+ * avits_cache_attention for sequences that have a prefix in common (an instruction, a
+ * document), which is read once for all of a group: sequence b of group g attends to the
+ * prefix->lens[g] tokens of row g of `prefix` and to the cache->lens[b] tokens of its own,
+ *
+ *     x_bhj = softmax_scale * <q_bh, k_j>     j over both
+ *     lse   = log sum_j exp(x_bhj),   o_bh = sum_j exp(x_bhj - lse) v_j
+ *
+ * cache  : the B sequences' own tokens (their places start at 0 behind the prefix).
+ * prefix : a cache of its own, one row per group: same type, Hkv and d, of the same pool
+ *          or another, with a page size and max_len of its own.  What is left of acc is not
+ *          used: the call gives no weights.
+ * group_start : [prefix->B + 1] int32: sequences group_start[g] .. group_start[g+1]-1 are
+ *          group g.  It does not decrease, from 0 or more to B or less; sequences before the
+ *          first and from the last on have no prefix.  Otherwise AVITS_ERR_PAGE is raised
+ *          and no sequence has one.
+ * A sequence without any token gets o = 0 and lse = -inf.  What avits_cache_attention says
+ * of infinite values, sizes and strides holds here (in bf16 the weights of prefixes enter
+ * the products as 2 bf16 parts too).
+ * workspace/ws_bytes : at least avits_cache_attention_shared_workspace(...) bytes,
+ *          16-byte aligned, of any content; not used by two calls at once.  It grows with
+ *          B H d, with the groups, and with the SMs, not with lengths. */
+avits_status avits_cache_attention_shared(const avits_kv_cache* cache, const avits_kv_cache* prefix,
+                                          const int32_t* group_start, const void* q, int H,
+                                          int64_t q_sb, int64_t q_sh, float softmax_scale, void* o,
+                                          int64_t o_sb, int64_t o_sh, float* lse_opt,
+                                          void* workspace, size_t ws_bytes, void* stream);
+
+/* Workspace bytes for these sizes on the CURRENT device (0 for invalid sizes). */
+size_t avits_cache_attention_shared_workspace(const avits_kv_cache* cache,
+                                              const avits_kv_cache* prefix, int H);
 
 /* ------------------------------------------------------------------------
  * Test hook for the failure detection of the device-side waits (a library

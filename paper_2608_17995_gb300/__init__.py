@@ -28,6 +28,8 @@ Calls:
   avits_norm_rotate         norm of each head and rotation by position (Rotary),
                             queries and keys in one pass
   avits_cache_append_rotated  the same, keys and values into a cache's pages
+  avits_cache_attention_shared  one new token per sequence over a prefix that its
+                            group shares and its own cached tokens
   avits_device_status       device-side error word (read and cleared)
 """
 from __future__ import annotations
@@ -50,7 +52,8 @@ __all__ = [
     "avits_merge_final", "avits_merge_final_workspace", "avits_device_status",
     "KVCache", "avits_cache_append", "avits_cache_attention", "avits_cache_attention_workspace",
     "avits_cache_evict", "avits_cache_plan", "Rotary", "avits_norm_rotate",
-    "avits_cache_append_rotated",
+    "avits_cache_append_rotated", "avits_cache_attention_shared",
+    "avits_cache_attention_shared_workspace",
     "avits_selftest_bounded_wait", "avits_status_string", "avits_version", "SpatialWorkspace",
 ]
 
@@ -125,6 +128,9 @@ def lib():
         "avits_cache_attention_workspace": [vp, i32, i32],
         "avits_cache_evict": [vp, vp, i32, i32, i32, vp, vp],
         "avits_cache_plan": [vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp],
+        "avits_cache_attention_shared": [vp, vp, vp, vp, i32, i64, i64, f32, vp, i64, i64, vp, vp, sz,
+                                         vp],
+        "avits_cache_attention_shared_workspace": [vp, vp, i32],
         "avits_rotary_frequencies": [i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double,
                                      ctypes.c_double, ctypes.c_double, vp],
         "avits_norm_rotate": [vp, i32, i32, i32, i32, vp, i64, i64, vp, i32, vp, vp, vp, vp, i32, vp,
@@ -143,7 +149,8 @@ def lib():
         fn.restype = ctypes.c_int
     for name in ("avits_score_spatial_workspace", "avits_merge_final_workspace",
                  "avits_score_spatial_noalloc_limit", "avits_attention_forward_workspace",
-                 "avits_selective_upsample_workspace", "avits_cache_attention_workspace"):
+                 "avits_selective_upsample_workspace", "avits_cache_attention_workspace",
+                 "avits_cache_attention_shared_workspace"):
         getattr(L, name).restype = ctypes.c_size_t
     for name in ("avits_status_string", "avits_last_error_string", "avits_version",
                  "avits_score_spatial_noalloc_error"):
@@ -580,7 +587,8 @@ class KVCache:
     """
     __slots__ = ("k_pages", "v_pages", "block_table", "lens", "acc", "B", "Hkv", "d", "dtype",
                  "page_size", "max_len", "device", "int32", "float32", "_index", "_struct", "_ref",
-                 "_need", "_alloc", "_free", "_append", "_attend", "_plan", "_append_rotated", "_evict")
+                 "_need", "_alloc", "_free", "_append", "_attend", "_plan", "_append_rotated", "_shared", "_shared_need",
+                 "_evict")
 
     def __init__(self, k_pages, v_pages, block_table, lens, acc=None, max_len: Optional[int] = None):
         torch = _torch()
@@ -634,6 +642,7 @@ class KVCache:
         self._free = torch._C._cuda_cudaCachingAllocator_raw_delete
         L = lib()
         self._append, self._attend = L.avits_cache_append, L.avits_cache_attention
+        self._shared, self._shared_need = L.avits_cache_attention_shared, {}
         self._plan, self._append_rotated = L.avits_cache_plan, L.avits_cache_append_rotated
         self._evict = L.avits_cache_evict
 
@@ -1035,3 +1044,76 @@ def avits_cache_append_rotated(cache: KVCache, rotary: Rotary, positions, slots,
     if rc != 0:
         _check("avits_cache_append_rotated", rc)
     return q_out
+
+
+def avits_cache_attention_shared_workspace(cache: KVCache, prefix: KVCache, H: int) -> int:
+    if not 0 < H <= _INT_MAX:
+        return 0
+    return int(lib().avits_cache_attention_shared_workspace(cache._ref, prefix._ref, H))
+
+
+def _shared_bytes(cache: KVCache, prefix: KVCache, H: int) -> int:
+    """The same by what it depends on of the prefix: kept with the cache."""
+    key = (H, prefix.B, prefix.max_len, prefix.page_size, prefix.Hkv, prefix.d, prefix.dtype,
+           prefix.k_pages.stride(), prefix.v_pages.stride())
+    need = cache._shared_need.get(key)
+    if need is None:
+        need = cache._shared_need[key] = avits_cache_attention_shared_workspace(cache, prefix, H)
+    return need
+
+
+def avits_cache_attention_shared(cache: KVCache, prefix: KVCache, group_start, q,
+                                 softmax_scale: float, o, lse=None, workspace=None, stream=None):
+    """avits_cache_attention for sequences that have a prefix in common: sequence b of
+    group g (group_start[g] <= b < group_start[g+1]; int32 [prefix.B + 1]) attends to row
+    g of ``prefix``, which is read once for the whole group, and to its own tokens in
+    ``cache``.  q [B,H,d] into o [B,H,d] and lse [B,H] fp32, as there; no weights.
+    ``workspace``: as there, avits_cache_attention_shared_workspace() bytes."""
+    B, H, d = shape = q.shape
+    if B != cache.B or d != cache.d or o.shape != shape:
+        raise ValueError("q and o must be [B, H, d] of the cache")
+    if H > _INT_MAX:
+        raise ValueError("more heads than 32 bits count")
+    if q.dtype != cache.dtype or o.dtype != cache.dtype or prefix.dtype != cache.dtype:
+        raise TypeError("q, o and the caches' dtypes differ")
+    if prefix.Hkv != cache.Hkv or prefix.d != d:
+        raise ValueError("the two caches' heads differ")
+    q_sb, q_sh, q_sd = q.stride()
+    o_sb, o_sh, o_sd = o.stride()
+    if q_sd != 1 or o_sd != 1:
+        raise ValueError("the head-dim axis must be contiguous")
+    if group_start.shape != (prefix.B + 1,) or group_start.dtype != cache.int32 or \
+            not group_start.is_contiguous():
+        raise ValueError("group_start must be a contiguous int32 [prefix.B + 1] tensor")
+    index = cache._index
+    if q.get_device() != index or o.get_device() != index or prefix._index != index or \
+            group_start.get_device() != index:
+        _elsewhere(cache, q, o, prefix.k_pages, group_start)
+    lse_at = None
+    if lse is not None:
+        if lse.shape != (B, H) or lse.dtype != cache.float32 or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous float32 [B,H] tensor")
+        if lse.get_device() != index:
+            _elsewhere(cache, lse)
+        lse_at = lse.data_ptr()
+    handle = _call_stream(cache, stream)
+    own = None
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        _elsewhere(cache, workspace)
+        ws_at, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    else:
+        # as avits_cache_attention's: of this call and its stream
+        ws_bytes = _shared_bytes(cache, prefix, H)
+        ws_at = own = cache._alloc(ws_bytes, handle) if ws_bytes else None
+    try:
+        rc = cache._shared(cache._ref, prefix._ref, group_start.data_ptr(), q.data_ptr(), H, q_sb,
+                           q_sh, softmax_scale, o.data_ptr(), o_sb, o_sh, lse_at, ws_at, ws_bytes,
+                           handle)
+    finally:
+        if own is not None:
+            cache._free(own)
+    if rc != 0:
+        _check("avits_cache_attention_shared", rc)
+    return o

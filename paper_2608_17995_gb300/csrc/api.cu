@@ -718,6 +718,53 @@ avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits
                                         static_cast<cudaStream_t>(stream)));
 }
 
+// Descriptions that avits_cache_attention_shared takes together, with H heads.
+static avits_status check_shared(const avits_kv_cache* cache, const avits_kv_cache* prefix, int H) {
+  for (const avits_kv_cache* c : {cache, prefix}) {
+    const avits_status ok = check_cache(c);
+    if (ok != AVITS_OK) return ok;
+  }
+  if (cache->dt != prefix->dt || cache->Hkv != prefix->Hkv || cache->d != prefix->d || H <= 0 ||
+      H % cache->Hkv)
+    return AVITS_ERR_INVALID_ARG;
+  CacheSharedCall call{};
+  call.cache = *cache;
+  call.prefix = *prefix;
+  call.H = H;
+  return cache_shared_sizes_ok(call) ? AVITS_OK : AVITS_ERR_UNSUPPORTED;
+}
+
+size_t avits_cache_attention_shared_workspace(const avits_kv_cache* cache,
+                                              const avits_kv_cache* prefix, int H) {
+  if (check_shared(cache, prefix, H) != AVITS_OK) return 0;
+  CacheSharedCall call{};
+  call.cache = *cache;
+  call.prefix = *prefix;
+  call.H = H;
+  return cache_shared_workspace(call, num_sms_current());
+}
+
+avits_status avits_cache_attention_shared(const avits_kv_cache* cache, const avits_kv_cache* prefix,
+                                          const int32_t* group_start, const void* q, int H,
+                                          int64_t q_sb, int64_t q_sh, float softmax_scale, void* o,
+                                          int64_t o_sb, int64_t o_sh, float* lse_opt,
+                                          void* workspace, size_t ws_bytes, void* stream) {
+  AVITS_RANGE();
+  if (!group_start || !q || !o || q_sb < 0 || q_sh < 0 || o_sb < 0 || o_sh < 0)
+    return AVITS_ERR_INVALID_ARG;
+  if (!(softmax_scale > 0.f) || !(softmax_scale < 3.0e38f)) return AVITS_ERR_INVALID_ARG;
+  const avits_status ok = check_shared(cache, prefix, H);
+  if (ok != AVITS_OK) return ok;
+  if (!rows_apart(cache->d, {cache->B, o_sb}, {H, o_sh})) return AVITS_ERR_INVALID_ARG;
+  const CacheSharedCall call{*cache, *prefix, group_start, q, H, q_sb, q_sh, softmax_scale,
+                             o, o_sb, o_sh, lse_opt, workspace};
+  const int sms = num_sms_current();
+  if (!workspace || !aligned16(workspace) || ws_bytes < cache_shared_workspace(call, sms))
+    return AVITS_ERR_INVALID_ARG;
+  return cuda_status(
+      launch_cache_shared(call, sms, status_word(), static_cast<cudaStream_t>(stream)));
+}
+
 avits_status avits_selftest_bounded_wait(unsigned long long limit_ns, long long* result,
                                          void* stream) {
   AVITS_RANGE();

@@ -216,4 +216,22 @@ struct RotateCall {
 cudaError_t launch_norm_rotate(const RotateCall& call, bool append, int num_sms,
                                unsigned int* status, cudaStream_t s);
 
+// One new token per sequence over its group's prefix and its own tokens.
+struct CacheSharedCall {
+  avits_kv_cache cache, prefix;
+  const int32_t* group_start;   // [prefix.B + 1]
+  const void* q;
+  int H;
+  int64_t q_sb, q_sh;
+  float scale;
+  void* o;
+  int64_t o_sb, o_sh;
+  float* lse;                   // [B,H] or NULL
+  void* ws;
+};
+bool cache_shared_sizes_ok(const CacheSharedCall& s);
+size_t cache_shared_workspace(const CacheSharedCall& s, int num_sms);
+cudaError_t launch_cache_shared(const CacheSharedCall& s, int num_sms, unsigned int* status,
+                                cudaStream_t stream);
+
 }  // namespace avits

@@ -44,6 +44,7 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
   // rows to a unit 22.0 us without it, 21.3 with).
   const int tid = threadIdx.x, w = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int unit = blockIdx.x / ncta, units = a.c.Hkv * a.groups;
+  const OwnUnits all{units, a.groups};
   const int b = unit / units, u = unit - b * units;
   const int hk = u / a.groups, row0 = (u - hk * a.groups) * kR;
   const int h0 = hk * a.G + row0, rows_here = min(kR, a.G - row0);
@@ -82,14 +83,14 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
 #pragma unroll
   for (int k = 0; k < kQEach; ++k)
     if (tid + k * kCta < Rows::kQPieces)
-      q[k] = Rows::load_q(a, b, h0, rows_here, tid + k * kCta);
+      q[k] = Rows::load_q(a, QRows{b, h0, rows_here, 0, 0}, tid + k * kCta);
   int fill = 0, use = 0;
   uint32_t phase = 0;
   int late = 0;         // a copy did not come in time: the others get little more
   auto issue = [&]() {
     if (cur.left > 0)
       copy_tile<Rows, W>(mk, mv, a, cur, ring + fill * Rows::kStage, &s_full[w][fill],
-                         &s_mask[w][fill], units, lane);
+                         &s_mask[w][fill], all, lane);
     fill = fill + 1 == NS ? 0 : fill + 1;
   };
 #pragma unroll 1

@@ -54,6 +54,40 @@ struct CacheAttn {
   float* logits;    // [B,H,ld] log2-domain logits (weights wanted)
   int64_t ld;
   unsigned int* status;
+  // attention over prefixes that groups of sequences share: the prefixes' cache is c, and
+  const int32_t* start;   // [c.B + 1] first sequence of each group
+  int seqs;               // sequences of the batch
+  int most;               // units that the workspace has room for
+  int* base;              // [c.B + 1] first unit of each group; the last: 1 if the groups rise
+};
+
+// Sequences [x, y) of group g.
+__device__ __forceinline__ int2 members_of(const int32_t* start, int seqs, int g) {
+  const int x = min(max(start[g], 0), seqs), y = min(max(start[g + 1], 0), seqs);
+  return make_int2(x, max(x, y));
+}
+
+// A sequence's units.  Its own tokens: each KV head's row groups, the same number in every
+// sequence.
+struct OwnUnits {
+  int n, groups;
+  __device__ __forceinline__ int of(const CacheAttn&, int) const { return n; }
+  __device__ __forceinline__ int head(const CacheAttn&, int, int u) const {
+    return groups == 1 ? u : u / groups;
+  }
+};
+// A prefix: each KV head's row groups over the query heads of all members.
+struct GroupUnits {
+  __device__ __forceinline__ static int row_groups(const CacheAttn& a, int g) {
+    const int2 m = members_of(a.start, a.seqs, g);
+    return ((m.y - m.x) * a.G + a.rows - 1) / a.rows;
+  }
+  __device__ __forceinline__ int of(const CacheAttn& a, int g) const {
+    return a.c.Hkv * row_groups(a, g);
+  }
+  __device__ __forceinline__ int head(const CacheAttn& a, int g, int u) const {
+    return u / row_groups(a, g);
+  }
 };
 
 // A row's maximum and sum -> what a weight is: exp2(x - .x) times .y.  Not exp2(x - lse):
@@ -94,15 +128,16 @@ struct Cursor {
   int left;         // tiles still to come
   int entry;        // table entry: of this lane's key, or of its box, of that tile
 
-  __device__ __forceinline__ void settle(const CacheAttn& a, int units) {
+  template <typename Units>
+  __device__ __forceinline__ void settle(const CacheAttn& a, const Units& units) {
     while (t >= nt) {
       t -= nt;
-      if (++u == units) {
+      if (++u == units.of(a, b)) {
         u = 0;
         do {
           len = cache_len(a.c, ++b);
           nt = tiles_of(a, len);
-        } while (nt == 0);
+        } while (nt == 0 || units.of(a, b) == 0);
       }
     }
   }
@@ -110,6 +145,17 @@ struct Cursor {
   __device__ __forceinline__ void look_up(const CacheAttn& a, int lane) {
     const int j = t * kTile + (a.box ? lane * a.box & (kTile - 1) : lane & (kTile - 1));
     entry = j < len ? a.c.block_table[(int64_t)b * a.c.table_sb + a.page.div(j)] : -1;
+  }
+};
+
+// A unit's rows: query heads h0 .. of sequence b, or, G > 0, rows of a group: row r is head
+// h0 + (r0 + r) % G of sequence b + (r0 + r) / G.
+struct QRows {
+  int b, h0, rows, r0, G;
+  __device__ __forceinline__ int64_t at(const CacheAttn& a, int row) const {
+    if (G == 0) return (int64_t)b * a.q_sb + (int64_t)(h0 + row) * a.q_sh;
+    const int x = (r0 + row) / G;
+    return (int64_t)(b + x) * a.q_sb + (int64_t)(h0 + r0 + row - x * G) * a.q_sh;
   }
 };
 
@@ -123,12 +169,12 @@ struct Cursor {
 // the width.  So the products run over whole widths of 64, 128 or 256 unchecked.
 // 48 x <= 1024 took 32.7 us by TMA and 35.3 by 16-byte copies, 40 x 24 heads of width
 // 64 54.2 and 58.4: a copy costs a warp instructions per row, a box one.
-template <typename Rows, int kStep>
+template <typename Rows, int kStep, typename Units>
 __device__ __forceinline__ void copy_tile(const CUtensorMap& mk, const CUtensorMap& mv,
                                           const CacheAttn& a, Cursor& cur, char* dst, uint64_t* bar,
-                                          uint32_t* mask, int units, int lane) {
+                                          uint32_t* mask, const Units& units, int lane) {
   constexpr int kTile = Rows::kTile, kEs = sizeof(typename Rows::T), D = Rows::D;
-  const int hk = a.groups == 1 ? cur.u : cur.u / a.groups;
+  const int hk = units.head(a, cur.b, cur.u);
   const int j0 = cur.t * kTile;
   unsigned ok;
   if (a.box) {
@@ -303,13 +349,11 @@ struct RowsBf16 {
   }
 
   // 16 bytes of Q: piece i of the unit's rows
-  __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, int b, int h0, int rows,
-                                                 int i) {
+  __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, const QRows& u, int i) {
     const int row = i / (D / 8), d = (i % (D / 8)) * 8;
     uint32_t w[4] = {0u, 0u, 0u, 0u};
-    if (row < rows && d < a.c.d) {
-      const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)b * a.q_sb +
-                          (int64_t)(h0 + row) * a.q_sh + d;
+    if (row < u.rows && d < a.c.d) {
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + u.at(a, row) + d;
       if ((reinterpret_cast<uintptr_t>(q) & 15u) == 0) return *reinterpret_cast<const uint4*>(q);
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = (uint32_t)q[2 * k] | ((uint32_t)q[2 * k + 1] << 16);
@@ -520,12 +564,10 @@ struct RowsF32 {
     return row * kColPitch + c * 16;
   }
 
-  __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, int b, int h0, int rows,
-                                                 int i) {
+  __device__ static __forceinline__ uint4 load_q(const CacheAttn& a, const QRows& u, int i) {
     const int row = i / (D / 4), d = (i % (D / 4)) * 4;
-    if (row >= rows || d >= a.c.d) return make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t* q = static_cast<const uint32_t*>(a.q) + (int64_t)b * a.q_sb +
-                        (int64_t)(h0 + row) * a.q_sh + d;
+    if (row >= u.rows || d >= a.c.d) return make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t* q = static_cast<const uint32_t*>(a.q) + u.at(a, row) + d;
     return make_uint4(q[0], q[1], q[2], q[3]);
   }
   __device__ static __forceinline__ void store_q(char* sq, int i, const uint4& v) {

@@ -217,3 +217,43 @@ def test_rotary_struct_matches_the_header():
 def test_binding_refuses_rotaries(kw):
     with pytest.raises(ValueError):
         av.Rotary(device="cpu", **kw)
+
+
+# -------------------------------------------------------- shared prefixes --
+def shared(lib, c, p, **kw):
+    a = dict(start=P, q=P, H=8, q_sb=512, q_sh=64, scale=0.1, o=P, o_sb=512, o_sh=64, lse=None, ws=P,
+             ws_bytes=1 << 40)
+    a.update(kw)
+    at = lambda s: s and ctypes.addressof(s)
+    return lib.avits_cache_attention_shared(at(c), at(p), *a.values(), None)
+
+
+@pytest.mark.parametrize("bad,code", BAD)
+def test_shared_caches_refused(lib, bad, code):
+    good, s = struct(), struct(**bad)
+    assert shared(lib, s, good) == code and shared(lib, good, s) == code
+    at = ctypes.addressof
+    assert lib.avits_cache_attention_shared_workspace(at(s), at(good), 8) == 0
+    assert lib.avits_cache_attention_shared_workspace(at(good), at(s), 8) == 0
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(start=None), INVALID), (dict(q=None), INVALID), (dict(o=None), INVALID), (dict(H=0), INVALID),
+    (dict(H=7), INVALID), (dict(q_sb=-1), INVALID), (dict(o_sh=-64), INVALID), (dict(scale=0.0), INVALID),
+    (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(o_sh=32), INVALID),
+    (dict(o_sb=64), INVALID), (dict(ws=None), INVALID), (dict(ws=P + 8), INVALID),
+    (dict(ws_bytes=16), INVALID), (dict(H=2 * 257, o_sb=2 * 257 * 64), UNSUPPORTED)])
+def test_shared_refused(lib, bad, code):
+    assert shared(lib, struct(), struct(B=2), **bad) == code
+
+
+@pytest.mark.parametrize("other", [dict(dt=0), dict(Hkv=4, acc=None), dict(d=32)])
+def test_shared_caches_that_differ(lib, other):
+    assert shared(lib, struct(), struct(**other)) == INVALID
+
+
+def test_shared_sizes(lib):
+    at = ctypes.addressof
+    long = struct(max_len=1 << 29, acc=None)
+    assert shared(lib, struct(B=1 << 20, acc=None), long) == UNSUPPORTED
+    assert lib.avits_cache_attention_shared_workspace(at(struct()), at(struct()), 9) == 0
