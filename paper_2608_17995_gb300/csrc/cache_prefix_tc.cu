@@ -1,0 +1,530 @@
+// cache_prefix_tc.cu — parts of the attention over shared prefixes on the tensor cores
+// (bf16, widths up to 128): the query heads of all of a group's sequences that share a KV
+// head are the rows of one product.
+//
+// Unit: (group, KV head, 128 rows).  All tiles of 64 keys of all units form one line, cut
+// into equal pieces, one per CTA; two CTAs share an SM, so that one's exponentials run
+// while the other's products do.  Roles of the 6 warps:
+//   0      loads keys and values through a ring of tiles (TMA, a box per page or part of
+//          one; what lies past the prefix or outside the pool comes as zeros), and says
+//          which keys of a tile are there
+//   1      issues the products: S(j+1) = Q K(j+1)^T, then O += P(j) V(j) as soon as P(j) is
+//          written, so that S is a tile ahead
+//   2-5    one row to a thread: the running maximum (moved when a tile's passes it by 2^8:
+//          O is rescaled then), exponentials, the fp32 sum, P to tensor memory over S
+// P enters the product in two bf16 parts, the weight cut to 8 bits and the rest, for an error
+// of 2^-16 of a weight.  The rest is taken of w (1 + 2^-20), so that it is above zero wherever w
+// is and an infinite value meets no zero; O is divided by 1 + 2^-20 at the end.
+//
+// Tensor memory of a CTA (256 columns): S of two tiles (64 columns each; P's parts over it, 32
+// columns each), O behind them.
+#include "cache_line.cuh"
+
+namespace avits {
+namespace cache {
+namespace {
+
+using namespace tc;
+
+constexpr int kBM = 128, kBN = 64;
+constexpr int kPreThreads = 192;
+constexpr int kTmemCols = 256;
+constexpr int kColO = 2 * kBN;
+constexpr int kMasks = 8;
+constexpr float kRise = 8.f;               // log2: a maximum that passes the reference by more
+constexpr float kUp = 1.f + 0x1p-20f;      // moves it
+constexpr int kMaxStages = 10;
+
+template <int D>
+struct Pre {
+  static constexpr int kCB = D / 64;
+  static constexpr int kTileBytes = kCB * kBN * 128;
+  static constexpr int kQBytes = kCB * kBM * 128;
+  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr uint32_t kIdescS = idesc_bf16(kBM, kBN, false);
+  static constexpr uint32_t kIdescPV = idesc_bf16(kBM, D, true);
+};
+
+struct PreBars {
+  uint64_t q_full, q_empty, o_full, o_empty, drain;
+  uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
+  uint64_t s_full[2], p_full[2], pv_done[2];
+  uint64_t mask_full[kMasks];
+  unsigned long long mask[kMasks];
+  uint32_t tmem_base;
+  int abort;
+};
+
+template <int D>
+constexpr int pre_smem() {
+  return Pre<D>::kQBytes + Pre<D>::kStages * Pre<D>::kTileBytes + (int)sizeof(PreBars);
+}
+// two CTAs to an SM: 228 KB with 1 KB of each block's kept by the system
+static_assert(pre_smem<128>() <= 113 * 1024 && pre_smem<64>() <= 113 * 1024, "two CTAs to an SM");
+
+// A CTA's piece of the line, segment by segment.
+struct Walk {
+  int g, u, t0, t1, nt, len, left, ubase, per;
+
+  // false: this CTA has none
+  __device__ __forceinline__ bool begin(const CacheAttn& a, int lane) {
+    const int B = a.c.B, each = (B + 31) / 32;
+    const int b0 = min(B, lane * each), b1 = min(B, b0 + each);
+    const GroupUnits all;
+    int sum = 0, usum = 0;
+    for (int b = b0; b < b1; ++b) {
+      const int n = all.of(a, b);
+      sum += tiles_of(a, cache_len(a.c, b)) * n;
+      usum += n;
+    }
+    int inc = sum, uinc = usum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o), z = __shfl_up_sync(0xffffffffu, uinc, o);
+      if (lane >= o) {
+        inc += y;
+        uinc += z;
+      }
+    }
+    const int total = __shfl_sync(0xffffffffu, inc, 31);
+    int base = uinc - usum;
+    const bool rise = __all_sync(0xffffffffu, groups_ok(a, b0, b1));
+    if (blockIdx.x == 0 && threadIdx.x < 32) {
+      for (int b = b0, at = base; b < b1; at += all.of(a, b++)) {
+        a.base[b] = at;
+        check_cache_len(a.c, b, a.status);
+      }
+      if (lane == 0) {
+        a.base[B] = rise;
+        if (!rise) raise_status(a.status, AVITS_ERR_PAGE);
+      }
+    }
+    per = max(a.least, (total + a.grid - 1) / a.grid);
+    const int first = blockIdx.x * per;
+    if (!rise || first >= total) return false;
+    int sb = b0, off = first - (inc - sum);
+    const bool here = off >= 0 && off < sum;
+    if (here)
+      for (;; ++sb) {
+        const int un = all.of(a, sb), n = tiles_of(a, cache_len(a.c, sb)) * un;
+        if (off < n) break;
+        off -= n;
+        base += un;
+      }
+    const int src = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+    g = __shfl_sync(0xffffffffu, sb, src);
+    off = __shfl_sync(0xffffffffu, off, src);
+    ubase = __shfl_sync(0xffffffffu, base, src);
+    left = min(per, total - first);
+    len = cache_len(a.c, g);
+    nt = tiles_of(a, len);
+    u = off / nt;
+    t0 = off - u * nt;
+    t1 = min(nt, t0 + left);
+    return true;
+  }
+  __device__ __forceinline__ bool next(const CacheAttn& a) {
+    left -= t1 - t0;
+    if (left <= 0) return false;
+    const GroupUnits all;
+    int un = all.of(a, g);
+    if (++u == un) {
+      u = 0;
+      do {
+        ubase += un;
+        len = cache_len(a.c, ++g);
+        nt = tiles_of(a, len);
+        un = all.of(a, g);
+      } while (nt == 0 || un == 0);
+    }
+    t0 = 0;
+    t1 = min(nt, left);
+    return true;
+  }
+  __device__ __forceinline__ QRows rows(const CacheAttn& a) const {
+    const int2 m = members_of(a.start, a.seqs, g);
+    const int n = (m.y - m.x) * a.G, rg = (n + kBM - 1) / kBM, hk = u / rg, r0 = (u - hk * rg) * kBM;
+    return QRows{m.x, hk * a.G, min(kBM, n - r0), r0, a.G};
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kPreThreads, 2)
+cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                    const __grid_constant__ CacheAttn a) {
+  using C = Pre<D>;
+  extern __shared__ __align__(1024) char smem[];
+  char* sQ = smem;
+  char* sKV = smem + C::kQBytes;
+  PreBars* bars = reinterpret_cast<PreBars*>(sKV + C::kStages * C::kTileBytes);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mk));
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mv));
+    mbar_init(&bars->q_full, 4);
+    mbar_init(&bars->q_empty, 1);
+    mbar_init(&bars->o_full, 1);
+    mbar_init(&bars->o_empty, 4);
+    mbar_init(&bars->drain, 1);
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(&bars->kv_full[i], 1);
+      mbar_init(&bars->kv_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->s_full[i], 1);
+      mbar_init(&bars->p_full[i], 4);
+      mbar_init(&bars->pv_done[i], 1);
+    }
+    for (int i = 0; i < kMasks; ++i) mbar_init(&bars->mask_full[i], 1);
+    bars->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_shared();
+  }
+  // what this call reads may come from the kernel before; the next one may start beside it
+  pdl_wait();
+  pdl_trigger();
+  Walk seg;
+  if (!seg.begin(a, lane)) return;         // the whole CTA
+  if (warp == 1) tmem_alloc(&bars->tmem_base, kTmemCols);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = bars->tmem_base;
+  volatile int* abort_flag = &bars->abort;
+
+  if (warp == 0) {
+    // --------------------------------------------------------- producer --
+    bool ok = true;
+    int loads = 0, tile = 0;
+    const int boxes = kBN / a.box;
+    do {
+      const QRows h = seg.rows(a);
+      const int hk = h.h0 / a.G;
+      // the box of a tile that this lane brings: its page and place in it
+      auto page_of = [&](int t) {
+        const int j = t * kBN + lane * a.box;
+        return lane < boxes && t < seg.t1 && j < seg.len
+                   ? a.c.block_table[(int64_t)seg.g * a.c.table_sb + a.page.div(j)]
+                   : -1;
+      };
+      auto load = [&](const CUtensorMap* map, int page, int t) {
+        const int st = loads % C::kStages;
+        ok = mbar_wait_bounded(&bars->kv_empty[st], ((uint32_t)(loads / C::kStages) & 1u) ^ 1u,
+                               abort_flag, a.status);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return;
+        ++loads;
+        if (lane == 0) mbar_arrive_expect_tx(&bars->kv_full[st], C::kTileBytes);
+        __syncwarp();
+        if (lane < boxes) {
+          const int j = t * kBN + lane * a.box, place = j - a.page.div(j) * a.c.page_size;
+          char* to = sKV + st * C::kTileBytes + lane * a.box * 128;
+#pragma unroll
+          for (int cb = 0; cb < C::kCB; ++cb)
+            tma_load_4d(to + cb * (kBN * 128), map, cb * 64, hk, place, page, &bars->kv_full[st]);
+        }
+        __syncwarp();
+      };
+      int entry = page_of(seg.t0), v_page = -1;
+      // in the order of the products: K(0), K(1), V(0), K(2), V(1), ...
+      for (int t = seg.t0; t <= seg.t1 && ok; ++t) {
+        int page = -1;
+        if (t < seg.t1) {
+          const int j = t * kBN + lane * a.box;
+          if (lane < boxes && j < seg.len) page = checked_page(a.c, entry, a.status);
+          const int n = min(a.box, seg.len - j);
+          unsigned long long bits = 0;
+          if (page >= 0) bits = (n >= 64 ? ~0ull : (1ull << n) - 1ull) << (lane * a.box);
+          const unsigned lo = __reduce_or_sync(0xffffffffu, (unsigned)bits);
+          const unsigned hi = __reduce_or_sync(0xffffffffu, (unsigned)(bits >> 32));
+          entry = page_of(t + 1);
+          load(&mk, page, t);
+          // the tile kMasks before is done: its S was, when this K's place came free
+          if (ok && lane == 0) {
+            bars->mask[tile % kMasks] = (unsigned long long)hi << 32 | lo;
+            mbar_arrive(&bars->mask_full[tile % kMasks]);
+          }
+          ++tile;
+        }
+        if (ok && t > seg.t0) load(&mv, v_page, t - 1);
+        v_page = page;
+      }
+    } while (ok && seg.next(a));
+    if (!ok)       // the copies in flight land before the CTA leaves
+      for (int i = loads > C::kStages ? loads - C::kStages : 0; i < loads; ++i)
+        mbar_wait_bounded(&bars->kv_full[i % C::kStages], (uint32_t)(i / C::kStages) & 1u, nullptr,
+                          a.status);
+  } else if (warp == 1) {
+    // --------------------------------------------------------- products --
+    const uint32_t q_lo = sw128_desc_lo(sQ), kv_lo = sw128_desc_lo(sKV);
+    const uint32_t v_lo0 = sw128_mn_desc_lo(sKV, kBN * 128), d_hi = sw128_desc_hi();
+    bool ok = true;
+    int loads = 0, tile = 0, n_seg = 0;
+    auto wait = [&](uint64_t* bar, int phase) {
+      if (ok) ok = mbar_wait_bounded(bar, (uint32_t)(phase & 1), abort_flag, a.status);
+    };
+    auto issue_s = [&](int at, bool last) {      // at: the tile's number
+      const int st = loads % C::kStages;
+      wait(&bars->kv_full[st], loads / C::kStages);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      ++loads;
+      fence_after();
+      if (elect_one()) {
+        const uint32_t k_lo = kv_lo + (uint32_t)((st * C::kTileBytes) >> 4);
+        const uint32_t tS = tmem + (uint32_t)((at & 1) * kBN);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          mma_ss(tS, q_lo + (uint32_t)(((kk >> 2) * (kBM * 128) + (kk & 3) * 32) >> 4),
+                 k_lo + (uint32_t)(((kk >> 2) * (kBN * 128) + (kk & 3) * 32) >> 4), d_hi, C::kIdescS,
+                 kk > 0 ? 1u : 0u);
+        mma_commit(&bars->s_full[at & 1]);
+        mma_commit(&bars->kv_empty[st]);
+        if (last) mma_commit(&bars->q_empty);
+      }
+      __syncwarp();
+    };
+    do {
+      const int n = seg.t1 - seg.t0;
+      wait(&bars->q_full, n_seg);
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok) issue_s(tile, n == 1);
+      for (int j = 0; j < n && ok; ++j, ++tile) {
+        // S(j+1) over P(j-1), whose product is before it in the pipe
+        if (j + 1 < n) issue_s(tile + 1, j + 2 == n);
+        if (!ok) break;
+        const int st = loads % C::kStages;
+        if (j == 0 && n_seg > 0) wait(&bars->o_empty, n_seg - 1);
+        wait(&bars->kv_full[st], loads / C::kStages);
+        wait(&bars->p_full[tile & 1], tile >> 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ++loads;
+        fence_after();
+        if (elect_one()) {
+          const uint32_t tP = tmem + (uint32_t)((tile & 1) * kBN), tO = tmem + (uint32_t)kColO;
+          const uint32_t v_lo = v_lo0 + (uint32_t)((st * C::kTileBytes) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < kBN / 16; ++kk) {
+            const uint32_t v_at = v_lo + (uint32_t)((kk * 16 * 128) >> 4);
+            mma_ts(tO, tP + (uint32_t)(kk * 8), v_at, d_hi, C::kIdescPV, j > 0 || kk > 0 ? 1u : 0u);
+            mma_ts(tO, tP + (uint32_t)(32 + kk * 8), v_at, d_hi, C::kIdescPV, 1u);
+          }
+          mma_commit(&bars->kv_empty[st]);
+          mma_commit(&bars->pv_done[tile & 1]);
+          if (j + 1 == n) mma_commit(&bars->o_full);
+        }
+        __syncwarp();
+      }
+      ++n_seg;
+    } while (ok && seg.next(a));
+    // everything issued has completed before tensor memory is given back
+    if (elect_one()) mma_commit(&bars->drain);
+    __syncwarp();
+    mbar_wait_bounded(&bars->drain, 0, nullptr, a.status);
+  } else {
+    // ------------------------------------------------ softmax, epilogue --
+    const int quad = warp & 3, row = quad * 32 + lane, part = threadIdx.x - 64;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    const uint32_t tO = tmem + lanes + (uint32_t)kColO;
+    bool ok = true;
+    int tile = 0, n_seg = 0, loads = 0;
+    auto wait = [&](uint64_t* bar, int phase) {
+      ok = ok && *abort_flag == 0 &&
+           mbar_wait_bounded(bar, (uint32_t)(phase & 1), abort_flag, a.status);
+      ok = __all_sync(0xffffffffu, ok);      // what follows are accesses of a whole warp
+      return ok;
+    };
+    // Q of a unit, a row to a thread, in the swizzled layout of the product
+    auto put_q = [&](const QRows& h) {
+      const bool live = row < h.rows;
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + (live ? h.at(a, row) : 0);
+      const bool vec = (reinterpret_cast<uintptr_t>(q) & 15u) == 0;
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        if (live && c * 8 < a.c.d) {
+          if (vec) {
+            const uint4 x = *reinterpret_cast<const uint4*>(q + c * 8);
+            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              w[k] = (uint32_t)q[c * 8 + 2 * k] | ((uint32_t)q[c * 8 + 2 * k + 1] << 16);
+          }
+        }
+        *reinterpret_cast<uint4*>(sQ + (c >> 3) * (kBM * 128) + row * 128 +
+                                  (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      fence_async_shared();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->q_full);
+    };
+    QRows h = seg.rows(a);
+    put_q(h);
+    bool more = true;
+    while (more) {
+      const int n = seg.t1 - seg.t0;
+      const int slot = seg.ubase + seg.u + (int)blockIdx.x;
+      if (seg.t0 == 0 && part == 0) {
+        // pieces of this unit: this CTA's and those of the CTAs that the rest reaches
+        const int over = seg.nt - seg.left;
+        a.rec[seg.ubase + seg.u] =
+            make_int2(slot, over <= 0 ? 1 : 1 + (over + seg.per - 1) / seg.per);
+      }
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < n; ++j, ++tile) {
+        const uint32_t tS = tmem + lanes + (uint32_t)((tile & 1) * kBN);
+        if (!wait(&bars->mask_full[tile % kMasks], tile / kMasks)) break;
+        const unsigned long long mask = bars->mask[tile % kMasks];
+        if (!wait(&bars->s_full[tile & 1], tile >> 1)) break;
+        fence_after();
+        uint32_t r0[32], r1[32];
+        tmem_ld64_wait(tS, r0, r1);
+        if (mask != ~0ull) {
+          const uint32_t m0 = (uint32_t)mask, m1 = (uint32_t)(mask >> 32);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            if (!((m0 >> e) & 1u)) r0[e] = 0xff800000u;
+            if (!((m1 >> e) & 1u)) r1[e] = 0xff800000u;
+          }
+        }
+        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          t4[e & 3] = max3(t4[e & 3], __uint_as_float(r0[e]), __uint_as_float(r1[e]));
+        const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * a.scale2;
+        const bool up = top > m + kRise || (m == -INFINITY && top > m);
+        if (__any_sync(0xffffffffu, up)) {
+          const float mn = up ? top : m, f = up ? avits::ex2(m - mn) : 1.f;
+          m = mn;
+          l *= f;
+          if (j > 0) {
+            if (!wait(&bars->pv_done[(tile - 1) & 1], (tile - 1) >> 1)) break;
+            fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              uint32_t x[32];
+              tmem_ld32_wait(tO + (uint32_t)c, x);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+              tmem_st32(tO + (uint32_t)c, x);
+            }
+          }
+        }
+        const float nm = m == -INFINITY ? 0.f : -m;
+        float s4[4] = {0.f, 0.f, 0.f, 0.f};
+        // keys 2e, 2e + 1: hi[e] the weights cut to bf16, lo[e] the rests
+        uint32_t hi[32], lo[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const uint32_t a0 = e < 16 ? r0[(2 * e) & 31] : r1[(2 * e) & 31];
+          const uint32_t a1 = e < 16 ? r0[(2 * e + 1) & 31] : r1[(2 * e + 1) & 31];
+          float x0, x1;
+          ffma2(__uint_as_float(a0), __uint_as_float(a1), a.scale2, nm, x0, x1);
+          x0 = avits::ex2(x0);
+          x1 = avits::ex2(x1);
+          fadd2(s4[2 * (e & 1)], s4[2 * (e & 1) + 1], x0, x1);
+          hi[e] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
+          lo[e] = pack_bf16x2(fmaf(x0, kUp, -__uint_as_float(__float_as_uint(x0) & 0xffff0000u)),
+                              fmaf(x1, kUp, -__uint_as_float(__float_as_uint(x1) & 0xffff0000u)));
+        }
+        l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+        tmem_st32(tS, hi);
+        tmem_st32(tS + 32u, lo);
+        tmem_wait_st();
+        if (mask != ~0ull) {
+          // values that are not there: a weight of zero times a NaN is one
+          const int v_at = loads + (j + 1 < n ? 2 * j + 2 : 2 * n - 1), st = v_at % C::kStages;
+          if (!wait(&bars->kv_full[st], v_at / C::kStages)) break;
+          char* v = sKV + st * C::kTileBytes;
+          for (int i = part; i < kBN * C::kCB * 8; i += 128) {
+            const int key = i / (C::kCB * 8), c = i - key * (C::kCB * 8);
+            if (!((mask >> key) & 1ull))
+              *reinterpret_cast<uint4*>(v + (c >> 3) * (kBN * 128) + key * 128 +
+                                        (((c & 7) ^ (key & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_async_shared();
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->p_full[tile & 1]);
+      }
+      if (!ok) break;
+      loads += 2 * n;
+      const int rows = h.rows;
+      more = seg.next(a);
+      if (more) {      // the next unit's Q, while the last product runs
+        if (!wait(&bars->q_empty, n_seg)) break;
+        h = seg.rows(a);
+        put_q(h);
+      }
+      if (!wait(&bars->o_full, n_seg)) break;
+      fence_after();
+      const int d4 = a.c.d / 4;
+      float4* po = reinterpret_cast<float4*>(a.po) + (int64_t)slot * d4 * kBM + row;
+#pragma unroll 1
+      for (int c = 0; c < D / 4; c += 8) {
+        uint32_t x[32];
+        tmem_ld32_wait(tO + (uint32_t)(c * 4), x);
+        if (row < rows) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c + e < d4)
+              po[(int64_t)(c + e) * kBM] =
+                  make_float4(__uint_as_float(x[4 * e]) * (1.f / kUp),
+                              __uint_as_float(x[4 * e + 1]) * (1.f / kUp),
+                              __uint_as_float(x[4 * e + 2]) * (1.f / kUp),
+                              __uint_as_float(x[4 * e + 3]) * (1.f / kUp));
+        }
+      }
+      if (row < rows) a.pml[slot * kBM + row] = make_float2(m, l);
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->o_empty);
+      ++n_seg;
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+template <int D>
+cudaError_t launch_width(const CacheAttn& a, cudaStream_t s) {
+  CUtensorMap mk{}, mv{};
+  using Rows = RowsBf16<D, 8>;
+  const avits_kv_cache& c = a.c;
+  if (!map_pages<Rows>(&mk, c.k_pages, c.k_sp, c.k_st, c.k_sh, c, a.box) ||
+      !map_pages<Rows>(&mv, c.v_pages, c.v_sp, c.v_st, c.v_sh, c, a.box))
+    return cudaErrorInvalidValue;
+  constexpr auto kernel = cache_prefix_kernel<D>;
+  const cudaError_t e = prefer_max_shared<kernel, pre_smem<D>()>();
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(a.grid), dim3(kPreThreads), pre_smem<D>(), s, mk, mv, a);
+}
+
+}  // namespace
+
+int prefix_tc_box(const avits_kv_cache& c) {
+  if (c.dt != AVITS_BF16 || c.d > 128 || c.page_size % 8 || !encode_fn()) return 0;
+  // what a tensor map takes; a stride of an axis of one entry is never used
+  const int64_t n[3] = {c.num_pages, c.page_size, c.Hkv};
+  const int64_t st[2][3] = {{c.k_sp, c.k_st, c.k_sh}, {c.v_sp, c.v_st, c.v_sh}};
+  for (int i = 0; i < 2; ++i)
+    for (int x = 0; x < 3; ++x)
+      if (n[x] > 1 && (st[i][x] <= 0 || st[i][x] >= (1ll << 39))) return 0;
+  int box = kBN;
+  while (c.page_size % box) box /= 2;
+  return box;
+}
+
+cudaError_t launch_prefix_tc(const CacheAttn& a, cudaStream_t s) {
+  return a.c.d <= 64 ? launch_width<64>(a, s) : launch_width<128>(a, s);
+}
+
+}  // namespace cache
+}  // namespace avits

@@ -24,21 +24,24 @@ size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 // One line of tiles: how it is cut and what it leaves.
 struct Line {
   int rows, groups, D, tile, grid, least;
+  int box;                     // prefixes on the tensor cores: tokens of a copy; else 0
   long long units, tiles;      // at most
   size_t rec, pml, po, base, end;
 };
 
 int width_of(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
+constexpr int kPrefixLeast = 2;
+
 void cut(Line& l, const avits_kv_cache& c, int num_sms) {
   const bool bf = c.dt == AVITS_BF16;
   l.D = width_of(c.d);
-  l.tile = bf ? 16 : 8;
-  const int longest = (c.max_len + l.tile - 1) / l.tile;
+  l.tile = l.box ? kPrefixTile : bf ? 16 : 8;
+  const int longest = (c.max_len + l.tile - 1) / l.tile, few = l.box ? kPrefixLeast : kWarps;
   l.tiles = l.units * longest;
-  l.least = longest < kWarps ? longest : kWarps;
+  l.least = longest < few ? longest : few;
   const long long most = (l.tiles + l.least - 1) / l.least;
-  long long full = (long long)num_sms * line_ctas(l.D, l.rows, bf);
+  long long full = (long long)num_sms * (l.box ? kPrefixCtas : line_ctas(l.D, l.rows, bf));
   if (full > kMaxGrid) full = kMaxGrid;
   l.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
 }
@@ -61,7 +64,8 @@ Shape shape_of(const CacheSharedCall& s, int num_sms) {
   x.own.rows = rows_of(bf, D, G);
   x.own.groups = (G + x.own.rows - 1) / x.own.rows;
   x.own.units = (long long)c.B * c.Hkv * x.own.groups;
-  x.pre.rows = rows_of(bf, D, ((long long)c.B + p.B - 1) / p.B * G);
+  x.pre.box = prefix_tc_box(p);
+  x.pre.rows = x.pre.box ? kPrefixRows : rows_of(bf, D, ((long long)c.B + p.B - 1) / p.B * G);
   x.pre.groups = 0;
   x.pre.units = c.Hkv * ((long long)c.B * G / x.pre.rows + p.B);
   cut(x.own, c, num_sms);
@@ -96,6 +100,7 @@ CacheAttn args_of(const CacheSharedCall& s, const avits_kv_cache& c, const Line&
   a.tile = l.tile;
   a.grid = l.grid;
   a.least = l.least;
+  a.box = l.box;
   a.scale2 = s.scale * kLog2e;
   a.rec = reinterpret_cast<int2*>(ws + l.rec);
   a.pml = reinterpret_cast<float2*>(ws + l.pml);
@@ -121,10 +126,17 @@ __device__ __forceinline__ float2 ml_of(const CacheAttn& o, const CacheAttn& p, 
   return k < x.n_own ? o.pml[x.own + k * x.own_step]
                      : p.pml[x.pre + (k - x.n_own) * x.pre_step];
 }
-__device__ __forceinline__ const float* o_of(const CacheAttn& o, const CacheAttn& p,
-                                             const Parts& x, int k) {
-  return k < x.n_own ? o.po + (int64_t)(x.own + k * x.own_step) * o.c.d
-                     : p.po + (int64_t)(x.pre + (k - x.n_own) * x.pre_step) * o.c.d;
+// Columns 4 col .. of a part.  From the tensor cores a part lies as [d / 4][128 rows][4],
+// so that a thread per row writes it in whole lines.
+__device__ __forceinline__ float4 o_of(const CacheAttn& o, const CacheAttn& p, const Parts& x, int k,
+                                       int col) {
+  const int d4 = o.c.d / 4;
+  if (k < x.n_own)
+    return reinterpret_cast<const float4*>(o.po)[(int64_t)(x.own + k * x.own_step) * d4 + col];
+  const int at = x.pre + (k - x.n_own) * x.pre_step;
+  const float4* po = reinterpret_cast<const float4*>(p.po);
+  if (p.rows != kPrefixRows) return po[(int64_t)at * d4 + col];
+  return po[(int64_t)(at / kPrefixRows) * d4 * kPrefixRows + col * kPrefixRows + at % kPrefixRows];
 }
 
 // Block (b, hk, some of its query heads): threads lie over the heads, their columns, and
@@ -190,14 +202,14 @@ cache_join_kernel(const __grid_constant__ CacheAttn o, const __grid_constant__ C
   }
   __syncthreads();
   const int d4 = o.c.d / 4, items = n * d4, lanes = kJoinThreads / items;
-  const int sub = tid / items, it = tid - sub * items, r = it / d4, col = it - r * d4;
+  const int sub = tid / items, it = tid - sub * items, col = it / n, r = it - col * n;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   float2 norm = make_float2(0.f, 0.f);
   if (sub < lanes) {
     const Parts x = s_parts[r];
     norm = s_ml[r];
     for (int k = sub; k < x.count(); k += lanes) {
-      const float4 y = *reinterpret_cast<const float4*>(o_of(o, p, x, k) + col * 4);
+      const float4 y = o_of(o, p, x, k, col);
       const float f = ex2(ml_of(o, p, x, k).x - norm.x);
       v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y);
       v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
@@ -250,8 +262,10 @@ bool cache_shared_sizes_ok(const CacheSharedCall& s) {
   const avits_kv_cache& c = s.cache;
   if (s.H / c.Hkv > kMaxGroup || (long long)c.B * s.H >= (1ll << 30)) return false;
   const Shape x = shape_of(s, 1);
-  return x.own.tiles < (1ll << 30) && x.pre.tiles < (1ll << 30) && x.pre.units < (1 << 26) &&
-         (long long)c.B * c.Hkv < (1ll << 31) - 1;
+  if ((long long)c.B * c.Hkv >= (1ll << 31) - 1) return false;
+  for (const Line* l : {&x.own, &x.pre})
+    if (l->tiles >= (1ll << 30) || (l->units + kMaxGrid) * l->rows >= (1ll << 31)) return false;
+  return true;
 }
 
 size_t cache_shared_workspace(const CacheSharedCall& s, int num_sms) {
@@ -262,7 +276,8 @@ cudaError_t launch_cache_shared(const CacheSharedCall& s, int num_sms, unsigned 
                                 cudaStream_t stream) {
   const Shape x = shape_of(s, num_sms);
   CacheAttn own = args_of(s, s.cache, x.own, status), pre = args_of(s, s.prefix, x.pre, status);
-  cudaError_t e = launch_parts<kGroup>(pre, x.pre.D, stream);
+  cudaError_t e = x.pre.box ? launch_prefix_tc(pre, stream)
+                          : launch_parts<kGroup>(pre, x.pre.D, stream);
   if (e == cudaSuccess) e = launch_parts<kOwn>(own, x.own.D, stream);
   if (e != cudaSuccess) return e;
   return s.cache.dt == AVITS_BF16 ? launch_join<__nv_bfloat16>(own, pre, stream)

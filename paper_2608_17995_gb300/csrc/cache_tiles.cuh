@@ -812,5 +812,11 @@ cudaError_t by_rows(const CacheAttn& a, int D, F f) {
 cudaError_t launch_line(CacheAttn& a, int D, int num_sms, cudaStream_t s);
 cudaError_t launch_cluster(CacheAttn& a, int D, int ncta, int warps, cudaStream_t s);
 
+// Prefixes on the tensor cores: units of 128 rows, tiles of 64 keys, two CTAs to an SM.  Tokens
+// of a copy, 0 where the type, the width or the pages' layout is not theirs.
+constexpr int kPrefixRows = 128, kPrefixTile = 64, kPrefixCtas = 2;
+int prefix_tc_box(const avits_kv_cache& c);
+cudaError_t launch_prefix_tc(const CacheAttn& a, cudaStream_t s);
+
 }  // namespace cache
 }  // namespace avits
