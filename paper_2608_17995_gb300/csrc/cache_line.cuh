@@ -17,16 +17,27 @@ __device__ __forceinline__ bool groups_ok(const CacheAttn& a, int g0, int g1) {
   return ok;
 }
 
+// The last group that starts at sequence b or before it.
+__device__ __forceinline__ int group_of(const int32_t* start, int groups, int b) {
+  int lo = 0, hi = groups - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (start[mid] <= b) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
 // kWhole: avits_cache_attention's first kernel.  Units that lie in one piece are finished.
 // The others leave every piece of a unit as a part: part (unit + CTA) of the line, which
 // has one more at each unit's and each CTA's border.
-//   kOwn    a batch's own tokens, beside the kernel before (which goes over the
-//           prefixes): it is waited for at the end
-//   kGroup  prefixes, whose rows are the query heads of all sequences of a group
+//   kOwn    a batch's own tokens, beside the kernel before, which goes over the prefixes and
+//           has waited for what both read: it is waited for at the end, for the join
+//   kGroup  prefixes, whose rows are the query heads of all sequences of a group; the
+//           kernel behind it may start beside it
 enum LineForm { kWhole = 0, kOwn = 1, kGroup = 2 };
 
 template <typename Rows, int kForm>
-__global__ void __launch_bounds__(kThreads, line_ctas(Rows::D, Rows::kR, Rows::kBf16))
+__global__ void __launch_bounds__(kThreads, kForm == kOwn ? own_ctas(Rows::D, Rows::kR, Rows::kBf16) : line_ctas(Rows::D, Rows::kR, Rows::kBf16))
 cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                   const __grid_constant__ CacheAttn a) {
   using T = typename Rows::T;

@@ -33,14 +33,15 @@ constexpr int kColO = 2 * kBN;
 constexpr int kMasks = 8;
 constexpr float kRise = 8.f;               // log2: a maximum that passes the reference by more
 constexpr float kUp = 1.f + 0x1p-20f;      // moves it
-constexpr int kMaxStages = 10;
+constexpr int kMaxStages = 8;
+constexpr int kOutBytes = kBM * 16 * 4;    // 16 columns of O
 
 template <int D>
 struct Pre {
   static constexpr int kCB = D / 64;
   static constexpr int kTileBytes = kCB * kBN * 128;
   static constexpr int kQBytes = kCB * kBM * 128;
-  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kStages = D == 128 ? 3 : 6;
   static constexpr uint32_t kIdescS = idesc_bf16(kBM, kBN, false);
   static constexpr uint32_t kIdescPV = idesc_bf16(kBM, D, true);
 };
@@ -57,25 +58,40 @@ struct PreBars {
 
 template <int D>
 constexpr int pre_smem() {
-  return Pre<D>::kQBytes + Pre<D>::kStages * Pre<D>::kTileBytes + (int)sizeof(PreBars);
+  return Pre<D>::kQBytes + Pre<D>::kStages * Pre<D>::kTileBytes + kOutBytes + (int)sizeof(PreBars);
 }
-// two CTAs to an SM: 228 KB with 1 KB of each block's kept by the system
-static_assert(pre_smem<128>() <= 113 * 1024 && pre_smem<64>() <= 113 * 1024, "two CTAs to an SM");
+// Two CTAs to an SM and beside them one of the kernel over the own tokens (2 warps, 128 wide), of
+// 228 KB with 1 KB of each block's kept by the system.
+static_assert(2 * (pre_smem<128>() + 1024) <= (228 - 40) * 1024, "room for own tokens");
 
 // A CTA's piece of the line, segment by segment.
 struct Walk {
   int g, u, t0, t1, nt, len, left, ubase, per;
+  int seq, n;            // the group's first sequence, and the rows of a KV head
 
+  __device__ __forceinline__ int units(const CacheAttn& a) const {
+    return a.c.Hkv * ((n + kBM - 1) / kBM);
+  }
+  __device__ __forceinline__ void look(const CacheAttn& a) {
+    const int2 m = members_of(a.start, a.seqs, g);
+    seq = m.x;
+    n = (m.y - m.x) * a.G;
+    len = cache_len(a.c, g);
+    nt = tiles_of(a, len);
+  }
   // false: this CTA has none
   __device__ __forceinline__ bool begin(const CacheAttn& a, int lane) {
     const int B = a.c.B, each = (B + 31) / 32;
     const int b0 = min(B, lane * each), b1 = min(B, b0 + each);
-    const GroupUnits all;
     int sum = 0, usum = 0;
-    for (int b = b0; b < b1; ++b) {
-      const int n = all.of(a, b);
-      sum += tiles_of(a, cache_len(a.c, b)) * n;
-      usum += n;
+    bool ok = true;
+    Walk mine{};                         // of the lane's last group
+    for (mine.g = b0; mine.g < b1; ++mine.g) {
+      mine.look(a);
+      const int x = a.start[mine.g], y = a.start[mine.g + 1];
+      ok = ok && x >= 0 && x <= y && y <= a.seqs;
+      sum += mine.nt * mine.units(a);
+      usum += mine.units(a);
     }
     int inc = sum, uinc = usum;
 #pragma unroll
@@ -88,11 +104,16 @@ struct Walk {
     }
     const int total = __shfl_sync(0xffffffffu, inc, 31);
     int base = uinc - usum;
-    const bool rise = __all_sync(0xffffffffu, groups_ok(a, b0, b1));
+    // groups that do not rise could be more units than there is room for: no prefix is read
+    const bool rise = __all_sync(0xffffffffu, ok);
     if (blockIdx.x == 0 && threadIdx.x < 32) {
-      for (int b = b0, at = base; b < b1; at += all.of(a, b++)) {
-        a.base[b] = at;
-        check_cache_len(a.c, b, a.status);
+      Walk x{};
+      x.ubase = base;
+      for (x.g = b0; x.g < b1; ++x.g) {
+        x.look(a);
+        a.base[x.g] = x.ubase;
+        x.ubase += x.units(a);
+        check_cache_len(a.c, x.g, a.status);
       }
       if (lane == 0) {
         a.base[B] = rise;
@@ -102,21 +123,25 @@ struct Walk {
     per = max(a.least, (total + a.grid - 1) / a.grid);
     const int first = blockIdx.x * per;
     if (!rise || first >= total) return false;
-    int sb = b0, off = first - (inc - sum);
+    int off = first - (inc - sum);
     const bool here = off >= 0 && off < sum;
-    if (here)
-      for (;; ++sb) {
-        const int un = all.of(a, sb), n = tiles_of(a, cache_len(a.c, sb)) * un;
-        if (off < n) break;
-        off -= n;
+    mine.g = b0;
+    if (here && each > 1)
+      for (;; ++mine.g) {
+        mine.look(a);
+        const int un = mine.units(a), tiles = mine.nt * un;
+        if (off < tiles) break;
+        off -= tiles;
         base += un;
       }
     const int src = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
-    g = __shfl_sync(0xffffffffu, sb, src);
+    g = __shfl_sync(0xffffffffu, mine.g, src);
+    seq = __shfl_sync(0xffffffffu, mine.seq, src);
+    n = __shfl_sync(0xffffffffu, mine.n, src);
+    len = __shfl_sync(0xffffffffu, mine.len, src);
     off = __shfl_sync(0xffffffffu, off, src);
     ubase = __shfl_sync(0xffffffffu, base, src);
     left = min(per, total - first);
-    len = cache_len(a.c, g);
     nt = tiles_of(a, len);
     u = off / nt;
     t0 = off - u * nt;
@@ -126,37 +151,38 @@ struct Walk {
   __device__ __forceinline__ bool next(const CacheAttn& a) {
     left -= t1 - t0;
     if (left <= 0) return false;
-    const GroupUnits all;
-    int un = all.of(a, g);
-    if (++u == un) {
+    if (++u == units(a)) {
       u = 0;
       do {
-        ubase += un;
-        len = cache_len(a.c, ++g);
-        nt = tiles_of(a, len);
-        un = all.of(a, g);
-      } while (nt == 0 || un == 0);
+        ubase += units(a);
+        ++g;
+        look(a);
+      } while (nt == 0 || n == 0);
     }
     t0 = 0;
     t1 = min(nt, left);
     return true;
   }
   __device__ __forceinline__ QRows rows(const CacheAttn& a) const {
-    const int2 m = members_of(a.start, a.seqs, g);
-    const int n = (m.y - m.x) * a.G, rg = (n + kBM - 1) / kBM, hk = u / rg, r0 = (u - hk * rg) * kBM;
-    return QRows{m.x, hk * a.G, min(kBM, n - r0), r0, a.G};
+    const int rg = (n + kBM - 1) / kBM, hk = u / rg, r0 = (u - hk * rg) * kBM;
+    return QRows{seq, hk * a.G, min(kBM, n - r0), r0, a.G};
   }
 };
 
+__device__ __forceinline__ void bar_arrive(int id, int count) {
+  asm volatile("barrier.cta.arrive %0, %1;" ::"r"(id), "r"(count) : "memory");
+}
+
 template <int D>
-__global__ void __launch_bounds__(kPreThreads, 2)
+__global__ void __launch_bounds__(256, 2)      // at most 128 registers: see the room left above
 cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                     const __grid_constant__ CacheAttn a) {
   using C = Pre<D>;
   extern __shared__ __align__(1024) char smem[];
   char* sQ = smem;
   char* sKV = smem + C::kQBytes;
-  PreBars* bars = reinterpret_cast<PreBars*>(sKV + C::kStages * C::kTileBytes);
+  char* sO = sKV + C::kStages * C::kTileBytes;
+  PreBars* bars = reinterpret_cast<PreBars*>(sO + kOutBytes);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mk));
@@ -185,12 +211,18 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
   pdl_trigger();
   Walk seg;
   if (!seg.begin(a, lane)) return;         // the whole CTA
-  if (warp == 1) tmem_alloc(&bars->tmem_base, kTmemCols);
-  fence_before();
-  __syncthreads();
-  fence_after();
-  const uint32_t tmem = bars->tmem_base;
   volatile int* abort_flag = &bars->abort;
+  uint32_t tmem = 0;
+  if (warp == 0) {
+    bar_arrive(1, kPreThreads);            // its copies need no tensor memory
+    __syncwarp();
+  } else {
+    if (warp == 1) tmem_alloc(&bars->tmem_base, kTmemCols);
+    fence_before();
+    bar_sync(1, kPreThreads);
+    fence_after();
+    tmem = bars->tmem_base;
+  }
 
   if (warp == 0) {
     // --------------------------------------------------------- producer --
@@ -335,26 +367,36 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
       ok = __all_sync(0xffffffffu, ok);      // what follows are accesses of a whole warp
       return ok;
     };
-    // Q of a unit, a row to a thread, in the swizzled layout of the product
+    // Q of a unit in the swizzled layout of the product: a warp brings its 32 rows, all
+    // loads at once.  (A row to a thread, 16 bytes at a time, took 5 us for 128 rows.)
     auto put_q = [&](const QRows& h) {
-      const bool live = row < h.rows;
-      const uint16_t* q = static_cast<const uint16_t*>(a.q) + (live ? h.at(a, row) : 0);
-      const bool vec = (reinterpret_cast<uintptr_t>(q) & 15u) == 0;
-#pragma unroll 4
-      for (int c = 0; c < D / 8; ++c) {
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (live && c * 8 < a.c.d) {
-          if (vec) {
-            const uint4 x = *reinterpret_cast<const uint4*>(q + c * 8);
-            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-          } else {
+      constexpr int kC = D / 8, kSide = 32 / kC, kSteps = 32 / kSide;   // pieces, rows at once
+      const int c = lane % kC, side = lane / kC;
+      const int64_t mine = row < h.rows ? h.at(a, row) : 0;
+      const uint16_t* q = static_cast<const uint16_t*>(a.q);
+      const bool vec = __all_sync(0xffffffffu, (reinterpret_cast<uintptr_t>(q + mine) & 15u) == 0);
+      uint4 x[kSteps];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              w[k] = (uint32_t)q[c * 8 + 2 * k] | ((uint32_t)q[c * 8 + 2 * k + 1] << 16);
+      for (int i = 0; i < kSteps; ++i) {
+        const int r = i * kSide + side;
+        const uint16_t* from = q + __shfl_sync(0xffffffffu, mine, r) + c * 8;
+        x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (quad * 32 + r < h.rows && c * 8 < a.c.d) {
+          if (vec) {
+            x[i] = *reinterpret_cast<const uint4*>(from);
+          } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = (uint32_t)from[2 * k] | ((uint32_t)from[2 * k + 1] << 16);
+            x[i] = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
-        *reinterpret_cast<uint4*>(sQ + (c >> 3) * (kBM * 128) + row * 128 +
-                                  (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int r = quad * 32 + i * kSide + side;
+        *reinterpret_cast<uint4*>(sQ + (c >> 3) * (kBM * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
+            x[i];
       }
       fence_async_shared();
       __syncwarp();
@@ -414,24 +456,27 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         }
         const float nm = m == -INFINITY ? 0.f : -m;
         float s4[4] = {0.f, 0.f, 0.f, 0.f};
-        // keys 2e, 2e + 1: hi[e] the weights cut to bf16, lo[e] the rests
-        uint32_t hi[32], lo[32];
+        // Half of the tile at a time (registers): of keys 2e, 2e + 1 the weights cut to bf16 and
+        // their rests, to columns e and 32 + e.
+        auto half = [&](const uint32_t (&r)[32], int at) {
+          uint32_t hi[16], lo[16];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const uint32_t a0 = e < 16 ? r0[(2 * e) & 31] : r1[(2 * e) & 31];
-          const uint32_t a1 = e < 16 ? r0[(2 * e + 1) & 31] : r1[(2 * e + 1) & 31];
-          float x0, x1;
-          ffma2(__uint_as_float(a0), __uint_as_float(a1), a.scale2, nm, x0, x1);
-          x0 = avits::ex2(x0);
-          x1 = avits::ex2(x1);
-          fadd2(s4[2 * (e & 1)], s4[2 * (e & 1) + 1], x0, x1);
-          hi[e] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
-          lo[e] = pack_bf16x2(fmaf(x0, kUp, -__uint_as_float(__float_as_uint(x0) & 0xffff0000u)),
-                              fmaf(x1, kUp, -__uint_as_float(__float_as_uint(x1) & 0xffff0000u)));
-        }
+          for (int e = 0; e < 16; ++e) {
+            float x0, x1;
+            ffma2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]), a.scale2, nm, x0, x1);
+            x0 = avits::ex2(x0);
+            x1 = avits::ex2(x1);
+            fadd2(s4[2 * (e & 1)], s4[2 * (e & 1) + 1], x0, x1);
+            hi[e] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
+            lo[e] = pack_bf16x2(fmaf(x0, kUp, -__uint_as_float(__float_as_uint(x0) & 0xffff0000u)),
+                                fmaf(x1, kUp, -__uint_as_float(__float_as_uint(x1) & 0xffff0000u)));
+          }
+          tmem_st16(tS + (uint32_t)at, hi);
+          tmem_st16(tS + 32u + (uint32_t)at, lo);
+        };
+        half(r0, 0);
+        half(r1, 16);
         l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-        tmem_st32(tS, hi);
-        tmem_st32(tS + 32u, lo);
         tmem_wait_st();
         if (mask != ~0ull) {
           // values that are not there: a weight of zero times a NaN is one
@@ -461,27 +506,40 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
       }
       if (!wait(&bars->o_full, n_seg)) break;
       fence_after();
-      const int d4 = a.c.d / 4;
-      float4* po = reinterpret_cast<float4*>(a.po) + (int64_t)slot * d4 * kBM + row;
+      // O by 16 columns through shared memory, so that a row's go out as whole sectors
 #pragma unroll 1
-      for (int c = 0; c < D / 4; c += 8) {
+      for (int c = 0; c < D; c += 32) {
         uint32_t x[32];
-        tmem_ld32_wait(tO + (uint32_t)(c * 4), x);
-        if (row < rows) {
+        tmem_ld32_wait(tO + (uint32_t)c, x);
+        if (c + 32 >= D) {        // O has been read
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->o_empty);
+        }
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (c + e < d4)
-              po[(int64_t)(c + e) * kBM] =
-                  make_float4(__uint_as_float(x[4 * e]) * (1.f / kUp),
-                              __uint_as_float(x[4 * e + 1]) * (1.f / kUp),
-                              __uint_as_float(x[4 * e + 2]) * (1.f / kUp),
-                              __uint_as_float(x[4 * e + 3]) * (1.f / kUp));
+        for (int hf = 0; hf < 2; ++hf) {
+          float4* buf = reinterpret_cast<float4*>(sO);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            buf[row * 4 + (e ^ ((row >> 1) & 3))] =
+                make_float4(__uint_as_float(x[16 * hf + 4 * e]) * (1.f / kUp),
+                            __uint_as_float(x[16 * hf + 4 * e + 1]) * (1.f / kUp),
+                            __uint_as_float(x[16 * hf + 4 * e + 2]) * (1.f / kUp),
+                            __uint_as_float(x[16 * hf + 4 * e + 3]) * (1.f / kUp));
+          __syncwarp();
+          const int col = lane & 3, at = c + 16 * hf + col * 4;
+          if (at < a.c.d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int r = quad * 32 + i * 8 + (lane >> 2);
+              if (r < rows)
+                *reinterpret_cast<float4*>(a.po + ((int64_t)slot * kBM + r) * a.c.d + at) =
+                    buf[r * 4 + (col ^ ((r >> 1) & 3))];
+            }
+          __syncwarp();
         }
       }
       if (row < rows) a.pml[slot * kBM + row] = make_float2(m, l);
-      fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->o_empty);
       ++n_seg;
     }
   }

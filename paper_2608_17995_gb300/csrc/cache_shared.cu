@@ -17,7 +17,7 @@ namespace {
 
 using namespace cache;
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 128, kJoinHeads = 64;
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
@@ -41,7 +41,7 @@ void cut(Line& l, const avits_kv_cache& c, int num_sms) {
   l.tiles = l.units * longest;
   l.least = longest < few ? longest : few;
   const long long most = (l.tiles + l.least - 1) / l.least;
-  long long full = (long long)num_sms * (l.box ? kPrefixCtas : line_ctas(l.D, l.rows, bf));
+  long long full = (long long)num_sms * (l.box ? kPrefixCtas : (l.groups ? own_ctas(l.D, l.rows, bf) : line_ctas(l.D, l.rows, bf)));
   if (full > kMaxGrid) full = kMaxGrid;
   l.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
 }
@@ -51,10 +51,33 @@ int rows_of(bool bf, int D, long long n) {
   return !bf ? (n <= 4 ? 4 : 8) : n <= 8 ? 8 : n <= 16 || D == 256 ? 16 : 32;
 }
 
+constexpr long long kAgainBytes = 64ll << 20;
+constexpr int kOwnShort = 1024, kOwnLong = 2048;
+
+// CTAs of a unit's cluster that goes over prefix and own tokens in one launch, 0 where parts
+// are faster.
+int both_of(const CacheSharedCall& s, const Line& own, int num_sms) {
+  const long long units = own.units, keys = (long long)s.cache.max_len + s.prefix.max_len;
+  const long long resident = (long long)num_sms * (own.D > 128 ? 1 : 2);
+  auto fits = [&](int n) { return (keys + n - 1) / n <= (n > 1 ? 512 : 1024); };
+  int n = 1;
+  while (n < 8 && !fits(n)) n *= 2;
+  if (!fits(n) || (n > 1 && units * n > resident) || units >= (1 << 30)) return 0;
+  const long long again = units * s.prefix.max_len * 2 * s.cache.d * (s.cache.dt == AVITS_BF16 ? 2 : 4);
+  if (again > kAgainBytes || units > 4ll * num_sms) return 0;
+  while (n < 8 && units * n * 2 <= resident && keys > n * 64) n *= 2;
+  if (units * n < num_sms && keys > n * 256) return 0;
+  return n;
+}
+
 struct Shape {
   Line own, pre;
+  int both;         // CTAs of a cluster that goes over prefix and own tokens; 0: parts
+  int warps;        // of a unit's CTA where own tokens are short; 0: the line of tiles
   size_t total;
 };
+
+
 
 Shape shape_of(const CacheSharedCall& s, int num_sms) {
   const avits_kv_cache &c = s.cache, &p = s.prefix;
@@ -70,9 +93,16 @@ Shape shape_of(const CacheSharedCall& s, int num_sms) {
   x.pre.units = c.Hkv * ((long long)c.B * G / x.pre.rows + p.B);
   cut(x.own, c, num_sms);
   cut(x.pre, p, num_sms);
+  x.both = both_of(s, x.own, num_sms);
+  x.warps = c.max_len <= kOwnLong ? 2 : 0;
+  if (x.warps) {       // runs of a unit
+    const int longest = (c.max_len + x.own.tile - 1) / x.own.tile;
+    x.own.least = c.max_len <= kOwnShort ? 16 : 32;
+    x.own.grid = (longest + x.own.least - 1) / x.own.least;
+  }
   size_t at = 0;
   for (Line* l : {&x.own, &x.pre}) {
-    const size_t parts = (size_t)(l->units + l->grid) * l->rows;
+    const size_t parts = (size_t)(l == &x.own && x.warps ? l->units * l->grid : l->units + l->grid) * l->rows;
     l->rec = at;
     l->pml = l->rec + up16((size_t)l->units * sizeof(int2));
     l->po = l->pml + up16(parts * sizeof(float2));
@@ -121,121 +151,124 @@ struct Parts {
   __device__ __forceinline__ int count() const { return n_own + n_pre; }
 };
 
-__device__ __forceinline__ float2 ml_of(const CacheAttn& o, const CacheAttn& p, const Parts& x,
-                                        int k) {
-  return k < x.n_own ? o.pml[x.own + k * x.own_step]
-                     : p.pml[x.pre + (k - x.n_own) * x.pre_step];
-}
-// Columns 4 col .. of a part.  From the tensor cores a part lies as [d / 4][128 rows][4],
-// so that a thread per row writes it in whole lines.
-__device__ __forceinline__ float4 o_of(const CacheAttn& o, const CacheAttn& p, const Parts& x, int k,
-                                       int col) {
-  const int d4 = o.c.d / 4;
-  if (k < x.n_own)
-    return reinterpret_cast<const float4*>(o.po)[(int64_t)(x.own + k * x.own_step) * d4 + col];
-  const int at = x.pre + (k - x.n_own) * x.pre_step;
-  const float4* po = reinterpret_cast<const float4*>(p.po);
-  if (p.rows != kPrefixRows) return po[(int64_t)at * d4 + col];
-  return po[(int64_t)(at / kPrefixRows) * d4 * kPrefixRows + col * kPrefixRows + at % kPrefixRows];
+// Part k of a row: its maximum and sum, and columns 4 col .. of its O.
+__device__ __forceinline__ void part_of(const CacheAttn& o, const CacheAttn& p, const Parts& x, int k,
+                                        int col, float4& v, float2& ml) {
+  const bool own = k < x.n_own;
+  const int at = own ? x.own + k * x.own_step : x.pre + (k - x.n_own) * x.pre_step;
+  v = reinterpret_cast<const float4*>(own ? o.po : p.po)[(int64_t)at * (o.c.d / 4) + col];
+  ml = (own ? o.pml : p.pml)[at];
 }
 
 // Block (b, hk, some of its query heads): threads lie over the heads, their columns, and
-// the parts.
+// the parts, kDeep of which a thread has under way at once.
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinThreads, 6)
 cache_join_kernel(const __grid_constant__ CacheAttn o, const __grid_constant__ CacheAttn p,
                   int heads) {
   __shared__ float4 s_sum[kJoinThreads];
-  __shared__ Parts s_parts[kJoinThreads];
   __shared__ float2 s_ml[kJoinThreads];
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  __shared__ Parts s_parts[kJoinHeads];
+  const int tid = threadIdx.x;
   const int b = blockIdx.x / o.c.Hkv, hk = blockIdx.x - b * o.c.Hkv;
   const int g0 = blockIdx.y * heads, n = min(heads, o.G - g0);
+  // what was there before this call: the group, lengths
+  const int gq = g0 + tid, rg = gq / o.rows;
+  int len = 0, lo = 0, len_p = 0;
+  int2 m = make_int2(0, 0);
+  if (tid < n) {
+    len = cache_len(o.c, b);
+    lo = group_of(p.start, p.c.B, b);
+    m = members_of(p.start, p.seqs, lo);
+    len_p = cache_len(p.c, lo);
+  }
   pdl_wait_then_trigger();
   if (tid < n) {
     Parts x{0, 0, 0, 0, o.rows, p.rows};
-    const int gq = g0 + tid;
-    if (cache_len(o.c, b) > 0) {
-      const int rg = gq / o.rows;
-      const int2 rec = o.rec[(b * o.c.Hkv + hk) * o.groups + rg];
-      x.own = rec.x * o.rows + gq - rg * o.rows;
-      x.n_own = rec.y;
-    }
-    // the last group that starts at b or before it
-    int lo = 0, hi = p.c.B - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (p.start[mid] <= b) lo = mid; else hi = mid - 1;
-    }
-    const int2 m = members_of(p.start, p.seqs, lo);
-    if (b >= m.x && b < m.y && p.base[p.c.B] && cache_len(p.c, lo) > 0) {
-      const int row = (b - m.x) * o.G + gq, rg = row / p.rows;
-      const int all = ((m.y - m.x) * o.G + p.rows - 1) / p.rows;
-      const int2 rec = p.rec[p.base[lo] + hk * all + rg];
-      x.pre = rec.x * p.rows + row - rg * p.rows;
+    const int row = (b - m.x) * o.G + gq, rgp = row / p.rows;
+    const int all = ((m.y - m.x) * o.G + p.rows - 1) / p.rows;
+    const int2 own = o.rec[(b * o.c.Hkv + hk) * o.groups + rg];     // of an empty one: not used
+    if (p.base[p.c.B] && b >= m.x && b < m.y && len_p > 0) {
+      const int2 rec = p.rec[p.base[lo] + hk * all + rgp];
+      x.pre = rec.x * p.rows + row - rgp * p.rows;
       x.n_pre = rec.y;
+    }
+    if (len > 0) {
+      x.own = own.x * o.rows + gq - rg * o.rows;
+      x.n_own = own.y;
     }
     s_parts[tid] = x;
   }
   __syncthreads();
-  for (int r = w; r < n; r += kJoinThreads / 32) {
-    const Parts x = s_parts[r];
-    float top = -INFINITY, l = 0.f;
-    for (int k = lane; k < x.count(); k += 32) {
-      const float2 y = ml_of(o, p, x, k);
-      const float mn = fmaxf(top, y.x), ref = mn == -INFINITY ? 0.f : mn;
-      l = l * ex2(top - ref) + y.y * ex2(y.x - ref);
-      top = mn;
-    }
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) {
-      const float tx = __shfl_xor_sync(0xffffffffu, top, s);
-      const float lx = __shfl_xor_sync(0xffffffffu, l, s);
-      const float mn = fmaxf(top, tx), ref = mn == -INFINITY ? 0.f : mn;
-      l = l * ex2(top - ref) + lx * ex2(tx - ref);
-      top = mn;
-    }
-    if (lane == 0) {
-      s_ml[r] = norm_of(top, l);
-      if (o.lse) o.lse[(int64_t)b * o.H + hk * o.G + g0 + r] = lse2_of(top, l) * kLn2;
-    }
-  }
-  __syncthreads();
+  constexpr int kDeep = 8;
   const int d4 = o.c.d / 4, items = n * d4, lanes = kJoinThreads / items;
-  const int sub = tid / items, it = tid - sub * items, col = it / n, r = it - col * n;
+  const int sub = tid / items, it = tid - sub * items, r = it / d4, col = it - r * d4;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  float2 norm = make_float2(0.f, 0.f);
+  float top = -INFINITY, l = 0.f;
   if (sub < lanes) {
     const Parts x = s_parts[r];
-    norm = s_ml[r];
-    for (int k = sub; k < x.count(); k += lanes) {
-      const float4 y = o_of(o, p, x, k, col);
-      const float f = ex2(ml_of(o, p, x, k).x - norm.x);
-      v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y);
-      v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
+    for (int k0 = sub; k0 < x.count(); k0 += lanes * kDeep) {
+      float4 y[kDeep];
+      float2 ml[kDeep];
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) {
+        const int k = k0 + i * lanes;
+        y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        ml[i] = make_float2(-INFINITY, 0.f);
+        if (k < x.count()) part_of(o, p, x, k, col, y[i], ml[i]);
+      }
+      float mn = top;
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) mn = fmaxf(mn, ml[i].x);
+      const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+      l *= f0;
+      v.x *= f0; v.y *= f0; v.z *= f0; v.w *= f0;
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) {
+        const float f = ex2(ml[i].x - ref);      // from -inf: 0
+        l = fmaf(f, ml[i].y, l);
+        v.x = fmaf(f, y[i].x, v.x); v.y = fmaf(f, y[i].y, v.y);
+        v.z = fmaf(f, y[i].z, v.z); v.w = fmaf(f, y[i].w, v.w);
+      }
+      top = mn;
     }
   }
   if (lanes > 1) {
     s_sum[tid] = v;
+    s_ml[tid] = make_float2(top, l);
     __syncthreads();
     if (sub != 0) return;
+    float mn = top;
+    for (int k = 1; k < lanes; ++k) mn = fmaxf(mn, s_ml[k * items + it].x);
+    const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+    l *= f0;
+    v.x *= f0; v.y *= f0; v.z *= f0; v.w *= f0;
     for (int k = 1; k < lanes; ++k) {
+      const float2 ml = s_ml[k * items + it];
       const float4 y = s_sum[k * items + it];
-      v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
+      const float f = ex2(ml.x - ref);
+      l = fmaf(f, ml.y, l);
+      v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y);
+      v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
     }
+    top = mn;
   }
   if (sub != 0) return;
-  T* out = static_cast<T*>(o.o) + (int64_t)b * o.o_sb + (int64_t)(hk * o.G + g0 + r) * o.o_sh +
-           col * 4;
-  store_elem(out, 0, v.x * norm.y);
-  store_elem(out, 1, v.y * norm.y);
-  store_elem(out, 2, v.z * norm.y);
-  store_elem(out, 3, v.w * norm.y);
+  const int h = hk * o.G + g0 + r;
+  if (col == 0 && o.lse) o.lse[(int64_t)b * o.H + h] = lse2_of(top, l) * kLn2;
+  const float inv = norm_of(top, l).y;
+  T* out = static_cast<T*>(o.o) + (int64_t)b * o.o_sb + (int64_t)h * o.o_sh + col * 4;
+  store_elem(out, 0, v.x * inv);
+  store_elem(out, 1, v.y * inv);
+  store_elem(out, 2, v.z * inv);
+  store_elem(out, 3, v.w * inv);
 }
 
 template <typename T>
 cudaError_t launch_join(const CacheAttn& o, const CacheAttn& p, cudaStream_t s) {
-  const int fit = kJoinThreads / (o.c.d / 4), heads = o.G < fit ? o.G : fit;
+  // heads of a block: a thread for each four of their columns
+  const int fit = kJoinThreads / (o.c.d / 4), most = fit < kJoinHeads ? fit : kJoinHeads;
+  const int heads = o.G < most ? o.G : most;
   const cudaError_t e = prefer_max_shared<cache_join_kernel<T>>();
   if (e != cudaSuccess) return e;
   return launch_pdl(cache_join_kernel<T>,
@@ -276,9 +309,12 @@ cudaError_t launch_cache_shared(const CacheSharedCall& s, int num_sms, unsigned 
                                 cudaStream_t stream) {
   const Shape x = shape_of(s, num_sms);
   CacheAttn own = args_of(s, s.cache, x.own, status), pre = args_of(s, s.prefix, x.pre, status);
+  if (x.both) return launch_both(own, pre, x.own.D, x.both, stream);
   cudaError_t e = x.pre.box ? launch_prefix_tc(pre, stream)
-                          : launch_parts<kGroup>(pre, x.pre.D, stream);
-  if (e == cudaSuccess) e = launch_parts<kOwn>(own, x.own.D, stream);
+                            : launch_parts<kGroup>(pre, x.pre.D, stream);
+  if (e == cudaSuccess)
+    e = x.warps ? launch_own_parts(own, x.own.D, x.warps, stream)
+                : launch_parts<kOwn>(own, x.own.D, stream);
   if (e != cudaSuccess) return e;
   return s.cache.dt == AVITS_BF16 ? launch_join<__nv_bfloat16>(own, pre, stream)
                                   : launch_join<float>(own, pre, stream);

@@ -723,6 +723,9 @@ constexpr int stages() { return 2; }
 constexpr int line_ctas(int D, int rows, bool bf16) {
   return D > 128 ? 1 : bf16 && rows > 8 ? 2 : D <= 64 ? 4 : bf16 ? 2 : 3;
 }
+constexpr int own_ctas(int D, int rows, bool bf16) {
+  return bf16 && rows == 8 && D == 128 ? 3 : line_ctas(D, rows, bf16);
+}
 // A cluster's CTAs hold to what their registers allow without spills.
 constexpr int cluster_ctas(int D, int rows, int warps) {
   return (D > 128 ? 4 : rows > 8 ? 8 : 12) / warps;
@@ -811,6 +814,11 @@ cudaError_t by_rows(const CacheAttn& a, int D, F f) {
 // The launchers of the two forms, by width (64, 128, 256) and rows of a unit.
 cudaError_t launch_line(CacheAttn& a, int D, int num_sms, cudaStream_t s);
 cudaError_t launch_cluster(CacheAttn& a, int D, int ncta, int warps, cudaStream_t s);
+
+// Shared prefixes: own tokens as parts, a CTA of `warps` warps per unit; prefix and own tokens in
+// one launch, a cluster of ncta CTAs per unit.
+cudaError_t launch_own_parts(CacheAttn& a, int D, int warps, cudaStream_t s);
+cudaError_t launch_both(CacheAttn& a, const CacheAttn& p, int D, int ncta, cudaStream_t s);
 
 // Prefixes on the tensor cores: units of 128 rows, tiles of 64 keys, two CTAs to an SM.  Tokens
 // of a copy, 0 where the type, the width or the pages' layout is not theirs.

@@ -193,6 +193,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       AVITS_I8(0), AVITS_I8(8), AVITS_I8(16), AVITS_I8(24)
       : "memory");
 }
+// 16 registers to consecutive columns.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, "
+      "%12, %13, %14, %15, %16};" ::"r"(taddr),
+      AVITS_I8(0), AVITS_I8(8)
+      : "memory");
+}
 // The thread's tcgen05.st have completed.
 __device__ __forceinline__ void tmem_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");

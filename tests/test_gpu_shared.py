@@ -123,6 +123,17 @@ CASES = [   # sizes, prefixes, own lengths, H, Hkv, d, page, layout
     ([1] * 30, [3 + i for i in range(30)], [i for i in range(30)], 8, 8, 64, 16, "tokens"),
     ([2], [5], [600, 900], 40, 1, 64, 16, "heads"),
     ([3, 3], [0, 40], [0, 2, 5, 0, 1, 0], 4, 2, 128, 16, "tokens"),
+    # by parts: prefixes too long for one launch, on the tensor cores or (page, width, type) not
+    ([3], [4200], [5, 0, 70], 8, 2, 128, 16, "tokens"),
+    ([2, 0, 3], [5000, 50, 9], [3, 1, 30, 2, 17], 6, 3, 64, 8, "heads"),
+    ([19, 1], [4100, 6000], [1 + 60 * i for i in range(20)], 16, 2, 96, 24, "joint"),
+    ([4, 4], [4310, 64], [2] * 8, 6, 2, 72, 5, "joint"),
+    ([5], [4177], [3, 9, 1, 0, 1500], 16, 1, 256, 16, "tokens"),
+    ([2, 2], [4500, 4096], [600, 9000, 0, 16], 40, 1, 64, 16, "heads"),
+    ([40, 41], [4257, 640], [9] * 81, 4, 1, 128, 128, "tokens"),
+    ([3, 2], [0, 4400], [0, 3, 0, 0, 4], 4, 2, 80, 48, "tokens"),
+    # and where they are many
+    ([90, 60], [70, 3], [i % 40 for i in range(150)], 8, 8, 64, 16, "heads"),
 ]
 
 
