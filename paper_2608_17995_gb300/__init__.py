@@ -586,8 +586,8 @@ class KVCache:
     The description is fixed: other tensors are another KVCache.
     """
     __slots__ = ("k_pages", "v_pages", "block_table", "lens", "acc", "B", "Hkv", "d", "dtype",
-                 "page_size", "max_len", "device", "int32", "float32", "_index", "_struct", "_ref",
-                 "_need", "_alloc", "_free", "_append", "_attend", "_plan", "_append_rotated", "_shared", "_shared_need",
+                 "page_size", "max_len", "device", "int32", "int64", "float32", "_index", "_struct", "_ref",
+                 "_need", "_alloc", "_free", "_append", "_attend", "_plan", "_append_rotated", "_shared", "_shared_need", "_shape",
                  "_evict")
 
     def __init__(self, k_pages, v_pages, block_table, lens, acc=None, max_len: Optional[int] = None):
@@ -634,9 +634,10 @@ class KVCache:
                                     block_table.stride(0), sa[0], sa[1], dt, B, Hkv, d, num_pages,
                                     page_size, self.max_len)
         self._ref = ctypes.addressof(self._struct)
+        self._shape = bytes(self._struct)[40:]   # strides, type and sizes
         self._need = {}   # (H, weights) -> workspace bytes
         # looked up once: the calls' host time is most of a small call's
-        self.int32, self.float32 = torch.int32, torch.float32
+        self.int32, self.int64, self.float32 = torch.int32, torch.int64, torch.float32
         # what torch.cuda.caching_allocator_alloc and _delete call
         self._alloc = torch._C._cuda_cudaCachingAllocator_raw_alloc
         self._free = torch._C._cuda_cudaCachingAllocator_raw_delete
@@ -810,33 +811,51 @@ def avits_cache_plan(cache: KVCache, change, free_pages, free_count, cu_new, slo
     slots [T] int64, seq, place, pos [T] int32 (pos optional: place + pos_base[b]):
     where each of the step's T rows goes, -1 for padding.  A sequence that finds no
     room is left as it was, its rows padding (avits_device_status: 7)."""
-    B, i32 = cache.B, cache.int32
-    T = slots.shape[0]
+    B, i32, index = cache.B, cache.int32, cache._index
     if lens is None:
         lens = cache.lens
     if free_out is None:
         free_out = free_count
+    if slots.dim() != 1 or slots.dtype != cache.int64 or not slots.is_contiguous():
+        raise ValueError("slots must be a contiguous int64 [T] tensor")
+    T = slots.numel()
     if T > _INT_MAX:
         raise ValueError("more rows than 32 bits count")
-    for t, n in ((change, B), (lens, B), (cu_new, B + 1), (free_count, 1), (free_out, 1), (seq, T),
-                 (place, T), (free_pages, cache._struct.num_pages)):
-        if t.shape != (n,) or t.dtype != i32 or not t.is_contiguous():
-            raise ValueError("change, lens [B], cu_new [B+1], free_count, free_out [1], seq, place [T] "
-                             "and free_pages [num_pages] must be contiguous int32 tensors")
-    if slots.dim() != 1 or slots.dtype != _torch().int64 or not slots.is_contiguous():
-        raise ValueError("slots must be a contiguous int64 [T] tensor")
-    if pos is not None and (pos.shape != (T,) or pos.dtype != i32 or not pos.is_contiguous()):
-        raise ValueError("pos must be a contiguous int32 [T] tensor")
-    if pos_base is not None and (pos is None or pos_base.shape != (B,) or pos_base.dtype != i32 or
-                                 not pos_base.is_contiguous()):
-        raise ValueError("pos_base must be a contiguous int32 [B] tensor, given with pos")
-    _elsewhere(cache, change, lens, cu_new, free_count, free_out, seq, place, free_pages, slots, pos,
-               pos_base)
+    batch, one, rows = (B,), (1,), (T,)
+    # in a row, not in a loop: 0.3 us a tensor there
+    if change.shape != batch or lens.shape != batch or cu_new.shape != (B + 1,) or \
+            free_count.shape != one or free_out.shape != one or seq.shape != rows or \
+            place.shape != rows or free_pages.shape != (cache._struct.num_pages,) or \
+            change.dtype != i32 or lens.dtype != i32 or cu_new.dtype != i32 or \
+            free_count.dtype != i32 or free_out.dtype != i32 or seq.dtype != i32 or \
+            place.dtype != i32 or free_pages.dtype != i32 or \
+            not (change.is_contiguous() and lens.is_contiguous() and cu_new.is_contiguous() and
+                 free_pages.is_contiguous() and seq.is_contiguous() and place.is_contiguous()):
+        raise ValueError("change, lens [B], cu_new [B+1], free_count, free_out [1], seq, place [T] "
+                         "and free_pages [num_pages] must be contiguous int32 tensors")
+    pos_at = base_at = None
+    if pos is not None:
+        if pos.shape != rows or pos.dtype != i32 or not pos.is_contiguous():
+            raise ValueError("pos must be a contiguous int32 [T] tensor")
+        pos_at = pos.data_ptr()
+    if pos_base is not None:
+        if pos is None or pos_base.shape != batch or pos_base.dtype != i32 or \
+                not pos_base.is_contiguous():
+            raise ValueError("pos_base must be a contiguous int32 [B] tensor, given with pos")
+        base_at = pos_base.data_ptr()
+    if change.get_device() != index or lens.get_device() != index or \
+            cu_new.get_device() != index or free_count.get_device() != index or \
+            free_out.get_device() != index or seq.get_device() != index or \
+            place.get_device() != index or free_pages.get_device() != index or \
+            slots.get_device() != index or \
+            (pos is not None and pos.get_device() != index) or \
+            (pos_base is not None and pos_base.get_device() != index):
+        _elsewhere(cache, change, lens, cu_new, free_count, free_out, seq, place, free_pages, slots,
+                   pos, pos_base)
     rc = cache._plan(cache._ref, lens.data_ptr(), change.data_ptr(), free_pages.data_ptr(),
                      free_count.data_ptr(), free_out.data_ptr(), T, cu_new.data_ptr(),
-                     slots.data_ptr(), seq.data_ptr(), place.data_ptr(),
-                     None if pos is None else pos.data_ptr(),
-                     None if pos_base is None else pos_base.data_ptr(), _call_stream(cache, stream))
+                     slots.data_ptr(), seq.data_ptr(), place.data_ptr(), pos_at, base_at,
+                     _call_stream(cache, stream))
     if rc != 0:
         _check("avits_cache_plan", rc)
 
@@ -865,7 +884,8 @@ class Rotary:
                  on, in between linearly)
     magnitude    of the rotated values
     """
-    __slots__ = ("rot", "axes", "freq", "device", "_struct", "_ref", "_index", "_call")
+    __slots__ = ("rot", "axes", "freq", "device", "_struct", "_ref", "_index", "_call",
+                 "int32", "codes")
 
     def __init__(self, rot: int, base: float = 10000.0, sections: Optional[Sequence[int]] = None,
                  interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
@@ -896,11 +916,10 @@ class Rotary:
         self._ref = ctypes.addressof(self._struct)
         self._index = self.freq.get_device()
         self._call = lib().avits_norm_rotate
+        self.int32, self.codes = torch.int32, {torch.bfloat16: BF16, torch.float32: F32}
 
 
 def _weight_at(w, d, dtype, index):
-    if w is None:
-        return None
     if w.shape != (d,) or w.dtype != dtype or not w.is_contiguous():
         raise ValueError("weights must be contiguous [d] tensors of the type of q")
     if w.get_device() != index:
@@ -908,14 +927,25 @@ def _weight_at(w, d, dtype, index):
     return w.data_ptr()
 
 
-def _axes4(t):
-    """Strides of [N,heads,d] or [B,N,heads,d], and the shape, as of the latter."""
-    st, sh = t.stride(), t.shape
-    if len(sh) == 3:
-        return (0, *st), (1, *sh)
-    if len(sh) != 4:
-        raise ValueError("[B, N, heads, d] or [N, heads, d] expected")
-    return st, sh
+@functools.lru_cache(maxsize=1024)
+def _strides_at(batch, token, head):
+    """An array of three strides (kept: making one takes 0.4 us) and its address."""
+    arr = _Int64x3(batch, token, head)
+    return arr, ctypes.addressof(arr)
+
+
+def _heads_of(t, name):
+    """Shape of [B,N,heads,d] or [N,heads,d] as of the former, and the address of its strides."""
+    st, shape = t.stride(), t.shape
+    if len(shape) == 4:
+        b, n, h, x = st
+    elif len(shape) == 3:
+        b, (n, h, x), shape = 0, st, (1, *shape)
+    else:
+        raise ValueError("%s: [B, N, heads, d] or [N, heads, d] expected" % name)
+    if x != 1:
+        raise ValueError("%s: the head-dim axis must be contiguous" % name)
+    return shape, _strides_at(b, n, h)[1]
 
 
 def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q_weight=None,
@@ -925,44 +955,38 @@ def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q
     16-byte aligned strides, d contiguous; without B for one sequence; an output may
     be its input).  positions int32 [B,N,axes] or [N,axes] (one axis: [B,N] or [N] as
     well; None if nothing turns), the axes contiguous."""
-    qs, (B, N, H, d) = _axes4(q)
-    os_, shape = _axes4(q_out)
+    (B, N, H, d), q_str = _heads_of(q, "q")
+    shape, qo_str = _heads_of(q_out, "q_out")
     dtype, index = q.dtype, rotary._index
     if tuple(shape) != (B, N, H, d) or (k is None) != (k_out is None):
         raise ValueError("q / q_out shapes disagree, or one of k and k_out is missing")
-    dt = _dtype_code(q)
-    tensors = [q, q_out]
+    code = rotary.codes.get(dtype)
+    if code is None or q_out.dtype != dtype:
+        raise TypeError("bfloat16 or float32 expected, the same for q, k and their outputs")
+    if q.get_device() != index or q_out.get_device() != index:
+        raise ValueError("q or q_out on %s, %s: the rotary is on %s" % (q.device, q_out.device,
+                                                                       rotary.device))
     Hkv = 0
-    k_at = ks = ko_at = kos = None
+    k_at = k_str = ko_at = ko_str = None
     if k is not None:
-        ks, (kB, kN, Hkv, kd) = _axes4(k)
-        kos, kshape = _axes4(k_out)
-        if (kB, kN, kd) != (B, N, d) or tuple(kshape) != (B, N, Hkv, d) or Hkv == 0:
+        (kB, kN, Hkv, kd), k_str = _heads_of(k, "k")
+        shape, ko_str = _heads_of(k_out, "k_out")
+        if (kB, kN, kd) != (B, N, d) or tuple(shape) != (B, N, Hkv, d) or Hkv == 0:
             raise ValueError("k / k_out must be [B, N, Hkv, d] beside q")
         if k.dtype != dtype or k_out.dtype != dtype:
-            raise TypeError("q, k and their outputs' dtypes differ")
-        tensors += [k, k_out]
-        if ks[3] != 1 or kos[3] != 1:
-            raise ValueError("the head-dim axis must be contiguous")
+            raise TypeError("bfloat16 or float32 expected, the same for q, k and their outputs")
+        if k.get_device() != index or k_out.get_device() != index:
+            raise ValueError("k or k_out on %s, %s: the rotary is on %s" % (k.device, k_out.device,
+                                                                           rotary.device))
         k_at, ko_at = k.data_ptr(), k_out.data_ptr()
-        ks, kos = _Int64x3(*ks[:3]), _Int64x3(*kos[:3])
-    if q_out.dtype != dtype:
-        raise TypeError("q, k and their outputs' dtypes differ")
-    if qs[3] != 1 or os_[3] != 1:
-        raise ValueError("the head-dim axis must be contiguous")
-    if max(B, N, H, Hkv, d) > _INT_MAX:
+    if B > _INT_MAX or N > _INT_MAX or H > _INT_MAX or Hkv > _INT_MAX or d > _INT_MAX:
         raise ValueError("sizes of more than 32 bits")
-    p_at, p_sb, p_sn = None, 0, 0
-    if rotary.rot:
-        p_at, p_sb, p_sn = _positions(rotary, positions, B, N)
-        tensors.append(positions)
-    for t in tensors:
-        if t.get_device() != index:
-            raise ValueError("tensor on %s, the rotary is on %s" % (t.device, rotary.device))
-    rc = rotary._call(rotary._ref, dt, B, N, d, p_at, p_sb, p_sn, q.data_ptr(), H, _Int64x3(*qs[:3]),
-                      q_out.data_ptr(), _Int64x3(*os_[:3]), k_at, Hkv, ks, ko_at, kos,
-                      1 if norm else 0, _weight_at(q_weight, d, dtype, index),
-                      _weight_at(k_weight, d, dtype, index), eps, _rotary_stream(rotary, stream))
+    p_at, p_sb, p_sn = _positions(rotary, positions, B, N) if rotary.rot else (None, 0, 0)
+    rc = rotary._call(rotary._ref, code, B, N, d, p_at, p_sb, p_sn, q.data_ptr(), H, q_str,
+                      q_out.data_ptr(), qo_str, k_at, Hkv, k_str, ko_at, ko_str, 1 if norm else 0,
+                      q_weight if q_weight is None else _weight_at(q_weight, d, dtype, index),
+                      k_weight if k_weight is None else _weight_at(k_weight, d, dtype, index), eps,
+                      _rotary_stream(rotary, stream))
     if rc != 0:
         _check("avits_norm_rotate", rc)
     return q_out
@@ -970,22 +994,22 @@ def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q
 
 def _positions(rotary: Rotary, p, B, N):
     """Address and strides (sequence, token) of the positions of [B,N] tokens."""
-    if p is None or p.dtype != _torch().int32:
+    if p is None or p.dtype != rotary.int32:
         raise ValueError("positions must be an int32 tensor")
-    shape, st = tuple(p.shape), p.stride()
-    if rotary.axes == 1 and shape == (N,):
+    if p.get_device() != rotary._index:
+        raise ValueError("positions on %s, the rotary is on %s" % (p.device, rotary.device))
+    shape, st, axes = p.shape, p.stride(), rotary.axes
+    if axes == 1 and shape == (N,):
         return p.data_ptr(), 0, st[0]
-    if rotary.axes == 1 and shape == (B, N):
+    if axes == 1 and shape == (B, N):
         return p.data_ptr(), st[0], st[1]
-    if shape == (N, rotary.axes):
-        at = (0, st[0])
-    elif shape == (B, N, rotary.axes):
-        at = (st[0], st[1])
-    else:
-        raise ValueError("positions must be [B, N, axes] or [N, axes]")
-    if rotary.axes > 1 and st[-1] != 1:
+    if axes > 1 and st[-1] != 1:
         raise ValueError("the positions' axes must be contiguous")
-    return (p.data_ptr(), *at)
+    if shape == (N, axes):
+        return p.data_ptr(), 0, st[0]
+    if shape == (B, N, axes):
+        return p.data_ptr(), st[0], st[1]
+    raise ValueError("positions must be [B, N, axes] or [N, axes]")
 
 
 def _rotary_stream(rotary: Rotary, stream):
@@ -1019,7 +1043,7 @@ def avits_cache_append_rotated(cache: KVCache, rotary: Rotary, positions, slots,
     v_st, v_sh, v_sd = v_new.stride()
     if q_sd != 1 or o_sd != 1 or k_sd != 1 or v_sd != 1:
         raise ValueError("the head-dim axis must be contiguous")
-    if slots.shape != (T,) or slots.dtype != _torch().int64 or not slots.is_contiguous():
+    if slots.shape != (T,) or slots.dtype != cache.int64 or not slots.is_contiguous():
         raise ValueError("slots must be a contiguous int64 [T] tensor")
     s_at = p_at = None
     if seq is not None or place is not None or cache.acc is not None:
@@ -1031,16 +1055,16 @@ def avits_cache_append_rotated(cache: KVCache, rotary: Rotary, positions, slots,
     x_at, x_st = None, 0
     if rotary.rot:
         x_at, _, x_st = _positions(rotary, positions, 1, T)
-        _elsewhere(cache, positions)
     if rotary._index != index or q.get_device() != index or q_out.get_device() != index or \
             k_new.get_device() != index or v_new.get_device() != index or slots.get_device() != index:
         _elsewhere(cache, rotary.freq, q, q_out, k_new, v_new, slots)
     rc = cache._append_rotated(cache._ref, rotary._ref, T, x_at, x_st, slots.data_ptr(), s_at, p_at,
                                q.data_ptr(), H, q_st, q_sh, q_out.data_ptr(), o_st, o_sh,
                                k_new.data_ptr(), k_st, k_sh, v_new.data_ptr(), v_st, v_sh,
-                               1 if norm else 0, _weight_at(q_weight, d, dtype, index),
-                               _weight_at(k_weight, d, dtype, index), eps,
-                               _call_stream(cache, stream))
+                               1 if norm else 0,
+                               q_weight if q_weight is None else _weight_at(q_weight, d, dtype, index),
+                               k_weight if k_weight is None else _weight_at(k_weight, d, dtype, index),
+                               eps, _call_stream(cache, stream))
     if rc != 0:
         _check("avits_cache_append_rotated", rc)
     return q_out
@@ -1054,8 +1078,7 @@ def avits_cache_attention_shared_workspace(cache: KVCache, prefix: KVCache, H: i
 
 def _shared_bytes(cache: KVCache, prefix: KVCache, H: int) -> int:
     """The same by what it depends on of the prefix: kept with the cache."""
-    key = (H, prefix.B, prefix.max_len, prefix.page_size, prefix.Hkv, prefix.d, prefix.dtype,
-           prefix.k_pages.stride(), prefix.v_pages.stride())
+    key = (H, prefix._shape)
     need = cache._shared_need.get(key)
     if need is None:
         need = cache._shared_need[key] = avits_cache_attention_shared_workspace(cache, prefix, H)

@@ -42,6 +42,24 @@ __device__ __forceinline__ int checked_page(const avits_kv_cache& c, int page, u
   return -1;
 }
 
+// The sequence of token t: the number of b in [1, B] with cu[b] <= t, found in
+// rounds of 32 probes.  B or more: past the last sequence.
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int t, int lane) {
+  int lo = 0, n = B;            // the answer lies in [lo, lo + n]
+  while (n > 0) {
+    const int step = (n + 31) / 32;
+    const int at = lo + min((lane + 1) * step, n);     // in [lo+1, lo+n]
+    const unsigned below = __ballot_sync(0xffffffffu, cu[at] <= t);
+    const int k = __popc(below);                        // probes at or below t
+    if (step == 1) return lo + min(k, n);
+    const int from = lo + min(k * step, n);
+    if (k == 32) return from;
+    n = min(step - 1, lo + n - from);
+    lo = from;
+  }
+  return lo;
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -8,9 +8,10 @@
 // Ranks (which page, which row) are sums over the sequences before it: two scans,
 // since the pages taken may be ones given back by a later sequence.
 //
-// The bytes are few (a step of 256 sequences 25 KB), so that latency is all: one CTA
-// scans and moves pages, a second kernel over all SMs writes the rows where they are
-// many.
+// The bytes are few (a step of 256 sequences 25 KB), so that latency is all: one CTA, a
+// thread to a sequence, scans and moves pages; what is more than a few pages or rows of a
+// sequence goes to whole warps.  Where the rows are many, a second kernel over all SMs
+// writes them.
 #include "cache_common.cuh"
 #include "avits_internal.h"
 
@@ -18,10 +19,10 @@ namespace avits {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kPlanWarps = kPlanThreads / 32;
-constexpr int kRowThreads = 256;
-constexpr int kOwnPages = 4;      // pages that a thread moves alone; more, and its warp does
-constexpr int kFewRows = 4096;    // rows that the first kernel's CTA writes itself
+constexpr int kRowThreads = 128;
+constexpr int kOwnPages = 2;      // pages, and rows, that a thread moves alone
+constexpr int kOwnRows = 4;
+constexpr int kFewRows = 8192;    // rows that the first kernel's CTA writes itself
 
 struct Plan {
   CachePlanCall p;
@@ -34,90 +35,91 @@ __device__ __forceinline__ int pages_of(const Plan& a, int n) {
   return a.page.div(n + a.p.cache.page_size - 1);
 }
 
-// Sums of x over the threads before this one, and over all; a barrier at each end.
-__device__ __forceinline__ long long block_scan(long long x, long long* s_warp, int tid,
-                                                long long& total) {
-  const int lane = tid & 31, w = tid >> 5;
-  long long inc = x;
+// Sums of x and y over the threads before this one, and over all.  The caller has a barrier
+// between two of these.
+__device__ __forceinline__ longlong2 block_scan(longlong2 x, longlong2* s_warp, longlong2& total) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  longlong2 inc = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += y;
+    const long long y = __shfl_up_sync(0xffffffffu, inc.x, o), z = __shfl_up_sync(0xffffffffu, inc.y, o);
+    if (lane >= o) {
+      inc.x += y;
+      inc.y += z;
+    }
   }
-  __syncthreads();
   if (lane == 31) s_warp[w] = inc;
   __syncthreads();
-  long long own = s_warp[lane], run = own;
+  const longlong2 own = lane < warps ? s_warp[lane] : make_longlong2(0, 0);
+  longlong2 run = own;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, run, o);
-    if (lane >= o) run += y;
+    const long long y = __shfl_up_sync(0xffffffffu, run.x, o), z = __shfl_up_sync(0xffffffffu, run.y, o);
+    if (lane >= o) {
+      run.x += y;
+      run.y += z;
+    }
   }
-  total = __shfl_sync(0xffffffffu, run, 31);
-  return __shfl_sync(0xffffffffu, run - own, w) + inc - x;
+  total = make_longlong2(__shfl_sync(0xffffffffu, run.x, 31), __shfl_sync(0xffffffffu, run.y, 31));
+  return make_longlong2(__shfl_sync(0xffffffffu, run.x - own.x, w) + inc.x - x.x,
+                        __shfl_sync(0xffffffffu, run.y - own.y, w) + inc.y - x.y);
 }
-static_assert(kPlanWarps == 32, "block_scan reads one sum per lane");
+static_assert(kPlanThreads == 32 * 32, "block_scan reads one sum per lane");
 
-// f(column, rank) for a sequence's columns col .. col+n-1, ranks from `rank` on: the
-// first few by its thread, the others by the warp (all of it calls this).
-template <typename F>
-__device__ __forceinline__ void over_pages(int b, int col, int n, long long rank, int lane, F f) {
-  const int own = min(n, kOwnPages);
-  for (int i = 0; i < own; ++i) f(b, col + i, rank + i);
-  unsigned more = __ballot_sync(0xffffffffu, n > own);
-  while (more) {
-    const int l = __ffs(more) - 1;
-    more &= more - 1;
-    const int bl = __shfl_sync(0xffffffffu, b, l), cl = __shfl_sync(0xffffffffu, col, l);
-    const int nl = __shfl_sync(0xffffffffu, n, l);
-    const long long rl = __shfl_sync(0xffffffffu, rank, l);
-    for (int i = kOwnPages + lane; i < nl; i += 32) f(bl, cl + i, rl + i);
-  }
-}
-
-// Row t of the step.  place[cu[b]], of a sequence's first row, is there already: -1 if
-// it got no pages.
-__device__ __forceinline__ void write_row(const Plan& a, const int32_t* cu, int t) {
+// Row t: token `place` of sequence b on page `page`; place < 0: padding.
+__device__ __forceinline__ void put_row(const Plan& a, int t, int b, int place, int col, int page) {
   const CachePlanCall& p = a.p;
-  int lo = 0, hi = p.cache.B;            // sequences whose rows end at t or before it
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid + 1] <= t) lo = mid + 1; else hi = mid;
-  }
-  const int b = lo;
   int64_t slot = -1;
-  int place = -1, pos = -1, seq = -1;
-  const int head = b < p.cache.B ? cu[b] : 0;
-  if (b < p.cache.B) place = p.place[head];
   if (place >= 0) {
-    place += t - head;
-    seq = b;
-    pos = place + (p.pos_base ? p.pos_base[b] : 0);
-    const int col = a.page.div(place);
-    const int page = p.cache.block_table[(int64_t)b * p.cache.table_sb + col];
     if ((unsigned)page < (unsigned)p.cache.num_pages)
       slot = (int64_t)page * p.cache.page_size + (place - col * p.cache.page_size);
     else
       raise_status(a.status, AVITS_ERR_PAGE);
   }
   p.slots[t] = slot;
-  p.seq[t] = seq;
-  if (b >= p.cache.B || t != head) p.place[t] = place;
-  if (p.pos) p.pos[t] = pos;
+  p.seq[t] = place >= 0 ? b : -1;
+  p.place[t] = place;
+  if (p.pos) p.pos[t] = place >= 0 ? place + (p.pos_base ? p.pos_base[b] : 0) : -1;
 }
+__device__ __forceinline__ void put_row(const Plan& a, int t, int b, int place) {
+  const int col = place >= 0 ? a.page.div(place) : 0;
+  const int page =
+      place >= 0 ? a.p.cache.block_table[(int64_t)b * a.p.cache.table_sb + col] : -1;
+  put_row(a, t, b, place, col, page);
+}
+
+// put(i, get(i)) for i < n over a warp's lanes, four reads on their way at once.
+template <typename Get, typename Put>
+__device__ __forceinline__ void by_four(int n, int lane, Get get, Put put) {
+  for (int i0 = lane; i0 < n; i0 += 128) {
+    int v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i0 + 32 * k < n) v[k] = get(i0 + 32 * k);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i0 + 32 * k < n) put(i0 + 32 * k, v[k]);
+  }
+}
+
+// A sequence's part of the plan that whole warps do.
+struct Big {
+  int b, col, n;             // pages: columns col .. col+n-1, ranks from `rank` on
+  int row, rows, place;      // rows, from `row` on; the first one's place, -1: padding
+  long long rank;
+};
 
 __global__ void __launch_bounds__(kPlanThreads)
 cache_plan_kernel(const __grid_constant__ Plan a) {
-  __shared__ long long s_warp[32];
-  __shared__ int s_taken;
+  __shared__ longlong2 s_warp[2][32];
+  __shared__ int s_taken, s_big;
+  __shared__ Big s_list[kPlanThreads];
   const CachePlanCall& p = a.p;
   const avits_kv_cache& c = p.cache;
   int32_t* table = const_cast<int32_t*>(c.block_table);
-  const int tid = threadIdx.x, lane = tid & 31;
-  if (tid == 0) s_taken = 0;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, step = blockDim.x;
+  if (tid == 0) s_taken = s_big = 0;
   pdl_wait_then_trigger();
-  const int each = (c.B + kPlanThreads - 1) / kPlanThreads;
-  const int b0 = min(c.B, tid * each), mine = min(c.B, b0 + each) - b0;
   const int had = *p.free_count;
   const int count = min(max(had, 0), c.num_pages);
   if (tid == 0 && had != count) raise_status(a.status, AVITS_ERR_PAGE);
@@ -127,7 +129,8 @@ cache_plan_kernel(const __grid_constant__ Plan a) {
     bool ok;                    // a length in range, and one that fits the table
   };
   auto item = [&](int b) {
-    Item x;
+    Item x{0, 0, 0, 0, true};
+    if (b >= c.B) return x;
     x.n0 = p.lens[b];
     const int ch = p.change[b];
     const int64_t n1 = (int64_t)x.n0 + ch;
@@ -137,66 +140,112 @@ cache_plan_kernel(const __grid_constant__ Plan a) {
     x.give = x.ok && ch < 0 ? pages_of(a, x.n0) - pages_of(a, x.n1) : 0;
     return x;
   };
+  // what the list holds, by whole warps; between two barriers
+  auto over_list = [&](auto f) {
+    __syncthreads();
+    const int n = s_big;
+    for (int e = w; e < n; e += step >> 5) f(s_list[e]);
+    __syncthreads();
+    if (tid == 0) s_big = 0;
+  };
 
-  long long rows = 0, give = 0, all_rows, all_give;
-  for (int i = 0; i < mine; ++i) {
-    const Item x = item(b0 + i);
-    rows += x.rows;
-    give += x.give;
+  // Pages given back, `step` sequences at a time.
+  Item x = item(tid);
+  longlong2 at = make_longlong2(0, 0), sum;     // rows and pages given back before the chunk
+  longlong2 mine = block_scan(make_longlong2(x.rows, x.give), s_warp[0], sum);
+  for (int b0 = 0;;) {
+    const long long rank = count + at.y + mine.y;
+    const int b = b0 + tid, col = x.give > 0 ? pages_of(a, x.n1) : 0;
+    const bool big = x.give > kOwnPages;
+    if (big) s_list[atomicAdd(&s_big, 1)] = Big{b, col, x.give, 0, 0, 0, rank};
+    for (int i = 0; !big && i < x.give; ++i)
+      if (rank + i < c.num_pages) p.free_pages[rank + i] = table[(int64_t)b * c.table_sb + col + i];
+    over_list([&](const Big& y) {
+      const int32_t* from = table + (int64_t)y.b * c.table_sb + y.col;
+      by_four(y.n, lane, [&](int i) { return from[i]; },
+              [&](int i, int v) {
+                if (y.rank + i < c.num_pages) p.free_pages[y.rank + i] = v;
+              });
+    });
+    at.x += sum.x;
+    at.y += sum.y;
+    b0 += step;
+    if (b0 >= c.B) break;
+    x = item(b0 + tid);
+    mine = block_scan(make_longlong2(x.rows, x.give), s_warp[0], sum);
   }
-  rows = block_scan(rows, s_warp, tid, all_rows);
-  give = block_scan(give, s_warp, tid, all_give);
+  const long long all_give = at.y, all_rows = at.x;
   if (tid == 0 && count + all_give > c.num_pages) raise_status(a.status, AVITS_ERR_PAGE);
   const int avail = (int)min(count + all_give, (long long)c.num_pages);
 
-  // pages given back; what is needed, now that the rows before each sequence are known
-  long long need = 0, all_need, row = rows;
-  for (int i = 0; i < each; ++i) {
-    Item x{};
-    const int b = b0 + i;
-    if (i < mine) {
-      x = item(b);
-      row += x.rows;
-      if (x.ok && x.rows > 0 && row <= p.T) need += pages_of(a, x.n1) - pages_of(a, x.n0);
-    }
-    over_pages(b, x.give > 0 ? pages_of(a, x.n1) : 0, x.give, count + give, lane,
-               [&](int bb, int col, long long at) {
-                 if (at < c.num_pages) p.free_pages[at] = table[(int64_t)bb * c.table_sb + col];
-               });
-    give += x.give;
-  }
-  need = block_scan(need, s_warp, tid, all_need);      // its barriers: the list is complete
-
+  // Pages taken, and rows.
+  const bool once = c.B <= step;      // else the rows before a chunk's sequences are summed again
+  longlong2 before = make_longlong2(0, 0);
+  long long chunk_rows = 0;
   int taken = 0;
-  row = rows;
-  for (int i = 0; i < each; ++i) {
-    const int b = b0 + i;
-    int n = 0, col = 0;
-    long long rank = 0;
-    if (i < mine) {
-      const Item x = item(b);
-      const long long before = row;
-      row += x.rows;
-      bool ok = x.ok && (x.rows == 0 || row <= p.T);
-      if (ok && x.rows > 0) {
-        col = pages_of(a, x.n0);
-        n = pages_of(a, x.n1) - col;
-        rank = need;
-        need += n;
-        if (n > 0 && need > avail) {
-          ok = false;
-          n = 0;
-        }
-        if (n > 0) taken = (int)need;
-      }
+  for (int b0 = 0; b0 < c.B; b0 += step) {
+    const int b = b0 + tid;
+    if (!once) {
+      x = item(b);
+      __syncthreads();
+      mine = block_scan(make_longlong2(x.rows, 0), s_warp[0], sum);
+      chunk_rows = sum.x;
+    }
+    const long long row = before.x + mine.x;
+    bool ok = x.ok && (x.rows == 0 || row + x.rows <= p.T);
+    int col = 0, n = 0;
+    // of the first row, if that page is there already
+    const int col0 = x.rows > 0 && x.n0 >= 0 ? a.page.div(x.n0) : 0;
+    int page = -1;
+    if (ok && x.rows > 0) {
+      col = pages_of(a, x.n0);
+      n = pages_of(a, x.n1) - col;
+      if (col0 < col) page = table[(int64_t)b * c.table_sb + col0];
+    }
+    const longlong2 need = block_scan(make_longlong2(n, 0), s_warp[1], sum);
+    const long long rank = before.y + need.x;
+    if (n > 0 && rank + n > avail) {
+      ok = false;
+      n = 0;
+    }
+    if (n > 0) taken = (int)(rank + n);
+    const bool rows_in = x.rows > 0 && row < p.T;
+    const int rows = rows_in ? (int)min((long long)x.rows, p.T - row) : 0;
+    if (b < c.B) {
       if (!ok) raise_status(a.status, AVITS_ERR_PAGE);
       c.lens[b] = ok ? x.n1 : x.n0;
-      p.cu_new[b + 1] = (int)min(row, (long long)p.T);
-      if (x.rows > 0 && before < p.T) p.place[before] = ok ? x.n0 : -1;
+      p.cu_new[b + 1] = (int)min(row + x.rows, (long long)p.T);
     }
-    over_pages(b, col, n, rank, lane, [&](int bb, int cc, long long at) {
-      table[(int64_t)bb * c.table_sb + cc] = p.free_pages[avail - 1 - at];
+    const bool big = n > kOwnPages || (a.rows_here && rows > kOwnRows);
+    if (big) {
+      s_list[atomicAdd(&s_big, 1)] =
+          Big{b, col, n, (int)row, rows, ok ? x.n0 : -1, rank};
+    } else {
+      for (int i = 0; i < n; ++i) {
+        const int got = p.free_pages[avail - 1 - (rank + i)];
+        table[(int64_t)b * c.table_sb + col + i] = got;
+        if (col + i == col0) page = got;
+      }
+      if (a.rows_here) {
+        if (rows > 0) put_row(a, (int)row, b, ok ? x.n0 : -1, col0, page);
+        for (int i = 1; i < rows; ++i) put_row(a, (int)row + i, b, ok ? x.n0 + i : -1);
+      } else if (rows > 0) {
+        p.place[row] = ok ? x.n0 : -1;
+      }
+    }
+    over_list([&](const Big& y) {
+      int32_t* to = table + (int64_t)y.b * c.table_sb + y.col;
+      const int32_t* from = p.free_pages + (avail - 1 - y.rank);
+      by_four(y.n, lane, [&](int i) { return from[-(int64_t)i]; }, [&](int i, int v) { to[i] = v; });
+      __syncwarp();
+      if (a.rows_here)
+        for (int i = lane; i < y.rows; i += 32)
+          put_row(a, y.row + i, y.b, y.place >= 0 ? y.place + i : -1);
+      else if (lane == 0 && y.rows > 0)
+        p.place[y.row] = y.place;
     });
+    before.x += chunk_rows;
+    before.y += sum.x;
   }
   taken = __reduce_max_sync(0xffffffffu, taken);
   if (lane == 0) atomicMax(&s_taken, taken);
@@ -205,16 +254,36 @@ cache_plan_kernel(const __grid_constant__ Plan a) {
     *p.free_out = avail - s_taken;
     p.cu_new[0] = 0;
   }
-  if (!a.rows_here) return;
-  __syncthreads();
-  for (int t = tid; t < p.T; t += kPlanThreads) write_row(a, p.cu_new, t);
+  if (a.rows_here)
+    for (long long t = min(all_rows, (long long)p.T) + tid; t < p.T; t += step) put_row(a, (int)t, 0, -1);
 }
 
+// Rows by many CTAs.  place[cu[b]], of a sequence's first row, is there already: -1 if it
+// got no pages.
 __global__ void __launch_bounds__(kRowThreads)
 cache_plan_rows_kernel(const __grid_constant__ Plan a) {
+  const CachePlanCall& p = a.p;
+  const int32_t* cu = p.cu_new;
+  const int t = blockIdx.x * kRowThreads + threadIdx.x, lane = threadIdx.x & 31, B = p.cache.B;
   pdl_wait_then_trigger();
-  const int t = blockIdx.x * kRowThreads + threadIdx.x;
-  if (t < a.p.T) write_row(a, a.p.cu_new, t);
+  int b = sequence_of(cu, B, t - lane, lane);      // of the warp's first row
+  if (t >= p.T) return;
+  for (int i = 0; i < 4 && b < B && cu[b + 1] <= t; ++i) ++b;
+  if (b < B && cu[b + 1] <= t) {
+    int top = B;
+    while (b < top) {
+      const int mid = (b + top) >> 1;
+      if (cu[mid + 1] <= t) b = mid + 1; else top = mid;
+    }
+  }
+  const int head = b < B ? cu[b] : t, first = b < B ? p.place[head] : -1;
+  if (b < B && t == head) {       // its place is there: other rows read it
+    const int col = first >= 0 ? a.page.div(first) : 0;
+    const int page = first >= 0 ? p.cache.block_table[(int64_t)b * p.cache.table_sb + col] : -1;
+    put_row(a, t, b, first, col, page);
+    return;
+  }
+  put_row(a, t, b, first >= 0 ? first + (t - head) : -1);
 }
 
 }  // namespace
@@ -227,7 +296,9 @@ cudaError_t launch_cache_plan(const CachePlanCall& call, unsigned int* status, c
   a.status = status;
   cudaError_t e = prefer_max_shared<cache_plan_kernel>();
   if (e != cudaSuccess) return e;
-  e = launch_pdl(cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+  int threads = 512;
+  while (threads < call.cache.B && threads < kPlanThreads) threads *= 2;
+  e = launch_pdl(cache_plan_kernel, dim3(1), dim3(threads), 0, s, a);
   if (e != cudaSuccess || a.rows_here) return e;
   e = prefer_max_shared<cache_plan_rows_kernel>();
   if (e != cudaSuccess) return e;
