@@ -27,50 +27,55 @@ namespace {
 using namespace tc;
 
 constexpr int kBM = 128, kBN = 64;
-constexpr int kPreThreads = 192;
-constexpr int kTmemCols = 256;
 constexpr int kColO = 2 * kBN;
-constexpr int kMasks = 8;
 constexpr float kRise = 8.f;               // log2: a maximum that passes the reference by more
 constexpr float kUp = 1.f + 0x1p-20f;      // moves it
 constexpr int kMaxStages = 8;
 constexpr int kOutBytes = kBM * 16 * 4;    // 16 columns of O
 
-template <int D>
+// kT row tiles of 128 share the ring of keys and values.
+template <int D, int kT>
 struct Pre {
   static constexpr int kCB = D / 64;
   static constexpr int kTileBytes = kCB * kBN * 128;
-  static constexpr int kQBytes = kCB * kBM * 128;
-  static constexpr int kStages = D == 128 ? 3 : 6;
+  static constexpr int kQBytes = kCB * kBM * 128;        // of a row tile
+  static constexpr int kStages = kT == 2 ? (D == 128 ? 6 : 8) : (D == 128 ? 4 : 8);
+  static constexpr int kRows = kT * kBM;
+  static constexpr int kThreads = 32 * (1 + kT + 4 * kT);
+  static constexpr int kTmemCols = 256;                  // of a row tile
   static constexpr uint32_t kIdescS = idesc_bf16(kBM, kBN, false);
   static constexpr uint32_t kIdescPV = idesc_bf16(kBM, D, true);
 };
 
-struct PreBars {
+struct TileBars {      // of a row tile
   uint64_t q_full, q_empty, o_full, o_empty, drain;
-  uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
   uint64_t s_full[2], p_full[2], pv_done[2];
-  uint64_t mask_full[kMasks];
-  unsigned long long mask[kMasks];
+};
+template <int kT>
+struct PreBars {
+  TileBars tile[kT];
+  uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
   uint32_t tmem_base;
   int abort;
 };
 
-template <int D>
+template <int D, int kT>
 constexpr int pre_smem() {
-  return Pre<D>::kQBytes + Pre<D>::kStages * Pre<D>::kTileBytes + kOutBytes + (int)sizeof(PreBars);
+  using C = Pre<D, kT>;
+  return kT * (C::kQBytes + kOutBytes) + C::kStages * C::kTileBytes + (int)sizeof(PreBars<kT>);
 }
-// Two CTAs to an SM and beside them one of the kernel over the own tokens (2 warps, 128 wide), of
-// 228 KB with 1 KB of each block's kept by the system.
-static_assert(2 * (pre_smem<128>() + 1024) <= (228 - 40) * 1024, "room for own tokens");
+// One row tile: two CTAs to an SM, of 228 KB with 1 KB of each block's kept by the system.
+static_assert(2 * (pre_smem<128, 1>() + 1024) <= 228 * 1024, "two CTAs to an SM");
+static_assert(pre_smem<128, 2>() <= 227 * 1024, "the opt-in limit");
 
 // A CTA's piece of the line, segment by segment.
+template <int kRows>
 struct Walk {
   int g, u, t0, t1, nt, len, left, ubase, per;
   int seq, n;            // the group's first sequence, and the rows of a KV head
 
   __device__ __forceinline__ int units(const CacheAttn& a) const {
-    return a.c.Hkv * ((n + kBM - 1) / kBM);
+    return a.c.Hkv * ((n + kRows - 1) / kRows);
   }
   __device__ __forceinline__ void look(const CacheAttn& a) {
     const int2 m = members_of(a.start, a.seqs, g);
@@ -163,9 +168,10 @@ struct Walk {
     t1 = min(nt, left);
     return true;
   }
-  __device__ __forceinline__ QRows rows(const CacheAttn& a) const {
-    const int rg = (n + kBM - 1) / kBM, hk = u / rg, r0 = (u - hk * rg) * kBM;
-    return QRows{seq, hk * a.G, min(kBM, n - r0), r0, a.G};
+  // rows of the unit's row tile t
+  __device__ __forceinline__ QRows rows(const CacheAttn& a, int t) const {
+    const int rg = (n + kRows - 1) / kRows, hk = u / rg, r0 = (u - hk * rg) * kRows + t * kBM;
+    return QRows{seq, hk * a.G, max(0, min(kBM, n - r0)), r0, a.G};
   }
 };
 
@@ -173,35 +179,44 @@ __device__ __forceinline__ void bar_arrive(int id, int count) {
   asm volatile("barrier.cta.arrive %0, %1;" ::"r"(id), "r"(count) : "memory");
 }
 
-template <int D>
-__global__ void __launch_bounds__(256, 2)      // at most 128 registers: see the room left above
+// (c0, c1) += (a0, a1) * b.
+__device__ __forceinline__ void fma2(float a0, float a1, float b, float& c0, float& c1) {
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\t"
+      "mov.b64 c, {%0, %1};\n\tfma.rn.f32x2 c, a, b, c;\n\tmov.b64 {%0, %1}, c;\n\t}"
+      : "+f"(c0), "+f"(c1)
+      : "f"(a0), "f"(a1), "f"(b));
+}
+
+template <int D, int kT>
+__global__ void __launch_bounds__(Pre<D, kT>::kThreads, 3 - kT)
 cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                     const __grid_constant__ CacheAttn a) {
-  using C = Pre<D>;
+  using C = Pre<D, kT>;
   extern __shared__ __align__(1024) char smem[];
-  char* sQ = smem;
-  char* sKV = smem + C::kQBytes;
-  char* sO = sKV + C::kStages * C::kTileBytes;
-  PreBars* bars = reinterpret_cast<PreBars*>(sO + kOutBytes);
+  char* sKV = smem + kT * C::kQBytes;
+  char* sOut = sKV + C::kStages * C::kTileBytes;
+  PreBars<kT>* bars = reinterpret_cast<PreBars<kT>*>(sOut + kT * kOutBytes);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mk));
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mv));
-    mbar_init(&bars->q_full, 4);
-    mbar_init(&bars->q_empty, 1);
-    mbar_init(&bars->o_full, 1);
-    mbar_init(&bars->o_empty, 4);
-    mbar_init(&bars->drain, 1);
+    for (int t = 0; t < kT; ++t) {
+      TileBars& x = bars->tile[t];
+      mbar_init(&x.q_full, 4);
+      mbar_init(&x.q_empty, 1);
+      mbar_init(&x.o_full, 1);
+      mbar_init(&x.o_empty, 4);
+      mbar_init(&x.drain, 1);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&x.s_full[i], 1);
+        mbar_init(&x.p_full[i], 4);
+        mbar_init(&x.pv_done[i], 1);
+      }
+    }
     for (int i = 0; i < C::kStages; ++i) {
       mbar_init(&bars->kv_full[i], 1);
-      mbar_init(&bars->kv_empty[i], 1);
+      mbar_init(&bars->kv_empty[i], kT);      // a commit per row tile
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars->s_full[i], 1);
-      mbar_init(&bars->p_full[i], 4);
-      mbar_init(&bars->pv_done[i], 1);
-    }
-    for (int i = 0; i < kMasks; ++i) mbar_init(&bars->mask_full[i], 1);
     bars->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
@@ -209,17 +224,17 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
   // what this call reads may come from the kernel before; the next one may start beside it
   pdl_wait();
   pdl_trigger();
-  Walk seg;
+  Walk<C::kRows> seg;
   if (!seg.begin(a, lane)) return;         // the whole CTA
   volatile int* abort_flag = &bars->abort;
   uint32_t tmem = 0;
   if (warp == 0) {
-    bar_arrive(1, kPreThreads);            // its copies need no tensor memory
+    bar_arrive(1, C::kThreads);            // its copies need no tensor memory
     __syncwarp();
   } else {
-    if (warp == 1) tmem_alloc(&bars->tmem_base, kTmemCols);
+    if (warp == 1) tmem_alloc(&bars->tmem_base, kT * C::kTmemCols);
     fence_before();
-    bar_sync(1, kPreThreads);
+    bar_sync(1, C::kThreads);
     fence_after();
     tmem = bars->tmem_base;
   }
@@ -227,11 +242,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
   if (warp == 0) {
     // --------------------------------------------------------- producer --
     bool ok = true;
-    int loads = 0, tile = 0;
+    int loads = 0;
     const int boxes = kBN / a.box;
     do {
-      const QRows h = seg.rows(a);
-      const int hk = h.h0 / a.G;
+      const int hk = seg.rows(a, 0).h0 / a.G;
       // the box of a tile that this lane brings: its page and place in it
       auto page_of = [&](int t) {
         const int j = t * kBN + lane * a.box;
@@ -264,19 +278,8 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         if (t < seg.t1) {
           const int j = t * kBN + lane * a.box;
           if (lane < boxes && j < seg.len) page = checked_page(a.c, entry, a.status);
-          const int n = min(a.box, seg.len - j);
-          unsigned long long bits = 0;
-          if (page >= 0) bits = (n >= 64 ? ~0ull : (1ull << n) - 1ull) << (lane * a.box);
-          const unsigned lo = __reduce_or_sync(0xffffffffu, (unsigned)bits);
-          const unsigned hi = __reduce_or_sync(0xffffffffu, (unsigned)(bits >> 32));
           entry = page_of(t + 1);
           load(&mk, page, t);
-          // the tile kMasks before is done: its S was, when this K's place came free
-          if (ok && lane == 0) {
-            bars->mask[tile % kMasks] = (unsigned long long)hi << 32 | lo;
-            mbar_arrive(&bars->mask_full[tile % kMasks]);
-          }
-          ++tile;
         }
         if (ok && t > seg.t0) load(&mv, v_page, t - 1);
         v_page = page;
@@ -286,9 +289,12 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
       for (int i = loads > C::kStages ? loads - C::kStages : 0; i < loads; ++i)
         mbar_wait_bounded(&bars->kv_full[i % C::kStages], (uint32_t)(i / C::kStages) & 1u, nullptr,
                           a.status);
-  } else if (warp == 1) {
+  } else if (warp <= kT) {
     // --------------------------------------------------------- products --
-    const uint32_t q_lo = sw128_desc_lo(sQ), kv_lo = sw128_desc_lo(sKV);
+    const int rt = warp - 1;
+    TileBars* const tb = &bars->tile[rt];
+    tmem += (uint32_t)(rt * C::kTmemCols);
+    const uint32_t q_lo = sw128_desc_lo(smem + rt * C::kQBytes), kv_lo = sw128_desc_lo(sKV);
     const uint32_t v_lo0 = sw128_mn_desc_lo(sKV, kBN * 128), d_hi = sw128_desc_hi();
     bool ok = true;
     int loads = 0, tile = 0, n_seg = 0;
@@ -310,15 +316,15 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
           mma_ss(tS, q_lo + (uint32_t)(((kk >> 2) * (kBM * 128) + (kk & 3) * 32) >> 4),
                  k_lo + (uint32_t)(((kk >> 2) * (kBN * 128) + (kk & 3) * 32) >> 4), d_hi, C::kIdescS,
                  kk > 0 ? 1u : 0u);
-        mma_commit(&bars->s_full[at & 1]);
+        mma_commit(&tb->s_full[at & 1]);
         mma_commit(&bars->kv_empty[st]);
-        if (last) mma_commit(&bars->q_empty);
+        if (last) mma_commit(&tb->q_empty);
       }
       __syncwarp();
     };
     do {
       const int n = seg.t1 - seg.t0;
-      wait(&bars->q_full, n_seg);
+      wait(&tb->q_full, n_seg);
       ok = __all_sync(0xffffffffu, ok);
       if (ok) issue_s(tile, n == 1);
       for (int j = 0; j < n && ok; ++j, ++tile) {
@@ -326,9 +332,9 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         if (j + 1 < n) issue_s(tile + 1, j + 2 == n);
         if (!ok) break;
         const int st = loads % C::kStages;
-        if (j == 0 && n_seg > 0) wait(&bars->o_empty, n_seg - 1);
+        if (j == 0 && n_seg > 0) wait(&tb->o_empty, n_seg - 1);
         wait(&bars->kv_full[st], loads / C::kStages);
-        wait(&bars->p_full[tile & 1], tile >> 1);
+        wait(&tb->p_full[tile & 1], tile >> 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         ++loads;
@@ -343,20 +349,25 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             mma_ts(tO, tP + (uint32_t)(32 + kk * 8), v_at, d_hi, C::kIdescPV, 1u);
           }
           mma_commit(&bars->kv_empty[st]);
-          mma_commit(&bars->pv_done[tile & 1]);
-          if (j + 1 == n) mma_commit(&bars->o_full);
+          mma_commit(&tb->pv_done[tile & 1]);
+          if (j + 1 == n) mma_commit(&tb->o_full);
         }
         __syncwarp();
       }
       ++n_seg;
     } while (ok && seg.next(a));
     // everything issued has completed before tensor memory is given back
-    if (elect_one()) mma_commit(&bars->drain);
+    if (elect_one()) mma_commit(&tb->drain);
     __syncwarp();
-    mbar_wait_bounded(&bars->drain, 0, nullptr, a.status);
+    mbar_wait_bounded(&tb->drain, 0, nullptr, a.status);
   } else {
     // ------------------------------------------------ softmax, epilogue --
-    const int quad = warp & 3, row = quad * 32 + lane, part = threadIdx.x - 64;
+    const int quad = warp & 3, row = quad * 32 + lane;
+    const int rt = (warp - 1 - kT) >> 2, part = (int)threadIdx.x - 32 * (1 + kT) - 128 * rt;
+    TileBars* const tb = &bars->tile[rt];
+    char* const sQ = smem + rt * C::kQBytes;
+    char* const sO = sOut + rt * kOutBytes;
+    tmem += (uint32_t)(rt * C::kTmemCols);
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const uint32_t tO = tmem + lanes + (uint32_t)kColO;
     bool ok = true;
@@ -400,26 +411,46 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
       }
       fence_async_shared();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->q_full);
+      if (lane == 0) mbar_arrive(&tb->q_full);
     };
-    QRows h = seg.rows(a);
+    QRows h = seg.rows(a, rt);
     put_q(h);
     bool more = true;
     while (more) {
       const int n = seg.t1 - seg.t0;
       const int slot = seg.ubase + seg.u + (int)blockIdx.x;
-      if (seg.t0 == 0 && part == 0) {
+      if (seg.t0 == 0 && part == 0 && rt == 0) {
         // pieces of this unit: this CTA's and those of the CTAs that the rest reaches
         const int over = seg.nt - seg.left;
         a.rec[seg.ubase + seg.u] =
             make_int2(slot, over <= 0 ? 1 : 1 + (over + seg.per - 1) / seg.per);
       }
+      // Which keys of a tile are there: those below the length whose page is one of the pool.  Each
+      // warp looks that up by itself, a tile ahead: told by the producer through a barrier, it
+      // cost 250 clocks of a tile's 2200.
+      auto entry_of = [&](int t) {
+        const int at = t * kBN + lane * a.box;
+        return lane * a.box < kBN && t < seg.t1 && at < seg.len
+                   ? a.c.block_table[(int64_t)seg.g * a.c.table_sb + a.page.div(at)]
+                   : -1;
+      };
+      int entry = entry_of(seg.t0);
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < n; ++j, ++tile) {
         const uint32_t tS = tmem + lanes + (uint32_t)((tile & 1) * kBN);
-        if (!wait(&bars->mask_full[tile % kMasks], tile / kMasks)) break;
-        const unsigned long long mask = bars->mask[tile % kMasks];
-        if (!wait(&bars->s_full[tile & 1], tile >> 1)) break;
+        const int t = seg.t0 + j;
+        const bool page_ok = (unsigned)entry < (unsigned)a.c.num_pages;
+        unsigned long long mask = ~0ull;
+        if ((t + 1) * kBN > seg.len || !__all_sync(0xffffffffu, page_ok || lane * a.box >= kBN)) {
+          unsigned long long bits = 0;
+          const int at = t * kBN + lane * a.box, here = min(a.box, seg.len - at);
+          if (page_ok && lane * a.box < kBN)
+            bits = (here >= 64 ? ~0ull : (1ull << here) - 1ull) << (lane * a.box);
+          mask = (unsigned long long)__reduce_or_sync(0xffffffffu, (unsigned)(bits >> 32)) << 32 |
+                 __reduce_or_sync(0xffffffffu, (unsigned)bits);
+        }
+        entry = entry_of(t + 1);
+        if (!wait(&tb->s_full[tile & 1], tile >> 1)) break;
         fence_after();
         uint32_t r0[32], r1[32];
         tmem_ld64_wait(tS, r0, r1);
@@ -442,7 +473,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
           m = mn;
           l *= f;
           if (j > 0) {
-            if (!wait(&bars->pv_done[(tile - 1) & 1], (tile - 1) >> 1)) break;
+            if (!wait(&tb->pv_done[(tile - 1) & 1], (tile - 1) >> 1)) break;
             fence_after();
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
@@ -468,8 +499,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             x1 = avits::ex2(x1);
             fadd2(s4[2 * (e & 1)], s4[2 * (e & 1) + 1], x0, x1);
             hi[e] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
-            lo[e] = pack_bf16x2(fmaf(x0, kUp, -__uint_as_float(__float_as_uint(x0) & 0xffff0000u)),
-                                fmaf(x1, kUp, -__uint_as_float(__float_as_uint(x1) & 0xffff0000u)));
+            float y0 = __uint_as_float((__float_as_uint(x0) & 0xffff0000u) ^ 0x80000000u);
+            float y1 = __uint_as_float((__float_as_uint(x1) & 0xffff0000u) ^ 0x80000000u);
+            fma2(x0, x1, kUp, y0, y1);
+            lo[e] = pack_bf16x2(y0, y1);
           }
           tmem_st16(tS + (uint32_t)at, hi);
           tmem_st16(tS + 32u + (uint32_t)at, lo);
@@ -493,18 +526,18 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         }
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->p_full[tile & 1]);
+        if (lane == 0) mbar_arrive(&tb->p_full[tile & 1]);
       }
       if (!ok) break;
       loads += 2 * n;
       const int rows = h.rows;
       more = seg.next(a);
       if (more) {      // the next unit's Q, while the last product runs
-        if (!wait(&bars->q_empty, n_seg)) break;
-        h = seg.rows(a);
+        if (!wait(&tb->q_empty, n_seg)) break;
+        h = seg.rows(a, rt);
         put_q(h);
       }
-      if (!wait(&bars->o_full, n_seg)) break;
+      if (!wait(&tb->o_full, n_seg)) break;
       fence_after();
       // O by 16 columns through shared memory, so that a row's go out as whole sectors
 #pragma unroll 1
@@ -514,7 +547,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         if (c + 32 >= D) {        // O has been read
           fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&bars->o_empty);
+          if (lane == 0) mbar_arrive(&tb->o_empty);
         }
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
@@ -533,13 +566,13 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             for (int i = 0; i < 4; ++i) {
               const int r = quad * 32 + i * 8 + (lane >> 2);
               if (r < rows)
-                *reinterpret_cast<float4*>(a.po + ((int64_t)slot * kBM + r) * a.c.d + at) =
+                *reinterpret_cast<float4*>(a.po + ((int64_t)slot * C::kRows + rt * kBM + r) * a.c.d + at) =
                     buf[r * 4 + (col ^ ((r >> 1) & 3))];
             }
           __syncwarp();
         }
       }
-      if (row < rows) a.pml[slot * kBM + row] = make_float2(m, l);
+      if (row < rows) a.pml[slot * C::kRows + rt * kBM + row] = make_float2(m, l);
       ++n_seg;
     }
   }
@@ -547,11 +580,11 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
   __syncthreads();
   if (warp == 1) {
     fence_after();
-    tmem_dealloc(tmem, kTmemCols);
+    tmem_dealloc(bars->tmem_base, kT * C::kTmemCols);
   }
 }
 
-template <int D>
+template <int D, int kT>
 cudaError_t launch_width(const CacheAttn& a, cudaStream_t s) {
   CUtensorMap mk{}, mv{};
   using Rows = RowsBf16<D, 8>;
@@ -559,10 +592,10 @@ cudaError_t launch_width(const CacheAttn& a, cudaStream_t s) {
   if (!map_pages<Rows>(&mk, c.k_pages, c.k_sp, c.k_st, c.k_sh, c, a.box) ||
       !map_pages<Rows>(&mv, c.v_pages, c.v_sp, c.v_st, c.v_sh, c, a.box))
     return cudaErrorInvalidValue;
-  constexpr auto kernel = cache_prefix_kernel<D>;
-  const cudaError_t e = prefer_max_shared<kernel, pre_smem<D>()>();
+  constexpr auto kernel = cache_prefix_kernel<D, kT>;
+  const cudaError_t e = prefer_max_shared<kernel, pre_smem<D, kT>()>();
   if (e != cudaSuccess) return e;
-  return launch_pdl(kernel, dim3(a.grid), dim3(kPreThreads), pre_smem<D>(), s, mk, mv, a);
+  return launch_pdl(kernel, dim3(a.grid), dim3(Pre<D, kT>::kThreads), pre_smem<D, kT>(), s, mk, mv, a);
 }
 
 }  // namespace
@@ -581,7 +614,8 @@ int prefix_tc_box(const avits_kv_cache& c) {
 }
 
 cudaError_t launch_prefix_tc(const CacheAttn& a, cudaStream_t s) {
-  return a.c.d <= 64 ? launch_width<64>(a, s) : launch_width<128>(a, s);
+  if (a.rows == kBM) return a.c.d <= 64 ? launch_width<64, 1>(a, s) : launch_width<128, 1>(a, s);
+  return a.c.d <= 64 ? launch_width<64, 2>(a, s) : launch_width<128, 2>(a, s);
 }
 
 }  // namespace cache

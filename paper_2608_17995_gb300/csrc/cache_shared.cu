@@ -41,7 +41,7 @@ void cut(Line& l, const avits_kv_cache& c, int num_sms) {
   l.tiles = l.units * longest;
   l.least = longest < few ? longest : few;
   const long long most = (l.tiles + l.least - 1) / l.least;
-  long long full = (long long)num_sms * (l.box ? kPrefixCtas : (l.groups ? own_ctas(l.D, l.rows, bf) : line_ctas(l.D, l.rows, bf)));
+  long long full = (long long)num_sms * (l.box ? 2 * kPrefixRows / l.rows : (l.groups ? own_ctas(l.D, l.rows, bf) : line_ctas(l.D, l.rows, bf)));
   if (full > kMaxGrid) full = kMaxGrid;
   l.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
 }
@@ -88,13 +88,14 @@ Shape shape_of(const CacheSharedCall& s, int num_sms) {
   x.own.groups = (G + x.own.rows - 1) / x.own.rows;
   x.own.units = (long long)c.B * c.Hkv * x.own.groups;
   x.pre.box = prefix_tc_box(p);
-  x.pre.rows = x.pre.box ? kPrefixRows : rows_of(bf, D, ((long long)c.B + p.B - 1) / p.B * G);
+  const long long rows = ((long long)c.B + p.B - 1) / p.B * G;      // of a group, by and large
+  x.pre.rows = !x.pre.box ? rows_of(bf, D, rows) : rows > kPrefixRows ? 2 * kPrefixRows : kPrefixRows;
   x.pre.groups = 0;
   x.pre.units = c.Hkv * ((long long)c.B * G / x.pre.rows + p.B);
   cut(x.own, c, num_sms);
   cut(x.pre, p, num_sms);
   x.both = both_of(s, x.own, num_sms);
-  x.warps = c.max_len <= kOwnLong ? 2 : 0;
+  x.warps = c.max_len <= kOwnLong ? (x.own.D > 128 ? 2 : 4) : 0;
   if (x.warps) {       // runs of a unit
     const int longest = (c.max_len + x.own.tile - 1) / x.own.tile;
     x.own.least = c.max_len <= kOwnShort ? 16 : 32;

@@ -820,9 +820,10 @@ cudaError_t launch_cluster(CacheAttn& a, int D, int ncta, int warps, cudaStream_
 cudaError_t launch_own_parts(CacheAttn& a, int D, int warps, cudaStream_t s);
 cudaError_t launch_both(CacheAttn& a, const CacheAttn& p, int D, int ncta, cudaStream_t s);
 
-// Prefixes on the tensor cores: units of 128 rows, tiles of 64 keys, two CTAs to an SM.  Tokens
-// of a copy, 0 where the type, the width or the pages' layout is not theirs.
-constexpr int kPrefixRows = 128, kPrefixTile = 64, kPrefixCtas = 2;
+// Prefixes on the tensor cores: units of 128 rows on two CTAs to an SM, or of 256 on one, tiles
+// of 64 keys.  prefix_tc_box: tokens of a copy, 0 where the type, the width or the pages' layout
+// is not theirs.
+constexpr int kPrefixRows = 128, kPrefixTile = 64;
 int prefix_tc_box(const avits_kv_cache& c);
 cudaError_t launch_prefix_tc(const CacheAttn& a, cudaStream_t s);
 
