@@ -741,6 +741,18 @@ size_t avits_cache_attention_shared_workspace(const avits_kv_cache* cache,
                                               const avits_kv_cache* prefix, int H);
 
 /* ------------------------------------------------------------------------
+ * The calls of a served batch's step with their arguments in an array, for bindings to
+ * which every argument of a foreign call costs (0.14 us each in Python's ctypes): `args`
+ * holds the arguments of the call in their order, 8 bytes each: addresses, 64-bit integers
+ * (an int that does not fit 32 bits is AVITS_ERR_INVALID_ARG), and doubles for floats. */
+typedef enum {
+  AVITS_CALL_CACHE_PLAN = 0, AVITS_CALL_NORM_ROTATE = 1, AVITS_CALL_CACHE_APPEND_ROTATED = 2,
+  AVITS_CALL_CACHE_ATTENTION_SHARED = 3
+} avits_call;
+
+avits_status avits_call_packed(int call, const void* args);
+
+/* ------------------------------------------------------------------------
  * Test hook for the failure detection of the device-side waits (a library
  * facility; the paper has no counterpart).  Every spin in the kernels is an
  * mbarrier wait bounded by a wall-clock limit: on expiry it records

@@ -37,6 +37,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from typing import Optional, Sequence
 
 from . import _build
@@ -131,6 +132,7 @@ def lib():
         "avits_cache_attention_shared": [vp, vp, vp, vp, i32, i64, i64, f32, vp, i64, i64, vp, vp, sz,
                                          vp],
         "avits_cache_attention_shared_workspace": [vp, vp, i32],
+        "avits_call_packed": [i32, ctypes.c_char_p],
         "avits_rotary_frequencies": [i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double,
                                      ctypes.c_double, ctypes.c_double, vp],
         "avits_norm_rotate": [vp, i32, i32, i32, i32, vp, i64, i64, vp, i32, vp, vp, vp, vp, i32, vp,
@@ -587,7 +589,7 @@ class KVCache:
     """
     __slots__ = ("k_pages", "v_pages", "block_table", "lens", "acc", "B", "Hkv", "d", "dtype",
                  "page_size", "max_len", "device", "int32", "int64", "float32", "_index", "_struct", "_ref",
-                 "_need", "_alloc", "_free", "_append", "_attend", "_plan", "_append_rotated", "_shared", "_shared_need", "_shape",
+                 "_need", "_alloc", "_free", "_append", "_attend", "_packed", "_shared_need", "_shape",
                  "_evict")
 
     def __init__(self, k_pages, v_pages, block_table, lens, acc=None, max_len: Optional[int] = None):
@@ -643,8 +645,7 @@ class KVCache:
         self._free = torch._C._cuda_cudaCachingAllocator_raw_delete
         L = lib()
         self._append, self._attend = L.avits_cache_append, L.avits_cache_attention
-        self._shared, self._shared_need = L.avits_cache_attention_shared, {}
-        self._plan, self._append_rotated = L.avits_cache_plan, L.avits_cache_append_rotated
+        self._packed, self._shared_need = L.avits_call_packed, {}
         self._evict = L.avits_cache_evict
 
     def __setattr__(self, name, value):
@@ -799,6 +800,12 @@ def avits_cache_evict(src: KVCache, dst: KVCache, keep: int, sinks: int, recent:
 
 
 # ------------------------------------------- a served batch's step around it --
+# These calls pass their many arguments as one array (avits_call_packed): 64-bit integers
+# and addresses (0: none), floats as doubles.
+_PLAN, _ROTATE = struct.Struct("=14q").pack, struct.Struct("=21qdq").pack
+_APPEND_ROTATED, _SHARED = struct.Struct("=24qdq").pack, struct.Struct("=7qd7q").pack
+
+
 def avits_cache_plan(cache: KVCache, change, free_pages, free_count, cu_new, slots, seq, place,
                      lens=None, pos=None, pos_base=None, free_out=None, stream=None):
     """A step's changes of length become pages.  change [B] int32: new tokens of
@@ -833,7 +840,7 @@ def avits_cache_plan(cache: KVCache, change, free_pages, free_count, cu_new, slo
                  free_pages.is_contiguous() and seq.is_contiguous() and place.is_contiguous()):
         raise ValueError("change, lens [B], cu_new [B+1], free_count, free_out [1], seq, place [T] "
                          "and free_pages [num_pages] must be contiguous int32 tensors")
-    pos_at = base_at = None
+    pos_at = base_at = 0
     if pos is not None:
         if pos.shape != rows or pos.dtype != i32 or not pos.is_contiguous():
             raise ValueError("pos must be a contiguous int32 [T] tensor")
@@ -852,10 +859,10 @@ def avits_cache_plan(cache: KVCache, change, free_pages, free_count, cu_new, slo
             (pos_base is not None and pos_base.get_device() != index):
         _elsewhere(cache, change, lens, cu_new, free_count, free_out, seq, place, free_pages, slots,
                    pos, pos_base)
-    rc = cache._plan(cache._ref, lens.data_ptr(), change.data_ptr(), free_pages.data_ptr(),
-                     free_count.data_ptr(), free_out.data_ptr(), T, cu_new.data_ptr(),
-                     slots.data_ptr(), seq.data_ptr(), place.data_ptr(), pos_at, base_at,
-                     _call_stream(cache, stream))
+    rc = cache._packed(0, _PLAN(
+        cache._ref, lens.data_ptr(), change.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+        free_out.data_ptr(), T, cu_new.data_ptr(), slots.data_ptr(), seq.data_ptr(),
+        place.data_ptr(), pos_at, base_at, _call_stream(cache, stream) or 0))
     if rc != 0:
         _check("avits_cache_plan", rc)
 
@@ -915,7 +922,7 @@ class Rotary:
                                      (ctypes.c_int32 * 4)(*parts), magnitude)
         self._ref = ctypes.addressof(self._struct)
         self._index = self.freq.get_device()
-        self._call = lib().avits_norm_rotate
+        self._call = lib().avits_call_packed
         self.int32, self.codes = torch.int32, {torch.bfloat16: BF16, torch.float32: F32}
 
 
@@ -967,7 +974,7 @@ def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q
         raise ValueError("q or q_out on %s, %s: the rotary is on %s" % (q.device, q_out.device,
                                                                        rotary.device))
     Hkv = 0
-    k_at = k_str = ko_at = ko_str = None
+    k_at = k_str = ko_at = ko_str = 0
     if k is not None:
         (kB, kN, Hkv, kd), k_str = _heads_of(k, "k")
         shape, ko_str = _heads_of(k_out, "k_out")
@@ -981,12 +988,13 @@ def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q
         k_at, ko_at = k.data_ptr(), k_out.data_ptr()
     if B > _INT_MAX or N > _INT_MAX or H > _INT_MAX or Hkv > _INT_MAX or d > _INT_MAX:
         raise ValueError("sizes of more than 32 bits")
-    p_at, p_sb, p_sn = _positions(rotary, positions, B, N) if rotary.rot else (None, 0, 0)
-    rc = rotary._call(rotary._ref, code, B, N, d, p_at, p_sb, p_sn, q.data_ptr(), H, q_str,
-                      q_out.data_ptr(), qo_str, k_at, Hkv, k_str, ko_at, ko_str, 1 if norm else 0,
-                      q_weight if q_weight is None else _weight_at(q_weight, d, dtype, index),
-                      k_weight if k_weight is None else _weight_at(k_weight, d, dtype, index), eps,
-                      _rotary_stream(rotary, stream))
+    p_at, p_sb, p_sn = _positions(rotary, positions, B, N) if rotary.rot else (0, 0, 0)
+    rc = rotary._call(1, _ROTATE(
+        rotary._ref, code, B, N, d, p_at, p_sb, p_sn, q.data_ptr(), H, q_str, q_out.data_ptr(),
+        qo_str, k_at, Hkv, k_str, ko_at, ko_str, 1 if norm else 0,
+        0 if q_weight is None else _weight_at(q_weight, d, dtype, index),
+        0 if k_weight is None else _weight_at(k_weight, d, dtype, index), eps,
+        _rotary_stream(rotary, stream) or 0))
     if rc != 0:
         _check("avits_norm_rotate", rc)
     return q_out
@@ -1045,26 +1053,25 @@ def avits_cache_append_rotated(cache: KVCache, rotary: Rotary, positions, slots,
         raise ValueError("the head-dim axis must be contiguous")
     if slots.shape != (T,) or slots.dtype != cache.int64 or not slots.is_contiguous():
         raise ValueError("slots must be a contiguous int64 [T] tensor")
-    s_at = p_at = None
+    s_at = p_at = 0
     if seq is not None or place is not None or cache.acc is not None:
         for t in (seq, place):
             if t is None or t.shape != (T,) or t.dtype != cache.int32 or not t.is_contiguous():
                 raise ValueError("seq and place must be contiguous int32 [T] tensors")
         _elsewhere(cache, seq, place)
         s_at, p_at = seq.data_ptr(), place.data_ptr()
-    x_at, x_st = None, 0
+    x_at, x_st = 0, 0
     if rotary.rot:
         x_at, _, x_st = _positions(rotary, positions, 1, T)
     if rotary._index != index or q.get_device() != index or q_out.get_device() != index or \
             k_new.get_device() != index or v_new.get_device() != index or slots.get_device() != index:
         _elsewhere(cache, rotary.freq, q, q_out, k_new, v_new, slots)
-    rc = cache._append_rotated(cache._ref, rotary._ref, T, x_at, x_st, slots.data_ptr(), s_at, p_at,
-                               q.data_ptr(), H, q_st, q_sh, q_out.data_ptr(), o_st, o_sh,
-                               k_new.data_ptr(), k_st, k_sh, v_new.data_ptr(), v_st, v_sh,
-                               1 if norm else 0,
-                               q_weight if q_weight is None else _weight_at(q_weight, d, dtype, index),
-                               k_weight if k_weight is None else _weight_at(k_weight, d, dtype, index),
-                               eps, _call_stream(cache, stream))
+    rc = cache._packed(2, _APPEND_ROTATED(
+        cache._ref, rotary._ref, T, x_at, x_st, slots.data_ptr(), s_at, p_at, q.data_ptr(), H, q_st,
+        q_sh, q_out.data_ptr(), o_st, o_sh, k_new.data_ptr(), k_st, k_sh, v_new.data_ptr(), v_st,
+        v_sh, 1 if norm else 0, 0 if q_weight is None else _weight_at(q_weight, d, dtype, index),
+        0 if k_weight is None else _weight_at(k_weight, d, dtype, index), eps,
+        _call_stream(cache, stream) or 0))
     if rc != 0:
         _check("avits_cache_append_rotated", rc)
     return q_out
@@ -1112,15 +1119,15 @@ def avits_cache_attention_shared(cache: KVCache, prefix: KVCache, group_start, q
     if q.get_device() != index or o.get_device() != index or prefix._index != index or \
             group_start.get_device() != index:
         _elsewhere(cache, q, o, prefix.k_pages, group_start)
-    lse_at = None
+    lse_at = 0
     if lse is not None:
         if lse.shape != (B, H) or lse.dtype != cache.float32 or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous float32 [B,H] tensor")
         if lse.get_device() != index:
             _elsewhere(cache, lse)
         lse_at = lse.data_ptr()
-    handle = _call_stream(cache, stream)
-    own = None
+    handle = _call_stream(cache, stream) or 0
+    own = 0
     if workspace is not None:
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
@@ -1129,13 +1136,13 @@ def avits_cache_attention_shared(cache: KVCache, prefix: KVCache, group_start, q
     else:
         # as avits_cache_attention's: of this call and its stream
         ws_bytes = _shared_bytes(cache, prefix, H)
-        ws_at = own = cache._alloc(ws_bytes, handle) if ws_bytes else None
+        ws_at = own = cache._alloc(ws_bytes, handle) if ws_bytes else 0
     try:
-        rc = cache._shared(cache._ref, prefix._ref, group_start.data_ptr(), q.data_ptr(), H, q_sb,
-                           q_sh, softmax_scale, o.data_ptr(), o_sb, o_sh, lse_at, ws_at, ws_bytes,
-                           handle)
+        rc = cache._packed(3, _SHARED(
+            cache._ref, prefix._ref, group_start.data_ptr(), q.data_ptr(), H, q_sb, q_sh,
+            softmax_scale, o.data_ptr(), o_sb, o_sh, lse_at, ws_at, ws_bytes, handle))
     finally:
-        if own is not None:
+        if own:
             cache._free(own)
     if rc != 0:
         _check("avits_cache_attention_shared", rc)

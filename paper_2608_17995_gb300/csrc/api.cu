@@ -2,7 +2,9 @@
 // checks, workspace sizing and dispatch to the kernels.  Nothing here
 // allocates device memory or synchronises, except avits_device_status().
 #include <algorithm>
+#include <climits>
 #include <cmath>
+#include <cstdint>
 #include <cstdio>
 #include <cstring>
 #include <string>
@@ -139,6 +141,31 @@ bool norm_ok(int norm, const void* q_weight, const void* k_weight, float eps) {
 bool same_strides(const int64_t* a, const int64_t* b, int64_t n0, int64_t n1, int64_t n2) {
   return (n0 == 1 || a[0] == b[0]) && (n1 == 1 || a[1] == b[1]) && (n2 == 1 || a[2] == b[2]);
 }
+
+// Arguments one after the other, 8 bytes each.
+struct Packed {
+  const char* at;
+  bool ok = true;
+  int64_t i64() {
+    int64_t x;
+    std::memcpy(&x, at, 8);
+    at += 8;
+    return x;
+  }
+  int i32() {
+    const int64_t x = i64();
+    ok = ok && x >= INT32_MIN && x <= INT32_MAX;
+    return (int)x;
+  }
+  float f32() {
+    double x;
+    std::memcpy(&x, at, 8);
+    at += 8;
+    return (float)x;
+  }
+  template <typename T>
+  T* ptr() { return reinterpret_cast<T*>((uintptr_t)i64()); }
+};
 
 }  // namespace
 
@@ -763,6 +790,76 @@ avits_status avits_cache_attention_shared(const avits_kv_cache* cache, const avi
     return AVITS_ERR_INVALID_ARG;
   return cuda_status(
       launch_cache_shared(call, sms, status_word(), static_cast<cudaStream_t>(stream)));
+}
+
+avits_status avits_call_packed(int call, const void* args) {
+  if (!args) return AVITS_ERR_INVALID_ARG;
+  Packed p{static_cast<const char*>(args)};
+  // braces: initialised in the order they are written
+  switch (call) {
+    case AVITS_CALL_CACHE_PLAN: {
+      struct {
+        const avits_kv_cache* cache; const int32_t *lens, *change; int32_t* free_pages;
+        const int32_t* free_count; int32_t* free_out; int T; int32_t* cu; int64_t* slots;
+        int32_t *seq, *place, *pos; const int32_t* base; void* stream;
+      } a{p.ptr<const avits_kv_cache>(), p.ptr<const int32_t>(), p.ptr<const int32_t>(),
+          p.ptr<int32_t>(), p.ptr<const int32_t>(), p.ptr<int32_t>(), p.i32(), p.ptr<int32_t>(),
+          p.ptr<int64_t>(), p.ptr<int32_t>(), p.ptr<int32_t>(), p.ptr<int32_t>(),
+          p.ptr<const int32_t>(), p.ptr<void>()};
+      if (!p.ok) return AVITS_ERR_INVALID_ARG;
+      return avits_cache_plan(a.cache, a.lens, a.change, a.free_pages, a.free_count, a.free_out, a.T,
+                              a.cu, a.slots, a.seq, a.place, a.pos, a.base, a.stream);
+    }
+    case AVITS_CALL_NORM_ROTATE: {
+      struct {
+        const avits_rotary* rot; int dt, B, N, d; const int32_t* positions; int64_t pos_sb, pos_sn;
+        const void* q; int H; const int64_t* q_str; void* q_out; const int64_t* qo_str;
+        const void* k; int Hkv; const int64_t* k_str; void* k_out; const int64_t* ko_str; int norm;
+        const void *q_weight, *k_weight; float eps; void* stream;
+      } a{p.ptr<const avits_rotary>(), p.i32(), p.i32(), p.i32(), p.i32(), p.ptr<const int32_t>(),
+          p.i64(), p.i64(), p.ptr<const void>(), p.i32(), p.ptr<const int64_t>(), p.ptr<void>(),
+          p.ptr<const int64_t>(), p.ptr<const void>(), p.i32(), p.ptr<const int64_t>(),
+          p.ptr<void>(), p.ptr<const int64_t>(), p.i32(), p.ptr<const void>(),
+          p.ptr<const void>(), p.f32(), p.ptr<void>()};
+      if (!p.ok) return AVITS_ERR_INVALID_ARG;
+      return avits_norm_rotate(a.rot, static_cast<avits_dtype>(a.dt), a.B, a.N, a.d, a.positions,
+                               a.pos_sb, a.pos_sn, a.q, a.H, a.q_str, a.q_out, a.qo_str, a.k, a.Hkv,
+                               a.k_str, a.k_out, a.ko_str, a.norm, a.q_weight, a.k_weight, a.eps,
+                               a.stream);
+    }
+    case AVITS_CALL_CACHE_APPEND_ROTATED: {
+      struct {
+        const avits_kv_cache* cache; const avits_rotary* rot; int T; const int32_t* positions;
+        int64_t pos_st; const int64_t* slots; const int32_t *seq, *place; const void* q; int H;
+        int64_t q_st, q_sh; void* q_out; int64_t qo_st, qo_sh; const void* k; int64_t k_st, k_sh;
+        const void* v; int64_t v_st, v_sh; int norm; const void *q_weight, *k_weight; float eps;
+        void* stream;
+      } a{p.ptr<const avits_kv_cache>(), p.ptr<const avits_rotary>(), p.i32(),
+          p.ptr<const int32_t>(), p.i64(), p.ptr<const int64_t>(), p.ptr<const int32_t>(),
+          p.ptr<const int32_t>(), p.ptr<const void>(), p.i32(), p.i64(), p.i64(), p.ptr<void>(),
+          p.i64(), p.i64(), p.ptr<const void>(), p.i64(), p.i64(), p.ptr<const void>(), p.i64(),
+          p.i64(), p.i32(), p.ptr<const void>(), p.ptr<const void>(), p.f32(), p.ptr<void>()};
+      if (!p.ok) return AVITS_ERR_INVALID_ARG;
+      return avits_cache_append_rotated(a.cache, a.rot, a.T, a.positions, a.pos_st, a.slots, a.seq,
+                                        a.place, a.q, a.H, a.q_st, a.q_sh, a.q_out, a.qo_st,
+                                        a.qo_sh, a.k, a.k_st, a.k_sh, a.v, a.v_st, a.v_sh, a.norm,
+                                        a.q_weight, a.k_weight, a.eps, a.stream);
+    }
+    case AVITS_CALL_CACHE_ATTENTION_SHARED: {
+      struct {
+        const avits_kv_cache *cache, *prefix; const int32_t* start; const void* q; int H;
+        int64_t q_sb, q_sh; float scale; void* o; int64_t o_sb, o_sh; float* lse; void* ws;
+        int64_t ws_bytes; void* stream;
+      } a{p.ptr<const avits_kv_cache>(), p.ptr<const avits_kv_cache>(), p.ptr<const int32_t>(),
+          p.ptr<const void>(), p.i32(), p.i64(), p.i64(), p.f32(), p.ptr<void>(), p.i64(), p.i64(),
+          p.ptr<float>(), p.ptr<void>(), p.i64(), p.ptr<void>()};
+      if (!p.ok || a.ws_bytes < 0) return AVITS_ERR_INVALID_ARG;
+      return avits_cache_attention_shared(a.cache, a.prefix, a.start, a.q, a.H, a.q_sb, a.q_sh,
+                                          a.scale, a.o, a.o_sb, a.o_sh, a.lse, a.ws,
+                                          (size_t)a.ws_bytes, a.stream);
+    }
+  }
+  return AVITS_ERR_INVALID_ARG;
 }
 
 avits_status avits_selftest_bounded_wait(unsigned long long limit_ns, long long* result,

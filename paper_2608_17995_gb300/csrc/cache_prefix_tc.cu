@@ -188,7 +188,8 @@ __device__ __forceinline__ void fma2(float a0, float a1, float b, float& c0, flo
 }
 
 template <int D, int kT>
-__global__ void __launch_bounds__(Pre<D, kT>::kThreads, 3 - kT)
+// Two row tiles: at most 128 registers (86 us for 128 x 32768, 88 with 161).
+__global__ void __launch_bounds__(kT == 2 ? 512 : Pre<D, kT>::kThreads, 3 - kT)
 cache_prefix_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                     const __grid_constant__ CacheAttn a) {
   using C = Pre<D, kT>;

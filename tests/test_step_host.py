@@ -257,3 +257,41 @@ def test_shared_sizes(lib):
     long = struct(max_len=1 << 29, acc=None)
     assert shared(lib, struct(B=1 << 20, acc=None), long) == UNSUPPORTED
     assert lib.avits_cache_attention_shared_workspace(at(struct()), at(struct()), 9) == 0
+
+
+# ------------------------------------------------- arguments in an array --
+def test_packed_calls(lib):
+    """The same answers as the calls themselves give, for refused and empty ones."""
+    call = lib.avits_call_packed
+    c, r = struct(**GOOD), rotary()
+    cp, rp = ctypes.addressof(c), ctypes.addressof(r)
+    # an append of nothing, one of something refused, a size past 32 bits
+    a = [cp, rp, 0, P, 1, P, P, P, P, 4, 256, 64, W, 256, 64, 2 * P, 128, 64, 3 * P, 128, 64, 1, 0, 0, 1e-6, 0]
+    assert call(2, av._APPEND_ROTATED(*a)) == 0
+    for at, bad, code in ((2, -1, INVALID), (2, 1 << 32, INVALID), (9, 0, INVALID), (9, (1 << 32) + 4, INVALID),
+                          (22, P + 8, UNSUPPORTED), (24, -1.0, INVALID), (4, -1, INVALID)):
+        b = list(a)
+        b[2] = 5
+        b[at] = bad
+        assert call(2, av._APPEND_ROTATED(*b)) == code, at
+    p = [cp, P, P, P, P, P, 8, P, P, P, P, 0, 0, 0]
+    for at, bad in ((0, 0), (1, 0), (6, -1), (6, 1 << 33), (8, 0)):
+        b = list(p)
+        b[at] = bad
+        assert call(0, av._PLAN(*b)) == INVALID, at
+    s = (ctypes.c_int64 * 3)(768, 256, 64)
+    sa = ctypes.addressof(s)
+    q = [rp, 1, 2, 3, 64, P, 0, 1, P, 4, sa, W, sa, 0, 0, 0, 0, 0, 1, 0, 0, 1e-6, 0]
+    for at, bad, code in ((1, 2, INVALID), (2, 0, INVALID), (9, 1 << 40, INVALID), (8, P + 8, UNSUPPORTED),
+                          (21, float("nan"), INVALID), (13, P, INVALID)):
+        b = list(q)
+        b[at] = bad
+        assert call(1, av._ROTATE(*b)) == code, at
+    h = [cp, cp, P, P, 8, 512, 64, 0.1, P, 512, 64, 0, P, 1 << 40, 0]
+    for at, bad, code in ((2, 0, INVALID), (4, 7, INVALID), (7, 0.0, INVALID), (13, 16, INVALID),
+                          (13, -1, INVALID), (12, 0, INVALID)):
+        b = list(h)
+        b[at] = bad
+        assert call(3, av._SHARED(*b)) == code, at
+    assert call(4, av._PLAN(*p)) == INVALID and call(-1, av._PLAN(*p)) == INVALID
+    assert call(0, None) == INVALID
