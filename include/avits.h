@@ -725,11 +725,11 @@ avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits
  *          first and from the last on have no prefix.  Otherwise AVITS_ERR_PAGE is raised
  *          and no sequence has one.
  * A sequence without any token gets o = 0 and lse = -inf.  What avits_cache_attention says
- * of infinite values, sizes and strides holds here (in bf16 the weights of prefixes enter
- * the products as 2 bf16 parts too).
+ * of infinite values, sizes and strides holds here, but that an infinite value of a prefix
+ * gives NaN where its token's weight, relative to the largest, is below 2^-106.
  * workspace/ws_bytes : at least avits_cache_attention_shared_workspace(...) bytes,
  *          16-byte aligned, of any content; not used by two calls at once.  It grows with
- *          B H d, with the groups, and with the SMs, not with lengths. */
+ *          B H d (4 to 32 bytes of it, by cache->max_len), with the groups and the SMs. */
 avits_status avits_cache_attention_shared(const avits_kv_cache* cache, const avits_kv_cache* prefix,
                                           const int32_t* group_start, const void* q, int H,
                                           int64_t q_sb, int64_t q_sh, float softmax_scale, void* o,

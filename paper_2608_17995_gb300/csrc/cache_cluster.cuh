@@ -39,8 +39,15 @@ constexpr int cluster_smem(int warps, int rows, int keys) {   // keys: logits' r
 // the rows over the banks.
 inline int logit_stride(int keys) { return (keys + 23) / 32 * 32 + 8; }
 
+// CTAs to an SM that the registers have to allow: parts of 8 rows need no more than 128.
 template <typename Rows, int W, int kForm>
-__global__ void __launch_bounds__(32 * W, kForm == kParts && Rows::kBf16 && Rows::D <= 128 && Rows::kR == 8 ? 16 / W : cluster_ctas(Rows::D, Rows::kR, W))
+constexpr int cluster_min() {
+  return kForm == kParts && Rows::kBf16 && Rows::D <= 128 && Rows::kR == 8
+             ? 16 / W : cluster_ctas(Rows::D, Rows::kR, W);
+}
+
+template <typename Rows, int W, int kForm>
+__global__ void __launch_bounds__(32 * W, cluster_min<Rows, W, kForm>())
 cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                      const __grid_constant__ CacheAttn a, int stride,
                      const __grid_constant__ Beside<kForm> x) {

@@ -37,7 +37,7 @@ __device__ __forceinline__ int group_of(const int32_t* start, int groups, int b)
 enum LineForm { kWhole = 0, kOwn = 1, kGroup = 2 };
 
 template <typename Rows, int kForm>
-__global__ void __launch_bounds__(kThreads, kForm == kOwn ? own_ctas(Rows::D, Rows::kR, Rows::kBf16) : line_ctas(Rows::D, Rows::kR, Rows::kBf16))
+__global__ void __launch_bounds__(kThreads, line_ctas(Rows::D, Rows::kR, Rows::kBf16))
 cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                   const __grid_constant__ CacheAttn a) {
   using T = typename Rows::T;

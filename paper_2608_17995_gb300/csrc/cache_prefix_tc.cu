@@ -2,22 +2,30 @@
 // (bf16, widths up to 128): the query heads of all of a group's sequences that share a KV
 // head are the rows of one product.
 //
-// Unit: (group, KV head, 128 rows).  All tiles of 64 keys of all units form one line, cut
-// into equal pieces, one per CTA; two CTAs share an SM, so that one's exponentials run
-// while the other's products do.  Roles of the 6 warps:
-//   0      loads keys and values through a ring of tiles (TMA, a box per page or part of
-//          one; what lies past the prefix or outside the pool comes as zeros), and says
-//          which keys of a tile are there
-//   1      issues the products: S(j+1) = Q K(j+1)^T, then O += P(j) V(j) as soon as P(j) is
-//          written, so that S is a tile ahead
-//   2-5    one row to a thread: the running maximum (moved when a tile's passes it by 2^8:
-//          O is rescaled then), exponentials, the fp32 sum, P to tensor memory over S
+// Unit: (group, KV head, 128 kT rows), kT = 1 or 2 row tiles.  All tiles of 64 keys of all
+// units form one line, cut into equal pieces, one per CTA.  kT = 1: two CTAs share an SM, so
+// that one's exponentials run while the other's products do; kT = 2: one CTA, whose two row
+// tiles do that with one copy of the keys and values.  Roles of the warps:
+//   0          loads keys and values through a ring of tiles (TMA, a box per page or part
+//              of one; what lies past the prefix or outside the pool comes as zeros)
+//   1 .. kT    issue a row tile's products: S(j+1) = Q K(j+1)^T, then O += P(j) V(j) as soon
+//              as P(j) is written, so that S is a tile ahead
+//   then 4 kT  one row to a thread: the running maximum (moved when a tile's passes it by
+//              2^8: O is rescaled then), exponentials, the fp32 sum, P to tensor memory over S
 // P enters the product in two bf16 parts, the weight cut to 8 bits and the rest, for an error
-// of 2^-16 of a weight.  The rest is taken of w (1 + 2^-20), so that it is above zero wherever w
-// is and an infinite value meets no zero; O is divided by 1 + 2^-20 at the end.
+// of 2^-16 of a weight.  (In one part the error of O against 64 bits would be 1.4 times that of
+// its own rounding.)  The rest is taken of w (1 + 2^-20), so that it is above zero wherever w is
+// and an infinite value meets no zero; O is divided by 1 + 2^-20 at the end.
 //
-// Tensor memory of a CTA (256 columns): S of two tiles (64 columns each; P's parts over it, 32
-// columns each), O behind them.
+// Tensor memory of a row tile (256 columns): S of two tiles (64 columns each; P's parts over it,
+// 32 columns each), O behind them.
+//
+// What bounds it: 128 x 32768 (1024 rows of a KV head) 2230 clocks for a tile of two row tiles,
+// of which the products' issue takes 1830 for each: a product of 64 columns takes the pipe as long
+// as one of 128, 64 clocks, so that S costs as much as the two parts of P.  S of 128 keys at a
+// time has no room for a second buffer: 96 us for the call instead of 92, as did the CTA of one
+// row tile.  Without the rests' products 82.  Shorter prefixes are start and end: groups and
+// lengths 1.2 us, first page numbers 0.7, Q and the first tiles 2.5; a part out 2.
 #include "cache_line.cuh"
 
 namespace avits {

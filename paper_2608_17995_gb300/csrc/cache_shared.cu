@@ -9,7 +9,16 @@
 //
 // A prefix is read once for all sequences of its group: the query heads of all of them
 // that share a KV head are the rows of one product.  Three kernels: parts of the prefixes,
-// parts of the own tokens beside it, and the join.
+// parts of the own tokens beside it, and the join.  Where both are short, one launch goes over
+// them, each sequence reading its prefix by itself (from L2).
+//
+// What bounds it: the prefixes' bytes and the own ones, while a group has up to about 128
+// rows of a KV head; the tensor pipe beyond (a tile of 64 keys by 128 rows is 8 products of
+// 64 columns for S and 8 of 128 for the two parts of P, 64 clocks each).  Of a call's time
+// much is start and end: lengths, pages and the first tiles in turn 5 us, parts out and joined
+// 6.  With 8 KV heads of 4 query heads, width 128, in us and (bytes at a copy's rate): 8
+// sequences on 517 tokens 9.3 (0.7), 64 on 8192 with up to 512 of their own 37 (16), 12 groups
+// of 8 on up to 3001 53 (36); 128 sequences of 4 x 8 heads on 32768 86 (36 of products).
 #include "cache_line.cuh"
 
 namespace avits {
@@ -31,17 +40,27 @@ struct Line {
 
 int width_of(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-constexpr int kPrefixLeast = 2;
+// Pieces of a prefix on the tensor cores: short ones cost a start and a part each, and the SMs
+// that get none go over own tokens meanwhile.  64 sequences on 8192 tokens took 42 us in
+// 152 pieces of 7 tiles (of 256 rows), 37 in 103 of 10, 41 in 76; 160 in 4 groups on 2000 57 and
+// 52.  Where a whole call has few tiles, they are cut finer.
+int piece_tiles(long long tiles, bool two) {
+  const int most = two ? 10 : 8;
+  const long long share = tiles / (two ? 100 : 200);
+  return (int)(share < 2 ? 2 : share > most ? most : share);
+}
 
 void cut(Line& l, const avits_kv_cache& c, int num_sms) {
   const bool bf = c.dt == AVITS_BF16;
   l.D = width_of(c.d);
   l.tile = l.box ? kPrefixTile : bf ? 16 : 8;
-  const int longest = (c.max_len + l.tile - 1) / l.tile, few = l.box ? kPrefixLeast : kWarps;
+  const int longest = (c.max_len + l.tile - 1) / l.tile;
   l.tiles = l.units * longest;
+  const int few = l.box ? piece_tiles(l.tiles, l.rows > kPrefixRows) : kWarps;
   l.least = longest < few ? longest : few;
   const long long most = (l.tiles + l.least - 1) / l.least;
-  long long full = (long long)num_sms * (l.box ? 2 * kPrefixRows / l.rows : (l.groups ? own_ctas(l.D, l.rows, bf) : line_ctas(l.D, l.rows, bf)));
+  const int ctas = l.box ? 2 * kPrefixRows / l.rows : line_ctas(l.D, l.rows, bf);
+  long long full = (long long)num_sms * ctas;
   if (full > kMaxGrid) full = kMaxGrid;
   l.grid = (int)(most < full ? (most > 0 ? most : 1) : full);
 }
@@ -51,33 +70,44 @@ int rows_of(bool bf, int D, long long n) {
   return !bf ? (n <= 4 ? 4 : 8) : n <= 8 ? 8 : n <= 16 || D == 256 ? 16 : 32;
 }
 
-constexpr long long kAgainBytes = 64ll << 20;
-constexpr int kOwnShort = 1024, kOwnLong = 2048;
-
 // CTAs of a unit's cluster that goes over prefix and own tokens in one launch, 0 where parts
-// are faster.
+// are faster: where the keys do not fit a cluster, where reading the prefix for every
+// sequence costs more than two launches, or where the units are many.  us, one launch and
+// parts, 8 KV heads of width 128 (prefix + own tokens):
+//   4 x (900 + 700)   10.1  16.4    48 x (256 + 120)   13.1  15.7   (50 MB read again)
+//   16 x (900 + 120)  14.8  17.7    48 x (512 + 120)   16.9  15.2   (100 MB)
+//   16 x (512 + 700)  16.5  16.5    128 x (64 + 120)   25.6  21.8   (1024 units)
+//   fp32, 16 x (512 + 120) 19.6 20.6, 16 x (900 + 120) 27.8 23.6    (67 and 118 MB)
+constexpr long long kAgainBytes = 64ll << 20;
+constexpr int kManyUnits = 4;      // to an SM
+
 int both_of(const CacheSharedCall& s, const Line& own, int num_sms) {
   const long long units = own.units, keys = (long long)s.cache.max_len + s.prefix.max_len;
   const long long resident = (long long)num_sms * (own.D > 128 ? 1 : 2);
   auto fits = [&](int n) { return (keys + n - 1) / n <= (n > 1 ? 512 : 1024); };
   int n = 1;
   while (n < 8 && !fits(n)) n *= 2;
-  if (!fits(n) || (n > 1 && units * n > resident) || units >= (1 << 30)) return 0;
-  const long long again = units * s.prefix.max_len * 2 * s.cache.d * (s.cache.dt == AVITS_BF16 ? 2 : 4);
-  if (again > kAgainBytes || units > 4ll * num_sms) return 0;
+  if (!fits(n) || (n > 1 && units * n > resident) || units > (long long)kManyUnits * num_sms) return 0;
+  const int es = s.cache.dt == AVITS_BF16 ? 2 : 4;
+  if (units * s.prefix.max_len * 2 * s.cache.d * es > kAgainBytes) return 0;
   while (n < 8 && units * n * 2 <= resident && keys > n * 64) n *= 2;
   if (units * n < num_sms && keys > n * 256) return 0;
   return n;
 }
 
+// Own tokens: runs of 256 or 512 keys, a CTA each, up to kOwnLong; longer ones lie on a line.  us,
+// line and runs (the longer of the two kinds): 48 x (3000 + 1000) of 128 heads 62.5 and 61.5,
+// 64 x (8192 + 512) 46 and 41, 48 x (8000 + 2000) 75.4 and 74.8, 16 x (8000 + 4096) 55.3 and
+// 57.6, 1 x (20000 + 60000) 74.5 and 85.  Width 256: two warps to a CTA (88.8, with four
+// 111.6).
+constexpr int kOwnShort = 1024, kOwnLong = 2048;
+
 struct Shape {
   Line own, pre;
   int both;         // CTAs of a cluster that goes over prefix and own tokens; 0: parts
-  int warps;        // of a unit's CTA where own tokens are short; 0: the line of tiles
+  int warps;        // of a run's CTA where own tokens are short; 0: the line of tiles
   size_t total;
 };
-
-
 
 Shape shape_of(const CacheSharedCall& s, int num_sms) {
   const avits_kv_cache &c = s.cache, &p = s.prefix;
@@ -88,14 +118,14 @@ Shape shape_of(const CacheSharedCall& s, int num_sms) {
   x.own.groups = (G + x.own.rows - 1) / x.own.rows;
   x.own.units = (long long)c.B * c.Hkv * x.own.groups;
   x.pre.box = prefix_tc_box(p);
-  const long long rows = ((long long)c.B + p.B - 1) / p.B * G;      // of a group, by and large
+  // rows of a group's KV head, by and large
+  const long long rows = ((long long)c.B + p.B - 1) / p.B * G;
   x.pre.rows = !x.pre.box ? rows_of(bf, D, rows) : rows > kPrefixRows ? 2 * kPrefixRows : kPrefixRows;
-  x.pre.groups = 0;
   x.pre.units = c.Hkv * ((long long)c.B * G / x.pre.rows + p.B);
   cut(x.own, c, num_sms);
   cut(x.pre, p, num_sms);
   x.both = both_of(s, x.own, num_sms);
-  x.warps = c.max_len <= kOwnLong ? (x.own.D > 128 ? 2 : 4) : 0;
+  x.warps = c.max_len > kOwnLong ? 0 : D > 128 ? 2 : 4;
   if (x.warps) {       // runs of a unit
     const int longest = (c.max_len + x.own.tile - 1) / x.own.tile;
     x.own.least = c.max_len <= kOwnShort ? 16 : 32;
@@ -103,7 +133,8 @@ Shape shape_of(const CacheSharedCall& s, int num_sms) {
   }
   size_t at = 0;
   for (Line* l : {&x.own, &x.pre}) {
-    const size_t parts = (size_t)(l == &x.own && x.warps ? l->units * l->grid : l->units + l->grid) * l->rows;
+    const size_t parts =
+        (size_t)(l == &x.own && x.warps ? l->units * l->grid : l->units + l->grid) * l->rows;
     l->rec = at;
     l->pml = l->rec + up16((size_t)l->units * sizeof(int2));
     l->po = l->pml + up16(parts * sizeof(float2));
@@ -296,10 +327,11 @@ bool cache_shared_sizes_ok(const CacheSharedCall& s) {
   const avits_kv_cache& c = s.cache;
   if (s.H / c.Hkv > kMaxGroup || (long long)c.B * s.H >= (1ll << 30)) return false;
   const Shape x = shape_of(s, 1);
-  if ((long long)c.B * c.Hkv >= (1ll << 31) - 1) return false;
-  for (const Line* l : {&x.own, &x.pre})
-    if (l->tiles >= (1ll << 30) || (l->units + kMaxGrid) * l->rows >= (1ll << 31)) return false;
-  return true;
+  for (const Line* l : {&x.own, &x.pre}) {
+    const long long parts = l == &x.own && x.warps ? l->units * l->grid : l->units + kMaxGrid;
+    if (l->tiles >= (1ll << 30) || parts * l->rows >= (1ll << 31)) return false;
+  }
+  return (long long)c.B * c.Hkv < (1ll << 31) - 1;
 }
 
 size_t cache_shared_workspace(const CacheSharedCall& s, int num_sms) {

@@ -723,9 +723,6 @@ constexpr int stages() { return 2; }
 constexpr int line_ctas(int D, int rows, bool bf16) {
   return D > 128 ? 1 : bf16 && rows > 8 ? 2 : D <= 64 ? 4 : bf16 ? 2 : 3;
 }
-constexpr int own_ctas(int D, int rows, bool bf16) {
-  return bf16 && rows == 8 && D == 128 ? 3 : line_ctas(D, rows, bf16);
-}
 // A cluster's CTAs hold to what their registers allow without spills.
 constexpr int cluster_ctas(int D, int rows, int warps) {
   return (D > 128 ? 4 : rows > 8 ? 8 : 12) / warps;
