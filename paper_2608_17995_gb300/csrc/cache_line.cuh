@@ -37,7 +37,13 @@ __device__ __forceinline__ int group_of(const int32_t* start, int groups, int b)
 enum LineForm { kWhole = 0, kOwn = 1, kGroup = 2 };
 
 template <typename Rows, int kForm>
-__global__ void __launch_bounds__(kThreads, line_ctas(Rows::D, Rows::kR, Rows::kBf16))
+constexpr int line_min() {
+  return kForm == kOwn ? own_ctas(Rows::D, Rows::kR, Rows::kBf16)
+                       : line_ctas(Rows::D, Rows::kR, Rows::kBf16);
+}
+
+template <typename Rows, int kForm>
+__global__ void __launch_bounds__(kThreads, line_min<Rows, kForm>())
 cache_line_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                   const __grid_constant__ CacheAttn a) {
   using T = typename Rows::T;

@@ -59,7 +59,9 @@ void cut(Line& l, const avits_kv_cache& c, int num_sms) {
   const int few = l.box ? piece_tiles(l.tiles, l.rows > kPrefixRows) : kWarps;
   l.least = longest < few ? longest : few;
   const long long most = (l.tiles + l.least - 1) / l.least;
-  const int ctas = l.box ? 2 * kPrefixRows / l.rows : line_ctas(l.D, l.rows, bf);
+  const int ctas = l.box      ? 2 * kPrefixRows / l.rows
+                   : l.groups ? own_ctas(l.D, l.rows, bf)      // groups: of own tokens
+                              : line_ctas(l.D, l.rows, bf);
   long long full = (long long)num_sms * ctas;
   if (full > kMaxGrid) full = kMaxGrid;
   l.grid = (int)(most < full ? (most > 0 ? most : 1) : full);

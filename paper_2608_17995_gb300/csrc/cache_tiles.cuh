@@ -723,6 +723,11 @@ constexpr int stages() { return 2; }
 constexpr int line_ctas(int D, int rows, bool bf16) {
   return D > 128 ? 1 : bf16 && rows > 8 ? 2 : D <= 64 ? 4 : bf16 ? 2 : 3;
 }
+// Own tokens beside shared prefixes on the line, 8 rows of width 128: 3 CTAs (16 sequences of
+// 4096 beside 8000 52.3 us, with 2 55.2; one of 60000 beside 20000 73.6 and 71.9).
+constexpr int own_ctas(int D, int rows, bool bf16) {
+  return bf16 && rows == 8 && D == 128 ? 3 : line_ctas(D, rows, bf16);
+}
 // A cluster's CTAs hold to what their registers allow without spills.
 constexpr int cluster_ctas(int D, int rows, int warps) {
   return (D > 128 ? 4 : rows > 8 ? 8 : 12) / warps;
