@@ -8,13 +8,20 @@ cudaError_t launch_norm_rotate(const RotateCall& call, bool append, int num_sms,
   using namespace rotate;
   Rotate a{};
   a.r = call;
-  const int E = call.dt == AVITS_BF16 ? 8 : 4;
-  a.pieces = call.d / E;
-  const int half = call.rot.rot / 2;
-  const int form = call.rot.interleaved ? kPairs : half % E == 0 ? kHalves : kHalvesAny;
-  int lanes = 4;                   // of a row: two pieces each
-  while (2 * lanes < a.pieces) lanes *= 2;
-  const int per = 32 / lanes;
+  const int es = call.dt == AVITS_BF16 ? 2 : 4, half = call.rot.rot / 2;
+  Cut c{};
+  // pieces that halves are whole numbers of, if 32 lanes hold the row, two to a lane
+  c.bytes = 16;
+  if (!call.rot.interleaved) {
+    while (half * es % c.bytes) c.bytes /= 2;
+    if (c.bytes < 4 || (es == 4 && c.bytes < 8) || call.d * es / c.bytes > 64) c.bytes = 2;
+  }
+  c.form = call.rot.interleaved ? kPairs : c.bytes == 2 ? kHalvesAny : kHalves;
+  if (c.form == kHalvesAny) c.bytes = 16;
+  a.pieces = call.d * es / c.bytes;
+  c.lanes = c.bytes < 16 ? 16 : 4;
+  while (2 * c.lanes < a.pieces) c.lanes *= 2;
+  const int per = 32 / c.lanes;
   a.q_steps = (call.H + per - 1) / per;
   a.k_steps = (call.Hkv + per - 1) / per;
   a.steps = a.q_steps + a.k_steps * (append ? 2 : 1);
@@ -31,9 +38,9 @@ cudaError_t launch_norm_rotate(const RotateCall& call, bool append, int num_sms,
   a.page = FastDiv::of(append ? call.cache.page_size : 1);
   a.status = status;
   const long long units = (long long)call.tokens * a.parts;
-  const int grid = (int)((units + kRotWarps - 1) / kRotWarps);
-  return call.dt == AVITS_BF16 ? launch_type<__nv_bfloat16>(a, form, append, lanes, grid, s)
-                               : launch_f32(a, form, append, lanes, grid, s);
+  c.grid = (int)((units + kRotWarps - 1) / kRotWarps);
+  return call.dt == AVITS_BF16 ? launch_type<__nv_bfloat16>(a, append, c, s)
+                               : launch_f32(a, append, c, s);
 }
 
 }  // namespace avits

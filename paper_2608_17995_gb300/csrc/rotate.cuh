@@ -25,33 +25,79 @@ constexpr int kRotThreads = 128;
 constexpr int kRotWarps = kRotThreads / 32;
 constexpr int kDeep = 3;       // steps whose rows are under way at once
 
-template <typename T>
-struct Piece;
+// What a lane reads and writes at once: E values, 16 bytes, or 8 or 4 where that is what
+// halves are whole numbers of.
+template <int kBytes>
+struct Word;
 template <>
-struct Piece<__nv_bfloat16> {
-  static constexpr int E = 8;
-  __device__ static void unpack(const uint4& w, float (&x)[8]) {
-    x[0] = bf16_lo(w.x); x[1] = bf16_hi(w.x); x[2] = bf16_lo(w.y); x[3] = bf16_hi(w.y);
-    x[4] = bf16_lo(w.z); x[5] = bf16_hi(w.z); x[6] = bf16_lo(w.w); x[7] = bf16_hi(w.w);
-  }
-  __device__ static uint32_t two(float a, float b) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-  __device__ static uint4 pack(const float (&x)[8]) {
-    return make_uint4(two(x[0], x[1]), two(x[2], x[3]), two(x[4], x[5]), two(x[6], x[7]));
+struct Word<16> {
+  using V = uint4;
+  __device__ static V zero() { return make_uint4(0u, 0u, 0u, 0u); }
+  __device__ static uint32_t at(const V& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+  __device__ static V of(const uint32_t (&w)[4]) { return make_uint4(w[0], w[1], w[2], w[3]); }
+  // memory that this kernel may write again in place: no read-only path
+  __device__ static V load(const void* p) {
+    V v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
   }
 };
 template <>
-struct Piece<float> {
-  static constexpr int E = 4;
-  __device__ static void unpack(const uint4& w, float (&x)[4]) {
-    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y);
-    x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+struct Word<8> {
+  using V = uint2;
+  __device__ static V zero() { return make_uint2(0u, 0u); }
+  __device__ static uint32_t at(const V& v, int i) { return i == 0 ? v.x : v.y; }
+  __device__ static V of(const uint32_t (&w)[2]) { return make_uint2(w[0], w[1]); }
+  __device__ static V load(const void* p) {
+    V v;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
   }
-  __device__ static uint4 pack(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
-                      __float_as_uint(x[3]));
+};
+template <>
+struct Word<4> {
+  using V = uint32_t;
+  __device__ static V zero() { return 0u; }
+  __device__ static uint32_t at(const V& v, int) { return v; }
+  __device__ static V of(const uint32_t (&w)[1]) { return w[0]; }
+  __device__ static V load(const void* p) {
+    V v;
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+  }
+};
+
+template <typename T, int kBytes>
+struct Piece {
+  static constexpr int E = kBytes / (int)sizeof(T), kWords = kBytes / 4;
+  using W = Word<kBytes>;
+  using V = typename W::V;
+  __device__ static void unpack(const V& v, float (&x)[E]) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const uint32_t w = W::at(v, i);
+      if constexpr (sizeof(T) == 2) {
+        x[2 * i] = bf16_lo(w);
+        x[2 * i + 1] = bf16_hi(w);
+      } else {
+        x[i] = __uint_as_float(w);
+      }
+    }
+  }
+  __device__ static V pack(const float (&x)[E]) {
+    uint32_t w[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&v);
+      } else {
+        w[i] = __float_as_uint(x[i]);
+      }
+    }
+    return W::of(w);
   }
 };
 
@@ -68,15 +114,6 @@ __device__ __forceinline__ void turn(uint64_t f, int p, float m, float& c, float
   }
   c *= m;
   s *= m;
-}
-
-// 16 bytes that this kernel may write again in place: no read-only path.
-__device__ __forceinline__ uint4 ld_piece(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
-  return v;
 }
 
 // Two values to an instruction.
@@ -110,11 +147,13 @@ struct Rotate {
   unsigned int* status;
 };
 
-// kLanes to a row.
-template <typename T, int kForm, bool kAppend, int kLanes>
+// kLanes to a row, pieces of kBytes.
+template <typename T, int kForm, bool kAppend, int kLanes, int kBytes>
 __global__ void __launch_bounds__(kRotThreads)
 norm_rotate_kernel(const __grid_constant__ Rotate a) {
-  constexpr int E = Piece<T>::E, kAngles = kForm == kHalvesAny ? 2 * E : E, kPer = 32 / kLanes;
+  using Piece = Piece<T, kBytes>;
+  using V = typename Piece::V;
+  constexpr int E = Piece::E, kAngles = kForm == kHalvesAny ? 2 * E : E, kPer = 32 / kLanes;
   extern __shared__ float s_rows[];
   const RotateCall& r = a.r;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -180,18 +219,18 @@ norm_rotate_kernel(const __grid_constant__ Rotate a) {
                      : static_cast<T*>(r.k_out) + (int64_t)b * r.ko_str[0] + (int64_t)n * r.ko_str[1];
   // A ring of kDeep steps' rows.  Lanes without a piece keep the zeros, lanes past the rows
   // what they had (it stays in their row's lanes).
-  uint4 va[kDeep], vb[kDeep];
+  V va[kDeep], vb[kDeep];
 #pragma unroll
-  for (int k = 0; k < kDeep; ++k) va[k] = vb[k] = make_uint4(0u, 0u, 0u, 0u);
-  auto load = [&](uint4& x, uint4& y, int st) {
+  for (int k = 0; k < kDeep; ++k) va[k] = vb[k] = Piece::W::zero();
+  auto load = [&](V& x, V& y, int st) {
     if (st >= s1) return;
     const int kind = kind_of(st), row = row_of(st, kind);
     if (row >= (kind == 0 ? r.H : r.Hkv)) return;
     const T* in = kind == 0   ? q_in + row * r.q_str[2]
                   : kind == 1 ? k_in + row * r.k_str[2]
                               : v_in + row * r.v_sh;
-    if (ha) x = ld_piece(in + pa * E);
-    if (hb) y = ld_piece(in + pb * E);
+    if (ha) x = Piece::W::load(in + pa * E);
+    if (hb) y = Piece::W::load(in + pb * E);
   };
   // the first rows are on their way while the angles are computed
 #pragma unroll
@@ -257,8 +296,8 @@ norm_rotate_kernel(const __grid_constant__ Rotate a) {
                : kind == 1 ? k_out + row * (kAppend ? r.cache.k_sh : r.ko_str[2])
                            : static_cast<T*>(r.cache.v_pages) + v_at + row * r.cache.v_sh;
       if (kAppend && kind == 2) {          // a value: as it came
-        if (live && ha) *reinterpret_cast<uint4*>(out + pa * E) = va[k];
-        if (live && hb) *reinterpret_cast<uint4*>(out + pb * E) = vb[k];
+        if (live && ha) *reinterpret_cast<V*>(out + pa * E) = va[k];
+        if (live && hb) *reinterpret_cast<V*>(out + pb * E) = vb[k];
         load(va[k], vb[k], st + kDeep);
         continue;
       }
@@ -270,8 +309,8 @@ norm_rotate_kernel(const __grid_constant__ Rotate a) {
           float x0[E], x1[E];
 #pragma unroll
           for (int e = 0; e < E; ++e) x0[e] = x1[e] = 1.f;
-          if (ha) Piece<T>::unpack(__ldg(reinterpret_cast<const uint4*>(w + pa * E)), x0);
-          if (hb) Piece<T>::unpack(__ldg(reinterpret_cast<const uint4*>(w + pb * E)), x1);
+          if (ha) Piece::unpack(__ldg(reinterpret_cast<const V*>(w + pa * E)), x0);
+          if (hb) Piece::unpack(__ldg(reinterpret_cast<const V*>(w + pb * E)), x1);
 #pragma unroll
           for (int e = 0; e < E / 2; ++e) {
             wa[e] = make_float2(x0[2 * e], x0[2 * e + 1]);
@@ -281,8 +320,8 @@ norm_rotate_kernel(const __grid_constant__ Rotate a) {
       }
       {
         float fu[E], fv[E];
-        Piece<T>::unpack(va[k], fu);
-        Piece<T>::unpack(vb[k], fv);
+        Piece::unpack(va[k], fu);
+        Piece::unpack(vb[k], fv);
         load(va[k], vb[k], st + kDeep);
         float2 u[E / 2], v[E / 2];
 #pragma unroll
@@ -369,16 +408,16 @@ norm_rotate_kernel(const __grid_constant__ Rotate a) {
           fv[2 * e] = v[e].x;
           fv[2 * e + 1] = v[e].y;
         }
-        if (live && ha) *reinterpret_cast<uint4*>(out + pa * E) = Piece<T>::pack(fu);
-        if (live && hb) *reinterpret_cast<uint4*>(out + pb * E) = Piece<T>::pack(fv);
+        if (live && ha) *reinterpret_cast<V*>(out + pa * E) = Piece::pack(fu);
+        if (live && hb) *reinterpret_cast<V*>(out + pb * E) = Piece::pack(fv);
       }
     }
   }
 }
 
-template <typename T, int kForm, bool kAppend, int kLanes>
+template <typename T, int kForm, bool kAppend, int kLanes, int kBytes = 16>
 cudaError_t launch_lanes(const Rotate& a, int grid, cudaStream_t s) {
-  constexpr auto kernel = norm_rotate_kernel<T, kForm, kAppend, kLanes>;
+  constexpr auto kernel = norm_rotate_kernel<T, kForm, kAppend, kLanes, kBytes>;
   const cudaError_t e = prefer_max_shared<kernel>();
   if (e != cudaSuccess) return e;
   const size_t smem = kForm == kHalvesAny
@@ -386,29 +425,42 @@ cudaError_t launch_lanes(const Rotate& a, int grid, cudaStream_t s) {
   return launch_pdl(kernel, dim3((unsigned)grid), dim3(kRotThreads), smem, s, a);
 }
 
+// How a call's rows lie over lanes (launch_norm_rotate).
+struct Cut {
+  int form, bytes, lanes, grid;
+};
+
 template <typename T, int kForm, bool kAppend>
-cudaError_t launch_form(const Rotate& a, int lanes, int grid, cudaStream_t s) {
-  if (lanes <= 4) return launch_lanes<T, kForm, kAppend, 4>(a, grid, s);
-  if (lanes <= 8) return launch_lanes<T, kForm, kAppend, 8>(a, grid, s);
-  if (sizeof(T) == 2 || lanes <= 16) return launch_lanes<T, kForm, kAppend, 16>(a, grid, s);
-  if constexpr (sizeof(T) == 4) return launch_lanes<T, kForm, kAppend, 32>(a, grid, s);
+cudaError_t launch_form(const Rotate& a, const Cut& c, cudaStream_t s) {
+  if constexpr (kForm == kHalves) {
+    if (c.bytes == 8)
+      return c.lanes <= 16 ? launch_lanes<T, kForm, kAppend, 16, 8>(a, c.grid, s)
+                           : launch_lanes<T, kForm, kAppend, 32, 8>(a, c.grid, s);
+    if constexpr (sizeof(T) == 2)
+      if (c.bytes == 4)
+        return c.lanes <= 16 ? launch_lanes<T, kForm, kAppend, 16, 4>(a, c.grid, s)
+                             : launch_lanes<T, kForm, kAppend, 32, 4>(a, c.grid, s);
+  }
+  if (c.lanes <= 4) return launch_lanes<T, kForm, kAppend, 4>(a, c.grid, s);
+  if (c.lanes <= 8) return launch_lanes<T, kForm, kAppend, 8>(a, c.grid, s);
+  if (sizeof(T) == 2 || c.lanes <= 16) return launch_lanes<T, kForm, kAppend, 16>(a, c.grid, s);
+  if constexpr (sizeof(T) == 4) return launch_lanes<T, kForm, kAppend, 32>(a, c.grid, s);
   return cudaErrorInvalidValue;
 }
 
 template <typename T>
-cudaError_t launch_type(const Rotate& a, int form, bool append, int lanes, int grid,
-                        cudaStream_t s) {
+cudaError_t launch_type(const Rotate& a, bool append, const Cut& c, cudaStream_t s) {
   if (append) {
-    if (form == kPairs) return launch_form<T, kPairs, true>(a, lanes, grid, s);
-    if (form == kHalves) return launch_form<T, kHalves, true>(a, lanes, grid, s);
-    return launch_form<T, kHalvesAny, true>(a, lanes, grid, s);
+    if (c.form == kPairs) return launch_form<T, kPairs, true>(a, c, s);
+    if (c.form == kHalves) return launch_form<T, kHalves, true>(a, c, s);
+    return launch_form<T, kHalvesAny, true>(a, c, s);
   }
-  if (form == kPairs) return launch_form<T, kPairs, false>(a, lanes, grid, s);
-  if (form == kHalves) return launch_form<T, kHalves, false>(a, lanes, grid, s);
-  return launch_form<T, kHalvesAny, false>(a, lanes, grid, s);
+  if (c.form == kPairs) return launch_form<T, kPairs, false>(a, c, s);
+  if (c.form == kHalves) return launch_form<T, kHalves, false>(a, c, s);
+  return launch_form<T, kHalvesAny, false>(a, c, s);
 }
 
-cudaError_t launch_f32(const Rotate& a, int form, bool append, int lanes, int grid, cudaStream_t s);
+cudaError_t launch_f32(const Rotate& a, bool append, const Cut& c, cudaStream_t s);
 
 }  // namespace rotate
 }  // namespace avits

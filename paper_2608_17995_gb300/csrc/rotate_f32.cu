@@ -4,9 +4,8 @@
 namespace avits {
 namespace rotate {
 
-cudaError_t launch_f32(const Rotate& a, int form, bool append, int lanes, int grid,
-                       cudaStream_t s) {
-  return launch_type<float>(a, form, append, lanes, grid, s);
+cudaError_t launch_f32(const Rotate& a, bool append, const Cut& c, cudaStream_t s) {
+  return launch_type<float>(a, append, c, s);
 }
 
 }  // namespace rotate

@@ -291,7 +291,10 @@ ROTATIONS = [   # B, N, H, Hkv, d, rot, sections, interleaved
     (2, 3, 7, 2, 256, 256, None, False), (2, 3, 2, 2, 256, 2, None, True),
     (1, 50, 6, 6, 128, 128, [8, 28, 28], True), (2, 20, 4, 4, 64, 64, [16, 16], False),
     (1, 6, 2, 1, 64, 32, [0, 3, 13, 0], True), (1, 4, 2, 1, 8, 8, None, False), (1, 4, 2, 1, 16, 4, None, True),
-    (1, 5, 40, 8, 64, 0, None, False), (1, 3000, 2, 1, 64, 32, None, False), (2, 77, 1, 1, 24, 10, None, False)]
+    (1, 5, 40, 8, 64, 0, None, False), (1, 3000, 2, 1, 64, 32, None, False), (2, 77, 1, 1, 24, 10, None, False),
+    # halves that are whole numbers of 8 and 4 bytes only, of none, and of rows too wide for those
+    (2, 9, 5, 2, 72, 72, None, False), (1, 40, 3, 1, 72, 18, None, False), (3, 5, 2, 2, 96, 24, [4, 8], False),
+    (1, 6, 3, 1, 256, 20, None, False), (1, 6, 3, 1, 256, 24, None, False), (2, 3, 17, 5, 248, 124, None, False)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
