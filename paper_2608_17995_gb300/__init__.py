@@ -890,6 +890,8 @@ class Rotary:
                  a pair makes low turns or fewer within original_len, unchanged from high
                  on, in between linearly)
     magnitude    of the rotated values
+
+    The description is fixed: other frequencies are another Rotary.
     """
     __slots__ = ("rot", "axes", "freq", "device", "_struct", "_ref", "_index", "_call",
                  "int32", "codes")
@@ -922,8 +924,13 @@ class Rotary:
                                      (ctypes.c_int32 * 4)(*parts), magnitude)
         self._ref = ctypes.addressof(self._struct)
         self._index = self.freq.get_device()
-        self._call = lib().avits_call_packed
         self.int32, self.codes = torch.int32, {torch.bfloat16: BF16, torch.float32: F32}
+        self._call = lib().avits_call_packed
+
+    def __setattr__(self, name, value):
+        if hasattr(self, "_call"):        # set last
+            raise AttributeError("a Rotary's description is fixed: make another one")
+        object.__setattr__(self, name, value)
 
 
 def _weight_at(w, d, dtype, index):

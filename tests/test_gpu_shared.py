@@ -132,6 +132,10 @@ CASES = [   # sizes, prefixes, own lengths, H, Hkv, d, page, layout
     ([2, 2], [4500, 4096], [600, 9000, 0, 16], 40, 1, 64, 16, "heads"),
     ([40, 41], [4257, 640], [9] * 81, 4, 1, 128, 128, "tokens"),
     ([3, 2], [0, 4400], [0, 3, 0, 0, 4], 4, 2, 80, 48, "tokens"),
+    # more groups than lanes of a warp, some of them empty
+    ([i % 4 for i in range(75)], [(i * 37) % 200 for i in range(75)], [(5 * i) % 30 for i in range(111)], 12, 6,
+     64, 16, "tokens"),
+    ([3, 1] * 35, [(i * 53) % 90 for i in range(70)], [i % 9 for i in range(140)], 24, 8, 80, 24, "heads"),
     # and where they are many
     ([90, 60], [70, 3], [i % 40 for i in range(150)], 8, 8, 64, 16, "heads"),
 ]
@@ -308,6 +312,59 @@ def test_strided_queries(av):
     assert av.avits_device_status() == 0
     assert t.equal(out[..., 101:165], first[0]) and t.equal(lse, first[1])
     assert t.all(out[..., :101] == 3) and t.all(out[..., 165:] == 3)
+
+
+def test_uneven_groups(av):
+    """One group of many rows among small ones: two row tiles to a CTA, the second empty."""
+    w = World(av, "bf16", [200, 1, 1], [500, 4200, 64], [3] * 202, 6, 2, 128, 16, seed=8)
+    w.check(*w.run(), seqs=[0, 1, 41, 42, 43, 85, 86, 127, 128, 199, 200, 201])
+    w = World(av, "bf16", [100], [4500], [1] * 100, 8, 2, 64, 8, seed=9)
+    w.check(*w.run(), seqs=[0, 31, 32, 33, 63, 64, 65, 99])
+
+
+def test_infinite_values_by_parts(av):
+    """As above where the prefix is on the tensor cores: of either part of a group's rows."""
+    w = World(av, "bf16", [70], [4400], [6] * 70, 8, 2, 64, 16, std=1.0, seed=3)
+    pg = int(w.prefix.block_table[0, 4399 // 16])
+    w.prefix.v_pages[pg, 4399 % 16, 1, 5] = float("inf")
+    w.prefix.v_pages[int(w.prefix.block_table[0, 0]), 3, 0, 7] = float("-inf")
+    o, _ = w.run()
+    o = o.float().cpu().numpy()
+    assert np.all(np.isposinf(o[:, 4:, 5])) and np.all(np.isneginf(o[:, :4, 7]))
+    bad = np.zeros_like(o, bool)
+    bad[:, 4:, 5] = True
+    bad[:, :4, 7] = True
+    assert np.all(np.isfinite(o[~bad]))
+
+
+@pytest.mark.parametrize("page", [16, 24])
+def test_bad_pages_by_parts(av, page):
+    """Numbers outside the pool in a prefix on the tensor cores: those tokens are masked."""
+    w = World(av, "bf16", [40, 2], [4300, 130], [20] * 42, 8, 2, 64, page, seed=4)
+    w.prefix.block_table[0, 1] = -1
+    w.prefix.block_table[0, 100] = 1 << 20
+    w.prefix.block_table[1, 0] = -5
+    o, lse = w.run(status=7)
+
+    def keys(b):
+        g = w.group_of(b)
+        gone = {c * page + i for c in ((1, 100) if g == 0 else (0,)) for i in range(page)}
+        pre = [x[:, [j for j in range(w.pre[g]) if j not in gone]] for x in take(w.prefix, g, w.pre[g])]
+        return [np.concatenate(x, 1) for x in zip(pre, take(w.cache, b, w.lens[b]))]
+
+    w.check(o, lse, keys=keys, seqs=[0, 20, 39, 40, 41])
+
+
+def test_steep_by_parts(av):
+    """Logits that rise along the keys: the reference moves and O is rescaled."""
+    t = _torch()
+    w = World(av, "bf16", [50, 40], [4500, 4500], [10] * 90, 8, 2, 128, 16, std=1.0, seed=12)
+    for g in range(2):
+        place = t.arange(4500, device=DEV)
+        pg = w.prefix.block_table[g].long()[place // 16]
+        scale = (0.2 + 40.0 * (place % 1500) / 1500).to(t.bfloat16)[:, None, None]
+        w.prefix.k_pages[pg, place % 16] = (w.prefix.k_pages[pg, place % 16] * scale)
+    w.check(*w.run(), seqs=[0, 17, 49, 50, 89])
 
 
 def test_refused_by_the_binding(av):

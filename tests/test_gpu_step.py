@@ -149,6 +149,28 @@ def test_plan_short_of_pages(av, spare, extra):
     p.check(bad=True)
 
 
+@pytest.mark.parametrize("B,seed", [(3, 0), (700, 1), (2100, 2)])
+def test_plan_many_rows(av, B, seed):
+    """Rows that a kernel of their own writes, among long runs of sequences without any."""
+    rng = np.random.default_rng(seed)
+    lens, change = [0] * B, [0] * B
+    for b in list(rng.integers(0, B, 40)) + [0, B - 1]:
+        lens[b], change[b] = int(rng.integers(0, 50)), int(rng.integers(1, 900))
+    lens[1], change[1] = 4000, -3900
+    lens[B // 2], change[B // 2] = 5000, 9000
+    p = Pages(av, lens, change, 16, 14000, 4000, seed=seed)
+    assert p.T > 8192 + 3
+    p.call()
+    p.check()
+
+
+def test_plan_many_rows_without_room(av):
+    """The same where a prompt finds no pages: its rows are padding."""
+    p = Pages(av, [0, 10, 0, 7], [9000, 1, 5000, 1], 16, 10000, 400, T=14010)
+    p.call()
+    p.check(bad=True)
+
+
 def test_plan_takes_pages_given_back_behind(av):
     """The pages come from a sequence later in the batch; without positions."""
     p = Pages(av, [4, 12], [8, -12], 4, 12, 0, base=False)
@@ -372,6 +394,28 @@ def test_rotate_views(av):
     alone = t.empty(N, H, d, dtype=t.bfloat16, device=DEV)
     av.avits_norm_rotate(rotary, pos, keep[1, :, :H], alone)
     assert t.equal(alone, x[1, :, :H])
+
+
+def test_rotary_is_fixed(av):
+    r = av.Rotary(64)
+    with pytest.raises(AttributeError):
+        r.freq = r.freq + 1
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rot,inter", [(32, False), (32, True), (36, False)])
+def test_rotate_infinities_with_norm(av, dt, rot, inter):
+    """A row with an infinity is NaN there and zero elsewhere, as the formula gives; the
+    others do not see it."""
+    t = _torch()
+    x = data(dt, (3, 2, 72), 3)
+    x[1, 0, 71] = float("inf")
+    out = t.empty_like(x)
+    av.avits_norm_rotate(av.Rotary(rot, interleaved=inter), t.tensor([3, 4, 5], dtype=t.int32, device=DEV),
+                         x, out)
+    assert t.isnan(out[1, 0, 71]) and not out[1, 0, :71].any()
+    out[1, 0] = 0
+    assert t.isfinite(out).all() and out[1, 1].any() and out[2].any()
 
 
 def test_rotate_joint_ladder(av):

@@ -2,6 +2,9 @@
 frequencies, and what the library and its binding refuse before anything is launched."""
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -207,8 +210,25 @@ def test_append_pages_that_meet(lib):
 
 
 # ------------------------------------------------------------- the binding --
-def test_rotary_struct_matches_the_header():
-    assert ctypes.sizeof(av._RotaryStruct) == 8 + 3 * 4 + 4 * 4 + 4
+def test_rotary_struct_matches_the_header(tmp_path):
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if cc is None:
+        pytest.skip("no C compiler")
+    names = [n for n, _ in av._RotaryStruct._fields_]
+    src = tmp_path / "offsets.c"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "avits.h"\nint main(void) {\n'
+                   '  printf("%zu\\n", sizeof(avits_rotary));\n' +
+                   "".join('  printf("%%zu %%zu\\n", offsetof(avits_rotary, %s), '
+                           'sizeof(((avits_rotary*)0)->%s));\n' % (n, n) for n in names) +
+                   "  return 0;\n}\n")
+    exe = str(tmp_path / "offsets")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.check_call([cc, str(src), "-I" + os.path.join(root, "include"), "-o", exe])
+    out = subprocess.check_output([exe], text=True).split("\n")
+    assert int(out[0]) == ctypes.sizeof(av._RotaryStruct)
+    for n, line in zip(names, out[1:]):
+        field = getattr(av._RotaryStruct, n)
+        assert [field.offset, field.size] == [int(x) for x in line.split()], n
 
 
 @pytest.mark.parametrize("kw", [dict(rot=7), dict(rot=258), dict(rot=-2), dict(rot=8, sections=[3]),
