@@ -91,10 +91,11 @@ cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_consta
   if constexpr (kForm == kBoth) {
     const CacheAttn& p = x.p;
     const int each = (p.c.B + 31) / 32, g0 = min(p.c.B, lane * each);
-    const bool rise = __all_sync(0xffffffffu, groups_ok(p, g0, min(p.c.B, g0 + each)));
     g = group_of(p.start, p.c.B, b);
     const int2 m = members_of(p.start, p.seqs, g);
-    if (rise && b >= m.x && b < m.y) len_p = cache_len(p.c, g);
+    const int n = cache_len(p.c, g);              // all of these reads at once
+    const bool rise = __all_sync(0xffffffffu, groups_ok(p, g0, min(p.c.B, g0 + each)));
+    if (rise && b >= m.x && b < m.y) len_p = n;
     nt_p = tiles_of(p, len_p);
     if (blockIdx.x == 0 && w == 0) {
       for (int y = lane; y < p.c.B; y += 32) check_cache_len(p.c, y, a.status);

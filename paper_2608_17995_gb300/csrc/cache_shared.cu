@@ -17,7 +17,7 @@
 // 64 columns for S and 8 of 128 for the two parts of P, 64 clocks each).  Of a call's time
 // much is start and end: lengths, pages and the first tiles in turn 5 us, parts out and joined
 // 6.  With 8 KV heads of 4 query heads, width 128, in us and (bytes at a copy's rate): 8
-// sequences on 517 tokens 9.3 (0.7), 64 on 8192 with up to 512 of their own 37 (16), 12 groups
+// sequences on 517 tokens 8.9 (0.7), 64 on 8192 with up to 512 of their own 37 (16), 12 groups
 // of 8 on up to 3001 53 (36); 128 sequences of 4 x 8 heads on 32768 86 (36 of products).
 #include "cache_line.cuh"
 
@@ -85,7 +85,11 @@ constexpr int kManyUnits = 4;      // to an SM
 
 int both_of(const CacheSharedCall& s, const Line& own, int num_sms) {
   const long long units = own.units, keys = (long long)s.cache.max_len + s.prefix.max_len;
-  const long long resident = (long long)num_sms * (own.D > 128 ? 1 : 2);
+  // CTAs at once.  3 to an SM do not all find a place as clusters of 8: 448 of them took 15.3 us
+  // where 224 in clusters of 4 took 10.8, but 384 7.7 and 192 8.2.
+  const long long resident = own.D > 128   ? num_sms
+                             : own.rows > 8 ? 2ll * num_sms
+                                            : 8ll * num_sms / 3;
   auto fits = [&](int n) { return (keys + n - 1) / n <= (n > 1 ? 512 : 1024); };
   int n = 1;
   while (n < 8 && !fits(n)) n *= 2;
