@@ -15,8 +15,8 @@ namespace {
 //   kBoth   a prefix's tokens and then the sequence's own, in one launch; every sequence
 //           reads its prefix by itself (from L2)
 //   kParts  the own tokens, a CTA for each run of a unit's tiles (a.least of them, a.grid runs to
-//           a unit), as parts to be joined, beside the kernel before, which goes over the prefixes and has waited for what both read: the last
-//           CTA waits for it, for the join
+//           a unit), as parts to be joined, beside the kernel before, which goes over the
+//           prefixes and has waited for what both read: the last CTA waits for it, for the join
 enum ClusterForm { kAlone = 0, kBoth = 1, kParts = 2 };
 
 template <int kForm>
@@ -27,10 +27,6 @@ struct Beside<kBoth> {
   CacheAttn p;
 };
 
-// A cluster of CTAs per unit, each with an equal run of its
-// tiles and their logits in shared memory.  The CTAs' maxima, sums and O meet
-// through distributed shared memory; then every CTA writes a slice of O and the
-// weights of its own keys.  No workspace, no second kernel.
 template <typename Rows>
 constexpr int cluster_smem(int warps, int rows, int keys) {   // keys: logits' row stride, 0: none
   return smem_bytes<Rows>(warps) + Rows::kR * Rows::D * 4 + rows * keys * 4;
@@ -46,6 +42,10 @@ constexpr int cluster_min() {
              ? 16 / W : cluster_ctas(Rows::D, Rows::kR, W);
 }
 
+// A cluster of CTAs per unit, each with an equal run of its
+// tiles and their logits in shared memory.  The CTAs' maxima, sums and O meet
+// through distributed shared memory; then every CTA writes a slice of O and the
+// weights of its own keys.  No workspace, no second kernel.
 template <typename Rows, int W, int kForm>
 __global__ void __launch_bounds__(32 * W, cluster_min<Rows, W, kForm>())
 cache_cluster_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,

@@ -176,7 +176,6 @@ CacheAttn args_of(const CacheSharedCall& s, const avits_kv_cache& c, const Line&
   a.base = reinterpret_cast<int*>(ws + l.base);
   a.start = s.group_start;
   a.seqs = s.cache.B;
-  a.most = (int)l.units;
   a.status = status;
   return a;
 }

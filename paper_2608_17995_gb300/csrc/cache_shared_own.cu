@@ -11,9 +11,7 @@ cudaError_t launch_own_parts(CacheAttn& a, int D, int warps, cudaStream_t s) {
     CUtensorMap mk{}, mv{};
     map_cache<Rows>(a, &mk, &mv);
     const Beside<kParts> none{};
-    if constexpr (Rows::kBf16 && Rows::kR <= 16)
-      if (warps == 1) return launch_rows<Rows, 1, kParts>(mk, mv, a, 1, 0, none, s);
-    if (warps <= 2) return launch_rows<Rows, 2, kParts>(mk, mv, a, 1, 0, none, s);
+    if (warps == 2) return launch_rows<Rows, 2, kParts>(mk, mv, a, 1, 0, none, s);
     return launch_rows<Rows, 4, kParts>(mk, mv, a, 1, 0, none, s);
   });
 }

@@ -57,7 +57,6 @@ struct CacheAttn {
   // attention over prefixes that groups of sequences share: the prefixes' cache is c, and
   const int32_t* start;   // [c.B + 1] first sequence of each group
   int seqs;               // sequences of the batch
-  int most;               // units that the workspace has room for
   int* base;              // [c.B + 1] first unit of each group; the last: 1 if the groups rise
 };
 
