@@ -1,7 +1,35 @@
 // rotate.cu — norm and rotation of bf16 heads, and the launch of both types.
 #include "rotate.cuh"
 
+#include <climits>
+
 namespace avits {
+
+namespace {
+
+// Warps of a token: the fewest rounds of warps, each as long as its steps and about three more
+// for the angles.  Tokens of 48 bf16 heads of 128, us with 1, 2, 4, .. warps: 512 of them 5.6
+// with 4, 7.0 with 8, 7.6 with 12; 2048 13.8, 14.9, 15.9, 20.2; 4096 25.0, 23.9, 28.6; 8192 41.9, 42.9.
+// 1554 of 20 fp32 heads of 80 9.0, 7.6, 7.7, 9.1.
+constexpr int kAnglesSteps = 3;
+constexpr int kWarpsBf16 = 20, kWarpsF32 = 32;      // on an SM at once, by registers
+
+int parts_of(const rotate::Rotate& a, int es, int num_sms) {
+  const long long once = (long long)num_sms * (es == 2 ? kWarpsBf16 : kWarpsF32);
+  long long least = LLONG_MAX;
+  int best = 1;
+  for (int n = 1;; n = 2 * n < a.steps ? 2 * n : a.steps) {
+    const long long rounds = (a.r.tokens * (long long)n + once - 1) / once;
+    const long long cost = rounds * (kAnglesSteps + (a.steps + n - 1) / n);
+    if (cost < least) {
+      least = cost;
+      best = n;
+    }
+    if (n >= a.steps) return best;
+  }
+}
+
+}  // namespace
 
 cudaError_t launch_norm_rotate(const RotateCall& call, bool append, int num_sms,
                                unsigned int* status, cudaStream_t s) {
@@ -26,10 +54,7 @@ cudaError_t launch_norm_rotate(const RotateCall& call, bool append, int num_sms,
   a.k_steps = (call.Hkv + per - 1) / per;
   a.steps = a.q_steps + a.k_steps * (append ? 2 : 1);
   a.inv_d = 1.f / (float)call.d;
-  // a warp for each token, or several where tokens are too few to fill the SMs
-  a.parts = 1;
-  while (a.parts < a.steps && (long long)call.tokens * a.parts < 32ll * num_sms) a.parts *= 2;
-  if (a.parts > a.steps) a.parts = a.steps;
+  a.parts = parts_of(a, es, num_sms);
   a.first[0] = 0;
   for (int x = 1; x < 4; ++x)
     a.first[x] = x < call.rot.axes ? a.first[x - 1] + call.rot.sections[x - 1] : 1 << 30;
