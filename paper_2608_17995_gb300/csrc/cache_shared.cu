@@ -43,9 +43,12 @@ int width_of(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // Pieces of a prefix on the tensor cores: short ones cost a start and a part each, and the SMs
 // that get none go over own tokens meanwhile.  64 sequences on 8192 tokens took 42 us in
 // 152 pieces of 7 tiles (of 256 rows), 37 in 103 of 10, 41 in 76; 160 in 4 groups on 2000 57 and
-// 52.  Where a whole call has few tiles, they are cut finer.
-int piece_tiles(long long tiles, bool two) {
-  const int most = two ? 10 : 8;
+// 52.  Where a whole call has few tiles, they are cut finer.  Of 128 rows: 8 tiles where a unit
+// has many pieces to join (11 sequences on 46000 24.7, of 4 tiles 28.8; 8 on 16000 27.0, of 5
+// 28.3), else 5 (64 in 16 groups on up to 1000 23.7, of 8 29.8; 70 in 24 on 1282 22.0 and 27.3).
+constexpr int kManyTiles = 160;      // of a unit
+int piece_tiles(long long tiles, int longest, bool two) {
+  const int most = two ? 10 : longest > kManyTiles ? 8 : 5;
   const long long share = tiles / (two ? 100 : 200);
   return (int)(share < 2 ? 2 : share > most ? most : share);
 }
@@ -56,7 +59,7 @@ void cut(Line& l, const avits_kv_cache& c, int num_sms) {
   l.tile = l.box ? kPrefixTile : bf ? 16 : 8;
   const int longest = (c.max_len + l.tile - 1) / l.tile;
   l.tiles = l.units * longest;
-  const int few = l.box ? piece_tiles(l.tiles, l.rows > kPrefixRows) : kWarps;
+  const int few = l.box ? piece_tiles(l.tiles, longest, l.rows > kPrefixRows) : kWarps;
   l.least = longest < few ? longest : few;
   const long long most = (l.tiles + l.least - 1) / l.least;
   const int ctas = l.box      ? 2 * kPrefixRows / l.rows
@@ -101,12 +104,15 @@ int both_of(const CacheSharedCall& s, const Line& own, int num_sms) {
   return n;
 }
 
-// Own tokens: runs of 256 or 512 keys, a CTA each, up to kOwnLong; longer ones lie on a line.  us,
-// line and runs (the longer of the two kinds): 48 x (3000 + 1000) of 128 heads 62.5 and 61.5,
-// 64 x (8192 + 512) 46 and 41, 48 x (8000 + 2000) 75.4 and 74.8, 16 x (8000 + 4096) 55.3 and
-// 57.6, 1 x (20000 + 60000) 74.5 and 85.  Width 256: two warps to a CTA (88.8, with four
-// 111.6).
+// Own tokens: runs of 256 or 512 keys, a CTA each, up to kOwnLong or where the runs are few;
+// else they lie on a line.  us, line and runs (the longer of the two kinds): 48 x (3000 + 1000) of
+// 128 heads 62.5 and 61.5, 64 x (8192 + 512) 46 and 41, 48 x (8000 + 2000) 75.4 and 74.8; by the
+// number of runs 40 (1 x (500 + 2500)) 16.6 and 13.5, 256 (1 x (8000 + 16000)) 35.5 and 32.1, 384
+// (4 x (500 + 6000)) 28.3 and 20.8, 640 (16 x (500 + 2500)) 35.9 and 31.7, 944 (1 x (20000 +
+// 60000)) 74.5 and 85, 1024 (4 x (8000 + 16000)) 54.3 and 57.2, 1536 (16 x (8000 + 6000)) 67.5 and
+// 69.8.  Width 256: two warps to a CTA (88.8, with four 111.6).
 constexpr int kOwnShort = 1024, kOwnLong = 2048;
+constexpr int kFewRuns = 5;        // to an SM
 
 struct Shape {
   Line own, pre;
@@ -131,11 +137,13 @@ Shape shape_of(const CacheSharedCall& s, int num_sms) {
   cut(x.own, c, num_sms);
   cut(x.pre, p, num_sms);
   x.both = both_of(s, x.own, num_sms);
-  x.warps = c.max_len > kOwnLong ? 0 : D > 128 ? 2 : 4;
-  if (x.warps) {       // runs of a unit
-    const int longest = (c.max_len + x.own.tile - 1) / x.own.tile;
-    x.own.least = c.max_len <= kOwnShort ? 16 : 32;
-    x.own.grid = (longest + x.own.least - 1) / x.own.least;
+  // runs of a unit
+  const int longest = (c.max_len + x.own.tile - 1) / x.own.tile, run = c.max_len <= kOwnShort ? 16 : 32;
+  const int runs = (longest + run - 1) / run;
+  if (c.max_len <= kOwnLong || x.own.units * runs <= (long long)kFewRuns * num_sms) {
+    x.warps = D > 128 ? 2 : 4;
+    x.own.least = run;
+    x.own.grid = runs;
   }
   size_t at = 0;
   for (Line* l : {&x.own, &x.pre}) {
