@@ -322,6 +322,20 @@ def test_uneven_groups(av):
     w.check(*w.run(), seqs=[0, 31, 32, 33, 63, 64, 65, 99])
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,d,page", [("bf16", 8, 8, 64, 16), ("bf16", 32, 8, 128, 16),
+                                               ("bf16", 40, 4, 80, 24), ("bf16", 8, 8, 256, 16),
+                                               ("f32", 8, 8, 96, 24), ("f32", 40, 4, 128, 5)])
+def test_long_own_tokens(av, dtype, H, Hkv, d, page):
+    """Own tokens on one line of tiles: sequences that may be long, and many of them."""
+    lens = [(7 * i) % 40 for i in range(80)]
+    lens[0], lens[33], lens[79] = 2500, 2111, 300
+    w = World(av, dtype, [50, 0, 28], [1500, 8, 333], lens, H, Hkv, d, page, before=1, seed=13)
+    first = w.run()
+    w.check(*first, seqs=[0, 1, 2, 33, 40, 49, 50, 51, 77, 78, 79])
+    again = w.run()
+    assert _torch().equal(first[0], again[0]) and _torch().equal(first[1], again[1])
+
+
 def test_infinite_values_by_parts(av):
     """As above where the prefix is on the tensor cores: of either part of a group's rows."""
     w = World(av, "bf16", [70], [4400], [6] * 70, 8, 2, 64, 16, std=1.0, seed=3)
