@@ -20,12 +20,16 @@
 // Tensor memory of a row tile (256 columns): S of two tiles (64 columns each; P's parts over it,
 // 32 columns each), O behind them.
 //
-// What bounds it: 128 x 32768 (1024 rows of a KV head) 2230 clocks for a tile of two row tiles,
-// of which the products' issue takes 1830 for each: a product of 64 columns takes the pipe as long
-// as one of 128, 64 clocks, so that S costs as much as the two parts of P.  S of 128 keys at a
-// time has no room for a second buffer: 96 us for the call instead of 92, as did the CTA of one
-// row tile.  Without the rests' products 82.  Shorter prefixes are start and end: groups and
-// lengths 1.2 us, first page numbers 0.7, Q and the first tiles 2.5; a part out 2.
+// What bounds it, at 128 x 32768 (1024 rows of a KV head, 87 us for the call, 86 with two row
+// tiles): 2230 clocks for a tile of 256 rows, of which a tensor pipe's products are 2050 (a product of
+// 64 columns takes the pipe as long as one of 128, 64 clocks, so that S costs as much as the two
+// parts of P) and a softmax warp's work 2000 (535 instructions, of which 64 exponentials, for 64
+// keys of 32 rows, two such warps to a scheduler); neither alone is the bound: without the rests'
+// products 82 us, without the rests 77, without copies 85.  What did not help: S of 128 keys at a
+// time, or Q in tensor memory (96 and 109 us: no room for a second S), two threads to a row (94), one
+// warp that issues for both row tiles (120), registers moved to the softmax warps (90).  Shorter
+// prefixes are start and end: groups and lengths 1.2 us, first page numbers 0.7, Q and the first
+// tiles 2.5; a part out 2.
 #include "cache_line.cuh"
 
 namespace avits {

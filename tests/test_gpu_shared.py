@@ -336,6 +336,52 @@ def test_long_own_tokens(av, dtype, H, Hkv, d, page):
     assert _torch().equal(first[0], again[0]) and _torch().equal(first[1], again[1])
 
 
+def pairs_of_tiles(av, size, pre, lens, H, Hkv, d, page, **kw):
+    """Long own tokens by the bound, so that a prefix's rows go by two tiles to a CTA."""
+    return World(av, "bf16", size, pre, lens, H, Hkv, d, page, max_len=(152 << 10) // (len(lens) * Hkv) + 1, **kw)
+
+
+@pytest.mark.parametrize("size,pre,lens,H,Hkv,d,page,seqs", [
+    ([200, 1, 1], [500, 4200, 64], [3] * 202, 6, 2, 128, 16, [0, 1, 41, 42, 43, 85, 86, 127, 128, 199, 200, 201]),
+    ([100], [4500], [1] * 100, 8, 2, 64, 8, [0, 31, 32, 33, 63, 64, 65, 99]),
+    ([64, 60], [1500, 0], [(5 * i) % 90 for i in range(124)], 12, 3, 80, 24, [0, 1, 2, 21, 42, 63, 64, 65, 123]),
+    ([0, 130], [70, 1999], [0] * 130, 16, 8, 128, 64, [0, 1, 63, 64, 65, 127, 128, 129]),
+])
+def test_pairs_of_row_tiles(av, size, pre, lens, H, Hkv, d, page, seqs):
+    w = pairs_of_tiles(av, size, pre, lens, H, Hkv, d, page, seed=8)
+    first = w.run()
+    w.check(*first, seqs=seqs)
+    again = w.run()
+    assert _torch().equal(first[0], again[0]) and _torch().equal(first[1], again[1])
+
+
+def test_odd_values_in_pairs_of_row_tiles(av):
+    """Infinite values, page numbers outside the pool and logits that rise along the keys."""
+    t = _torch()
+    w = pairs_of_tiles(av, [64], [4400], [6] * 64, 8, 2, 64, 16, std=1.0, seed=3)
+    w.prefix.v_pages[int(w.prefix.block_table[0, 4399 // 16]), 4399 % 16, 1, 5] = float("inf")
+    o = w.run()[0].float().cpu().numpy()
+    assert np.all(np.isposinf(o[:, 4:, 5])) and np.isfinite(o).sum() == o.size - 64 * 4
+    w = pairs_of_tiles(av, [64], [4300], [20] * 64, 8, 2, 128, 24, seed=4)
+    w.prefix.block_table[0, 1] = -1
+    w.prefix.block_table[0, 100] = 1 << 20
+    o, lse = w.run(status=7)
+    gone = {c * 24 + i for c in (1, 100) for i in range(24)}
+
+    def keys(b):
+        pre = [x[:, [j for j in range(4300) if j not in gone]] for x in take(w.prefix, 0, 4300)]
+        return [np.concatenate(x, 1) for x in zip(pre, take(w.cache, b, w.lens[b]))]
+
+    w.check(o, lse, keys=keys, seqs=[0, 31, 32, 33, 63])
+    w = pairs_of_tiles(av, [30, 34], [2500, 2500], [10] * 64, 12, 2, 128, 16, std=1.0, seed=12)
+    for g in range(2):
+        place = t.arange(2500, device=DEV)
+        pg = w.prefix.block_table[g].long()[place // 16]
+        scale = (0.2 + 40.0 * (place % 1500) / 1500).to(t.bfloat16)[:, None, None]
+        w.prefix.k_pages[pg, place % 16] = (w.prefix.k_pages[pg, place % 16] * scale)
+    w.check(*w.run(), seqs=[0, 17, 29, 30, 63])
+
+
 def test_infinite_values_by_parts(av):
     """As above where the prefix is on the tensor cores: of either part of a group's rows."""
     w = World(av, "bf16", [70], [4400], [6] * 70, 8, 2, 64, 16, std=1.0, seed=3)
