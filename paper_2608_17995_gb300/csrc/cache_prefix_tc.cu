@@ -20,8 +20,8 @@
 // Tensor memory of a row tile (256 columns): S of two tiles (64 columns each; P's parts over it,
 // 32 columns each), O behind them.
 //
-// What bounds it, at 128 x 32768 (1024 rows of a KV head, 87 us for the call, 86 with two row
-// tiles): 2230 clocks for a tile of 256 rows, of which a tensor pipe's products are 2050 (a product of
+// What bounds it, at 128 x 32768 (1024 rows of a KV head, 86 us for the call, 87 with one row
+// tile): 2230 clocks for a tile of 256 rows, of which a tensor pipe's products are 2050 (a product of
 // 64 columns takes the pipe as long as one of 128, 64 clocks, so that S costs as much as the two
 // parts of P) and a softmax warp's work 2000 (535 instructions, of which 64 exponentials, for 64
 // keys of 32 rows, two such warps to a scheduler); neither alone is the bound: without the rests'

@@ -18,7 +18,7 @@
 // much is start and end: lengths, pages and the first tiles in turn 5 us, parts out and joined
 // 6.  With 8 KV heads of 4 query heads, width 128, in us and (bytes at a copy's rate): 8
 // sequences on 517 tokens 8.9 (0.7), 64 on 8192 with up to 512 of their own 37 (16), 12 groups
-// of 8 on up to 3001 53 (36); 128 sequences of 4 x 8 heads on 32768 87 (36 of products).
+// of 8 on up to 3001 53 (36); 128 sequences of 4 x 8 heads on 32768 86 (36 of products).
 #include "cache_line.cuh"
 
 namespace avits {
@@ -77,17 +77,19 @@ int rows_of(bool bf, int D, long long n) {
 
 // Rows of a unit on the tensor cores, for groups of n rows of a KV head.  Two row tiles to a CTA
 // leave room on its SM for a CTA of own tokens, and SMs without a piece to more: taken where the
-// tiles come in pairs, their pieces fit the SMs at once and there are own tokens for the rest.  us,
-// 128 and 256 rows: 64 x (2000 + 50) 23.8 and 27.7, + 300 28.4 and 30.9, + 512 36.4 and 33.1, + 2000
-// 79.0 and 73.8; 64 x (8192 + 200) 33.9 and 36.0, + 400 42.1 and 37.6, + 1000 62.3 and 58.2; 128 x
-// (2000 + 50) 28.3 and 31.7, + 200 36.6 and 34.1; more pieces 128 x (8192 + 512) 70.3 and 71.1, 4 KV
-// heads of 128 x (32768 + 300) 87.2 and 86.0, + 100 80.3 and 83.0; an odd tile 324 rows on 30145 59.9
-// and 70.2, 1136 on 16837 123 and 132.
-constexpr long long kAtOnce = 152 * 10, kMuchOwn = 152 * 1024;      // tiles, keys of KV heads
+// tiles come in pairs, there are own tokens for the rest, and the prefix is one or the pieces fit
+// the SMs at once.  us, 128 and 256 rows: 64 x (2000 + 50) 23.8 and 27.7, + 300 28.4 and 30.9, + 512
+// 36.4 and 33.1, + 2000 79.0 and 73.8; 64 x (8192 + 200) 33.9 and 36.0, + 400 42.1 and 37.6, + 1000
+// 62.3 and 58.2; 128 x (2000 + 50) 28.3 and 31.7, + 200 36.6 and 34.1; more pieces 64 x (20000 + 300)
+// 50.9 and 49.3, 128 x (8192 + 512) 70.3 and 71.1, 4 KV heads of 128 x (32768 + 300) 87.2 and 86.0, +
+// 100 80.3 and 83.0, three prefixes 96 x (8000 + 300) 60.3 and 64.6; an odd tile 324 rows on 30145
+// 59.9 and 70.2, 1136 on 16837 123 and 132.
+constexpr long long kAtOnce = 152 * 10, kMuchOwn = 128 * 1024;      // tiles, keys of KV heads
 int prefix_rows(const avits_kv_cache& c, const avits_kv_cache& p, long long n) {
   const long long tiles = (n + kPrefixRows - 1) / kPrefixRows, pairs = (tiles + 1) / 2;
   const bool two = tiles > 1 && 40 * pairs <= 21 * tiles &&
-                   pairs * c.Hkv * p.B * ((p.max_len + kPrefixTile - 1) / kPrefixTile) <= kAtOnce &&
+                   (p.B == 1 ||
+                    pairs * c.Hkv * p.B * ((p.max_len + kPrefixTile - 1) / kPrefixTile) <= kAtOnce) &&
                    (long long)c.B * c.Hkv * c.max_len >= kMuchOwn;
   return two ? 2 * kPrefixRows : kPrefixRows;
 }
