@@ -943,13 +943,14 @@ def _weight_at(w, d, dtype, index):
 
 @functools.lru_cache(maxsize=1024)
 def _strides_at(batch, token, head):
-    """An array of three strides (kept: making one takes 0.4 us) and its address."""
+    """An array of three strides (kept: making one takes 0.4 us) and its address, which is
+    good as long as the caller holds the array: other look-ups may push it out of here."""
     arr = _Int64x3(batch, token, head)
     return arr, ctypes.addressof(arr)
 
 
 def _heads_of(t, name):
-    """Shape of [B,N,heads,d] or [N,heads,d] as of the former, and the address of its strides."""
+    """Shape of [B,N,heads,d] or [N,heads,d] as of the former, and its strides (_strides_at)."""
     st, shape = t.stride(), t.shape
     if len(shape) == 4:
         b, n, h, x = st
@@ -959,7 +960,7 @@ def _heads_of(t, name):
         raise ValueError("%s: [B, N, heads, d] or [N, heads, d] expected" % name)
     if x != 1:
         raise ValueError("%s: the head-dim axis must be contiguous" % name)
-    return shape, _strides_at(b, n, h)[1]
+    return shape, _strides_at(b, n, h)
 
 
 def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q_weight=None,
@@ -969,6 +970,7 @@ def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q
     16-byte aligned strides, d contiguous; without B for one sequence; an output may
     be its input).  positions int32 [B,N,axes] or [N,axes] (one axis: [B,N] or [N] as
     well; None if nothing turns), the axes contiguous."""
+    # the four strides stay in these names until the call is back: it reads them
     (B, N, H, d), q_str = _heads_of(q, "q")
     shape, qo_str = _heads_of(q_out, "q_out")
     dtype, index = q.dtype, rotary._index
@@ -981,7 +983,8 @@ def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q
         raise ValueError("q or q_out on %s, %s: the rotary is on %s" % (q.device, q_out.device,
                                                                        rotary.device))
     Hkv = 0
-    k_at = k_str = ko_at = ko_str = 0
+    k_at = ko_at = 0
+    k_str = ko_str = (None, 0)
     if k is not None:
         (kB, kN, Hkv, kd), k_str = _heads_of(k, "k")
         shape, ko_str = _heads_of(k_out, "k_out")
@@ -997,8 +1000,8 @@ def avits_norm_rotate(rotary: Rotary, positions, q, q_out, k=None, k_out=None, q
         raise ValueError("sizes of more than 32 bits")
     p_at, p_sb, p_sn = _positions(rotary, positions, B, N) if rotary.rot else (0, 0, 0)
     rc = rotary._call(1, _ROTATE(
-        rotary._ref, code, B, N, d, p_at, p_sb, p_sn, q.data_ptr(), H, q_str, q_out.data_ptr(),
-        qo_str, k_at, Hkv, k_str, ko_at, ko_str, 1 if norm else 0,
+        rotary._ref, code, B, N, d, p_at, p_sb, p_sn, q.data_ptr(), H, q_str[1], q_out.data_ptr(),
+        qo_str[1], k_at, Hkv, k_str[1], ko_at, ko_str[1], 1 if norm else 0,
         0 if q_weight is None else _weight_at(q_weight, d, dtype, index),
         0 if k_weight is None else _weight_at(k_weight, d, dtype, index), eps,
         _rotary_stream(rotary, stream) or 0))
