@@ -1093,11 +1093,16 @@ def avits_cache_attention_shared_workspace(cache: KVCache, prefix: KVCache, H: i
     return int(lib().avits_cache_attention_shared_workspace(cache._ref, prefix._ref, H))
 
 
+_SHARED_SIZES = 64      # kept with a cache; a program has a few prefix layouts at a time
+
+
 def _shared_bytes(cache: KVCache, prefix: KVCache, H: int) -> int:
     """The same by what it depends on of the prefix: kept with the cache."""
     key = (H, prefix._shape)
     need = cache._shared_need.get(key)
     if need is None:
+        if len(cache._shared_need) >= _SHARED_SIZES:
+            cache._shared_need.clear()
         need = cache._shared_need[key] = avits_cache_attention_shared_workspace(cache, prefix, H)
     return need
 

@@ -46,3 +46,21 @@ def call_of_q(args, seen):
     assert (a[13], a[15], a[16], a[17]) == (0, 0, 0, 0)      # no keys: no strides of theirs
     seen.extend(tuple((ctypes.c_int64 * 3).from_address(a[i])) for i in (10, 12))
     return 0
+
+
+def test_workspace_sizes_kept_are_few(monkeypatch):
+    """A program that makes a prefix per length does not grow what a cache keeps."""
+    asked = []
+
+    def need(cache, prefix, H):
+        asked.append(prefix.n)
+        return 16 * prefix.n + H
+
+    monkeypatch.setattr(av, "avits_cache_attention_shared_workspace", need)
+    cache = types.SimpleNamespace(_shared_need={})
+    prefixes = [types.SimpleNamespace(n=n, _shape=n.to_bytes(4, "little")) for n in range(1000)]
+    for p in prefixes:
+        for H in (8, 8, 40):
+            assert av._shared_bytes(cache, p, H) == 16 * p.n + H
+    assert len(cache._shared_need) <= 64
+    assert len(asked) == 2000                  # the second of the same was kept
