@@ -10,9 +10,9 @@
 //
 // The bytes are few (a step of 256 sequences 25 KB), so that latency is all: one CTA, a
 // thread to a sequence, scans and moves pages; what is more than a few pages or rows of a
-// sequence goes to whole warps.  Where the rows are many, a second kernel over all SMs
-// writes them.  A step of 256 sequences takes 4.9 us, 96 prompts with 108000 rows and 7000 pages
-// 8.8: the chain lengths, scan, list, scan, list, table.
+// sequence is shared out among the block's threads.  Where the rows are many, a second kernel over
+// all SMs writes them.  A step of 256 sequences takes 5.0 us, 96 prompts with 108000 rows and 7000
+// pages 8.9: the chain lengths, scan, list, scan, list, table.
 #include "cache_common.cuh"
 #include "avits_internal.h"
 
@@ -21,15 +21,22 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kRowThreads = 128;
-// Pages, and rows, of a sequence that a thread moves alone; more go to a whole warp.  us, 256
-// sequences of a token 5.0, all by warps 11.9; 96 of 6 tokens by one CTA 6.4, by warps 7.7.
+// Pages, and rows, of a sequence that a thread moves alone; more go to several threads.  us with
+// up to 4, 8 and 16 rows alone: 128 sequences of 8 tokens 4.5, 5.5 and 5.5; 64 of 16 4.3, 4.3, 7.0.
 constexpr int kOwnPages = 2;
-constexpr int kOwnRows = 8;
-// Rows that the first kernel's CTA writes itself.  us, so and by the second kernel: 256
-// sequences of 1, 2 and 4 tokens 5.0 and 7.9, 4.9 and 7.0, 6.2 and 6.9; 8 of 128 4.5 and 5.6, of
-// 900 10.9 and 5.9; 96 of 8 7.5 and 5.8; one of 256 5.0 and 5.5, of 512 6.5 and 5.4, of 1024 9.5
-// and 5.5.
-constexpr int kFewRows = 512;
+constexpr int kOwnRows = 4;
+// log2 of the fewest threads that share such a sequence's rows (4, 8 and 16 threads: 113 of 9
+// tokens 5.1, 5.8 and 7.1 us; 60 of 17 5.0, 5.0, 5.9) and its pages (a warp; 96 prompts of 7000
+// pages 8.9, with 4 threads 9.7).
+constexpr int kRowBits = 2, kPageBits = 5;
+// Rows that the first kernel's CTA writes itself: threads lie over sequences and rows evenly, so
+// that the number of rows decides, however they lie in sequences.  us, so and by the second
+// kernel: 256 sequences of 1, 2 and 4 tokens 3.6 and 6.4, 4.0 and 6.8, 4.8 and 6.8; 102 of 10 5.1
+// and 6.0; 8 of 128 4.3 and 5.8; one of 512 4.0 and 5.6, of 1024 4.3 and 5.7; 255 of one beside one
+// of 700 5.0 and 7.0.  Past the border both win somewhere: 150 of 10 6.6 and 6.0, 300 of 5 7.3 and
+// 6.8, 200 of 10 6.7 and 6.1, 256 of 8 6.1 and 6.2, one of 2048 4.9 and 5.6, of 4096 6.2 and 5.7, 8
+// of 900 9.1 and 6.0.
+constexpr int kFewRows = 1024;
 
 struct Plan {
   CachePlanCall p;
@@ -95,21 +102,21 @@ __device__ __forceinline__ void put_row(const Plan& a, int t, int b, int place) 
   put_row(a, t, b, place, col, page);
 }
 
-// put(i, get(i)) for i < n over a warp's lanes, four reads on their way at once.
+// put(i, get(i)) for i < n by threads `at` of `all`, four reads on their way at once.
 template <typename Get, typename Put>
-__device__ __forceinline__ void by_four(int n, int lane, Get get, Put put) {
-  for (int i0 = lane; i0 < n; i0 += 128) {
+__device__ __forceinline__ void by_four(int n, int at, int all, Get get, Put put) {
+  for (int i0 = at; i0 < n; i0 += 4 * all) {
     int v[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (i0 + 32 * k < n) v[k] = get(i0 + 32 * k);
+      if (i0 + all * k < n) v[k] = get(i0 + all * k);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (i0 + 32 * k < n) put(i0 + 32 * k, v[k]);
+      if (i0 + all * k < n) put(i0 + all * k, v[k]);
   }
 }
 
-// A sequence's part of the plan that whole warps do.
+// A sequence's part of the plan that several threads do.
 struct Big {
   int b, col, n;             // pages: columns col .. col+n-1, ranks from `rank` on
   int row, rows, place;      // rows, from `row` on; the first one's place, -1: padding
@@ -124,7 +131,7 @@ cache_plan_kernel(const __grid_constant__ Plan a) {
   const CachePlanCall& p = a.p;
   const avits_kv_cache& c = p.cache;
   int32_t* table = const_cast<int32_t*>(c.block_table);
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, step = blockDim.x;
+  const int tid = threadIdx.x, lane = tid & 31, step = blockDim.x;
   if (tid == 0) s_taken = s_big = 0;
   pdl_wait_then_trigger();
   const int had = *p.free_count;
@@ -147,11 +154,14 @@ cache_plan_kernel(const __grid_constant__ Plan a) {
     x.give = x.ok && ch < 0 ? pages_of(a, x.n0) - pages_of(a, x.n1) : 0;
     return x;
   };
-  // what the list holds, by whole warps; between two barriers
-  auto over_list = [&](auto f) {
+  // What the list holds, the block's threads shared out among its entries, a power of two of
+  // them to each, 2^least or more: f(entry, thread of so many).  Between two barriers.
+  auto over_list = [&](int least, auto f) {
     __syncthreads();
     const int n = s_big;
-    for (int e = w; e < n; e += step >> 5) f(s_list[e]);
+    const int bits = n > 0 ? max(least, __clz(n - 1) - 1 - __clz(step)) : least;
+    for (int e = tid >> bits; e < n; e += step >> bits)
+      f(s_list[e], tid & ((1 << bits) - 1), 1 << bits);
     __syncthreads();
     if (tid == 0) s_big = 0;
   };
@@ -167,9 +177,9 @@ cache_plan_kernel(const __grid_constant__ Plan a) {
     if (big) s_list[atomicAdd(&s_big, 1)] = Big{b, col, x.give, 0, 0, 0, rank};
     for (int i = 0; !big && i < x.give; ++i)
       if (rank + i < c.num_pages) p.free_pages[rank + i] = table[(int64_t)b * c.table_sb + col + i];
-    over_list([&](const Big& y) {
+    over_list(kPageBits, [&](const Big& y, int thread, int all) {
       const int32_t* from = table + (int64_t)y.b * c.table_sb + y.col;
-      by_four(y.n, lane, [&](int i) { return from[i]; },
+      by_four(y.n, thread, all, [&](int i) { return from[i]; },
               [&](int i, int v) {
                 if (y.rank + i < c.num_pages) p.free_pages[y.rank + i] = v;
               });
@@ -228,28 +238,47 @@ cache_plan_kernel(const __grid_constant__ Plan a) {
       s_list[atomicAdd(&s_big, 1)] =
           Big{b, col, n, (int)row, rows, ok ? x.n0 : -1, rank};
     } else {
-      for (int i = 0; i < n; ++i) {
-        const int got = p.free_pages[avail - 1 - (rank + i)];
-        table[(int64_t)b * c.table_sb + col + i] = got;
-        if (col + i == col0) page = got;
+      int got[kOwnPages];
+#pragma unroll
+      for (int i = 0; i < kOwnPages; ++i) {
+        got[i] = -1;
+        if (i < n) {
+          got[i] = p.free_pages[avail - 1 - (rank + i)];
+          table[(int64_t)b * c.table_sb + col + i] = got[i];
+        }
       }
       if (a.rows_here) {
-        if (rows > 0) put_row(a, (int)row, b, ok ? x.n0 : -1, col0, page);
-        for (int i = 1; i < rows; ++i) put_row(a, (int)row + i, b, ok ? x.n0 + i : -1);
+        for (int i = 0; i < rows; ++i) {
+          const int place = ok ? x.n0 + i : -1, at_col = ok ? a.page.div(place) : 0;
+          int on = page;          // of column col0, the only one that was there before
+#pragma unroll
+          for (int k = 0; k < kOwnPages; ++k)
+            if (k < n && at_col == col + k) on = got[k];
+          put_row(a, (int)row + i, b, place, at_col, on);
+        }
       } else if (rows > 0) {
         p.place[row] = ok ? x.n0 : -1;
       }
     }
-    over_list([&](const Big& y) {
+    // rows read new pages from the free list, so that they wait for no other thread's table entries
+    over_list(a.rows_here ? kRowBits : kPageBits, [&](const Big& y, int thread, int all) {
       int32_t* to = table + (int64_t)y.b * c.table_sb + y.col;
       const int32_t* from = p.free_pages + (avail - 1 - y.rank);
-      by_four(y.n, lane, [&](int i) { return from[-(int64_t)i]; }, [&](int i, int v) { to[i] = v; });
-      __syncwarp();
-      if (a.rows_here)
-        for (int i = lane; i < y.rows; i += 32)
-          put_row(a, y.row + i, y.b, y.place >= 0 ? y.place + i : -1);
-      else if (lane == 0 && y.rows > 0)
+      by_four(y.n, thread, all, [&](int i) { return from[-(int64_t)i]; },
+              [&](int i, int v) { to[i] = v; });
+      if (a.rows_here) {
+        auto page_of = [&](int i) {
+          if (y.place < 0) return -1;
+          const int k = a.page.div(y.place + i) - y.col;
+          return k >= 0 ? from[-(int64_t)k] : to[k];
+        };
+        by_four(y.rows, thread, all, page_of, [&](int i, int v) {
+          const int place = y.place >= 0 ? y.place + i : -1;
+          put_row(a, y.row + i, y.b, place, place >= 0 ? a.page.div(place) : 0, v);
+        });
+      } else if (thread == 0 && y.rows > 0) {
         p.place[y.row] = y.place;
+      }
     });
     before.x += chunk_rows;
     before.y += sum.x;
