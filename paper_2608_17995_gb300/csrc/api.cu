@@ -746,7 +746,8 @@ avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits
 }
 
 // Descriptions that avits_cache_attention_shared takes together, with H heads.
-static avits_status check_shared(const avits_kv_cache* cache, const avits_kv_cache* prefix, int H) {
+static avits_status check_shared(const avits_kv_cache* cache, const avits_kv_cache* prefix, int H,
+                                 int sms) {
   for (const avits_kv_cache* c : {cache, prefix}) {
     const avits_status ok = check_cache(c);
     if (ok != AVITS_OK) return ok;
@@ -758,17 +759,18 @@ static avits_status check_shared(const avits_kv_cache* cache, const avits_kv_cac
   call.cache = *cache;
   call.prefix = *prefix;
   call.H = H;
-  return cache_shared_sizes_ok(call) ? AVITS_OK : AVITS_ERR_UNSUPPORTED;
+  return cache_shared_sizes_ok(call, sms) ? AVITS_OK : AVITS_ERR_UNSUPPORTED;
 }
 
 size_t avits_cache_attention_shared_workspace(const avits_kv_cache* cache,
                                               const avits_kv_cache* prefix, int H) {
-  if (check_shared(cache, prefix, H) != AVITS_OK) return 0;
+  const int sms = std::max(1, num_sms_current());
+  if (check_shared(cache, prefix, H, sms) != AVITS_OK) return 0;
   CacheSharedCall call{};
   call.cache = *cache;
   call.prefix = *prefix;
   call.H = H;
-  return cache_shared_workspace(call, num_sms_current());
+  return cache_shared_workspace(call, sms);
 }
 
 avits_status avits_cache_attention_shared(const avits_kv_cache* cache, const avits_kv_cache* prefix,
@@ -780,12 +782,12 @@ avits_status avits_cache_attention_shared(const avits_kv_cache* cache, const avi
   if (!group_start || !q || !o || q_sb < 0 || q_sh < 0 || o_sb < 0 || o_sh < 0)
     return AVITS_ERR_INVALID_ARG;
   if (!(softmax_scale > 0.f) || !(softmax_scale < 3.0e38f)) return AVITS_ERR_INVALID_ARG;
-  const avits_status ok = check_shared(cache, prefix, H);
+  const int sms = std::max(1, num_sms_current());
+  const avits_status ok = check_shared(cache, prefix, H, sms);
   if (ok != AVITS_OK) return ok;
   if (!rows_apart(cache->d, {cache->B, o_sb}, {H, o_sh})) return AVITS_ERR_INVALID_ARG;
   const CacheSharedCall call{*cache, *prefix, group_start, q, H, q_sb, q_sh, softmax_scale,
                              o, o_sb, o_sh, lse_opt, workspace};
-  const int sms = num_sms_current();
   if (!workspace || !aligned16(workspace) || ws_bytes < cache_shared_workspace(call, sms))
     return AVITS_ERR_INVALID_ARG;
   return cuda_status(

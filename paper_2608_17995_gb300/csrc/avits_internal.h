@@ -229,7 +229,7 @@ struct CacheSharedCall {
   float* lse;                   // [B,H] or NULL
   void* ws;
 };
-bool cache_shared_sizes_ok(const CacheSharedCall& s);
+bool cache_shared_sizes_ok(const CacheSharedCall& s, int num_sms);
 size_t cache_shared_workspace(const CacheSharedCall& s, int num_sms);
 cudaError_t launch_cache_shared(const CacheSharedCall& s, int num_sms, unsigned int* status,
                                 cudaStream_t stream);

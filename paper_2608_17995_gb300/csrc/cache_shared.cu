@@ -47,9 +47,9 @@ int width_of(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // has many pieces to join (11 sequences on 46000 24.7, of 4 tiles 28.8; 8 on 16000 27.0, of 5
 // 28.3), else 5 (64 in 16 groups on up to 1000 23.7, of 8 29.8; 70 in 24 on 1282 22.0 and 27.3).
 constexpr int kManyTiles = 160;      // of a unit
-int piece_tiles(long long tiles, int longest, bool two) {
+int piece_tiles(long long tiles, int longest, bool two, int num_sms) {
   const int most = two ? 10 : longest > kManyTiles ? 8 : 5;
-  const long long share = tiles / (two ? 100 : 200);
+  const long long share = tiles * 38 / (25ll * num_sms * (two ? 1 : 2));      // 100 and 200 on 152 SMs
   return (int)(share < 2 ? 2 : share > most ? most : share);
 }
 
@@ -59,7 +59,7 @@ void cut(Line& l, const avits_kv_cache& c, int num_sms) {
   l.tile = l.box ? kPrefixTile : bf ? 16 : 8;
   const int longest = (c.max_len + l.tile - 1) / l.tile;
   l.tiles = l.units * longest;
-  const int few = l.box ? piece_tiles(l.tiles, longest, l.rows > kPrefixRows) : kWarps;
+  const int few = l.box ? piece_tiles(l.tiles, longest, l.rows > kPrefixRows, num_sms) : kWarps;
   l.least = longest < few ? longest : few;
   const long long most = (l.tiles + l.least - 1) / l.least;
   const int ctas = l.box      ? 2 * kPrefixRows / l.rows
@@ -84,13 +84,14 @@ int rows_of(bool bf, int D, long long n) {
 // 50.9 and 49.3, 128 x (8192 + 512) 70.3 and 71.1, 4 KV heads of 128 x (32768 + 300) 87.2 and 86.0, +
 // 100 80.3 and 83.0, three prefixes 96 x (8000 + 300) 60.3 and 64.6; an odd tile 324 rows on 30145
 // 59.9 and 70.2, 1136 on 16837 123 and 132.
-constexpr long long kAtOnce = 152 * 10, kMuchOwn = 128 * 1024;      // tiles, keys of KV heads
-int prefix_rows(const avits_kv_cache& c, const avits_kv_cache& p, long long n) {
+constexpr int kAtOnce = 10, kMuchOwn = 862;      // tiles, keys of KV heads: to an SM
+int prefix_rows(const avits_kv_cache& c, const avits_kv_cache& p, long long n, int num_sms) {
   const long long tiles = (n + kPrefixRows - 1) / kPrefixRows, pairs = (tiles + 1) / 2;
   const bool two = tiles > 1 && 40 * pairs <= 21 * tiles &&
                    (p.B == 1 ||
-                    pairs * c.Hkv * p.B * ((p.max_len + kPrefixTile - 1) / kPrefixTile) <= kAtOnce) &&
-                   (long long)c.B * c.Hkv * c.max_len >= kMuchOwn;
+                    pairs * c.Hkv * p.B * ((p.max_len + kPrefixTile - 1) / kPrefixTile) <=
+                        (long long)kAtOnce * num_sms) &&
+                   (long long)c.B * c.Hkv * c.max_len >= (long long)kMuchOwn * num_sms;
   return two ? 2 * kPrefixRows : kPrefixRows;
 }
 
@@ -151,7 +152,7 @@ Shape shape_of(const CacheSharedCall& s, int num_sms) {
   x.pre.box = prefix_tc_box(p);
   // rows of a group's KV head, by and large
   const long long rows = ((long long)c.B + p.B - 1) / p.B * G;
-  x.pre.rows = x.pre.box ? prefix_rows(c, p, rows) : rows_of(bf, D, rows);
+  x.pre.rows = x.pre.box ? prefix_rows(c, p, rows, num_sms) : rows_of(bf, D, rows);
   x.pre.units = c.Hkv * ((long long)c.B * G / x.pre.rows + p.B);
   cut(x.own, c, num_sms);
   cut(x.pre, p, num_sms);
@@ -355,10 +356,10 @@ cudaError_t launch_parts(CacheAttn& a, int D, cudaStream_t s) {
 
 }  // namespace
 
-bool cache_shared_sizes_ok(const CacheSharedCall& s) {
+bool cache_shared_sizes_ok(const CacheSharedCall& s, int num_sms) {
   const avits_kv_cache& c = s.cache;
   if (s.H / c.Hkv > kMaxGroup || (long long)c.B * s.H >= (1ll << 30)) return false;
-  const Shape x = shape_of(s, 1);
+  const Shape x = shape_of(s, num_sms);
   for (const Line* l : {&x.own, &x.pre}) {
     const long long parts = l == &x.own && x.warps ? l->units * l->grid : l->units + kMaxGrid;
     if (l->tiles >= (1ll << 30) || parts * l->rows >= (1ll << 31)) return false;
