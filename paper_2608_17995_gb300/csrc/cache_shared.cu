@@ -19,6 +19,8 @@
 // 6.  With 8 KV heads of 4 query heads, width 128, in us and (bytes at a copy's rate): 8
 // sequences on 517 tokens 8.9 (0.7), 64 on 8192 with up to 512 of their own 37 (16), 12 groups
 // of 8 on up to 3001 53 (36); 128 sequences of 4 x 8 heads on 32768 86 (36 of products).
+#include <algorithm>
+
 #include "cache_line.cuh"
 
 namespace avits {
@@ -52,6 +54,10 @@ int piece_tiles(long long tiles, int longest, bool two, int num_sms) {
   const long long share = tiles * 38 / (25ll * num_sms * (two ? 1 : 2));      // 100 and 200 on 152 SMs
   return (int)(share < 2 ? 2 : share > most ? most : share);
 }
+// Units of groups of prefixes with units of so many rows.
+long long units_at_most(const avits_kv_cache& c, const avits_kv_cache& p, int G, int rows) {
+  return c.Hkv * ((long long)c.B * G / rows + p.B);
+}
 
 void cut(Line& l, const avits_kv_cache& c, int num_sms) {
   const bool bf = c.dt == AVITS_BF16;
@@ -78,21 +84,38 @@ int rows_of(bool bf, int D, long long n) {
 // Rows of a unit on the tensor cores, for groups of n rows of a KV head.  Two row tiles to a CTA
 // leave room on its SM for a CTA of own tokens, and SMs without a piece to more: taken where the
 // tiles come in pairs, there are own tokens for the rest, and the prefix is one or the pieces fit
-// the SMs at once.  us, 128 and 256 rows: 64 x (2000 + 50) 23.8 and 27.7, + 300 28.4 and 30.9, + 512
-// 36.4 and 33.1, + 2000 79.0 and 73.8; 64 x (8192 + 200) 33.9 and 36.0, + 400 42.1 and 37.6, + 1000
-// 62.3 and 58.2; 128 x (2000 + 50) 28.3 and 31.7, + 200 36.6 and 34.1; more pieces 64 x (20000 + 300)
-// 50.9 and 49.3, 128 x (8192 + 512) 70.3 and 71.1, 4 KV heads of 128 x (32768 + 300) 87.2 and 86.0, +
-// 100 80.3 and 83.0, three prefixes 96 x (8000 + 300) 60.3 and 64.6; an odd tile 324 rows on 30145
-// 59.9 and 70.2, 1136 on 16837 123 and 132.
-constexpr int kAtOnce = 10, kMuchOwn = 862;      // tiles, keys of KV heads: to an SM
-int prefix_rows(const avits_kv_cache& c, const avits_kv_cache& p, long long n, int num_sms) {
+// the SMs at once.  It takes more own tokens where one prefix's pieces are few and run from one
+// unit into the next (a second start and end in some CTAs), and for long prefixes at width 64,
+// whose own tokens are half the bytes.  us, 128 and 256 rows, 8 KV heads of width 128, 64 sequences:
+//   own       100          200          300          400          512          2000
+//   on 1000                22.2  20.9   26.2  25.2   29.4  28.1   33.1  31.5
+//      2000   23.8* 27.7*  25.5  29.3   28.7  30.6   32.0  32.1   36.3  33.4   79.0  73.8
+//      4000                26.9  34.7   31.4  35.9   34.6  37.8   39.1  39.6
+//      8192                33.9  36.0   38.4  36.9   42.7  37.6   47.2  40.8          (* own 50)
+//     16000                41.5  42.4   45.7  46.2   49.7  49.6   54.3  54.6
+// 63 tiles in pieces of 7, 4 KV heads of 512 rows on 4000 + 600 30.6 and 26.9.  128 sequences on 3000
+// + 150 38.0 and 36.3, 5500 + 150 41.6 and 42.2, 8192 + 256 54.6 and 55.6, 16000 + 200 65.4 and 64.8; 4
+// KV heads of 1024 rows on 32768 + 200 84.8 and 84.9, + 300 88.5 and 87.6.  Three prefixes 96 x (8000 +
+// 300) 60.3 and 64.6.  Width 64: 128 x (12174 + 622) of 2 KV heads 30.0 and 33.7, 128 x (6618 + 640)
+// of 4 27.4 and 23.3, 256 x (1389 + 149) of 4 24.6 and 23.6.  An odd tile: 324 rows on 30145 59.9 and
+// 70.2, 1136 on 16837 123 and 132.  Of 230 drawn sizes the choice costs 0.6 % on average, more than 5
+// on 8 of them and at most 11 (three uneven groups of width 64; 256 x (800 + 61)).
+constexpr int kAtOnce = 10, kMuchOwn = 862, kMoreOwn = 1536;      // tiles, keys of KV heads: to an SM
+constexpr int kShortTiles = 40;
+int prefix_rows(const avits_kv_cache& c, const avits_kv_cache& p, int G, long long n, int num_sms) {
   const long long tiles = (n + kPrefixRows - 1) / kPrefixRows, pairs = (tiles + 1) / 2;
-  const bool two = tiles > 1 && 40 * pairs <= 21 * tiles &&
-                   (p.B == 1 ||
-                    pairs * c.Hkv * p.B * ((p.max_len + kPrefixTile - 1) / kPrefixTile) <=
-                        (long long)kAtOnce * num_sms) &&
-                   (long long)c.B * c.Hkv * c.max_len >= (long long)kMuchOwn * num_sms;
-  return two ? 2 * kPrefixRows : kPrefixRows;
+  if (tiles < 2 || 40 * pairs > 21 * tiles) return kPrefixRows;
+  const int longest = (p.max_len + kPrefixTile - 1) / kPrefixTile;
+  const long long all = pairs * c.Hkv * p.B * longest, own = (long long)c.B * c.Hkv * c.max_len;
+  if (p.B > 1 && all > (long long)kAtOnce * num_sms) return kPrefixRows;
+  long long much = kMuchOwn;
+  if (p.B == 1) {
+    const long long at_most = units_at_most(c, p, G, 2 * kPrefixRows) * longest;
+    const int piece = piece_tiles(at_most, longest, true, num_sms);
+    if (longest % piece != 0 && 5 * ((all + piece - 1) / piece) < 2ll * num_sms) much = kMoreOwn;
+  }
+  if (c.d <= 64 && longest > kShortTiles) much = std::max(much, 2ll * kMuchOwn);
+  return own < much * num_sms ? kPrefixRows : 2 * kPrefixRows;
 }
 
 // CTAs of a unit's cluster that goes over prefix and own tokens in one launch, 0 where parts
@@ -152,8 +175,8 @@ Shape shape_of(const CacheSharedCall& s, int num_sms) {
   x.pre.box = prefix_tc_box(p);
   // rows of a group's KV head, by and large
   const long long rows = ((long long)c.B + p.B - 1) / p.B * G;
-  x.pre.rows = x.pre.box ? prefix_rows(c, p, rows, num_sms) : rows_of(bf, D, rows);
-  x.pre.units = c.Hkv * ((long long)c.B * G / x.pre.rows + p.B);
+  x.pre.rows = x.pre.box ? prefix_rows(c, p, G, rows, num_sms) : rows_of(bf, D, rows);
+  x.pre.units = units_at_most(c, p, G, x.pre.rows);
   cut(x.own, c, num_sms);
   cut(x.pre, p, num_sms);
   x.both = both_of(s, x.own, num_sms);
