@@ -640,8 +640,8 @@ avits_status avits_cache_plan(const avits_kv_cache* cache, const int32_t* lens,
  *
  * freq  : device [rot/2], turns per position as fractions of 2^64
  *         (avits_rotary_frequencies).  The product with a position is taken modulo a
- *         turn in integers, so that positions of any size, and negative ones, are exact
- *         to 2^-32 of a turn.
+ *         turn in integers, so that positions of any size, and negative ones, add
+ *         nothing to the table's own error but the cut to 2^-32 of a turn.
  * rot   : even, 0 <= rot <= d; 0: the norm alone (freq, positions not read).
  * axes  : 1 .. 4; sections of the axes sum to rot/2.
  * ---------------------------------------------------------------------- */
@@ -660,7 +660,10 @@ typedef struct {
  *                       turns within original_len, original_len f_i, go from low to high
  * Several axes with ladders of their own: one call for each, one behind the other.
  * width even, 0 < width <= 256; base > 0; factor >= 1; low < high, original_len > 0
- * (PARTS).  f_i must be below half a turn. */
+ * (PARTS).  f_i must be below half a turn.
+ * They are computed in 64-bit floating point, to 2^-53 of a turn per position (bases of
+ * 10000 and more): the angle at position p is off by p 2^-53 turns, 2^-22 at the ends of
+ * int32. */
 typedef enum {
   AVITS_SCALE_NONE = 0, AVITS_SCALE_LINEAR = 1, AVITS_SCALE_BASE = 2, AVITS_SCALE_PARTS = 3
 } avits_scaling;

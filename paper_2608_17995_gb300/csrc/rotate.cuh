@@ -6,9 +6,10 @@
 //   (y_a, y_b) of pair i -> m (y_a cos t - y_b sin t, y_b cos t + y_a sin t),
 //   t = 2 pi p f_i, pairs (2i, 2i+1) or (i, i + rot/2), i < rot/2; the rest stays.
 // All in fp32, rounded once.  Angles: f_i is a 64-bit binary fraction of a turn, so that
-// p f_i mod 1 is the low 64 bits of an integer product, off by p 2^-65 turns; its top
+// p f_i mod 1 is the low 64 bits of an integer product, exact for the f_i given; its top
 // 32 bits become an fp32 angle in [-pi, pi).  No table of cosines is read, and far
-// positions are as exact as near ones.
+// positions add nothing but p times the error of f_i (avits_rotary_frequencies computes them
+// in fp64, off by up to 2^-53: p 2^-53 turns).
 //
 // Bytes bound it: q and k once in, once out.  A row's 16-byte pieces lie over 4 to 32
 // lanes, two to a lane, chosen so that a pair's halves are in one lane; a warp has
