@@ -21,13 +21,16 @@
 // 32 columns each), O behind them.
 //
 // What bounds it, at 128 x 32768 (1024 rows of a KV head, 86 us for the call, 87 with one row
-// tile): 2230 clocks for a tile of 256 rows, of which a tensor pipe's products are 2050 (a product of
-// 64 columns takes the pipe as long as one of 128, 64 clocks, so that S costs as much as the two
-// parts of P) and a softmax warp's work 2000 (535 instructions, of which 64 exponentials, for 64
-// keys of 32 rows, two such warps to a scheduler); neither alone is the bound: without the rests'
-// products 82 us, without the rests 77, without copies 85.  What did not help: S of 128 keys at a
-// time, or Q in tensor memory (96 and 109 us: no room for a second S), two threads to a row (94), one
-// warp that issues for both row tiles (120), registers moved to the softmax warps (90).  Shorter
+// tile): 2230 clocks for a tile of 256 rows, of which the products alone, issued without a pause by
+// the two warps, are 1773 (a product of S, 64 columns, takes 48 clocks: its 6 KB of operands at 128
+// bytes a clock, where its arithmetic is 32; one of P V, 128 columns with P in tensor memory, 64) and
+// a softmax warp's work 2000 (535 instructions, of which 64 exponentials, for 64 keys of 32 rows, two
+// such warps to a scheduler).  The pipe's counter, 68 % over the whole kernel, counts the arithmetic:
+// 1536 clocks of 2230.  Neither side alone is the bound, but the chain of S, softmax and P V over
+// two row tiles: without the rests' products 82 us, without the rests 77, without copies 85.  What did
+// not help: S of 128 keys at a time, or Q in tensor memory (96 and 109 us: no room for a second S),
+// two threads to a row (94), one warp that issues for both row tiles (120), registers moved to the
+// softmax warps (90).  Shorter
 // prefixes are start and end: groups and lengths 1.2 us, first page numbers 0.7, Q and the first
 // tiles 2.5; a part out 2.
 #include "cache_line.cuh"

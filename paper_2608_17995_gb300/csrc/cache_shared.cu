@@ -13,8 +13,9 @@
 // them, each sequence reading its prefix by itself (from L2).
 //
 // What bounds it: the prefixes' bytes and the own ones, while a group has up to about 128
-// rows of a KV head; the tensor pipe beyond (a tile of 64 keys by 128 rows is 8 products of
-// 64 columns for S and 8 of 128 for the two parts of P, 64 clocks each).  Of a call's time
+// rows of a KV head; products and softmax in turn beyond (a tile of 64 keys by 128 rows is 8
+// products of 64 columns for S, 48 clocks each, and 8 of 128 for the two parts of P, 64 each: 887
+// clocks on the pipe of the 1115 that it takes; cache_prefix_tc.cu).  Of a call's time
 // much is start and end: lengths, pages and the first tiles in turn 5 us, parts out and joined
 // 6.  With 8 KV heads of 4 query heads, width 128, in us and (bytes at a copy's rate): 8
 // sequences on 517 tokens 8.9 (0.7), 64 on 8192 with up to 512 of their own 37 (16), 12 groups
