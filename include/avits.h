@@ -44,7 +44,8 @@
  *                             and keys in one pass (also of an image's tokens)
  *   avits_cache_append_rotated  the same, keys and values into the pages
  *   avits_cache_attention_shared  one new token per sequence over a prefix that its
- *                             group shares, read once, and its own cached tokens
+ *                             group shares, read for many of them at once, and its own
+ *                             cached tokens
  *
  * Conventions shared by every call
  * --------------------------------
@@ -713,7 +714,7 @@ avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits
 
 /* ------------------------------------------------------------------------
  * avits_cache_attention for sequences that have a prefix in common (an instruction, a
- * document), which is read once for all of a group: sequence b of group g attends to the
+ * document), which is read for many of a group at once: sequence b of group g attends to the
  * prefix->lens[g] tokens of row g of `prefix` and to the cache->lens[b] tokens of its own,
  *
  *     x_bhj = softmax_scale * <q_bh, k_j>     j over both
@@ -727,6 +728,10 @@ avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits
  *          group g.  It does not decrease, from 0 or more to B or less; sequences before the
  *          first and from the last on have no prefix.  Otherwise AVITS_ERR_PAGE is raised
  *          and no sequence has one.
+ * The rows of one reading of a prefix are the query heads of its group's sequences that share a
+ * KV head: 128 or 256 of them in bf16 of widths to 128 with pages of a multiple of 8 tokens, 8
+ * to 32 with other pages, 8 or 16 at larger widths, 4 or 8 in fp32.  Where prefixes and own tokens
+ * are short, each sequence may read its prefix by itself.
  * A sequence without any token gets o = 0 and lse = -inf.  What avits_cache_attention says
  * of infinite values, sizes and strides holds here, but that an infinite value of a prefix
  * gives NaN where its token's weight, relative to the largest, is below 2^-106.

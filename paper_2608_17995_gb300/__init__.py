@@ -1111,7 +1111,7 @@ def avits_cache_attention_shared(cache: KVCache, prefix: KVCache, group_start, q
                                  softmax_scale: float, o, lse=None, workspace=None, stream=None):
     """avits_cache_attention for sequences that have a prefix in common: sequence b of
     group g (group_start[g] <= b < group_start[g+1]; int32 [prefix.B + 1]) attends to row
-    g of ``prefix``, which is read once for the whole group, and to its own tokens in
+    g of ``prefix``, which is read for many of the group at once, and to its own tokens in
     ``cache``.  q [B,H,d] into o [B,H,d] and lse [B,H] fp32, as there; no weights.
     ``workspace``: as there, avits_cache_attention_shared_workspace() bytes."""
     B, H, d = shape = q.shape
