@@ -735,8 +735,8 @@ avits_status avits_cache_append_rotated(const avits_kv_cache* cache, const avits
  * A sequence without any token gets o = 0 and lse = -inf.  What avits_cache_attention says
  * of infinite values, sizes and strides holds here, but that an infinite value of a prefix
  * gives NaN where its token's weight, relative to the largest, is below 2^-106, and that the
- * sums over a prefix may count from a logit that is up to 2^8 below the largest, so that finite
- * values beyond 3.4e38 / (256 prefix->lens[g]) can pass the range of fp32.
+ * sums over a prefix may be relative to a weight of 2^-8 of the largest, so that finite values
+ * beyond 3.4e38 / (256 prefix->lens[g]) can pass the range of fp32.
  * workspace/ws_bytes : at least avits_cache_attention_shared_workspace(...) bytes,
  *          16-byte aligned, of any content; not used by two calls at once.  It grows with
  *          B H d (4 to 32 bytes of it, by cache->max_len), with the groups and the SMs. */
